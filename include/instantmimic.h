@@ -528,6 +528,175 @@ enum {
 im_status im_ppo_read(im_ctx *ctx, int32_t buffer, int32_t layer, void *dst, int64_t *rows,
                       int64_t *cols, int64_t *elem_bytes, void *stream);
 
+/*
+ * Layers of experts.  A policy for many clips chooses a layer's weights by the
+ * env (one expert per clip or group of clips).  The calls below are such a
+ * layer, its norm and what its training keeps.  They need no context: all
+ * arrays are device memory of the caller on the current HIP device, a call
+ * that needs scratch memory takes it as a workspace, and a workspace serves
+ * one call at a time.  Like the hot calls above they validate on the host in
+ * O(1), enqueue on `stream`, allocate nothing, never synchronise and may be
+ * captured into a HIP graph.  Matrices are row-major with a row stride `ld` in
+ * elements (>= the row's length); rows need no alignment beyond their
+ * element's (rows of a multiple of 16 bytes are fastest).  Results do not
+ * depend on timing: every sum has a fixed order.  Outputs must not overlap
+ * inputs unless a call says so.
+ */
+
+/*
+ * Rows by expert: a stable counting sort.
+ *   expert  [n] int32: each row's expert; a value outside [0, n_experts) is a
+ *           row without one (an env that is not played)
+ *   offsets [n_experts + 1] int32, rows [n] int32: written.  Expert e's rows are
+ *           rows[offsets[e]] .. rows[offsets[e + 1] - 1] in ascending order; rows
+ *           without an expert follow from rows[offsets[n_experts]] on.
+ * 0 <= n <= 2^30, 1 <= n_experts <= IM_MAX_EXPERTS (IM_ERR_UNSUPPORTED above).
+ * workspace: im_group_rows_workspace(n, n_experts) bytes, 4-byte aligned.
+ */
+#define IM_MAX_EXPERTS 1024
+int64_t im_group_rows_workspace(int64_t n, int32_t n_experts);
+im_status im_group_rows(const int32_t *expert, int64_t n, int32_t n_experts, int32_t *offsets,
+                        int32_t *rows, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * An activation kept in 8 bits for the backward pass.  Along a row, 32
+ * consecutive values (the last block of a row may be shorter) share a power of
+ * two: value = q 2^(scale - 133), q in -127..127, where scale - 127 is the
+ * exponent of the block's largest magnitude, one more where that would round
+ * to 128 steps, and q is rounded to nearest even.  A stored value is at most
+ * half a step from the original, 1/127.5 of the block's largest magnitude
+ * (blocks whose largest magnitude exceeds 2^127 * 255/128 saturate at 127 steps
+ * of 2^121).  A block that holds a NaN or an infinity has scale 255 and is NaN
+ * throughout when restored; a block of zeros has scale 0 and q 0.  Restored
+ * values are exact in bf16 and fp32.  33/32 bytes a value.
+ *   q [n][ld_q] int8, scale [n][ld_scale] uint8 (ld_scale >= ceil(d / 32))
+ */
+typedef struct {
+    int8_t *q;
+    uint8_t *scale;
+    int64_t ld_q, ld_scale;
+} im_checkpoint;
+
+/* x [n][d] (float, or bf16 bit patterns: dtype) into the checkpoint, and back. */
+im_status im_checkpoint_store(const void *x, int64_t ld_x, int32_t dtype, int64_t n, int64_t d,
+                              const im_checkpoint *c, void *stream);
+im_status im_checkpoint_load(const im_checkpoint *c, int64_t n, int64_t d, void *x, int64_t ld_x,
+                             int32_t dtype, void *stream);
+
+/*
+ * Layer norm over the rows of x [n][d]: mean = sum x / d,
+ * rstd = 1 / sqrt(sum (x - mean)^2 / d + eps), y = (x - mean) rstd gamma + beta,
+ * in fp32, y rounded once to `dtype` (x's and y's).  gamma, beta [d] float (NULL: 1
+ * and 0); mean, rstd [n] float (NULL: not written); checkpoint (NULL: none): x
+ * in 8 bits, from the same read.  y may be x.  0 <= n, 1 <= d <= IM_NORM_MAX_WIDTH
+ * (IM_ERR_UNSUPPORTED above), eps >= 0.
+ */
+#define IM_NORM_MAX_WIDTH 8192
+typedef struct {
+    int64_t n, d;
+    int32_t dtype;
+    float eps;
+    const void *x;
+    int64_t ld_x;
+    const float *gamma, *beta;
+    void *y;
+    int64_t ld_y;
+    float *mean, *rstd;
+    const im_checkpoint *checkpoint;
+} im_norm;
+im_status im_layer_norm(const im_norm *a, void *stream);
+
+/*
+ * Its gradient at x (or, x NULL, at the values that the checkpoint restores),
+ * with the forward's mean and rstd: h = (x - mean) rstd, g = dy gamma,
+ *   dx = rstd (g - sum g / d - h sum (g h) / d),  dgamma = sum_rows dy h,
+ *   dbeta = sum_rows dy.
+ * dy, x, dx of `dtype`; dx may be dy or x (or NULL: not wanted); dgamma and dbeta
+ * [d] float (either NULL: not wanted), overwritten (zero for n = 0).  workspace:
+ * im_layer_norm_grad_workspace(n, d) bytes, 4-byte aligned (not needed without
+ * dgamma and dbeta).
+ */
+typedef struct {
+    int64_t n, d;
+    int32_t dtype;
+    const void *dy;
+    int64_t ld_dy;
+    const void *x;
+    int64_t ld_x;
+    const im_checkpoint *checkpoint;
+    const float *gamma, *mean, *rstd;
+    void *dx;
+    int64_t ld_dx;
+    float *dgamma, *dbeta;
+    void *workspace;
+    int64_t workspace_bytes;
+} im_norm_grad;
+int64_t im_layer_norm_grad_workspace(int64_t n, int64_t d);
+im_status im_layer_norm_grad(const im_norm_grad *a, void *stream);
+
+/*
+ * Linear layer with each row's own expert's weights:
+ *   y[r] = W_e x[r] + b_e (then max(., 0) with relu), e the expert of row r.
+ * offsets and rows are im_group_rows'; rows NULL: row i is at place i of the
+ * grouping (the rows lie grouped already).  x and y keep the rows' own order.
+ * Rows without an expert get y = 0; rows that `rows` does not name keep their y
+ * (an entry outside [0, n) is skipped, offsets are held within [0, n]).
+ *   x [n][in] bf16, w [n_experts][out][in] bf16 (row stride ld_w, expert stride
+ *   out * ld_w), bias [n_experts][out] float or NULL, y [n][out] of y_dtype.
+ * Products of bf16 values summed in fp32, one rounding at the end.  bf16 only
+ * (dtype IM_DTYPE_F32: IM_ERR_UNSUPPORTED).  n <= 2^30, in and out <= 2^20.
+ */
+typedef struct {
+    int64_t n;
+    int32_t n_experts, in, out;
+    int32_t dtype, y_dtype, relu;
+    const int32_t *offsets, *rows;
+    const void *x;
+    int64_t ld_x;
+    const void *w;
+    int64_t ld_w;
+    const float *bias;
+    void *y;
+    int64_t ld_y;
+} im_expert_layer;
+im_status im_expert_linear(const im_expert_layer *a, void *stream);
+
+/*
+ * Its gradients, dy [n][out] bf16 the loss's gradient before any ReLU of y:
+ *   dx[r] = W_e^T dy[r] bf16, with relu_x zero where not x[r] > 0 (x is a ReLU's
+ *           output: dx is then the gradient before that ReLU); zero for rows
+ *           without an expert
+ *   dw_e  = sum over e's rows of dy[r] x[r]^T, float [n_experts][out][in] (row
+ *           stride ld_dw), db_e = sum of dy[r], float [n_experts][out]; an expert
+ *           without rows gets zeros
+ * x [n][in] bf16, or x NULL: the values that the checkpoint restores.  dx, dw and
+ * db may each be NULL: not wanted (x is needed for dw and relu_x, w for dx).
+ * workspace: im_expert_linear_grad_workspace(...) bytes, 16-byte aligned (not
+ * needed without dw and db).
+ */
+typedef struct {
+    int64_t n;
+    int32_t n_experts, in, out;
+    int32_t dtype, relu_x;
+    const int32_t *offsets, *rows;
+    const void *dy;
+    int64_t ld_dy;
+    const void *x;
+    int64_t ld_x;
+    const im_checkpoint *checkpoint;
+    const void *w;
+    int64_t ld_w;
+    void *dx;
+    int64_t ld_dx;
+    float *dw;
+    int64_t ld_dw;
+    float *db;
+    void *workspace;
+    int64_t workspace_bytes;
+} im_expert_layer_grad;
+int64_t im_expert_linear_grad_workspace(int64_t n, int32_t n_experts, int32_t in, int32_t out);
+im_status im_expert_linear_grad(const im_expert_layer_grad *a, void *stream);
+
 const char *im_status_str(im_status s);
 const char *im_last_error(void);
 

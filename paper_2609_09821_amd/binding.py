@@ -98,6 +98,46 @@ PPO_STATS = ("loss_pi", "loss_v", "kl", "clip_frac", "grad_norm", "minibatches",
 PPO_BUFFERS = ("input", "actor_hidden", "critic_hidden", "mean", "value", "dmean", "dvalue")
 
 
+class ImCheckpoint(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("scale", C.c_void_p), ("ld_q", C.c_int64),
+                ("ld_scale", C.c_int64)]
+
+
+class ImNorm(C.Structure):
+    _fields_ = [("n", C.c_int64), ("d", C.c_int64), ("dtype", C.c_int32), ("eps", C.c_float),
+                ("x", C.c_void_p), ("ld_x", C.c_int64), ("gamma", C.c_void_p),
+                ("beta", C.c_void_p), ("y", C.c_void_p), ("ld_y", C.c_int64),
+                ("mean", C.c_void_p), ("rstd", C.c_void_p),
+                ("checkpoint", C.POINTER(ImCheckpoint))]
+
+
+class ImNormGrad(C.Structure):
+    _fields_ = [("n", C.c_int64), ("d", C.c_int64), ("dtype", C.c_int32), ("dy", C.c_void_p),
+                ("ld_dy", C.c_int64), ("x", C.c_void_p), ("ld_x", C.c_int64),
+                ("checkpoint", C.POINTER(ImCheckpoint)), ("gamma", C.c_void_p),
+                ("mean", C.c_void_p), ("rstd", C.c_void_p), ("dx", C.c_void_p),
+                ("ld_dx", C.c_int64), ("dgamma", C.c_void_p), ("dbeta", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
+
+
+class ImExpertLayer(C.Structure):
+    _fields_ = [("n", C.c_int64), ("n_experts", C.c_int32), ("in_", C.c_int32), ("out", C.c_int32),
+                ("dtype", C.c_int32), ("y_dtype", C.c_int32), ("relu", C.c_int32),
+                ("offsets", C.c_void_p), ("rows", C.c_void_p), ("x", C.c_void_p),
+                ("ld_x", C.c_int64), ("w", C.c_void_p), ("ld_w", C.c_int64), ("bias", C.c_void_p),
+                ("y", C.c_void_p), ("ld_y", C.c_int64)]
+
+
+class ImExpertLayerGrad(C.Structure):
+    _fields_ = [("n", C.c_int64), ("n_experts", C.c_int32), ("in_", C.c_int32), ("out", C.c_int32),
+                ("dtype", C.c_int32), ("relu_x", C.c_int32), ("offsets", C.c_void_p),
+                ("rows", C.c_void_p), ("dy", C.c_void_p), ("ld_dy", C.c_int64), ("x", C.c_void_p),
+                ("ld_x", C.c_int64), ("checkpoint", C.POINTER(ImCheckpoint)), ("w", C.c_void_p),
+                ("ld_w", C.c_int64), ("dx", C.c_void_p), ("ld_dx", C.c_int64), ("dw", C.c_void_p),
+                ("ld_dw", C.c_int64), ("db", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_int64)]
+
+
 class ImInfo(C.Structure):
     _fields_ = [("n_bodies", C.c_int32), ("obs_dim", C.c_int32), ("action_dim", C.c_int32),
                 ("n_clips", C.c_int32), ("n_layers", C.c_int32), ("policy_dtype", C.c_int32),
@@ -108,7 +148,10 @@ EXPORTED = ["im_create", "im_destroy", "im_get_info", "im_env_step_fused", "im_p
             "im_reset_envs", "im_standin_physics", "im_set_critic", "im_value",
             "im_policy_act_value", "im_gae", "im_gae_noalloc",
             "im_ppo_setup", "im_ppo_update", "im_ppo_grad", "im_ppo_params_get",
-            "im_ppo_read", "im_status_str", "im_last_error"]
+            "im_ppo_read", "im_group_rows_workspace", "im_group_rows", "im_checkpoint_store",
+            "im_checkpoint_load", "im_layer_norm", "im_layer_norm_grad_workspace",
+            "im_layer_norm_grad", "im_expert_linear", "im_expert_linear_grad_workspace",
+            "im_expert_linear_grad", "im_status_str", "im_last_error"]
 # measurement probes of the GPU (include/instantmimic_calib.h), not the method
 CALIB_EXPORTED = ["im_calib_mfma", "im_calib_lds", "im_calib_read"]
 IM_CALIB_MFMA_BF16, IM_CALIB_MFMA_F32 = 0, 1
@@ -166,6 +209,29 @@ def lib():
     L.im_ppo_read.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.POINTER(C.c_int64),
                               C.POINTER(C.c_int64), C.POINTER(C.c_int64), C.c_void_p]
     L.im_ppo_read.restype = st
+    L.im_group_rows_workspace.argtypes = [C.c_int64, C.c_int32]
+    L.im_group_rows_workspace.restype = C.c_int64
+    L.im_group_rows.argtypes = [C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p,
+                                C.c_void_p, C.c_int64, C.c_void_p]
+    L.im_group_rows.restype = st
+    L.im_checkpoint_store.argtypes = [C.c_void_p, C.c_int64, C.c_int32, C.c_int64, C.c_int64,
+                                      C.POINTER(ImCheckpoint), C.c_void_p]
+    L.im_checkpoint_store.restype = st
+    L.im_checkpoint_load.argtypes = [C.POINTER(ImCheckpoint), C.c_int64, C.c_int64, C.c_void_p,
+                                     C.c_int64, C.c_int32, C.c_void_p]
+    L.im_checkpoint_load.restype = st
+    L.im_layer_norm.argtypes = [C.POINTER(ImNorm), C.c_void_p]
+    L.im_layer_norm.restype = st
+    L.im_layer_norm_grad_workspace.argtypes = [C.c_int64, C.c_int64]
+    L.im_layer_norm_grad_workspace.restype = C.c_int64
+    L.im_layer_norm_grad.argtypes = [C.POINTER(ImNormGrad), C.c_void_p]
+    L.im_layer_norm_grad.restype = st
+    L.im_expert_linear.argtypes = [C.POINTER(ImExpertLayer), C.c_void_p]
+    L.im_expert_linear.restype = st
+    L.im_expert_linear_grad_workspace.argtypes = [C.c_int64, C.c_int32, C.c_int32, C.c_int32]
+    L.im_expert_linear_grad_workspace.restype = C.c_int64
+    L.im_expert_linear_grad.argtypes = [C.POINTER(ImExpertLayerGrad), C.c_void_p]
+    L.im_expert_linear_grad.restype = st
     L.im_status_str.argtypes = [C.c_int]
     L.im_status_str.restype = C.c_char_p
     L.im_last_error.argtypes = []
@@ -291,6 +357,36 @@ def im_ppo_read(ctx, buffer, layer, dst_ptr=None, stream=None):
     r, c, e = C.c_int64(), C.c_int64(), C.c_int64()
     _check(lib().im_ppo_read(ctx, buffer, layer, dst_ptr, C.byref(r), C.byref(c), C.byref(e), stream))
     return r.value, c.value, e.value
+
+
+def im_group_rows(expert_ptr, n, n_experts, offsets_ptr, rows_ptr, workspace_ptr=None,
+                  workspace_bytes=0, stream=None):
+    _check(lib().im_group_rows(expert_ptr, n, n_experts, offsets_ptr, rows_ptr, workspace_ptr,
+                               workspace_bytes, stream))
+
+
+def im_checkpoint_store(x_ptr, ld_x, dtype, n, d, ckpt, stream=None):
+    _check(lib().im_checkpoint_store(x_ptr, ld_x, dtype, n, d, C.byref(ckpt), stream))
+
+
+def im_checkpoint_load(ckpt, n, d, x_ptr, ld_x, dtype, stream=None):
+    _check(lib().im_checkpoint_load(C.byref(ckpt), n, d, x_ptr, ld_x, dtype, stream))
+
+
+def im_layer_norm(args, stream=None):
+    _check(lib().im_layer_norm(C.byref(args), stream))
+
+
+def im_layer_norm_grad(args, stream=None):
+    _check(lib().im_layer_norm_grad(C.byref(args), stream))
+
+
+def im_expert_linear(args, stream=None):
+    _check(lib().im_expert_linear(C.byref(args), stream))
+
+
+def im_expert_linear_grad(args, stream=None):
+    _check(lib().im_expert_linear_grad(C.byref(args), stream))
 
 
 # ------------------------------------------------------------- conveniences
@@ -578,3 +674,224 @@ def ppo_batch(ro, perm, lr, stats=None):
                       ro.mean.data_ptr(), ro.logp.data_ptr(), ro.value.data_ptr(),
                       ro.advantage.data_ptr(), ro.ret.data_ptr(), ro.summary.data_ptr(),
                       perm.data_ptr(), lr.data_ptr(), None if stats is None else stats.data_ptr())
+
+
+# ---------------------------------------------------------- layers of experts
+def _dtype(t):
+    import torch
+    if t.dtype == torch.bfloat16:
+        return IM_DTYPE_BF16
+    if t.dtype == torch.float32:
+        return IM_DTYPE_F32
+    raise ValueError("expected a float32 or bfloat16 tensor, got %s" % t.dtype)
+
+
+def _ld(t, n, d, name, dev, dtype=None):
+    """Row stride of a matrix argument [n][d] of the current device."""
+    if tuple(t.shape) != (n, d) or (dtype is not None and t.dtype != dtype):
+        raise ValueError("%s must be [%d][%d]%s, got %s %s" % (
+            name, n, d, "" if dtype is None else " of %s" % dtype, list(t.shape), t.dtype))
+    if t.get_device() != dev:
+        raise ValueError("%s is not on the current device" % name)
+    if d > 1 and t.stride(1) != 1:
+        raise ValueError("%s: the values of a row must lie together" % name)
+    return max(t.stride(0), d) if n > 1 else d
+
+
+def _vec(t, n, name, dev, dtype):
+    """Pointer of a contiguous argument of n values (None: NULL)."""
+    if t is None:
+        return None
+    if t.numel() != n or t.dtype != dtype or not t.is_contiguous() or t.get_device() != dev:
+        raise ValueError("%s must be %d contiguous values of %s on the current device" % (
+            name, n, dtype))
+    return t.data_ptr()
+
+
+def _call_stream(stream):
+    """(device index, stream) of a call."""
+    import torch
+    if stream is None:
+        stream = torch.cuda.current_stream()
+    return stream.device_index, stream
+
+
+def _space(nbytes):
+    import torch
+    if nbytes < 0:
+        raise ValueError("sizes out of range")
+    return torch.empty(max(nbytes, 16), dtype=torch.uint8, device="cuda")
+
+
+def _workspace(given, need, stream):
+    """A call's workspace: the given one, or one of its own."""
+    if given is None:
+        given = need()
+        given.record_stream(stream)
+    return given.data_ptr(), given.numel() * given.element_size()
+
+
+class Checkpoint:
+    """An activation [n][d] kept in 8 bits: q int8 [n][d] and scale uint8
+    [n][ceil(d / 32)] tensors (rows may be strided)."""
+
+    def __init__(self, q, scale):
+        self.q, self.scale = q, scale
+
+    @classmethod
+    def empty(cls, n, d, device="cuda"):
+        import torch
+        return cls(torch.empty((n, d), dtype=torch.int8, device=device),
+                   torch.empty((n, -(-d // 32)), dtype=torch.uint8, device=device))
+
+    @property
+    def shape(self):
+        return self.q.shape
+
+    def struct(self, n, d, dev):
+        import torch
+        return ImCheckpoint(self.q.data_ptr(), self.scale.data_ptr(),
+                            _ld(self.q, n, d, "q", dev, torch.int8),
+                            _ld(self.scale, n, -(-d // 32), "scale", dev, torch.uint8))
+
+
+def checkpoint_store(x, ckpt, stream=None):
+    """x (float32 or bfloat16 [n][d]) into the checkpoint."""
+    dev, stream = _call_stream(stream)
+    n, d = x.shape
+    im_checkpoint_store(x.data_ptr(), _ld(x, n, d, "x", dev), _dtype(x), n, d,
+                        ckpt.struct(n, d, dev), stream.cuda_stream)
+
+
+def checkpoint_load(ckpt, x, stream=None):
+    """The checkpoint's values into x (float32 or bfloat16 [n][d])."""
+    dev, stream = _call_stream(stream)
+    n, d = x.shape
+    im_checkpoint_load(ckpt.struct(n, d, dev), n, d, x.data_ptr(), _ld(x, n, d, "x", dev),
+                       _dtype(x), stream.cuda_stream)
+
+
+def group_rows_workspace(n, n_experts):
+    """A workspace tensor for group_rows."""
+    return _space(lib().im_group_rows_workspace(n, n_experts))
+
+
+def group_rows(expert, offsets, rows, workspace=None, stream=None):
+    """Rows by expert: expert [n] int32 into offsets [n_experts + 1] and rows [n]
+    (int32)."""
+    import torch
+    dev, stream = _call_stream(stream)
+    n, e = expert.numel(), offsets.numel() - 1
+    i32 = torch.int32
+    ws, nbytes = _workspace(workspace, lambda: group_rows_workspace(n, e), stream)
+    im_group_rows(_vec(expert, n, "expert", dev, i32), n, e,
+                  _vec(offsets, e + 1, "offsets", dev, i32), _vec(rows, n, "rows", dev, i32),
+                  ws, nbytes, stream.cuda_stream)
+
+
+def layer_norm(x, gamma, beta, y, mean=None, rstd=None, eps=1e-5, checkpoint=None, stream=None):
+    """y = layer norm of the rows of x [n][d] (float32 or bfloat16), optionally its
+    row statistics [n] and the checkpoint of x."""
+    import torch
+    dev, stream = _call_stream(stream)
+    n, d = x.shape
+    f32 = torch.float32
+    ck = None if checkpoint is None else C.pointer(checkpoint.struct(n, d, dev))
+    im_layer_norm(ImNorm(n, d, _dtype(x), eps, x.data_ptr(), _ld(x, n, d, "x", dev),
+                         _vec(gamma, d, "gamma", dev, f32), _vec(beta, d, "beta", dev, f32),
+                         y.data_ptr(), _ld(y, n, d, "y", dev, x.dtype),
+                         _vec(mean, n, "mean", dev, f32), _vec(rstd, n, "rstd", dev, f32), ck),
+                  stream.cuda_stream)
+
+
+def layer_norm_grad_workspace(n, d):
+    """A workspace tensor for layer_norm_grad."""
+    return _space(lib().im_layer_norm_grad_workspace(n, d))
+
+
+def layer_norm_grad(dy, x, gamma, mean, rstd, dx=None, dgamma=None, dbeta=None, workspace=None,
+                    stream=None):
+    """Gradient of layer_norm; x: its input or the Checkpoint of it."""
+    import torch
+    dev, stream = _call_stream(stream)
+    n, d = dy.shape
+    f32 = torch.float32
+    ws, nbytes = None, 0
+    if dgamma is not None or dbeta is not None:
+        ws, nbytes = _workspace(workspace, lambda: layer_norm_grad_workspace(n, d), stream)
+    if isinstance(x, Checkpoint):
+        xp, ldx, ck = None, 0, C.pointer(x.struct(n, d, dev))
+    else:
+        xp, ldx, ck = x.data_ptr(), _ld(x, n, d, "x", dev, dy.dtype), None
+    im_layer_norm_grad(
+        ImNormGrad(n, d, _dtype(dy), dy.data_ptr(), _ld(dy, n, d, "dy", dev), xp, ldx, ck,
+                   _vec(gamma, d, "gamma", dev, f32), _vec(mean, n, "mean", dev, f32),
+                   _vec(rstd, n, "rstd", dev, f32), _dptr(dx),
+                   0 if dx is None else _ld(dx, n, d, "dx", dev, dy.dtype),
+                   _vec(dgamma, d, "dgamma", dev, f32), _vec(dbeta, d, "dbeta", dev, f32),
+                   ws, nbytes), stream.cuda_stream)
+
+
+def _expert_ld(t, e, out, in_, name, dev, dtype):
+    """Row stride of [n_experts][out][in] weights."""
+    if tuple(t.shape) != (e, out, in_) or t.dtype != dtype or t.get_device() != dev:
+        raise ValueError("%s must be [%d][%d][%d] of %s on the current device, got %s %s" % (
+            name, e, out, in_, dtype, list(t.shape), t.dtype))
+    ld = max(t.stride(1), in_) if out > 1 else (t.stride(0) if e > 1 else in_)
+    if (in_ > 1 and t.stride(2) != 1) or (e > 1 and t.stride(0) != out * ld):
+        raise ValueError("%s: rows of values that lie together, one stride over all rows" % name)
+    return ld
+
+
+def expert_linear(x, w, bias, offsets, rows, y, relu=False, stream=None):
+    """y[r] = w[e] x[r] + bias[e] (ReLU with relu), e the expert of row r by group_rows'
+    offsets and rows (rows None: grouped already).  x [n][in] and w [n_experts][out][in]
+    bfloat16, bias [n_experts][out] float32 or None, y [n][out] bfloat16 or float32."""
+    import torch
+    dev, stream = _call_stream(stream)
+    n, in_ = x.shape
+    e, out = w.shape[0], w.shape[1]
+    i32 = torch.int32
+    im_expert_linear(
+        ImExpertLayer(n, e, in_, out, _dtype(x), _dtype(y), 1 if relu else 0,
+                      _vec(offsets, e + 1, "offsets", dev, i32), _vec(rows, n, "rows", dev, i32),
+                      x.data_ptr(), _ld(x, n, in_, "x", dev), w.data_ptr(),
+                      _expert_ld(w, e, out, in_, "w", dev, x.dtype),
+                      _vec(bias, e * out, "bias", dev, torch.float32), y.data_ptr(),
+                      _ld(y, n, out, "y", dev)), stream.cuda_stream)
+
+
+def expert_linear_grad_workspace(n, n_experts, in_, out):
+    """A workspace tensor for expert_linear_grad."""
+    return _space(lib().im_expert_linear_grad_workspace(n, n_experts, in_, out))
+
+
+def expert_linear_grad(dy, x, w, offsets, rows, dx=None, dw=None, db=None, relu_x=False,
+                       workspace=None, stream=None):
+    """Gradients of expert_linear for dy [n][out] bfloat16: dx [n][in] bfloat16, dw
+    [n_experts][out][in] and db [n_experts][out] float32 (each may be None).  x: the
+    layer's input or the Checkpoint of it; relu_x: it is a ReLU's output, dx is the
+    gradient before it."""
+    import torch
+    dev, stream = _call_stream(stream)
+    n, out = dy.shape
+    e, _, in_ = w.shape
+    i32, f32, bf16 = torch.int32, torch.float32, torch.bfloat16
+    ws, nbytes = None, 0
+    if dw is not None or db is not None:
+        ws, nbytes = _workspace(workspace, lambda: expert_linear_grad_workspace(n, e, in_, out),
+                                stream)
+    xp, ldx, ck = None, 0, None
+    if isinstance(x, Checkpoint):
+        ck = C.pointer(x.struct(n, in_, dev))
+    elif x is not None:
+        xp, ldx = x.data_ptr(), _ld(x, n, in_, "x", dev, dy.dtype)
+    im_expert_linear_grad(
+        ImExpertLayerGrad(n, e, in_, out, _dtype(dy), 1 if relu_x else 0,
+                          _vec(offsets, e + 1, "offsets", dev, i32),
+                          _vec(rows, n, "rows", dev, i32), dy.data_ptr(),
+                          _ld(dy, n, out, "dy", dev), xp, ldx, ck, w.data_ptr(),
+                          _expert_ld(w, e, out, in_, "w", dev, bf16), _dptr(dx),
+                          0 if dx is None else _ld(dx, n, in_, "dx", dev, bf16), _dptr(dw),
+                          0 if dw is None else _expert_ld(dw, e, out, in_, "dw", dev, f32),
+                          _vec(db, e * out, "db", dev, f32), ws, nbytes), stream.cuda_stream)

@@ -17,7 +17,8 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libinstantmimic.so")
 SOURCES = ["api.hip", "env_kernels.hip", "policy_kernels.hip", "layer_kernels.hip",
-           "rollout_kernels.hip", "train_kernels.hip", "calib_kernels.hip"]
+           "rollout_kernels.hip", "train_kernels.hip", "calib_kernels.hip", "expert_kernels.hip",
+           "norm_kernels.hip", "expert_api.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

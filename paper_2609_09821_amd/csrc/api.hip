@@ -12,6 +12,7 @@
 #include <vector>
 
 #include "../../include/instantmimic.h"
+#include "expert.h"
 #include "launch.h"
 
 using namespace im;
@@ -92,6 +93,15 @@ im_status hip_fail(hipError_t e, const char *what)
 {
     return fail(IM_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
 }
+
+}  // namespace
+
+namespace im {
+im_status api_fail(im_status s, const char *msg) { return fail(s, msg); }
+im_status api_hip_fail(hipError_t e, const char *what) { return hip_fail(e, what); }
+}  // namespace im
+
+namespace {
 
 int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
