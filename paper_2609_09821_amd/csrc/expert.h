@@ -79,16 +79,13 @@ struct ExpertArgs {
     float *dw;                       // [E][out][in], null: not wanted
     int64_t ld_dw;
     float *db;                       // [E][out], null: not wanted
-    // weight gradient: pieces of at most `piece` rows of one expert; an expert of
-    // several pieces leaves each one's sums in `part` ([piece][out][in4], in4 = in
-    // rounded up to 4) and `part_db` ([piece][out])
-    int piece;
+    // weight gradient: parts of the experts that several teams' runs share, 2 slots a team of
+    // [out][in4] (in4 = in rounded up to 4) and of [out]
     float *part, *part_db;
 };
 hipError_t launch_expert_linear(const ExpertArgs &a, hipStream_t s);
-// Pieces of the weight gradient: rows of one (a multiple of 64) and a bound on their number.
-int expert_piece_rows(int64_t n, int n_experts, int in, int out);
-int64_t expert_pieces(int64_t n, int n_experts, int in, int out);
+// Teams of blocks among which the weight gradient's rows are divided.
+int expert_grad_teams(int64_t n, int in, int out);
 hipError_t launch_expert_grad(const ExpertArgs &a, hipStream_t s);
 
 }  // namespace im

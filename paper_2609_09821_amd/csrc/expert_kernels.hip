@@ -202,24 +202,20 @@ struct Piece {
     int e;         // its expert; E: the places without one; -1: no such tile
     int first;     // first place
     int count;     // places (<= unit)
-    int index;     // the tile's number among its expert's
-    int of;        // tiles of its expert
 };
 
 // Tile t when each expert's places are cut into tiles of `unit` places (the last one
-// shorter), the places without an expert after them if REST.  Every lane of the
-// wavefront calls it with the same t; offsets are held within [0, n].  EVEN: an expert's
-// tiles are of one size, a multiple of 64 places.
-template <bool REST, bool EVEN>
+// shorter), the places without an expert after them.  Every lane of the wavefront
+// calls it with the same t; offsets are held within [0, n].
 __device__ __forceinline__ Piece find_piece(const int32_t *offsets, int E, int n, int t, int unit)
 {
     const int lane = threadIdx.x & 63;
-    Piece p{-1, 0, 0, 0, 0};
+    Piece p{-1, 0, 0};
     int carry = 0;
     for (int e0 = 0; e0 <= E; e0 += 64) {
         const int e = e0 + lane;
         int a = 0, b = 0;
-        if (e < E || (REST && e == E)) {
+        if (e <= E) {
             a = min(max(offsets[e], 0), n);
             b = e < E ? min(max(offsets[e + 1], a), n) : n;
         }
@@ -235,11 +231,9 @@ __device__ __forceinline__ Piece find_piece(const int32_t *offsets, int E, int n
             const int l = __builtin_ctzll(hit);
             const int la = __builtin_amdgcn_readlane(a, l), lb = __builtin_amdgcn_readlane(b, l);
             p.e = e0 + l;
-            p.of = __builtin_amdgcn_readlane(k, l);
-            p.index = t - (carry + __builtin_amdgcn_readlane(s, l) - p.of);
-            const int size = EVEN ? ((lb - la + p.of - 1) / p.of + 63) / 64 * 64 : unit;
-            p.first = min(la + p.index * size, lb);
-            p.count = min(size, lb - p.first);
+            const int index = t - (carry + __builtin_amdgcn_readlane(s, l) - __builtin_amdgcn_readlane(k, l));
+            p.first = la + index * unit;
+            p.count = min(unit, lb - p.first);
             return p;
         }
         carry += __builtin_amdgcn_readlane(s, 63);
@@ -261,143 +255,296 @@ __device__ __forceinline__ int row_at(const ExpertArgs &a, int p)
 //   dw       q = output, p = input,  k = row      Q = dy^T, P = x^T (k across)
 // A block of WP x WQ wavefronts forms BP x BQ of C, a wavefront TP x TQ tiles of
 // v_mfma_f32_32x32x16_bf16, whose accumulator gives a lane one q and four
-// consecutive p per register group.  K steps of 64 through two LDS stages, the
-// next step's loads in flight in registers while a step is multiplied.
+// consecutive p per register group.
 //
-// A tile with k along its rows lies in LDS rows of 72 bf16 (144 bytes: fragment
-// reads meet no bank twice); one with k across lies as in memory, [64 k][columns],
-// in rows of 32 more columns, and its fragments are read transposed (in every
-// 16-lane group, lane 4j+q addresses row k0+j, columns c0+4q.., and lane l receives
-// rows k0..k0+3 of column c0+l).
+// K steps of BK go through a ring of NS stages in LDS.  Operands whose rows are 16-byte
+// aligned are copied into it by direct loads (16 bytes a lane, no registers between),
+// NS - 1 steps ahead; others (odd row strides) pass through D sets of registers, D steps
+// ahead.  A step waits for its own loads only (vmcnt counts the later ones) and has
+// one barrier.
+//
+// A direct load writes 64 consecutive 16-byte pieces, so a stage has no padding;
+// pieces are permuted in their row instead, by the address that each lane loads:
+//   k along: rows of BK values, piece c of row r at c ^ (r / (128 / BK)) mod (BK / 8):
+//     16 rows' pieces of one k cover all banks;
+//   k across: rows of N columns, 64-byte quarters permuted by the row: the four rows x
+//     64 bytes that a half wavefront reads transposed cover all banks (in every 16-lane
+//     group, lane 4j+q addresses row k0+j, columns c0+4q.., and lane l receives rows
+//     k0..k0+3 of column c0+l).
 // ---------------------------------------------------------------------------
-enum { OP_FORWARD, OP_DX, OP_DW };
+enum { OP_FORWARD, OP_DX };
 
-constexpr int BK = 64;
+__device__ const uint4 zero_piece = {0, 0, 0, 0};
 
-// LDS elements of a tile of C columns (rows) and 64 k.
-constexpr int along_lds(int rows) { return rows * (BK + 8); }
-constexpr int across_lds(int cols) { return BK * (cols + 32); }
+// Copies 16 bytes a lane to LDS at `to` (the same in every lane) + 16 lane.
+__device__ __forceinline__ void copy_to_lds(const void *from, char *to)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)from,
+                                     (IM_LDS3 uint32_t *)to, 16, 0, 0);
+}
 
-// 16-byte pieces of a tile with k along its rows: thread t holds piece t % 8 of
-// the rows t / 8 + c NT / 8.
-template <int R, int NT>
+// Copies a byte a lane, as a word, to `to` + 4 lane.
+__device__ __forceinline__ void copy_byte_to_lds(const void *from, char *to)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)from,
+                                     (IM_LDS3 uint32_t *)to, 1, 0, 0);
+}
+
+// All but the wavefront's N last loads are done, and its LDS accesses.
+template <int N>
+__device__ __forceinline__ void wait_loads()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+}
+
+// The block meets; LDS accesses stay on their side.
+__device__ __forceinline__ void meet()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Waits for a step that `later` steps of L loads each follow (M of them at most).
+template <int L, int M>
+__device__ __forceinline__ void wait_for_step(int later)
+{
+    if constexpr (M > 0) {
+        if (later >= M) wait_loads<M * L>();
+        else wait_for_step<L, M - 1>(later);
+    } else {
+        wait_loads<0>();
+    }
+}
+
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
+// The first nv values (of eight at p, the row ending at p + nv; nv may be negative) of a
+// row that holds at least 8, zeros after them: the row's last eight, shifted.
+__device__ __forceinline__ u32x4_r load8_end(const uint16_t *p, int nv)
+{
+    const int n = min(nv, 8);
+    u32x4_r r = *(const u32x4_a2 *)(p + (n - 8));
+    uint64_t lo = r[0] | (uint64_t)r[1] << 32, hi = r[2] | (uint64_t)r[3] << 32;
+    int gone = 8 - max(n, 0);
+    if (gone >= 4) lo = hi, hi = 0, gone -= 4;
+    if (gone == 4) lo = 0;
+    const int s = 16 * (gone & 3);
+    if (s) lo = lo >> s | hi << (64 - s), hi >>= s;
+    const u32x4_r o = {(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+    return o;
+}
+
+// A tile of R rows with k along them.  Thread t holds pieces u of the rows row(u).
+template <int R, int NT, int BK, int D>
 struct AlongTile {
-    static constexpr int C = R * 8 / NT;
-    const uint16_t *p[C];
-    u32x4_r v[C];
-    // row(i): the address of row i of the tile (one that can be read, for all i < R)
+    static constexpr int PITCH = BK * 2, SLOTS = BK / 8, U = R * PITCH / (NT * 16), BYTES = R * PITCH;
+    static constexpr int READS = 1;      // LDS reads of a fragment
+    static_assert(U * NT * 16 == BYTES, "whole pieces");
+    const uint16_t *p[U];
+    u32x4_r v[D][U];
+    __device__ static int row(int u) { return (u * (NT / 64) + wave_id()) * (64 / SLOTS) + (threadIdx.x & 63) / SLOTS; }
+    __device__ static int perm(int r) { return BK == 32 ? (r >> 2) & 3 : (r >> 1) & 7; }
+    __device__ static int col() { return (((int)threadIdx.x & (SLOTS - 1)) ^ perm(row(0))) * 8; }
+    // at(i): the address of row i of the tile (one that can be read, for all i < R)
     template <typename F>
-    __device__ __forceinline__ void init(F row)
+    __device__ __forceinline__ void init(F at)
     {
 #pragma unroll
-        for (int c = 0; c < C; ++c) p[c] = row(threadIdx.x / 8 + c * (NT / 8)) + (threadIdx.x & 7) * 8;
+        for (int u = 0; u < U; ++u) p[u] = at(row(u)) + col();
     }
-    // K step kt of K values
-    __device__ __forceinline__ void load(int kt, int K)
+    // piece u of a step of BK values
+    __device__ __forceinline__ void copy(int u, int kt, char *lds)
     {
+        copy_to_lds(p[u] + kt * BK, lds + (u * (NT / 64) + wave_id()) * 1024);
+    }
+    // the step's valid ones of K values in all, through register set d
+    __device__ __forceinline__ void load(int d, int kt, int K)
+    {
+        const int nv = K - kt * BK - col();
         if ((kt + 1) * BK <= K) {
 #pragma unroll
-            for (int c = 0; c < C; ++c) v[c] = *(const u32x4_a2 *)(p[c] + kt * BK);
+            for (int u = 0; u < U; ++u) v[d][u] = *(const u32x4_a2 *)(p[u] + kt * BK);
+        } else if (K >= 8) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[d][u] = load8_end(p[u] + kt * BK, nv);
         } else {
-            const int nv = K - kt * BK - (threadIdx.x & 7) * 8;
 #pragma unroll
-            for (int c = 0; c < C; ++c) v[c] = load8_bits(p[c] + kt * BK, nv);
+            for (int u = 0; u < U; ++u) v[d][u] = load8_bits(p[u] + kt * BK, nv);
         }
     }
-    __device__ __forceinline__ void store(uint16_t *lds) const
+    __device__ __forceinline__ void store(int d, char *lds) const
     {
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-            *(u32x4_r *)(lds + (threadIdx.x / 8 + c * (NT / 8)) * (BK + 8) + (threadIdx.x & 7) * 8) = v[c];
+        for (int u = 0; u < U; ++u)
+            *(u32x4_r *)(lds + (u * (NT / 64) + wave_id()) * 1024 + (threadIdx.x & 63) * 16) = v[d][u];
+    }
+    // 8 consecutive k (of substep s) of 32 rows: lane l row l % 32, k + 8 (l / 32)..
+    __device__ static bf16x8_t frag(const char *lds, int row, int s)
+    {
+        const int lane = threadIdx.x & 63, r = lane & 31;
+        const int at = r * PITCH + (((lane >> 5) ^ perm(r)) << 4);
+        return *(const bf16x8_t *)(lds + row * PITCH + (at ^ (s << 5)));
     }
 };
 
-// A fragment (8 consecutive k of 32 rows) of such a tile: lane l row l % 32, k + 8 (l / 32)..
-__device__ __forceinline__ bf16x8_t along_frag(const uint16_t *lds, int row, int k)
-{
-    const int lane = threadIdx.x & 63;
-    return *(const bf16x8_t *)(lds + (row + (lane & 31)) * (BK + 8) + k + 8 * (lane >> 5));
-}
-
-// A tile of 64 k rows of N columns: thread t holds the 16-byte piece t % (N / 8) of
-// rows t / (N / 8) + c NT / (N / 8).
-template <int N, int NT>
+// A tile of BK k rows of N columns, of which the thread's nv columns from its own first one
+// on exist.
+template <int N, int NT, int BK, int D>
 struct AcrossTile {
-    static constexpr int PR = N / 8, C = BK * PR / NT;
-    u32x4_r v[C];
-    __device__ static int piece() { return threadIdx.x % PR; }
-    __device__ static int krow(int c) { return threadIdx.x / PR + c * (NT / PR); }
-    // row(i): the address of k row i of the step, null for none; nv: valid columns from
-    // this thread's piece on
+    static constexpr int PITCH = N * 2, SLOTS = N / 8, U = BK * PITCH / (NT * 16), BYTES = BK * PITCH;
+    static constexpr int READS = 2;
+    static_assert(U * NT * 16 == BYTES, "whole pieces");
+    u32x4_r v[D][U];
+    __device__ static int krow(int u) { return ((u * (NT / 64) + wave_id()) * 64 + (threadIdx.x & 63)) / SLOTS; }
+    // quarter permutation of row k; the same for the rows of one thread
+    __device__ static int perm(int k) { return N >= 128 ? k & 3 : (k >> 1) & 1; }
+    __device__ static int col() { return (((int)threadIdx.x & (SLOTS - 1)) ^ (perm(krow(0)) << 2)) * 8; }
+    // Piece u from `from`, the address of this thread's first column in k row krow(u), null
+    // for none.  A piece that holds a valid column is read whole: 16 aligned bytes lie in one
+    // page, and what they hold past the row's end meets columns that are not stored.
+    __device__ __forceinline__ void copy(int u, const uint16_t *from, char *lds)
+    {
+        copy_to_lds(from ? (const void *)from : (const void *)&zero_piece, lds + (u * (NT / 64) + wave_id()) * 1024);
+    }
+    // at(u): that address for any nv; whole: nv >= 8 in all threads; wide: the row holds 8
     template <typename F>
-    __device__ __forceinline__ void load(F row, int nv)
+    __device__ __forceinline__ void load(int d, F at, int nv, bool whole, bool wide)
     {
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const uint16_t *p = row(krow(c));
-            v[c] = load8_bits(p + piece() * 8, p ? nv : 0);
+        for (int u = 0; u < U; ++u) {
+            const uint16_t *p = at(u);
+            if (whole) v[d][u] = *(const u32x4_a2 *)(p ? p : (const uint16_t *)&zero_piece);
+            else if (wide) v[d][u] = load8_end(p ? p : (const uint16_t *)&zero_piece, p ? nv : 8);
+            else v[d][u] = load8_bits(p, p ? nv : 0);
         }
     }
-    __device__ __forceinline__ void store(uint16_t *lds) const
+    __device__ __forceinline__ void store(int d, char *lds) const
     {
 #pragma unroll
-        for (int c = 0; c < C; ++c) *(u32x4_r *)(lds + krow(c) * (N + 32) + piece() * 8) = v[c];
+        for (int u = 0; u < U; ++u)
+            *(u32x4_r *)(lds + (u * (NT / 64) + wave_id()) * 1024 + (threadIdx.x & 63) * 16) = v[d][u];
+    }
+    __device__ static bf16x8_t frag(const char *lds, int col, int s)
+    {
+        const int lane = threadIdx.x & 63, gi = lane >> 4, si = lane & 15;
+        const int k = 8 * (gi >> 1) + (si >> 2);
+        const char *p = lds + (s * 16 + k) * PITCH + (((col >> 5) ^ perm(k)) << 6) + 32 * (gi & 1) + 8 * (si & 3);
+        const v4s_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((IM_LDS3 v4s_t *)p);
+        const v4s_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((IM_LDS3 v4s_t *)(p + 4 * PITCH));
+        const short v8[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        return __builtin_bit_cast(bf16x8_t, v8);
     }
 };
 
-// The same from a checkpoint: bytes and scales are held until the store, which
-// restores the values (exact in bf16).
-template <int N, int NT>
-struct AcrossCkpt {
-    static constexpr int PR = N / 8, C = BK * PR / NT;
-    u32x2_r v[C];
-    int scale[C];
-    __device__ static int piece() { return threadIdx.x % PR; }
-    __device__ static int krow(int c) { return threadIdx.x / PR + c * (NT / PR); }
-    // row(i): k row i's index, negative for none; col: the tile's first column
+// The same from a checkpoint through registers: bytes and scales are held until the
+// store, which restores the values (exact in bf16).
+template <int N, int NT, int BK, int D>
+struct AcrossCkpt : AcrossTile<N, NT, BK, 1> {
+    using B = AcrossTile<N, NT, BK, 1>;
+    u32x2_r q[D][B::U];
+    int scale[D][B::U];
+    // row(u): the index of k row krow(u), negative for none; col: this thread's first column
     template <typename F>
-    __device__ __forceinline__ void load(const im_checkpoint &q, F row, int col, int nv)
+    __device__ __forceinline__ void load(int d, const im_checkpoint &c, F row, int col, int nv)
     {
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int r = row(krow(c));
-            const int m = r >= 0 ? nv : 0;
-            const int at = col + piece() * 8;
-            v[c] = load8_bytes(q.q + (int64_t)r * q.ld_q + at, m);
-            scale[c] = m > 0 ? q.scale[(int64_t)r * q.ld_scale + (at >> 5)] : 0;
+        for (int u = 0; u < B::U; ++u) {
+            const int r = row(u), m = r >= 0 ? nv : 0;
+            q[d][u] = load8_bytes(c.q + (int64_t)r * c.ld_q + col, m);
+            scale[d][u] = m > 0 ? c.scale[(int64_t)r * c.ld_scale + (col >> 5)] : 0;
         }
     }
-    __device__ __forceinline__ void store(uint16_t *lds) const
+    __device__ __forceinline__ void store(int d, char *lds)
     {
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
+        for (int u = 0; u < B::U; ++u) {
             float f[8];
-            ckpt_unpack(v[c], scale[c], f);
-            *(u32x4_r *)(lds + krow(c) * (N + 32) + piece() * 8) = pack8(f);
+            ckpt_unpack(q[d][u], scale[d][u], f);
+            this->v[0][u] = pack8(f);
+        }
+        B::store(0, lds);
+    }
+};
+
+// A checkpoint by direct loads: the bytes of BK rows x N columns go to a ring of their own
+// in LDS, 16 a lane with their scale; each lane restores what it copied itself into the
+// tile that the fragments are read from.
+template <int N, int NT, int BK>
+struct CkptBytes {
+    static constexpr int SLOTS = N / 16, U = BK * N / (NT * 16), BYTES = BK * N + U * NT * 4;
+    static_assert(U * NT * 16 == BK * N, "whole pieces");
+    __device__ static int krow(int u) { return ((u * (NT / 64) + wave_id()) * 64 + (threadIdx.x & 63)) / SLOTS; }
+    __device__ static int col() { return ((int)threadIdx.x & (SLOTS - 1)) * 16; }
+    // row: k row krow(u)'s index, negative for none; col: this thread's first column, < 0 past the last
+    __device__ __forceinline__ static void copy(int u, const im_checkpoint &c, int64_t row, int col, char *lds)
+    {
+        const bool on = row >= 0 && col >= 0;
+        const int at = u * (NT / 64) + wave_id();
+        copy_to_lds(on ? (const void *)(c.q + row * c.ld_q + col) : (const void *)&zero_piece, lds + at * 1024);
+        copy_byte_to_lds(on ? (const void *)(c.scale + row * c.ld_scale + (col >> 5)) : (const void *)&zero_piece,
+                         lds + BK * N + at * 256);
+    }
+    __device__ __forceinline__ static void restore(const char *lds, char *tile)
+    {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int at = u * (NT / 64) + wave_id(), k = krow(u);
+            const u32x4_r q = *(const u32x4_r *)(lds + at * 1024 + lane * 16);
+            const int scale = *(const int *)(lds + BK * N + at * 256 + lane * 4);
+            float f[16];
+            ckpt_unpack(u32x2_r{q[0], q[1]}, scale, f);
+            ckpt_unpack(u32x2_r{q[2], q[3]}, scale, f + 8);
+            char *to = tile + k * (N * 2) + (((col() >> 3) ^ (AcrossTile<N, NT, BK, 1>::perm(k) << 2)) << 4);
+            *(u32x4_r *)to = pack8(f);
+            *(u32x4_r *)(to + 16) = pack8(f + 8);
         }
     }
 };
 
-template <int N>
-__device__ __forceinline__ bf16x8_t across_frag(const uint16_t *lds, int col, int k)
+// One K step's products from a stage in LDS.  The fragments of a substep are read while
+// the one before is multiplied, and the next steps' direct loads (copy(u), u < COPIES) are
+// issued a few at a time: a read after each MFMA and a load now and then, held there by
+// the scheduler.  Left alone it reads a few fragments, waits for them and multiplies;
+// with all loads first, every wavefront stands at its loads before its first product.
+// last(): work for the vector units beside the last substep's products.
+template <typename P, typename Q, int TP, int TQ, int BK, int COPIES, typename F, typename G>
+__device__ __forceinline__ void multiply_step(const char *ps, const char *qs, int wp, int wq, f32x16_t (&acc)[TP][TQ],
+                                              F copy, G last)
 {
-    const int lane = threadIdx.x & 63, gi = lane >> 4, si = lane & 15;
-    const uint16_t *p = lds + (k + 8 * (gi >> 1) + (si >> 2)) * (N + 32) + col + 16 * (gi & 1) + 4 * (si & 3);
-    const v4s_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((IM_LDS3 v4s_t *)p);
-    const v4s_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((IM_LDS3 v4s_t *)(p + 4 * (N + 32)));
-    const short v8[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-    return __builtin_bit_cast(bf16x8_t, v8);
+    constexpr int S = BK / 16;
+    bf16x8_t fp[2][TP], fq[2][TQ];
+    auto read = [&](int s) {
+#pragma unroll
+        for (int i = 0; i < TP; ++i) fp[s & 1][i] = P::frag(ps, wp + 32 * i, s);
+#pragma unroll
+        for (int j = 0; j < TQ; ++j) fq[s & 1][j] = Q::frag(qs, wq + 32 * j, s);
+    };
+    read(0);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+        constexpr int READS = TP * P::READS + TQ * Q::READS, M = TP * TQ, EACH = (READS + M - 1) / M;
+        const int c0 = COPIES * s / S, c1 = COPIES * (s + 1) / S;
+        if (s + 1 < S) read(s + 1);
+#pragma unroll
+        for (int u = c0; u < c1; ++u) copy(u);
+        if (s + 1 == S) last();
+#pragma unroll
+        for (int i = 0; i < TP; ++i)
+#pragma unroll
+            for (int j = 0; j < TQ; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp[s & 1][i], fq[s & 1][j], acc[i][j], 0, 0, 0);
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            if (s + 1 < S && m * EACH < READS) __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
+            if ((m + 1) * (c1 - c0) / M > m * (c1 - c0) / M) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
 }
-
-template <int OP, int WP, int WQ, int TP, int TQ>
-struct Tile {
-    static constexpr int NT = 64 * WP * WQ, BP = 32 * WP * TP, BQ = 32 * WQ * TQ;
-    static constexpr int P_LDS = OP == OP_FORWARD ? along_lds(BP) : across_lds(BP);
-    static constexpr int Q_LDS = OP == OP_DW ? across_lds(BQ) : along_lds(BQ);
-    static constexpr int STAGE = P_LDS + Q_LDS;
-    static constexpr int LDO = BP + 8;      // epilogue rows
-    static constexpr int LDS = 2 * STAGE > BQ * LDO || OP == OP_DW ? 2 * STAGE : BQ * LDO;
-};
 
 template <int TP, int TQ>
 __device__ __forceinline__ void clear(f32x16_t (&acc)[TP][TQ])
@@ -414,22 +561,39 @@ __device__ __forceinline__ void clear(f32x16_t (&acc)[TP][TQ])
 // Forward and input gradient: C rows are places.  Blocks p-tile fastest, blocks of
 // one XCD consecutive: the tiles that read one set of rows share an L2.
 // ---------------------------------------------------------------------------
-template <int OP, int WP, int WQ, int TP, int TQ>
-__global__ __launch_bounds__(64 * WP * WQ) void expert_rows_kernel(ExpertArgs a, int p_tiles)
+template <int OP, int WP, int WQ, int TP, int TQ, int BK, int D>
+struct RowsTile {
+    static constexpr int NT = 64 * WP * WQ, BP = 32 * WP * TP, BQ = 32 * WQ * TQ;
+    using P = std::conditional_t<OP == OP_FORWARD, AlongTile<BP, NT, BK, D>, AcrossTile<BP, NT, BK, D>>;
+    using Q = AlongTile<BQ, NT, BK, D>;
+    static constexpr int STAGE = P::BYTES + Q::BYTES;
+    static constexpr int LDO = BP + 8;      // epilogue rows
+};
+
+// DIRECT: by direct loads, NS stages (D register sets for the last, shorter step: 1); else
+// through D register sets and two stages.
+template <int OP, int WP, int WQ, int TP, int TQ, int BK, int NS, int D, bool DIRECT>
+__global__ __launch_bounds__(64 * WP * WQ, 2) void expert_rows_kernel(ExpertArgs a, int p_tiles)
 {
-    using T = Tile<OP, WP, WQ, TP, TQ>;
+    static_assert(DIRECT ? D == 1 : NS == 2, "stages");
+    using T = RowsTile<OP, WP, WQ, TP, TQ, BK, D>;
     constexpr int NT = T::NT, BP = T::BP, BQ = T::BQ;
-    __shared__ __attribute__((aligned(16))) uint16_t lds[T::LDS];
+    constexpr int LDS = std::max(NS * T::STAGE, BQ * T::LDO * 2);
+    __shared__ __attribute__((aligned(1024))) char lds[LDS];
     __shared__ int row_of[BQ];
+    __shared__ __attribute__((aligned(16))) float bias[OP == OP_FORWARD ? BP : 4];
     const int id = xcd_order(blockIdx.x, gridDim.x);
-    const Piece pc = find_piece<true, false>(a.offsets, a.E, a.n, id / p_tiles, BQ);
+    const Piece pc = find_piece(a.offsets, a.E, a.n, id / p_tiles, BQ);
     if (pc.e < 0) return;
     const int p0 = id % p_tiles * BP;
     const int NP = OP == OP_FORWARD ? a.out : a.in, K = OP == OP_FORWARD ? a.in : a.out;
     for (int i = threadIdx.x; i < BQ; i += NT) row_of[i] = i < pc.count ? row_at(a, pc.first + i) : -1;
+    if constexpr (OP == OP_FORWARD)
+        for (int i = threadIdx.x; i < BP; i += NT)
+            bias[i] = a.bias && pc.e < a.E && p0 + i < NP ? a.bias[(int64_t)pc.e * a.out + p0 + i] : 0.0f;
     __syncthreads();
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
     const int wp = wave % WP * TP * 32, wq = wave / WP * TQ * 32;
     f32x16_t acc[TP][TQ];
     clear(acc);
@@ -437,69 +601,101 @@ __global__ __launch_bounds__(64 * WP * WQ) void expert_rows_kernel(ExpertArgs a,
         const uint16_t *q = OP == OP_FORWARD ? a.x : a.dy;
         const int64_t ldq = OP == OP_FORWARD ? a.ld_x : a.ld_dy;
         const uint16_t *w = a.w + (int64_t)pc.e * a.out * a.ld_w;
-        AlongTile<BQ, NT> tq;
+        typename T::P tp;
+        typename T::Q tq;
         // rows past the tile's last read row 0: their sums are not stored
         tq.init([&](int i) { return q + (int64_t)max(row_of[i], 0) * ldq; });
-        const int nk = (K + BK - 1) / BK;
-        auto multiply = [&](const uint16_t *ps, const uint16_t *qs) {
-#pragma unroll
-            for (int s = 0; s < BK; s += 16) {
-                bf16x8_t fp[TP], fq[TQ];
-#pragma unroll
-                for (int i = 0; i < TP; ++i) {
-                    if constexpr (OP == OP_FORWARD) fp[i] = along_frag(ps, wp + 32 * i, s);
-                    else fp[i] = across_frag<BP>(ps, wp + 32 * i, s);
-                }
-#pragma unroll
-                for (int j = 0; j < TQ; ++j) fq[j] = along_frag(qs, wq + 32 * j, s);
-#pragma unroll
-                for (int i = 0; i < TP; ++i)
-#pragma unroll
-                    for (int j = 0; j < TQ; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp[i], fq[j], acc[i][j], 0, 0, 0);
-            }
-        };
-        auto loop = [&](auto &tp, auto load_p) {
-            load_p(0);
-            tq.load(0, K);
-            tp.store(lds);
-            tq.store(lds + T::P_LDS);
-            __syncthreads();
-            if (nk > 1) load_p(1), tq.load(1, K);
-            for (int kt = 0; kt < nk; ++kt) {
-                const uint16_t *st = lds + (kt & 1) * T::STAGE;
-                multiply(st, st + T::P_LDS);
-                if (kt + 1 < nk) {
-                    uint16_t *nx = lds + (~kt & 1) * T::STAGE;
-                    tp.store(nx);
-                    tq.store(nx + T::P_LDS);
-                }
-                if (kt + 2 < nk) load_p(kt + 2), tq.load(kt + 2, K);
-                __syncthreads();
-            }
-        };
+        const uint16_t *wcol = nullptr;
+        int nvp = 0;
         if constexpr (OP == OP_FORWARD) {
-            AlongTile<BP, NT> tp;
             tp.init([&](int i) { return w + (int64_t)min(p0 + i, NP - 1) * a.ld_w; });
-            loop(tp, [&](int kt) { tp.load(kt, K); });
         } else {
-            AcrossTile<BP, NT> tp;
-            const int nv = NP - p0 - tp.piece() * 8;
-            loop(tp, [&](int kt) {
-                tp.load([&](int k) { return kt * BK + k < K ? w + (int64_t)(kt * BK + k) * a.ld_w + p0 : nullptr; }, nv);
-            });
+            nvp = NP - p0 - tp.col();
+            wcol = w + p0 + tp.col();
+        }
+        constexpr int L = T::P::U + T::Q::U;      // direct loads of a step
+        auto copy = [&](int u, int kt, char *st) {
+            if (u >= T::P::U) tq.copy(u - T::P::U, kt, st + T::P::BYTES);
+            else if constexpr (OP == OP_FORWARD) tp.copy(u, kt, st);
+            else tp.copy(u, nvp > 0 ? wcol + (int64_t)(kt * BK + tp.krow(u)) * a.ld_w : nullptr, st);
+        };
+        auto load = [&](int d, int kt) {
+            if constexpr (OP == OP_FORWARD)
+                tp.load(d, kt, K);
+            else
+                tp.load(d, [&](int u) -> const uint16_t * {
+                    const int k = kt * BK + tp.krow(u);
+                    return k < K ? wcol + (int64_t)k * a.ld_w : nullptr;
+                }, nvp, NP - p0 >= BP, NP >= 8);
+            tq.load(d, kt, K);
+        };
+        auto store = [&](int d, char *st) {
+            tp.store(d, st);
+            tq.store(d, st + T::P::BYTES);
+        };
+        int now = 0;     // stage of step kt
+        // a step's products, with `copies` direct loads of the step that comes NS - 1 later
+        auto multiply = [&](auto copies, int kt) {
+            const char *st = lds + now * T::STAGE;
+            char *ahead = lds + (now == 0 ? NS - 1 : now - 1) * T::STAGE;
+            multiply_step<typename T::P, typename T::Q, TP, TQ, BK, decltype(copies)::value>(
+                st, st + T::P::BYTES, wp, wq, acc, [&](int u) { copy(u, kt + NS - 1, ahead); }, [] {});
+            now = now + 1 == NS ? 0 : now + 1;
+        };
+        using NoCopies = std::integral_constant<int, 0>;
+        if constexpr (DIRECT) {
+            const int nk = K / BK;
+            // the last, shorter step comes first, through registers and the last stage
+            const bool rest = K % BK != 0;
+            if (rest) load(0, nk);
+            for (int kt = 0; kt < NS - 1 && kt < nk; ++kt)
+#pragma unroll
+                for (int u = 0; u < L; ++u) copy(u, kt, lds + kt * T::STAGE);
+            if (rest) {
+                now = NS - 1;
+                store(0, lds + now * T::STAGE);
+                meet();
+                multiply(NoCopies(), 0);
+            }
+            int kt = 0;
+            for (; kt + NS - 1 < nk; ++kt) {
+                wait_loads<(NS - 2) * L>();
+                meet();
+                multiply(std::integral_constant<int, L>(), kt);
+            }
+            for (; kt < nk; ++kt) {
+                wait_for_step<L, NS - 2>(nk - 1 - kt);
+                meet();
+                multiply(NoCopies(), kt);
+            }
+        } else {
+            const int nk = (K + BK - 1) / BK;
+            load(0, 0);
+#pragma unroll
+            for (int d = 1; d < D; ++d)
+                if (d < nk) load(d, d);
+            store(0, lds);
+            if (D < nk) load(0, D);
+            for (int k0 = 0; k0 < nk; k0 += D) {
+#pragma unroll
+                for (int d = 0; d < D; ++d) {
+                    const int kt = k0 + d, next = (d + 1) % D;      // step, register set of the next one
+                    if (kt >= nk) break;
+                    meet();
+                    if (kt + 1 < nk) store(next, lds + (now ^ 1) * T::STAGE);
+                    if (kt + 1 + D < nk) load(next, kt + 1 + D);
+                    multiply(NoCopies(), kt);
+                }
+            }
         }
     }
+    meet();
 
     // lane l: place wq + 32 j + l % 32, features wp + 32 i + 8 g + 4 (l / 32) + 0..3
-    const bool has = pc.e < a.E;
+    // f: feature of the tile
     auto finish = [&](int f, f32x4_r v) {
         if constexpr (OP == OP_FORWARD) {
-            if (a.bias && has) {
-                const float *b = a.bias + (int64_t)pc.e * a.out + f;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) v[k] += f + k < NP ? b[k] : 0.0f;
-            }
+            v += *(const f32x4_r *)(bias + f);
             if (a.relu)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) v[k] = v[k] < 0.0f ? 0.0f : v[k];   // NaN stays
@@ -517,7 +713,7 @@ __global__ __launch_bounds__(64 * WP * WQ) void expert_rows_kernel(ExpertArgs a,
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
                     const int f = p0 + wp + 32 * i + 8 * g + 4 * (lane >> 5);
-                    const f32x4_r v = finish(f, f32x4_r{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2],
+                    const f32x4_r v = finish(f - p0, f32x4_r{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2],
                                                         acc[i][j][4 * g + 3]});
                     if (f + 4 <= NP) {
                         *(f32x4_a4 *)(y + f) = v;
@@ -530,7 +726,8 @@ __global__ __launch_bounds__(64 * WP * WQ) void expert_rows_kernel(ExpertArgs a,
         }
         return;
     }
-    // bf16 rows meet in LDS and leave in 16-byte pieces (the last K step ended at a barrier)
+    // bf16 rows meet in LDS and leave in 16-byte pieces
+    uint16_t *out = (uint16_t *)lds;
 #pragma unroll
     for (int j = 0; j < TQ; ++j)
 #pragma unroll
@@ -538,200 +735,366 @@ __global__ __launch_bounds__(64 * WP * WQ) void expert_rows_kernel(ExpertArgs a,
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int f = wp + 32 * i + 8 * g + 4 * (lane >> 5);
-                const f32x4_r v = finish(p0 + f, f32x4_r{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2],
+                const f32x4_r v = finish(f, f32x4_r{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2],
                                                          acc[i][j][4 * g + 3]});
                 const u32x2_r o = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-                *(u32x2_r *)(lds + (wq + 32 * j + (lane & 31)) * T::LDO + f) = o;
+                *(u32x2_r *)(out + (wq + 32 * j + (lane & 31)) * T::LDO + f) = o;
             }
     __syncthreads();
-#pragma unroll 4
-    for (int t = tid; t < BQ * (BP / 8); t += NT) {
-        const int i = t / (BP / 8), f = t % (BP / 8) * 8;
-        const int r = row_of[i], nv = NP - p0 - f;
-        if (r < 0 || nv <= 0) continue;
-        u32x4_r o = *(const u32x4_r *)(lds + i * T::LDO + f);
-        if constexpr (OP == OP_FORWARD) {
-            store8_bits((uint16_t *)a.y + (int64_t)r * a.ld_y + p0 + f, nv, o);
-        } else {
-            if (a.relu) {
-                // keep the values whose input is positive
-                uint32_t keep = 0;
+    // a thread's pieces: features f.. of the places i0, i0 + NT / (BP / 8), ...; what masks
+    // them is loaded eight pieces at a time, before the first of them is stored
+    constexpr int PIECES = BQ * (BP / 8) / NT, B = PIECES < 8 ? PIECES : 8;
+    const int i0 = tid / (BP / 8), f = tid % (BP / 8) * 8, nv = NP - p0 - f;
+    if (nv <= 0) return;
+#pragma unroll 1
+    for (int c0 = 0; c0 < PIECES; c0 += B) {
+        int r[B];
+        u32x4_r h[B];
+        int scale[B];
+#pragma unroll
+        for (int c = 0; c < B; ++c) r[c] = row_of[i0 + (c0 + c) * (NT / (BP / 8))];
+        if (OP == OP_DX && a.relu) {
+#pragma unroll
+            for (int c = 0; c < B; ++c) {
+                const int64_t row = max(r[c], 0);
                 if (a.x) {
-                    const u32x4_r h = load8_bits(a.x + (int64_t)r * a.ld_x + p0 + f, nv);
-                    float x[8];
-                    unpack8(h, x);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) keep |= (x[k] > 0.0f ? 1u : 0u) << k;
+                    h[c] = load8_bits(a.x + row * a.ld_x + p0 + f, nv);
                 } else {
-                    const u32x2_r h = load8_bytes(a.c.q + (int64_t)r * a.c.ld_q + p0 + f, nv);
-                    const bool nan = a.c.scale[(int64_t)r * a.c.ld_scale + ((p0 + f) >> 5)] == 255;
-#pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        keep |= ((int8_t)(h[k >> 2] >> (8 * (k & 3))) > 0 && !nan ? 1u : 0u) << k;
+                    const u32x2_r q = load8_bytes(a.c.q + row * a.c.ld_q + p0 + f, nv);
+                    h[c] = u32x4_r{q[0], q[1], 0, 0};
+                    scale[c] = a.c.scale[row * a.c.ld_scale + ((p0 + f) >> 5)];
                 }
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    o[k] &= ((keep >> (2 * k)) & 1 ? 0x0000FFFFu : 0u) | ((keep >> (2 * k + 1)) & 1 ? 0xFFFF0000u : 0u);
             }
-            store8_bits(a.dx + (int64_t)r * a.ld_dx + p0 + f, nv, o);
+        }
+#pragma unroll
+        for (int c = 0; c < B; ++c) {
+            u32x4_r o = *(const u32x4_r *)(out + (i0 + (c0 + c) * (NT / (BP / 8))) * T::LDO + f);
+            if (OP == OP_DX && a.relu) {
+                // keep the values whose input is positive: not zero, no sign, no NaN
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    uint32_t keep;
+                    if (a.x) {
+                        const uint32_t lo = h[c][k] & 0xFFFFu, hi = h[c][k] >> 16;
+                        keep = (lo - 1 < 0x7F80u ? 0x0000FFFFu : 0u) | (hi - 1 < 0x7F80u ? 0xFFFF0000u : 0u);
+                    } else {
+                        const uint32_t t = h[c][k >> 1] >> (16 * (k & 1));
+                        keep = ((t & 0xFFu) - 1 < 127u ? 0x0000FFFFu : 0u) |
+                               (((t >> 8) & 0xFFu) - 1 < 127u ? 0xFFFF0000u : 0u);
+                        if (scale[c] == 255) keep = 0;
+                    }
+                    o[k] &= keep;
+                }
+            }
+            if (r[c] >= 0) {
+                uint16_t *to = OP == OP_FORWARD ? (uint16_t *)a.y + (int64_t)r[c] * a.ld_y : a.dx + (int64_t)r[c] * a.ld_dx;
+                store8_bits(to + p0 + f, nv, o);
+            }
         }
     }
 }
 
 // ---------------------------------------------------------------------------
-// Weight gradient.  An expert's rows are cut into pieces of at most a.piece; a
-// block forms BQ outputs x BP inputs of one piece.  The blocks of the first inputs
-// also form db: dy times a fragment of ones.
+// Weight gradient.  The blocks are TEAMS teams of one block for each tile (BQ outputs x
+// BP inputs).  The places with an expert are counted in units of 64 of one expert, and each
+// team takes an equal run of the units, whatever the experts' sizes; its blocks, which
+// read the same rows, are neighbours in an L2.  Within its run a team forms one product for
+// each expert.  An expert that lies in one run is written to dw; one that spans several
+// leaves each team's part in the workspace: slot 2 t if team t's run began with it, slot
+// 2 t + 1 if it goes on past the run's end (so at most two parts a team), which
+// expert_dw_sum_kernel adds up in the teams' order.
+// The blocks of the first inputs also sum dy's columns for db, from the stages in LDS.
+// CK: x from its checkpoint; DIRECT: dy, and x where it is no checkpoint, by direct loads.
 // ---------------------------------------------------------------------------
-template <int WP, int WQ, int TP, int TQ, bool CK>
-__global__ __launch_bounds__(64 * WP * WQ) void expert_dw_kernel(ExpertArgs a, int p_tiles, int q_tiles)
+constexpr int DW_UNIT = 64;
+
+// Places and units of expert e.
+struct Span {
+    int first, count, units;
+};
+__device__ __forceinline__ Span span_of(const ExpertArgs &a, int e)
 {
-    using T = Tile<OP_DW, WP, WQ, TP, TQ>;
-    constexpr int NT = T::NT, BP = T::BP, BQ = T::BQ;
-    __shared__ __attribute__((aligned(16))) uint16_t lds[T::LDS];
+    const int f = min(max(a.offsets[e], 0), a.n), l = min(max(a.offsets[e + 1], f), a.n);
+    return Span{f, l - f, (l - f + DW_UNIT - 1) / DW_UNIT};
+}
+
+// Sum over a wavefront, in every lane.
+__device__ __forceinline__ int wave_sum(int x)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
+    return x;
+}
+
+// Units of the experts before `last` (all lanes).
+__device__ __forceinline__ int units_before(const ExpertArgs &a, int last)
+{
+    int s = 0;
+    for (int e = threadIdx.x & 63; e < last; e += 64) s += span_of(a, e).units;
+    return wave_sum(s);
+}
+
+// Units of a team's run.
+__device__ __forceinline__ int run_units(int all, int teams) { return max((all + teams - 1) / teams, 1); }
+
+// Places whose row indices are held in LDS ahead of their use, a power of two.
+constexpr int DW_ROWS = 512;
+
+template <int WP, int WQ, int TP, int TQ, int BK, int NS, int D, bool DIRECT, bool CK>
+__global__ __launch_bounds__(64 * WP * WQ, 2) void expert_dw_kernel(ExpertArgs a, int p_tiles, int q_tiles)
+{
+    static_assert(DIRECT ? D == 1 : NS == 2, "stages");
+    static_assert(DW_ROWS / BK > NS + 1 && DW_ROWS / BK > D + 2, "row indices are there a step before they are used");
+    constexpr int NT = 64 * WP * WQ, BP = 32 * WP * TP, BQ = 32 * WQ * TQ;
+    constexpr bool BYTES = DIRECT && CK;      // x's bytes by direct loads
+    using P = std::conditional_t<CK && !DIRECT, AcrossCkpt<BP, NT, BK, D>, AcrossTile<BP, NT, BK, D>>;
+    using Q = AcrossTile<BQ, NT, BK, D>;
+    using R = CkptBytes<BP, NT, BK>;
+    // direct loads of a step
+    constexpr int LP = BYTES ? R::U : P::U, L = (BYTES ? 2 * R::U : P::U) + Q::U;
+    // LDS: NS tiles of dy, of x (2 restored ones and NS of bytes), two sets of row indices
+    constexpr int PS = BYTES ? 2 : NS, P_AT = NS * Q::BYTES, R_AT = P_AT + PS * P::BYTES;
+    constexpr int ROWS_AT = R_AT + (BYTES ? NS * R::BYTES : 0);
+    __shared__ __attribute__((aligned(1024))) char lds[ROWS_AT + 2 * DW_ROWS * 4];
+    int *rows = (int *)(lds + ROWS_AT);
     const int id = xcd_order(blockIdx.x, gridDim.x);
-    const int piece = id / (p_tiles * q_tiles);
-    const Piece pc = find_piece<false, true>(a.offsets, a.E, a.n, piece, a.piece);
-    if (pc.e < 0) return;
+    const int tiles = p_tiles * q_tiles, team = id / tiles, teams = gridDim.x / tiles;
     const int p0 = id % p_tiles * BP, q0 = id / p_tiles % q_tiles * BQ;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int lane = threadIdx.x & 63, wave = wave_id();
     const int wp = wave % WP * TP * 32, wq = wave / WP * TQ * 32;
-    const bool with_db = a.db && p0 == 0 && wp == 0;
-    const int K = pc.count, nk = (K + BK - 1) / BK;
-
-    AcrossTile<BQ, NT> tq;
-    std::conditional_t<CK, AcrossCkpt<BP, NT>, AcrossTile<BP, NT>> tp;
-    // rows of the step after the one that is being loaded
-    int rq[tq.C], rp[tp.C];
-    auto rows_of = [&](int kt) {
-#pragma unroll
-        for (int c = 0; c < tq.C; ++c) {
-            const int k = kt * BK + tq.krow(c);
-            rq[c] = k < K ? row_at(a, pc.first + k) : -1;
-        }
-#pragma unroll
-        for (int c = 0; c < tp.C; ++c) {
-            const int k = kt * BK + tp.krow(c);
-            rp[c] = k < K ? row_at(a, pc.first + k) : -1;
-        }
-    };
-    const int nvq = a.out - q0 - tq.piece() * 8, nvp = a.dw ? a.in - p0 - tp.piece() * 8 : 0;
-    auto load = [&]() {
-        int c = 0;
-        tq.load([&](int) { const int r = rq[c++]; return r >= 0 ? a.dy + (int64_t)r * a.ld_dy + q0 : nullptr; }, nvq);
-        c = 0;
-        if constexpr (CK) {
-            tp.load(a.c, [&](int) { return rp[c++]; }, p0, nvp);
-        } else {
-            tp.load([&](int) { const int r = rp[c++]; return r >= 0 ? a.x + (int64_t)r * a.ld_x + p0 : nullptr; }, nvp);
-        }
-    };
-
-    f32x16_t acc[TP][TQ], sums[1][TQ];
-    clear(acc);
-    clear(sums);
-    bf16x8_t ones;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) ones[k] = (__bf16)1.0f;
-    if (nk > 0) {
-        rows_of(0);
-        load();
-        if (nk > 1) rows_of(1);
-        tp.store(lds);
-        tq.store(lds + T::P_LDS);
-        __syncthreads();
-        if (nk > 1) load();
-        if (nk > 2) rows_of(2);
-    }
-    for (int kt = 0; kt < nk; ++kt) {
-        const uint16_t *ps = lds + (kt & 1) * T::STAGE, *qs = ps + T::P_LDS;
-#pragma unroll
-        for (int s = 0; s < BK; s += 16) {
-            bf16x8_t fp[TP], fq[TQ];
-#pragma unroll
-            for (int i = 0; i < TP; ++i) fp[i] = across_frag<BP>(ps, wp + 32 * i, s);
-#pragma unroll
-            for (int j = 0; j < TQ; ++j) fq[j] = across_frag<BQ>(qs, wq + 32 * j, s);
-#pragma unroll
-            for (int i = 0; i < TP; ++i)
-#pragma unroll
-                for (int j = 0; j < TQ; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp[i], fq[j], acc[i][j], 0, 0, 0);
-            if (with_db)
-#pragma unroll
-                for (int j = 0; j < TQ; ++j)
-                    sums[0][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ones, fq[j], sums[0][j], 0, 0, 0);
-        }
-        if (kt + 1 < nk) {
-            uint16_t *nx = lds + (~kt & 1) * T::STAGE;
-            tp.store(nx);
-            tq.store(nx + T::P_LDS);
-        }
-        if (kt + 2 < nk) load();
-        if (kt + 3 < nk) rows_of(kt + 3);
-        __syncthreads();
-    }
-
+    const bool with_db = a.db && p0 == 0;
     const int in4 = (a.in + 3) & ~3;
-    const bool alone = pc.of == 1;
-    float *c = alone ? a.dw + (int64_t)pc.e * a.out * a.ld_dw : a.part + (int64_t)piece * a.out * in4;
-    float *db = alone ? a.db + (int64_t)pc.e * a.out : a.part_db + (int64_t)piece * a.out;
-    const int64_t ldc = alone ? a.ld_dw : in4;
+
+    const int all = units_before(a, a.E), run = run_units(all, teams);
+    const int begin = min(team * run, all), end = min(begin + run, all);
+
+    P tp;
+    Q tq;
+    const int in = a.dw ? a.in : 0;      // db alone: x is not read
+    const int pcol = p0 + tp.col(), qcol = q0 + tq.col(), rcol = p0 + R::col() < in ? p0 + R::col() : -1;
+    const int nvp = in - pcol, nvq = a.out - qcol;
+    f32x16_t acc[TP][TQ];
+    float db[2];
+    // db: a thread sums two columns of DB_ROWS rows of each step
+    constexpr int PAIRS = BQ / 2, DB_ROWS = BK / (NT / PAIRS);
+
+    // the product of K places from `first` on
+    auto product = [&](int first, int K) {
+        const int nk = (K + BK - 1) / BK;
+        // row indices of places c DW_ROWS .. of the product: set c % 2
+        constexpr int RU = DW_ROWS / NT;
+        int held[RU];
+        auto fetch = [&](int c) {
 #pragma unroll
-    for (int j = 0; j < TQ; ++j) {
-        const int o = q0 + wq + 32 * j + (lane & 31);
-        if (o >= a.out) continue;
-        if (with_db && lane < 32) db[o] = sums[0][j][0];
-        if (!a.dw) continue;
+            for (int u = 0; u < RU; ++u) {
+                const int k = c * DW_ROWS + u * NT + (int)threadIdx.x;
+                held[u] = k < K ? row_at(a, first + k) : -1;
+            }
+        };
+        auto keep = [&](int c) {
 #pragma unroll
-        for (int i = 0; i < TP; ++i)
+            for (int u = 0; u < RU; ++u) rows[(c & 1) * DW_ROWS + u * NT + threadIdx.x] = held[u];
+        };
+        auto row = [&](int kt, int k) { return rows[(kt * BK + k) & (2 * DW_ROWS - 1)]; };
+        fetch(0);
+        keep(0);
+        fetch(1);
+        keep(1);
+        fetch(2);
+        __syncthreads();
+
+        auto x_at = [&](int kt, int u) -> const uint16_t * {
+            const int r = row(kt, tp.krow(u));
+            return r >= 0 && in > 0 ? a.x + (int64_t)r * a.ld_x + pcol : nullptr;
+        };
+        auto dy_at = [&](int kt, int u) -> const uint16_t * {
+            const int r = row(kt, tq.krow(u));
+            return r >= 0 ? a.dy + (int64_t)r * a.ld_dy + qcol : nullptr;
+        };
+        // direct loads: dy of step kt, x of step kt (its bytes of step kt + 1)
+        auto copy = [&](int u, int kt) {
+            char *q = lds + kt % NS * Q::BYTES;
+            if (u >= LP) {
+                tq.copy(u - LP, nvq > 0 ? dy_at(kt, u - LP) : nullptr, q);
+            } else if constexpr (BYTES) {
+                R::copy(u, a.c, row(kt + 1, R::krow(u)), rcol, lds + R_AT + (kt + 1) % NS * R::BYTES);
+            } else {
+                tp.copy(u, nvp > 0 ? x_at(kt, u) : nullptr, lds + P_AT + kt % NS * P::BYTES);
+            }
+        };
+        // through register set d
+        auto load = [&](int d, int kt) {
+            tq.load(d, [&](int u) { return dy_at(kt, u); }, nvq, a.out - q0 >= BQ, a.out >= 8);
+            if constexpr (CK && !DIRECT) tp.load(d, a.c, [&](int u) { return row(kt, tp.krow(u)); }, pcol, nvp);
+            else tp.load(d, [&](int u) { return x_at(kt, u); }, nvp, in - p0 >= BP, in >= 8);
+        };
+        auto store = [&](int d, int stage) {
+            tq.store(d, lds + stage * Q::BYTES);
+            tp.store(d, lds + P_AT + stage * P::BYTES);
+        };
+        auto restore = [&](int kt) { R::restore(lds + R_AT + kt % NS * R::BYTES, lds + P_AT + (kt & 1) * P::BYTES); };
+        // a step after its loads: the next row indices now and then, db, the products
+        auto step = [&](int kt, auto copies) {
+            if (kt > 0 && kt * BK % DW_ROWS == 0) {
+                keep(kt * BK / DW_ROWS + 1);
+                fetch(kt * BK / DW_ROWS + 2);
+            }
+            const char *qs = lds + kt % NS * Q::BYTES, *ps = lds + P_AT + kt % PS * P::BYTES;
+            if (with_db) {
+                const int pair = threadIdx.x % PAIRS, k0 = threadIdx.x / PAIRS * DB_ROWS;
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int f = p0 + wp + 32 * i + 8 * g + 4 * (lane >> 5);
-                const f32x4_r v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-                if (f + 4 <= a.in) {
-                    *(f32x4_a4 *)(c + o * ldc + f) = v;
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        if (f + k < a.in) c[o * ldc + f + k] = v[k];
+                for (int k = k0; k < k0 + DB_ROWS; ++k) {
+                    const uint32_t v = *(const uint32_t *)(qs + k * Q::PITCH + ((pair >> 2) ^ (Q::perm(k) << 2)) * 16 +
+                                                           (pair & 3) * 4);
+                    db[0] += __uint_as_float(v << 16);
+                    db[1] += __uint_as_float(v & 0xFFFF0000u);
                 }
             }
+            multiply_step<P, Q, TP, TQ, BK, decltype(copies)::value>(
+                ps, qs, wp, wq, acc, [&](int u) { copy(u, kt + NS - 1); },
+                [&] { if constexpr (BYTES) restore(kt + 1); });
+        };
+        clear(acc);
+        db[0] = db[1] = 0.0f;
+        if constexpr (DIRECT) {
+            // steps past the last have no rows: their loads bring zeros that nothing reads
+            if constexpr (BYTES)
+#pragma unroll
+                for (int u = 0; u < R::U; ++u) R::copy(u, a.c, row(0, R::krow(u)), rcol, lds + R_AT);
+            for (int kt = 0; kt < NS - 1; ++kt)
+#pragma unroll
+                for (int u = 0; u < LP + Q::U; ++u) copy(u, kt);
+            if constexpr (BYTES) {
+                wait_loads<(NS - 1) * L>();
+                restore(0);
+            }
+            for (int kt = 0; kt < nk; ++kt) {
+                wait_loads<(NS - 2) * L>();
+                meet();
+                step(kt, std::integral_constant<int, LP + Q::U>());
+            }
+        } else {
+#pragma unroll
+            for (int d = 0; d < D; ++d) load(d, d);
+            store(0, 0);
+            load(0, D);
+            for (int k0 = 0; k0 < nk; k0 += D) {
+#pragma unroll
+                for (int d = 0; d < D; ++d) {
+                    const int kt = k0 + d, next = (d + 1) % D;
+                    if (kt >= nk) break;
+                    meet();
+                    store(next, (kt + 1) & 1);
+                    load(next, kt + 1 + D);
+                    step(kt, std::integral_constant<int, 0>());
+                }
+            }
+        }
+        wait_loads<0>();
+        meet();
+    };
+
+    // the experts of the run; `u`: the units before expert e
+    int e = 0, u = 0;
+    {
+        // the last expert with begin at or after its first unit, 64 at a time
+        int carry = 0;
+        for (int e0 = 0; e0 < a.E; e0 += 64) {
+            const int j = e0 + lane;
+            const int k = j < a.E ? span_of(a, j).units : 0;
+            int s = k;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const int t = __shfl_up(s, d);
+                s += lane >= d ? t : 0;
+            }
+            const uint64_t hit = __ballot(carry + s > begin);
+            if (hit) {
+                const int l = __builtin_ctzll(hit);
+                e = e0 + l;
+                u = carry + __builtin_amdgcn_readlane(s, l) - __builtin_amdgcn_readlane(k, l);
+                break;
+            }
+            carry += __builtin_amdgcn_readlane(s, 63);
+        }
+    }
+    for (; u < end && e < a.E; ++e) {
+        const Span sp = span_of(a, e);
+        if (sp.units == 0) continue;
+        const int ub = max(begin, u), ue = min(end, u + sp.units);
+        const int k0 = (ub - u) * DW_UNIT, k1 = min((ue - u) * DW_UNIT, sp.count);
+        product(__builtin_amdgcn_readfirstlane(sp.first + k0), __builtin_amdgcn_readfirstlane(k1 - k0));
+
+        const bool whole = u >= begin && u + sp.units <= end;
+        const int64_t slot = 2 * team + (u >= begin ? 1 : 0);
+        float *c = whole ? a.dw + (int64_t)e * a.out * a.ld_dw : a.part + slot * a.out * in4;
+        const int64_t ldc = whole ? a.ld_dw : in4;
+        if (with_db) {
+            float *red = (float *)lds;      // [NT / PAIRS][BQ]
+            red[threadIdx.x / PAIRS * BQ + threadIdx.x % PAIRS * 2] = db[0];
+            red[threadIdx.x / PAIRS * BQ + threadIdx.x % PAIRS * 2 + 1] = db[1];
+            __syncthreads();
+            float *d = whole ? a.db + (int64_t)e * a.out : a.part_db + slot * a.out;
+            for (int i = threadIdx.x; i < BQ && q0 + i < a.out; i += NT) {
+                float t = 0.0f;
+#pragma unroll
+                for (int r = 0; r < NT / PAIRS; ++r) t += red[r * BQ + i];
+                d[q0 + i] = t;
+            }
+            __syncthreads();
+        }
+        if (a.dw)
+#pragma unroll
+            for (int j = 0; j < TQ; ++j) {
+                const int o = q0 + wq + 32 * j + (lane & 31);
+                if (o >= a.out) continue;
+#pragma unroll
+                for (int i = 0; i < TP; ++i)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const int f = p0 + wp + 32 * i + 8 * g + 4 * (lane >> 5);
+                        const f32x4_r v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2],
+                                           acc[i][j][4 * g + 3]};
+                        if (f + 4 <= a.in) {
+                            *(f32x4_a4 *)(c + o * ldc + f) = v;
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                if (f + k < a.in) c[o * ldc + f + k] = v[k];
+                        }
+                    }
+            }
+        u += sp.units;
     }
 }
 
-// dw and db of the experts whose rows were not one piece: the pieces' sums in
-// order, zeros without a piece.  blockIdx.y: the expert; x over [out][in4 / 4], then
-// [out] of db.
-__global__ __launch_bounds__(256) void expert_dw_sum_kernel(ExpertArgs a)
+// dw and db of the experts that no single team's run holds: the parts in the teams' order,
+// zeros for an expert without rows.  blockIdx.y: the expert; x over [out][in4 / 4], then [out]
+// of db.
+__global__ __launch_bounds__(256) void expert_dw_sum_kernel(ExpertArgs a, int teams)
 {
-    const int e = blockIdx.y, lane = threadIdx.x & 63;
-    // pieces of the experts before e, and of e (every wavefront for itself)
-    int before = 0, mine = 0;
-    for (int e0 = 0; e0 <= e; e0 += 64) {
-        const int j = e0 + lane;
-        int k = 0;
-        if (j <= e) {
-            const int f = min(max(a.offsets[j], 0), a.n), l = min(max(a.offsets[j + 1], f), a.n);
-            k = (l - f + a.piece - 1) / a.piece;
-        }
-        if (j == e) mine = k;
-        else before += k;
+    const int e = blockIdx.y;
+    const int mine = span_of(a, e).units;
+    int t0 = 0, t1 = -1, u0 = 0, run = 1;
+    if (mine > 0) {
+        if (teams == 1) return;
+        u0 = units_before(a, e);
+        run = run_units(units_before(a, a.E), teams);
+        t0 = u0 / run;
+        t1 = (u0 + mine - 1) / run;
+        if (t0 == t1) return;
     }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        before += __shfl_xor(before, d);
-        mine += __shfl_xor(mine, d);
-    }
-    if (mine == 1) return;
+    // team t's part: its run began within the expert (slot 2 t), or goes on past it (2 t + 1)
     const int in4 = (a.in + 3) & ~3, q = in4 / 4;
     const int64_t size = (int64_t)a.out * q, t = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (t < size) {
         if (!a.dw) return;
         const int o = (int)(t / q), f = (int)(t % q) * 4;
         f32x4_r s = {0.0f, 0.0f, 0.0f, 0.0f};
-        const float *p = a.part + ((int64_t)before * a.out + o) * in4 + f;
-        for (int k = 0; k < mine; ++k) s += *(const f32x4_r *)(p + (int64_t)k * a.out * in4);
+        for (int k = t0; k <= t1; ++k) {
+            const int64_t slot = 2 * k + (u0 >= k * run ? 1 : 0);
+            s += *(const f32x4_r *)(a.part + (slot * a.out + o) * in4 + f);
+        }
         float *c = a.dw + ((int64_t)e * a.out + o) * a.ld_dw + f;
 #pragma unroll
         for (int k = 0; k < 4; ++k)
@@ -739,54 +1102,95 @@ __global__ __launch_bounds__(256) void expert_dw_sum_kernel(ExpertArgs a)
     } else if (a.db && t - size < a.out) {
         const int o = (int)(t - size);
         float s = 0.0f;
-        for (int k = 0; k < mine; ++k) s += a.part_db[((int64_t)before + k) * a.out + o];
+        for (int k = t0; k <= t1; ++k) s += a.part_db[(2 * k + (u0 >= k * run ? 1 : 0)) * (int64_t)a.out + o];
         a.db[(int64_t)e * a.out + o] = s;
     }
 }
 
-template <int OP, int WP, int WQ, int TP, int TQ>
+constexpr int64_t BIG_TILES = 512;
+constexpr int64_t DW_BIG_ROWS = 16384, DW_SMALL_BLOCKS = 1024, DW_RUN = 256;
+
+// Tiles of a launch over rows, for any group sizes: whole tiles, and a shorter one for
+// each expert and for the rest.
+static int64_t row_tiles(const ExpertArgs &a, int rows) { return a.n / rows + std::min<int64_t>(a.E + 1, a.n); }
+
+template <int OP, int WP, int WQ, int TP, int TQ, int BK, int NS, int D, bool DIRECT>
 static void rows_go(const ExpertArgs &a, hipStream_t s)
 {
-    using T = Tile<OP, WP, WQ, TP, TQ>;
+    using T = RowsTile<OP, WP, WQ, TP, TQ, BK, D>;
     const int p_tiles = (int)ceil_div(OP == OP_FORWARD ? a.out : a.in, T::BP);
-    // any group sizes: whole tiles, and a shorter one for each expert and for the rest
-    const int64_t tiles = a.n / T::BQ + std::min<int64_t>(a.E + 1, a.n);
-    expert_rows_kernel<OP, WP, WQ, TP, TQ><<<dim3((unsigned)(tiles * p_tiles)), dim3(T::NT), 0, s>>>(a, p_tiles);
+    expert_rows_kernel<OP, WP, WQ, TP, TQ, BK, NS, D, DIRECT>
+        <<<dim3((unsigned)(row_tiles(a, T::BQ) * p_tiles)), dim3(T::NT), 0, s>>>(a, p_tiles);
+}
+
+// Rows that direct loads can take: all at multiples of 16 bytes.
+static bool rows_aligned(const void *p, int64_t ld, int64_t size = 2)
+{
+    return ((uintptr_t)p & 15) == 0 && ld * size % 16 == 0;
+}
+
+template <int OP>
+static void rows_launch(const ExpertArgs &a, bool direct, hipStream_t s)
+{
+    const int64_t big = row_tiles(a, 128) * ceil_div(OP == OP_FORWARD ? a.out : a.in, 256);
+    if (big >= BIG_TILES) {
+        if (direct) rows_go<OP, 2, 2, 4, 2, 32, 3, 1, true>(a, s);
+        else rows_go<OP, 2, 2, 2, 2, 32, 2, 3, false>(a, s);
+    } else {
+        if (direct) rows_go<OP, 2, 2, 1, 1, 64, 4, 1, true>(a, s);
+        else rows_go<OP, 2, 2, 1, 1, 64, 2, 3, false>(a, s);
+    }
 }
 
 hipError_t launch_expert_linear(const ExpertArgs &a, hipStream_t s)
 {
-    rows_go<OP_FORWARD, 2, 2, 2, 2>(a, s);
+    rows_launch<OP_FORWARD>(a, rows_aligned(a.x, a.ld_x) && rows_aligned(a.w, a.ld_w), s);
     return hipGetLastError();
 }
 
-constexpr int DW_TILE = 128;
-
-int expert_piece_rows(int64_t n, int n_experts, int in, int out)
+// Tile of the weight gradient and its teams: 256 x 256 on the CUs' one block each where the
+// rows give every team at least DW_RUN of them, else 64 x 64.
+struct DwShape {
+    int tile, teams;
+};
+static DwShape dw_shape(int64_t n, int in, int out)
 {
-    const int64_t tiles = ceil_div(in, DW_TILE) * ceil_div(out, DW_TILE);
-    const int64_t pieces = std::max<int64_t>(1, ceil_div(512, tiles));
-    return (int)(ceil_div(std::max<int64_t>(ceil_div(n, pieces), 1024), 64) * 64);
+    const int64_t big = ceil_div(in, 256) * ceil_div(out, 256);
+    if (n >= DW_BIG_ROWS && in > 128 && out > 128) return {256, (int)std::max<int64_t>(1, 256 / big)};
+    const int64_t tiles = ceil_div(in, 64) * ceil_div(out, 64);
+    return {64, (int)std::max<int64_t>(1, std::min<int64_t>(DW_SMALL_BLOCKS / tiles, n / DW_RUN))};
 }
 
-int64_t expert_pieces(int64_t n, int n_experts, int in, int out)
+int expert_grad_teams(int64_t n, int in, int out) { return dw_shape(n, in, out).teams; }
+
+template <bool DIRECT, bool CK>
+static void dw_go(const ExpertArgs &a, const DwShape &d, hipStream_t s)
 {
-    return n / expert_piece_rows(n, n_experts, in, out) + std::min<int64_t>(n_experts, n);
+    const int p_tiles = a.dw ? (int)ceil_div(a.in, d.tile) : 1, q_tiles = (int)ceil_div(a.out, d.tile);
+    const dim3 g((unsigned)(d.teams * p_tiles * q_tiles));
+    if (d.tile == 256) {
+        if constexpr (DIRECT) expert_dw_kernel<2, 4, 4, 2, 32, 4, 1, true, CK><<<g, dim3(512), 0, s>>>(a, p_tiles, q_tiles);
+        else expert_dw_kernel<2, 4, 4, 2, 32, 2, 1, false, CK><<<g, dim3(512), 0, s>>>(a, p_tiles, q_tiles);
+    } else {
+        if constexpr (DIRECT) expert_dw_kernel<2, 2, 1, 1, 64, 4, 1, true, CK><<<g, dim3(256), 0, s>>>(a, p_tiles, q_tiles);
+        else expert_dw_kernel<2, 2, 1, 1, 64, 2, 3, false, CK><<<g, dim3(256), 0, s>>>(a, p_tiles, q_tiles);
+    }
 }
 
 hipError_t launch_expert_grad(const ExpertArgs &a, hipStream_t s)
 {
-    if (a.dx && a.n > 0) rows_go<OP_DX, 2, 2, 2, 2>(a, s);
+    const bool dy_ok = rows_aligned(a.dy, a.ld_dy);
+    if (a.dx && a.n > 0) rows_launch<OP_DX>(a, dy_ok && rows_aligned(a.w, a.ld_w), s);
     if (a.dw || a.db) {
-        const int p_tiles = a.dw ? (int)ceil_div(a.in, DW_TILE) : 1, q_tiles = (int)ceil_div(a.out, DW_TILE);
-        const int64_t pieces = expert_pieces(a.n, a.E, a.in, a.out);
-        const dim3 g((unsigned)(pieces * p_tiles * q_tiles));
-        if (pieces > 0) {
-            if (a.x || !a.dw) expert_dw_kernel<2, 2, 2, 2, false><<<g, dim3(256), 0, s>>>(a, p_tiles, q_tiles);
-            else expert_dw_kernel<2, 2, 2, 2, true><<<g, dim3(256), 0, s>>>(a, p_tiles, q_tiles);
+        const DwShape d = dw_shape(a.n, a.in, a.out);
+        if (a.n > 0) {
+            const bool ck = a.dw && !a.x;
+            const bool x_ok = !a.dw || (ck ? rows_aligned(a.c.q, a.c.ld_q, 1) : rows_aligned(a.x, a.ld_x));
+            if (ck) dy_ok && x_ok ? dw_go<true, true>(a, d, s) : dw_go<false, true>(a, d, s);
+            else dy_ok && x_ok ? dw_go<true, false>(a, d, s) : dw_go<false, false>(a, d, s);
         }
         const int64_t work = (int64_t)a.out * ((a.in + 3) / 4) + a.out;
-        expert_dw_sum_kernel<<<dim3((unsigned)ceil_div(work, 256), a.E), dim3(256), 0, s>>>(a);
+        expert_dw_sum_kernel<<<dim3((unsigned)ceil_div(work, 256), a.E), dim3(256), 0, s>>>(a, d.teams);
     }
     return hipGetLastError();
 }

@@ -137,9 +137,9 @@ __device__ __forceinline__ u32x2_r ckpt_pack(const float *v, int scale)
     return r;
 }
 
+// The step is a power of two (subnormal below scale 7): every product is exact.
 __device__ __forceinline__ void ckpt_unpack(u32x2_r r, int scale, float *v)
 {
-    // the step is a power of two (subnormal below scale 7): every product is exact
     const float s = scale == 255 ? __builtin_nanf("") : ldexpf(1.0f, scale - 133);
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] = (float)(int8_t)(r[k >> 2] >> (8 * (k & 3))) * s;

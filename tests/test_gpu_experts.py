@@ -671,3 +671,41 @@ def test_binding_refuses_tensors_that_do_not_fit():
         im.expert_linear_grad(y, xb, w, off, None)
     with pytest.raises(ValueError, match="rows must be"):
         im.group_rows(off, off, torch.zeros(2, dtype=torch.int32, device=DEV))
+
+
+# ------------------------------------------- sizes of the large tiles, both ways of loading
+@pytest.mark.parametrize("kept", [False, True])
+@pytest.mark.parametrize("n,E,din,dout,pad,form", [
+    (17000, 5, 264, 1000, 0, "holes"), (17000, 5, 1000, 264, 0, "even"), (16500, 3, 270, 1023, 2, "holes"),
+    (16500, 3, 270, 1023, 1, "even"), (30000, 40, 257, 801, 0, "even"), (16400, 2, 512, 896, 0, "one"),
+])
+def test_large_tiles(n, E, din, dout, pad, form, kept):
+    e, off, rows, x, w, b, g = _layer(n, E, din, dout, pad, n + dout, form)
+    y = _out(n, dout, pad, torch.bfloat16)
+    y.fill_(5.0)
+    im.expert_linear(x, w, b, off, rows, y, relu=True)
+    dy = _wide(torch.randn(n, dout, device=DEV, generator=g).bfloat16(), pad)
+    src, xin = x, x.double()
+    if kept:
+        src = im.Checkpoint(_out(n, din, pad, torch.int8), _out(n, -(-din // 32), pad, torch.uint8))
+        im.checkpoint_store(x, src)
+        xin = torch.from_numpy(_ckpt_ref(x)[2]).to(DEV)
+    dx = _out(n, din, pad, torch.bfloat16)
+    dx.fill_(5.0)
+    dw, db = torch.full((E, dout, din), 5.0, device=DEV), torch.full((E, dout), 5.0, device=DEV)
+    im.expert_linear_grad(dy, src, w, off, rows, dx, dw, db, relu_x=True)
+    none = torch.ones(n, dtype=torch.bool, device=DEV)
+    for k, r in enumerate(_by_expert(e, E)):
+        none[r] = False
+        v, d, m, wk = x[r].double(), dy[r].double(), xin[r], w[k].double()
+        want = (v @ wk.t() + b[k].double()).clamp(min=0)
+        _within(y[r], want, 2 * (din + 1) * U * (v.abs() @ wk.abs().t() + b[k].double().abs()) + BF * want, "y")
+        want = (d @ wk) * (m > 0)
+        _within(dx[r], want, 2 * dout * U * (d.abs() @ wk.abs()) + BF * want.abs(), "dx")
+        _within(dw[k], d.t() @ m, 2 * len(r) * U * (d.abs().t() @ m.abs()), "dw")
+        _within(db[k], d.sum(0), 2 * len(r) * U * d.abs().sum(0), "db")
+    assert not y[none].any() and not dx[none].any()
+    _pad_kept(y), _pad_kept(dx)
+    dw2, db2 = torch.zeros_like(dw), torch.zeros_like(db)
+    im.expert_linear_grad(dy, src, w, off, rows, dw=dw2, db=db2)
+    assert torch.equal(dw, dw2) and torch.equal(db, db2)
