@@ -677,43 +677,59 @@ def ppo_batch(ro, perm, lr, stats=None):
 
 
 # ---------------------------------------------------------- layers of experts
+# These calls are also made for a single env, where the launch's 4 us and this
+# marshalling are all of the time: checks are kept to a few tenths of a microsecond each.
+_torch = None
+
+
+def _call_stream(stream):
+    """(device index, hipStream_t) of a call on the current device."""
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    dev = _torch._C._cuda_getDevice()
+    if stream is None:
+        # torch.cuda.current_stream() without its Stream object (2.7 us)
+        return dev, _torch._C._cuda_getCurrentRawStream(dev)
+    if stream.device_index != dev:
+        raise ValueError("the stream is not on the current device")
+    return dev, stream.cuda_stream
+
+
 def _dtype(t):
-    import torch
-    if t.dtype == torch.bfloat16:
+    if t.dtype is _torch.bfloat16:
         return IM_DTYPE_BF16
-    if t.dtype == torch.float32:
+    if t.dtype is _torch.float32:
         return IM_DTYPE_F32
     raise ValueError("expected a float32 or bfloat16 tensor, got %s" % t.dtype)
 
 
 def _ld(t, n, d, name, dev, dtype=None):
     """Row stride of a matrix argument [n][d] of the current device."""
-    if tuple(t.shape) != (n, d) or (dtype is not None and t.dtype != dtype):
+    if t.shape != (n, d) or (dtype is not None and t.dtype is not dtype):
         raise ValueError("%s must be [%d][%d]%s, got %s %s" % (
             name, n, d, "" if dtype is None else " of %s" % dtype, list(t.shape), t.dtype))
     if t.get_device() != dev:
         raise ValueError("%s is not on the current device" % name)
-    if d > 1 and t.stride(1) != 1:
+    rows, cols = t.stride()
+    if cols != 1 and d > 1:
         raise ValueError("%s: the values of a row must lie together" % name)
-    return max(t.stride(0), d) if n > 1 else d
+    if n < 2:
+        return d
+    if rows < d:
+        raise ValueError("%s: rows overlap" % name)
+    return rows
 
 
 def _vec(t, n, name, dev, dtype):
     """Pointer of a contiguous argument of n values (None: NULL)."""
     if t is None:
         return None
-    if t.numel() != n or t.dtype != dtype or not t.is_contiguous() or t.get_device() != dev:
+    if t.dtype is not dtype or t.numel() != n or t.get_device() != dev or not t.is_contiguous():
         raise ValueError("%s must be %d contiguous values of %s on the current device" % (
             name, n, dtype))
     return t.data_ptr()
-
-
-def _call_stream(stream):
-    """(device index, stream) of a call."""
-    import torch
-    if stream is None:
-        stream = torch.cuda.current_stream()
-    return stream.device_index, stream
 
 
 def _space(nbytes):
@@ -724,10 +740,13 @@ def _space(nbytes):
 
 
 def _workspace(given, need, stream):
-    """A call's workspace: the given one, or one of its own."""
+    """Pointer and size of a call's workspace: the given one, or one of its own."""
     if given is None:
         given = need()
-        given.record_stream(stream)
+        if stream is not None:
+            given.record_stream(stream)
+    elif not given.is_cuda or not given.is_contiguous():
+        raise ValueError("a workspace is contiguous device memory")
     return given.data_ptr(), given.numel() * given.element_size()
 
 
@@ -749,26 +768,25 @@ class Checkpoint:
         return self.q.shape
 
     def struct(self, n, d, dev):
-        import torch
         return ImCheckpoint(self.q.data_ptr(), self.scale.data_ptr(),
-                            _ld(self.q, n, d, "q", dev, torch.int8),
-                            _ld(self.scale, n, -(-d // 32), "scale", dev, torch.uint8))
+                            _ld(self.q, n, d, "q", dev, _torch.int8),
+                            _ld(self.scale, n, -(-d // 32), "scale", dev, _torch.uint8))
 
 
 def checkpoint_store(x, ckpt, stream=None):
     """x (float32 or bfloat16 [n][d]) into the checkpoint."""
-    dev, stream = _call_stream(stream)
+    dev, raw = _call_stream(stream)
     n, d = x.shape
     im_checkpoint_store(x.data_ptr(), _ld(x, n, d, "x", dev), _dtype(x), n, d,
-                        ckpt.struct(n, d, dev), stream.cuda_stream)
+                        ckpt.struct(n, d, dev), raw)
 
 
 def checkpoint_load(ckpt, x, stream=None):
     """The checkpoint's values into x (float32 or bfloat16 [n][d])."""
-    dev, stream = _call_stream(stream)
+    dev, raw = _call_stream(stream)
     n, d = x.shape
     im_checkpoint_load(ckpt.struct(n, d, dev), n, d, x.data_ptr(), _ld(x, n, d, "x", dev),
-                       _dtype(x), stream.cuda_stream)
+                       _dtype(x), raw)
 
 
 def group_rows_workspace(n, n_experts):
@@ -779,29 +797,27 @@ def group_rows_workspace(n, n_experts):
 def group_rows(expert, offsets, rows, workspace=None, stream=None):
     """Rows by expert: expert [n] int32 into offsets [n_experts + 1] and rows [n]
     (int32)."""
-    import torch
-    dev, stream = _call_stream(stream)
+    dev, raw = _call_stream(stream)
     n, e = expert.numel(), offsets.numel() - 1
-    i32 = torch.int32
+    i32 = _torch.int32
     ws, nbytes = _workspace(workspace, lambda: group_rows_workspace(n, e), stream)
     im_group_rows(_vec(expert, n, "expert", dev, i32), n, e,
                   _vec(offsets, e + 1, "offsets", dev, i32), _vec(rows, n, "rows", dev, i32),
-                  ws, nbytes, stream.cuda_stream)
+                  ws, nbytes, raw)
 
 
 def layer_norm(x, gamma, beta, y, mean=None, rstd=None, eps=1e-5, checkpoint=None, stream=None):
     """y = layer norm of the rows of x [n][d] (float32 or bfloat16), optionally its
     row statistics [n] and the checkpoint of x."""
-    import torch
-    dev, stream = _call_stream(stream)
+    dev, raw = _call_stream(stream)
     n, d = x.shape
-    f32 = torch.float32
+    f32 = _torch.float32
     ck = None if checkpoint is None else C.pointer(checkpoint.struct(n, d, dev))
     im_layer_norm(ImNorm(n, d, _dtype(x), eps, x.data_ptr(), _ld(x, n, d, "x", dev),
                          _vec(gamma, d, "gamma", dev, f32), _vec(beta, d, "beta", dev, f32),
                          y.data_ptr(), _ld(y, n, d, "y", dev, x.dtype),
                          _vec(mean, n, "mean", dev, f32), _vec(rstd, n, "rstd", dev, f32), ck),
-                  stream.cuda_stream)
+                  raw)
 
 
 def layer_norm_grad_workspace(n, d):
@@ -812,10 +828,9 @@ def layer_norm_grad_workspace(n, d):
 def layer_norm_grad(dy, x, gamma, mean, rstd, dx=None, dgamma=None, dbeta=None, workspace=None,
                     stream=None):
     """Gradient of layer_norm; x: its input or the Checkpoint of it."""
-    import torch
-    dev, stream = _call_stream(stream)
+    dev, raw = _call_stream(stream)
     n, d = dy.shape
-    f32 = torch.float32
+    f32 = _torch.float32
     ws, nbytes = None, 0
     if dgamma is not None or dbeta is not None:
         ws, nbytes = _workspace(workspace, lambda: layer_norm_grad_workspace(n, d), stream)
@@ -829,16 +844,16 @@ def layer_norm_grad(dy, x, gamma, mean, rstd, dx=None, dgamma=None, dbeta=None, 
                    _vec(rstd, n, "rstd", dev, f32), _dptr(dx),
                    0 if dx is None else _ld(dx, n, d, "dx", dev, dy.dtype),
                    _vec(dgamma, d, "dgamma", dev, f32), _vec(dbeta, d, "dbeta", dev, f32),
-                   ws, nbytes), stream.cuda_stream)
+                   ws, nbytes), raw)
 
 
 def _expert_ld(t, e, out, in_, name, dev, dtype):
     """Row stride of [n_experts][out][in] weights."""
-    if tuple(t.shape) != (e, out, in_) or t.dtype != dtype or t.get_device() != dev:
+    if tuple(t.shape) != (e, out, in_) or t.dtype is not dtype or t.get_device() != dev:
         raise ValueError("%s must be [%d][%d][%d] of %s on the current device, got %s %s" % (
             name, e, out, in_, dtype, list(t.shape), t.dtype))
-    ld = max(t.stride(1), in_) if out > 1 else (t.stride(0) if e > 1 else in_)
-    if (in_ > 1 and t.stride(2) != 1) or (e > 1 and t.stride(0) != out * ld):
+    ld = t.stride(1) if out > 1 else (t.stride(0) if e > 1 else in_)
+    if (in_ > 1 and t.stride(2) != 1) or (e > 1 and t.stride(0) != out * ld) or ld < in_:
         raise ValueError("%s: rows of values that lie together, one stride over all rows" % name)
     return ld
 
@@ -847,18 +862,17 @@ def expert_linear(x, w, bias, offsets, rows, y, relu=False, stream=None):
     """y[r] = w[e] x[r] + bias[e] (ReLU with relu), e the expert of row r by group_rows'
     offsets and rows (rows None: grouped already).  x [n][in] and w [n_experts][out][in]
     bfloat16, bias [n_experts][out] float32 or None, y [n][out] bfloat16 or float32."""
-    import torch
-    dev, stream = _call_stream(stream)
+    dev, raw = _call_stream(stream)
     n, in_ = x.shape
     e, out = w.shape[0], w.shape[1]
-    i32 = torch.int32
+    i32 = _torch.int32
     im_expert_linear(
         ImExpertLayer(n, e, in_, out, _dtype(x), _dtype(y), 1 if relu else 0,
                       _vec(offsets, e + 1, "offsets", dev, i32), _vec(rows, n, "rows", dev, i32),
                       x.data_ptr(), _ld(x, n, in_, "x", dev), w.data_ptr(),
                       _expert_ld(w, e, out, in_, "w", dev, x.dtype),
-                      _vec(bias, e * out, "bias", dev, torch.float32), y.data_ptr(),
-                      _ld(y, n, out, "y", dev)), stream.cuda_stream)
+                      _vec(bias, e * out, "bias", dev, _torch.float32), y.data_ptr(),
+                      _ld(y, n, out, "y", dev)), raw)
 
 
 def expert_linear_grad_workspace(n, n_experts, in_, out):
@@ -872,11 +886,10 @@ def expert_linear_grad(dy, x, w, offsets, rows, dx=None, dw=None, db=None, relu_
     [n_experts][out][in] and db [n_experts][out] float32 (each may be None).  x: the
     layer's input or the Checkpoint of it; relu_x: it is a ReLU's output, dx is the
     gradient before it."""
-    import torch
-    dev, stream = _call_stream(stream)
+    dev, raw = _call_stream(stream)
     n, out = dy.shape
     e, _, in_ = w.shape
-    i32, f32, bf16 = torch.int32, torch.float32, torch.bfloat16
+    i32, f32, bf16 = _torch.int32, _torch.float32, _torch.bfloat16
     ws, nbytes = None, 0
     if dw is not None or db is not None:
         ws, nbytes = _workspace(workspace, lambda: expert_linear_grad_workspace(n, e, in_, out),
@@ -894,4 +907,4 @@ def expert_linear_grad(dy, x, w, offsets, rows, dx=None, dw=None, db=None, relu_
                           _expert_ld(w, e, out, in_, "w", dev, bf16), _dptr(dx),
                           0 if dx is None else _ld(dx, n, in_, "dx", dev, bf16), _dptr(dw),
                           0 if dw is None else _expert_ld(dw, e, out, in_, "dw", dev, f32),
-                          _vec(db, e * out, "db", dev, f32), ws, nbytes), stream.cuda_stream)
+                          _vec(db, e * out, "db", dev, f32), ws, nbytes), raw)

@@ -272,7 +272,8 @@ __device__ __forceinline__ int row_at(const ExpertArgs &a, int p)
 //     group, lane 4j+q addresses row k0+j, columns c0+4q.., and lane l receives rows
 //     k0..k0+3 of column c0+l).
 // ---------------------------------------------------------------------------
-enum { OP_FORWARD, OP_DX };
+// dx alone, or masked by its input being positive (bf16 or a checkpoint)
+enum { OP_FORWARD, OP_DX, OP_DX_X, OP_DX_CKPT };
 
 __device__ const uint4 zero_piece = {0, 0, 0, 0};
 
@@ -319,20 +320,27 @@ __device__ __forceinline__ void wait_for_step(int later)
 
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
-// The first nv values (of eight at p, the row ending at p + nv; nv may be negative) of a
-// row that holds at least 8, zeros after them: the row's last eight, shifted.
-__device__ __forceinline__ u32x4_r load8_end(const uint16_t *p, int nv)
+// Rows at any address, with an end inside a piece: the load takes eight values that end at
+// the row's end at the latest (`back` values before the piece), always, so that loads need
+// no branches, and end_of_row shifts them down, zeros after them, when they are stored.
+// nv: values of the row from the piece's first on, also none or fewer.  A row shorter than
+// eight values is read one by one (NARROW).
+__device__ __forceinline__ int window_back(int nv) { return 8 - min(nv, 8); }
+__device__ __forceinline__ u32x4_r end_of_row(u32x4_r r, int nv)
 {
-    const int n = min(nv, 8);
-    u32x4_r r = *(const u32x4_a2 *)(p + (n - 8));
     uint64_t lo = r[0] | (uint64_t)r[1] << 32, hi = r[2] | (uint64_t)r[3] << 32;
-    int gone = 8 - max(n, 0);
-    if (gone >= 4) lo = hi, hi = 0, gone -= 4;
-    if (gone == 4) lo = 0;
-    const int s = 16 * (gone & 3);
+    const int gone = 8 - max(min(nv, 8), 0), s = 16 * (gone & 3);
+    if (gone >= 4) lo = hi, hi = 0;
+    if (gone == 8) lo = 0;
     if (s) lo = lo >> s | hi << (64 - s), hi >>= s;
     const u32x4_r o = {(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
     return o;
+}
+__device__ __forceinline__ u32x2_r end_of_row(u32x2_r r, int nv)
+{
+    const int gone = 8 - max(min(nv, 8), 0);
+    const uint64_t w = gone == 8 ? 0 : (r[0] | (uint64_t)r[1] << 32) >> (8 * gone);
+    return u32x2_r{(uint32_t)w, (uint32_t)(w >> 32)};
 }
 
 // A tile of R rows with k along them.  Thread t holds pieces u of the rows row(u).
@@ -358,26 +366,26 @@ struct AlongTile {
     {
         copy_to_lds(p[u] + kt * BK, lds + (u * (NT / 64) + wave_id()) * 1024);
     }
-    // the step's valid ones of K values in all, through register set d
+    // a step (also one past the last) of K values in all, through register set d
+    template <bool NARROW>
     __device__ __forceinline__ void load(int d, int kt, int K)
     {
         const int nv = K - kt * BK - col();
-        if ((kt + 1) * BK <= K) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[d][u] = *(const u32x4_a2 *)(p[u] + kt * BK);
-        } else if (K >= 8) {
-#pragma unroll
-            for (int u = 0; u < U; ++u) v[d][u] = load8_end(p[u] + kt * BK, nv);
-        } else {
-#pragma unroll
-            for (int u = 0; u < U; ++u) v[d][u] = load8_bits(p[u] + kt * BK, nv);
+        for (int u = 0; u < U; ++u) {
+            const uint16_t *at = p[u] + kt * BK;
+            v[d][u] = NARROW ? load8_bits(at, nv) : *(const u32x4_a2 *)(at - window_back(nv));
         }
     }
-    __device__ __forceinline__ void store(int d, char *lds) const
+    template <bool NARROW>
+    __device__ __forceinline__ void store(int d, int kt, int K, char *lds) const
     {
+        const bool end = !NARROW && (kt + 1) * BK > K;
+        const int nv = K - kt * BK - col();
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            *(u32x4_r *)(lds + (u * (NT / 64) + wave_id()) * 1024 + (threadIdx.x & 63) * 16) = v[d][u];
+            *(u32x4_r *)(lds + (u * (NT / 64) + wave_id()) * 1024 + (threadIdx.x & 63) * 16) =
+                end ? end_of_row(v[d][u], nv) : v[d][u];
     }
     // 8 consecutive k (of substep s) of 32 rows: lane l row l % 32, k + 8 (l / 32)..
     __device__ static bf16x8_t frag(const char *lds, int row, int s)
@@ -407,23 +415,24 @@ struct AcrossTile {
     {
         copy_to_lds(from ? (const void *)from : (const void *)&zero_piece, lds + (u * (NT / 64) + wave_id()) * 1024);
     }
-    // at(u): that address for any nv; whole: nv >= 8 in all threads; wide: the row holds 8
-    template <typename F>
-    __device__ __forceinline__ void load(int d, F at, int nv, bool whole, bool wide)
+    // through register set d; at(u): that address, whatever nv; whole: all threads' nv >= 8
+    template <bool NARROW, typename F>
+    __device__ __forceinline__ void load(int d, F at, int nv)
     {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const uint16_t *p = at(u);
-            if (whole) v[d][u] = *(const u32x4_a2 *)(p ? p : (const uint16_t *)&zero_piece);
-            else if (wide) v[d][u] = load8_end(p ? p : (const uint16_t *)&zero_piece, p ? nv : 8);
-            else v[d][u] = load8_bits(p, p ? nv : 0);
+            v[d][u] = NARROW ? load8_bits(p, p ? nv : 0)
+                             : *(const u32x4_a2 *)(p ? p - window_back(nv) : (const uint16_t *)&zero_piece);
         }
     }
-    __device__ __forceinline__ void store(int d, char *lds) const
+    template <bool NARROW>
+    __device__ __forceinline__ void store(int d, int nv, bool whole, char *lds) const
     {
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            *(u32x4_r *)(lds + (u * (NT / 64) + wave_id()) * 1024 + (threadIdx.x & 63) * 16) = v[d][u];
+            *(u32x4_r *)(lds + (u * (NT / 64) + wave_id()) * 1024 + (threadIdx.x & 63) * 16) =
+                NARROW || whole ? v[d][u] : end_of_row(v[d][u], nv);
     }
     __device__ static bf16x8_t frag(const char *lds, int col, int s)
     {
@@ -445,25 +454,29 @@ struct AcrossCkpt : AcrossTile<N, NT, BK, 1> {
     u32x2_r q[D][B::U];
     int scale[D][B::U];
     // row(u): the index of k row krow(u), negative for none; col: this thread's first column
-    template <typename F>
+    template <bool NARROW, typename F>
     __device__ __forceinline__ void load(int d, const im_checkpoint &c, F row, int col, int nv)
     {
 #pragma unroll
         for (int u = 0; u < B::U; ++u) {
-            const int r = row(u), m = r >= 0 ? nv : 0;
-            q[d][u] = load8_bytes(c.q + (int64_t)r * c.ld_q + col, m);
-            scale[d][u] = m > 0 ? c.scale[(int64_t)r * c.ld_scale + (col >> 5)] : 0;
+            const int64_t r = row(u);
+            const int8_t *p = c.q + r * c.ld_q + col;
+            if constexpr (NARROW) q[d][u] = load8_bytes(p, r >= 0 ? nv : 0);
+            else q[d][u] = *(const u32x2_a1 *)(r >= 0 ? p - window_back(nv) : (const int8_t *)&zero_piece);
+            scale[d][u] = *(r >= 0 ? c.scale + r * c.ld_scale + (min(col, col + nv - 1) >> 5)
+                                   : (const uint8_t *)&zero_piece);
         }
     }
-    __device__ __forceinline__ void store(int d, char *lds)
+    template <bool NARROW>
+    __device__ __forceinline__ void store(int d, int nv, bool whole, char *lds)
     {
 #pragma unroll
         for (int u = 0; u < B::U; ++u) {
             float f[8];
-            ckpt_unpack(q[d][u], scale[d][u], f);
+            ckpt_unpack(NARROW || whole ? q[d][u] : end_of_row(q[d][u], nv), scale[d][u], f);
             this->v[0][u] = pack8(f);
         }
-        B::store(0, lds);
+        B::template store<true>(0, 0, true, lds);
     }
 };
 
@@ -546,6 +559,36 @@ __device__ __forceinline__ void multiply_step(const char *ps, const char *qs, in
     }
 }
 
+// Of eight values as four words, those that are positive (not zero, no sign, no NaN), in
+// the sign bits of the words' halves: bf16, and a checkpoint's bytes.
+__device__ __forceinline__ u32x4_r positive_bf16(u32x4_r h)
+{
+    typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
+    u32x4_r r;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        // 1 .. 0x7F80 becomes 0 .. 0x7F7F; 0x80 more sets the sign of what is above
+        const u16x2_t t = __builtin_bit_cast(u16x2_t, (uint32_t)h[k]) - (u16x2_t){1, 1};
+        const u16x2_t u = t + (u16x2_t){0x80, 0x80};
+        r[k] = ~(__builtin_bit_cast(uint32_t, t) | __builtin_bit_cast(uint32_t, u)) & 0x80008000u;
+    }
+    return r;
+}
+__device__ __forceinline__ u32x4_r positive_bytes(u32x2_r q, int scale)
+{
+    u32x4_r r;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const uint32_t w = q[k], any = (w & 0x7F7F7F7Fu) + 0x7F7F7F7Fu;
+        const uint32_t m = scale == 255 ? 0 : any & ~w & 0x80808080u;
+        r[2 * k] = __builtin_amdgcn_perm(m, m, 0x010C000Cu);       // bytes 0, 1 on top of the halves
+        r[2 * k + 1] = __builtin_amdgcn_perm(m, m, 0x030C020Cu);   // bytes 2, 3
+    }
+    return r;
+}
+// All bits of each half where its sign is set.
+__device__ __forceinline__ uint32_t half_signs(uint32_t w) { return __builtin_amdgcn_perm(w, w, 0x09090808u); }
+
 template <int TP, int TQ>
 __device__ __forceinline__ void clear(f32x16_t (&acc)[TP][TQ])
 {
@@ -570,11 +613,14 @@ struct RowsTile {
     static constexpr int LDO = BP + 8;      // epilogue rows
 };
 
-// DIRECT: by direct loads, NS stages (D register sets for the last, shorter step: 1); else
-// through D register sets and two stages.
-template <int OP, int WP, int WQ, int TP, int TQ, int BK, int NS, int D, bool DIRECT>
+// How operands come: by direct loads and NS stages, or through D register sets and two
+// stages, and that for rows of at least 8 values or of fewer.
+enum { BY_DIRECT, BY_REGISTERS, BY_VALUES };
+
+template <int OP, int WP, int WQ, int TP, int TQ, int BK, int NS, int D, int BY>
 __global__ __launch_bounds__(64 * WP * WQ, 2) void expert_rows_kernel(ExpertArgs a, int p_tiles)
 {
+    constexpr bool DIRECT = BY == BY_DIRECT, NARROW = BY == BY_VALUES;
     static_assert(DIRECT ? D == 1 : NS == 2, "stages");
     using T = RowsTile<OP, WP, WQ, TP, TQ, BK, D>;
     constexpr int NT = T::NT, BP = T::BP, BQ = T::BQ;
@@ -595,9 +641,47 @@ __global__ __launch_bounds__(64 * WP * WQ, 2) void expert_rows_kernel(ExpertArgs
 
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
     const int wp = wave % WP * TP * 32, wq = wave / WP * TQ * 32;
+    // the pieces of C that this thread stores: features f.. of the places i0, i0 + NT / (BP / 8), ..
+    constexpr int PIECES = BQ * (BP / 8) / NT;
+    constexpr bool MASKED = OP == OP_DX_X || OP == OP_DX_CKPT;
+    const int i0 = tid / (BP / 8), f = tid % (BP / 8) * 8, nv = NP - p0 - f;
+    const bool whole = NP - p0 >= BP;
+    // Which inputs are positive: words of two, in their halves' sign bits, are shifted into one
+    // register for four pieces, and read while the first steps load (at the end it would be
+    // the whole latency of a row read at random).
+    uint32_t positive[(PIECES + 3) / 4];
+    auto read_positive = [&] {
+        constexpr int B = PIECES < 4 ? PIECES : 4;
+#pragma unroll
+        for (int c0 = 0; c0 < PIECES; c0 += B) {
+            u32x4_r h[B];
+            u32x2_r q[B];
+            int scale[B];
+#pragma unroll
+            for (int c = 0; c < B; ++c) {
+                const int64_t r = max(row_of[i0 + (c0 + c) * (NT / (BP / 8))], 0);
+                if constexpr (OP == OP_DX_X) {
+                    h[c] = *(const u32x4_a2 *)(a.x + r * a.ld_x + p0 + f);
+                } else {
+                    q[c] = *(const u32x2_a1 *)(a.c.q + r * a.c.ld_q + p0 + f);
+                    scale[c] = a.c.scale[r * a.c.ld_scale + ((p0 + f) >> 5)];
+                }
+            }
+            uint32_t m = 0;
+#pragma unroll
+            for (int c = 0; c < B; ++c) {
+                if constexpr (OP == OP_DX_CKPT) h[c] = positive_bytes(q[c], scale[c]);
+                else h[c] = positive_bf16(h[c]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) m = m >> 1 | h[c][k];
+            }
+            positive[c0 / 4] = m;
+        }
+    };
+    const bool has_expert = pc.e < a.E;      // else zeros are stored
     f32x16_t acc[TP][TQ];
     clear(acc);
-    if (pc.e < a.E) {
+    if (has_expert) {
         const uint16_t *q = OP == OP_FORWARD ? a.x : a.dy;
         const int64_t ldq = OP == OP_FORWARD ? a.ld_x : a.ld_dy;
         const uint16_t *w = a.w + (int64_t)pc.e * a.out * a.ld_w;
@@ -619,19 +703,22 @@ __global__ __launch_bounds__(64 * WP * WQ, 2) void expert_rows_kernel(ExpertArgs
             else if constexpr (OP == OP_FORWARD) tp.copy(u, kt, st);
             else tp.copy(u, nvp > 0 ? wcol + (int64_t)(kt * BK + tp.krow(u)) * a.ld_w : nullptr, st);
         };
-        auto load = [&](int d, int kt) {
+        auto load = [&](auto narrow, int d, int kt) {
+            constexpr bool N = decltype(narrow)::value;
             if constexpr (OP == OP_FORWARD)
-                tp.load(d, kt, K);
+                tp.template load<N>(d, kt, K);
             else
-                tp.load(d, [&](int u) -> const uint16_t * {
+                tp.template load<N>(d, [&](int u) -> const uint16_t * {
                     const int k = kt * BK + tp.krow(u);
                     return k < K ? wcol + (int64_t)k * a.ld_w : nullptr;
-                }, nvp, NP - p0 >= BP, NP >= 8);
-            tq.load(d, kt, K);
+                }, nvp);
+            tq.template load<N>(d, kt, K);
         };
-        auto store = [&](int d, char *st) {
-            tp.store(d, st);
-            tq.store(d, st + T::P::BYTES);
+        auto store = [&](auto narrow, int d, int kt, char *st) {
+            constexpr bool N = decltype(narrow)::value;
+            if constexpr (OP == OP_FORWARD) tp.template store<N>(d, kt, K, st);
+            else tp.template store<N>(d, nvp, NP - p0 >= BP, st);
+            tq.template store<N>(d, kt, K, st + T::P::BYTES);
         };
         int now = 0;     // stage of step kt
         // a step's products, with `copies` direct loads of the step that comes NS - 1 later
@@ -647,13 +734,20 @@ __global__ __launch_bounds__(64 * WP * WQ, 2) void expert_rows_kernel(ExpertArgs
             const int nk = K / BK;
             // the last, shorter step comes first, through registers and the last stage
             const bool rest = K % BK != 0;
-            if (rest) load(0, nk);
+            const bool wide = K >= 8 && (OP == OP_FORWARD || NP >= 8);
+            if (rest && wide) load(std::false_type(), 0, nk);
             for (int kt = 0; kt < NS - 1 && kt < nk; ++kt)
 #pragma unroll
                 for (int u = 0; u < L; ++u) copy(u, kt, lds + kt * T::STAGE);
+            if (MASKED && whole) read_positive();
             if (rest) {
                 now = NS - 1;
-                store(0, lds + now * T::STAGE);
+                if (wide) {
+                    store(std::false_type(), 0, nk, lds + now * T::STAGE);
+                } else {
+                    load(std::true_type(), 0, nk);
+                    store(std::true_type(), 0, nk, lds + now * T::STAGE);
+                }
                 meet();
                 multiply(NoCopies(), 0);
             }
@@ -670,20 +764,20 @@ __global__ __launch_bounds__(64 * WP * WQ, 2) void expert_rows_kernel(ExpertArgs
             }
         } else {
             const int nk = (K + BK - 1) / BK;
-            load(0, 0);
+            const std::integral_constant<bool, NARROW> narrow;
 #pragma unroll
-            for (int d = 1; d < D; ++d)
-                if (d < nk) load(d, d);
-            store(0, lds);
-            if (D < nk) load(0, D);
+            for (int d = 0; d < D; ++d) load(narrow, d, d);
+            if (MASKED && whole) read_positive();
+            store(narrow, 0, 0, lds);
+            load(narrow, 0, D);
             for (int k0 = 0; k0 < nk; k0 += D) {
 #pragma unroll
                 for (int d = 0; d < D; ++d) {
                     const int kt = k0 + d, next = (d + 1) % D;      // step, register set of the next one
                     if (kt >= nk) break;
                     meet();
-                    if (kt + 1 < nk) store(next, lds + (now ^ 1) * T::STAGE);
-                    if (kt + 1 + D < nk) load(next, kt + 1 + D);
+                    store(narrow, next, kt + 1, lds + (now ^ 1) * T::STAGE);
+                    load(narrow, next, kt + 1 + D);
                     multiply(NoCopies(), kt);
                 }
             }
@@ -741,55 +835,37 @@ __global__ __launch_bounds__(64 * WP * WQ, 2) void expert_rows_kernel(ExpertArgs
                 *(u32x2_r *)(out + (wq + 32 * j + (lane & 31)) * T::LDO + f) = o;
             }
     __syncthreads();
-    // a thread's pieces: features f.. of the places i0, i0 + NT / (BP / 8), ...; what masks
-    // them is loaded eight pieces at a time, before the first of them is stored
-    constexpr int PIECES = BQ * (BP / 8) / NT, B = PIECES < 8 ? PIECES : 8;
-    const int i0 = tid / (BP / 8), f = tid % (BP / 8) * 8, nv = NP - p0 - f;
-    if (nv <= 0) return;
-#pragma unroll 1
-    for (int c0 = 0; c0 < PIECES; c0 += B) {
-        int r[B];
-        u32x4_r h[B];
-        int scale[B];
+    auto to = [&](int r) -> uint16_t * {
+        return (OP == OP_FORWARD ? (uint16_t *)a.y + (int64_t)r * a.ld_y : a.dx + (int64_t)r * a.ld_dx) + p0 + f;
+    };
+    if (whole) {
 #pragma unroll
-        for (int c = 0; c < B; ++c) r[c] = row_of[i0 + (c0 + c) * (NT / (BP / 8))];
-        if (OP == OP_DX && a.relu) {
+        for (int c = 0; c < PIECES; ++c) {
+            const int i = i0 + c * (NT / (BP / 8)), r = row_of[i];
+            u32x4_r o = *(const u32x4_r *)(out + i * T::LDO + f);
+            if constexpr (MASKED) {
+                constexpr int B = PIECES < 4 ? PIECES : 4;
 #pragma unroll
-            for (int c = 0; c < B; ++c) {
-                const int64_t row = max(r[c], 0);
-                if (a.x) {
-                    h[c] = load8_bits(a.x + row * a.ld_x + p0 + f, nv);
-                } else {
-                    const u32x2_r q = load8_bytes(a.c.q + row * a.c.ld_q + p0 + f, nv);
-                    h[c] = u32x4_r{q[0], q[1], 0, 0};
-                    scale[c] = a.c.scale[row * a.c.ld_scale + ((p0 + f) >> 5)];
-                }
+                for (int k = 0; k < 4; ++k)
+                    o[k] &= half_signs(has_expert ? positive[c / 4] << (4 * B - 1 - (4 * (c % 4) + k)) : 0);
             }
+            if (r >= 0) *(u32x4_a2 *)to(r) = o;
         }
+    } else if (nv > 0) {
+#pragma unroll 1
+        for (int c = 0; c < PIECES; ++c) {
+            const int i = i0 + c * (NT / (BP / 8)), r = row_of[i];
+            if (r < 0) continue;
+            u32x4_r o = *(const u32x4_r *)(out + i * T::LDO + f);
+            if constexpr (MASKED) {
+                u32x4_r h;
+                if constexpr (OP == OP_DX_X) h = positive_bf16(load8_bits(a.x + (int64_t)r * a.ld_x + p0 + f, nv));
+                else h = positive_bytes(load8_bytes(a.c.q + (int64_t)r * a.c.ld_q + p0 + f, nv),
+                                        a.c.scale[(int64_t)r * a.c.ld_scale + ((p0 + f) >> 5)]);
 #pragma unroll
-        for (int c = 0; c < B; ++c) {
-            u32x4_r o = *(const u32x4_r *)(out + (i0 + (c0 + c) * (NT / (BP / 8))) * T::LDO + f);
-            if (OP == OP_DX && a.relu) {
-                // keep the values whose input is positive: not zero, no sign, no NaN
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    uint32_t keep;
-                    if (a.x) {
-                        const uint32_t lo = h[c][k] & 0xFFFFu, hi = h[c][k] >> 16;
-                        keep = (lo - 1 < 0x7F80u ? 0x0000FFFFu : 0u) | (hi - 1 < 0x7F80u ? 0xFFFF0000u : 0u);
-                    } else {
-                        const uint32_t t = h[c][k >> 1] >> (16 * (k & 1));
-                        keep = ((t & 0xFFu) - 1 < 127u ? 0x0000FFFFu : 0u) |
-                               (((t >> 8) & 0xFFu) - 1 < 127u ? 0xFFFF0000u : 0u);
-                        if (scale[c] == 255) keep = 0;
-                    }
-                    o[k] &= keep;
-                }
+                for (int k = 0; k < 4; ++k) o[k] &= half_signs(h[k]);
             }
-            if (r[c] >= 0) {
-                uint16_t *to = OP == OP_FORWARD ? (uint16_t *)a.y + (int64_t)r[c] * a.ld_y : a.dx + (int64_t)r[c] * a.ld_dx;
-                store8_bits(to + p0 + f, nv, o);
-            }
+            store8_bits(to(r), nv, o);
         }
     }
 }
@@ -840,9 +916,10 @@ __device__ __forceinline__ int run_units(int all, int teams) { return max((all +
 // Places whose row indices are held in LDS ahead of their use, a power of two.
 constexpr int DW_ROWS = 512;
 
-template <int WP, int WQ, int TP, int TQ, int BK, int NS, int D, bool DIRECT, bool CK>
+template <int WP, int WQ, int TP, int TQ, int BK, int NS, int D, int BY, bool CK>
 __global__ __launch_bounds__(64 * WP * WQ, 2) void expert_dw_kernel(ExpertArgs a, int p_tiles, int q_tiles)
 {
+    constexpr bool DIRECT = BY == BY_DIRECT, NARROW = BY == BY_VALUES;
     static_assert(DIRECT ? D == 1 : NS == 2, "stages");
     static_assert(DW_ROWS / BK > NS + 1 && DW_ROWS / BK > D + 2, "row indices are there a step before they are used");
     constexpr int NT = 64 * WP * WQ, BP = 32 * WP * TP, BQ = 32 * WQ * TQ;
@@ -924,13 +1001,15 @@ __global__ __launch_bounds__(64 * WP * WQ, 2) void expert_dw_kernel(ExpertArgs a
         };
         // through register set d
         auto load = [&](int d, int kt) {
-            tq.load(d, [&](int u) { return dy_at(kt, u); }, nvq, a.out - q0 >= BQ, a.out >= 8);
-            if constexpr (CK && !DIRECT) tp.load(d, a.c, [&](int u) { return row(kt, tp.krow(u)); }, pcol, nvp);
-            else tp.load(d, [&](int u) { return x_at(kt, u); }, nvp, in - p0 >= BP, in >= 8);
+            tq.template load<NARROW>(d, [&](int u) { return dy_at(kt, u); }, nvq);
+            if constexpr (CK && !DIRECT)
+                tp.template load<NARROW>(d, a.c, [&](int u) { return in > 0 ? row(kt, tp.krow(u)) : -1; }, pcol, nvp);
+            else
+                tp.template load<NARROW>(d, [&](int u) { return x_at(kt, u); }, nvp);
         };
         auto store = [&](int d, int stage) {
-            tq.store(d, lds + stage * Q::BYTES);
-            tp.store(d, lds + P_AT + stage * P::BYTES);
+            tq.template store<NARROW>(d, nvq, a.out - q0 >= BQ, lds + stage * Q::BYTES);
+            tp.template store<NARROW>(d, nvp, in - p0 >= BP, lds + P_AT + stage * P::BYTES);
         };
         auto restore = [&](int kt) { R::restore(lds + R_AT + kt % NS * R::BYTES, lds + P_AT + (kt & 1) * P::BYTES); };
         // a step after its loads: the next row indices now and then, db, the products
@@ -1114,12 +1193,12 @@ constexpr int64_t DW_BIG_ROWS = 16384, DW_SMALL_BLOCKS = 1024, DW_RUN = 256;
 // each expert and for the rest.
 static int64_t row_tiles(const ExpertArgs &a, int rows) { return a.n / rows + std::min<int64_t>(a.E + 1, a.n); }
 
-template <int OP, int WP, int WQ, int TP, int TQ, int BK, int NS, int D, bool DIRECT>
+template <int OP, int WP, int WQ, int TP, int TQ, int BK, int NS, int D, int BY>
 static void rows_go(const ExpertArgs &a, hipStream_t s)
 {
     using T = RowsTile<OP, WP, WQ, TP, TQ, BK, D>;
     const int p_tiles = (int)ceil_div(OP == OP_FORWARD ? a.out : a.in, T::BP);
-    expert_rows_kernel<OP, WP, WQ, TP, TQ, BK, NS, D, DIRECT>
+    expert_rows_kernel<OP, WP, WQ, TP, TQ, BK, NS, D, BY>
         <<<dim3((unsigned)(row_tiles(a, T::BQ) * p_tiles)), dim3(T::NT), 0, s>>>(a, p_tiles);
 }
 
@@ -1133,12 +1212,14 @@ template <int OP>
 static void rows_launch(const ExpertArgs &a, bool direct, hipStream_t s)
 {
     const int64_t big = row_tiles(a, 128) * ceil_div(OP == OP_FORWARD ? a.out : a.in, 256);
-    if (big >= BIG_TILES) {
-        if (direct) rows_go<OP, 2, 2, 4, 2, 32, 3, 1, true>(a, s);
-        else rows_go<OP, 2, 2, 2, 2, 32, 2, 3, false>(a, s);
+    const bool narrow = a.in < 8 || (OP != OP_FORWARD && a.out < 8);
+    if (big >= BIG_TILES && !narrow) {
+        if (direct) rows_go<OP, 2, 2, 4, 2, 32, 3, 1, BY_DIRECT>(a, s);
+        else rows_go<OP, 2, 2, 2, 2, 32, 2, 2, BY_REGISTERS>(a, s);
     } else {
-        if (direct) rows_go<OP, 2, 2, 1, 1, 64, 4, 1, true>(a, s);
-        else rows_go<OP, 2, 2, 1, 1, 64, 2, 3, false>(a, s);
+        if (direct) rows_go<OP, 2, 2, 1, 1, 64, 4, 1, BY_DIRECT>(a, s);
+        else if (!narrow) rows_go<OP, 2, 2, 1, 1, 64, 2, 3, BY_REGISTERS>(a, s);
+        else rows_go<OP, 2, 2, 1, 1, 64, 2, 1, BY_VALUES>(a, s);
     }
 }
 
@@ -1163,31 +1244,39 @@ static DwShape dw_shape(int64_t n, int in, int out)
 
 int expert_grad_teams(int64_t n, int in, int out) { return dw_shape(n, in, out).teams; }
 
-template <bool DIRECT, bool CK>
+template <int BY, bool CK>
 static void dw_go(const ExpertArgs &a, const DwShape &d, hipStream_t s)
 {
     const int p_tiles = a.dw ? (int)ceil_div(a.in, d.tile) : 1, q_tiles = (int)ceil_div(a.out, d.tile);
     const dim3 g((unsigned)(d.teams * p_tiles * q_tiles));
-    if (d.tile == 256) {
-        if constexpr (DIRECT) expert_dw_kernel<2, 4, 4, 2, 32, 4, 1, true, CK><<<g, dim3(512), 0, s>>>(a, p_tiles, q_tiles);
-        else expert_dw_kernel<2, 4, 4, 2, 32, 2, 1, false, CK><<<g, dim3(512), 0, s>>>(a, p_tiles, q_tiles);
+    if constexpr (BY == BY_DIRECT) {
+        if (d.tile == 256) expert_dw_kernel<2, 4, 4, 2, 32, 4, 1, BY, CK><<<g, dim3(512), 0, s>>>(a, p_tiles, q_tiles);
+        else expert_dw_kernel<2, 2, 1, 1, 64, 4, 1, BY, CK><<<g, dim3(256), 0, s>>>(a, p_tiles, q_tiles);
+    } else if constexpr (BY == BY_REGISTERS) {
+        if (d.tile == 256) expert_dw_kernel<2, 4, 4, 2, 32, 2, 1, BY, CK><<<g, dim3(512), 0, s>>>(a, p_tiles, q_tiles);
+        else expert_dw_kernel<2, 2, 1, 1, 64, 2, 3, BY, CK><<<g, dim3(256), 0, s>>>(a, p_tiles, q_tiles);
     } else {
-        if constexpr (DIRECT) expert_dw_kernel<2, 2, 1, 1, 64, 4, 1, true, CK><<<g, dim3(256), 0, s>>>(a, p_tiles, q_tiles);
-        else expert_dw_kernel<2, 2, 1, 1, 64, 2, 3, false, CK><<<g, dim3(256), 0, s>>>(a, p_tiles, q_tiles);
+        expert_dw_kernel<2, 2, 1, 1, 64, 2, 1, BY, CK><<<g, dim3(256), 0, s>>>(a, p_tiles, q_tiles);
     }
 }
 
 hipError_t launch_expert_grad(const ExpertArgs &a, hipStream_t s)
 {
     const bool dy_ok = rows_aligned(a.dy, a.ld_dy);
-    if (a.dx && a.n > 0) rows_launch<OP_DX>(a, dy_ok && rows_aligned(a.w, a.ld_w), s);
+    if (a.dx && a.n > 0) {
+        const bool direct = dy_ok && rows_aligned(a.w, a.ld_w);
+        if (!a.relu) rows_launch<OP_DX>(a, direct, s);
+        else if (a.x) rows_launch<OP_DX_X>(a, direct, s);
+        else rows_launch<OP_DX_CKPT>(a, direct, s);
+    }
     if (a.dw || a.db) {
         const DwShape d = dw_shape(a.n, a.in, a.out);
         if (a.n > 0) {
             const bool ck = a.dw && !a.x;
             const bool x_ok = !a.dw || (ck ? rows_aligned(a.c.q, a.c.ld_q, 1) : rows_aligned(a.x, a.ld_x));
-            if (ck) dy_ok && x_ok ? dw_go<true, true>(a, d, s) : dw_go<false, true>(a, d, s);
-            else dy_ok && x_ok ? dw_go<true, false>(a, d, s) : dw_go<false, false>(a, d, s);
+            if (dy_ok && x_ok) ck ? dw_go<BY_DIRECT, true>(a, d, s) : dw_go<BY_DIRECT, false>(a, d, s);
+            else if (a.out >= 8 && (a.in >= 8 || !a.dw)) ck ? dw_go<BY_REGISTERS, true>(a, d, s) : dw_go<BY_REGISTERS, false>(a, d, s);
+            else ck ? dw_go<BY_VALUES, true>(a, d, s) : dw_go<BY_VALUES, false>(a, d, s);
         }
         const int64_t work = (int64_t)a.out * ((a.in + 3) / 4) + a.out;
         expert_dw_sum_kernel<<<dim3((unsigned)ceil_div(work, 256), a.E), dim3(256), 0, s>>>(a, d.teams);
