@@ -84,8 +84,8 @@ struct ExpertArgs {
     float *part, *part_db;
 };
 hipError_t launch_expert_linear(const ExpertArgs &a, hipStream_t s);
-// Teams of blocks among which the weight gradient's rows are divided.
-int expert_grad_teams(int64_t n, int in, int out);
+// Teams of blocks among which the weight gradient's rows are divided (0: one for each expert).
+int expert_grad_teams(int64_t n, int n_experts, int in, int out);
 hipError_t launch_expert_grad(const ExpertArgs &a, hipStream_t s);
 
 }  // namespace im

@@ -2,6 +2,8 @@
 // then the launches.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "../../include/instantmimic.h"
 #include "expert.h"
 
@@ -220,7 +222,7 @@ int64_t im_expert_linear_grad_workspace(int64_t n, int32_t n_experts, int32_t in
     if (n < 0 || n > MAX_ROWS || n_experts < 1 || n_experts > IM_MAX_EXPERTS || in < 1 || in > MAX_WIDTH ||
         out < 1 || out > MAX_WIDTH)
         return -1;
-    const int64_t teams = expert_grad_teams(n, in, out);
+    const int64_t teams = std::max(1, expert_grad_teams(n, n_experts, in, out));
     return 2 * teams * (out * pad4(in) + out) * (int64_t)sizeof(float);
 }
 
@@ -263,7 +265,7 @@ im_status im_expert_linear_grad(const im_expert_layer_grad *p, void *stream)
     a.db = p->db;
     if (sums) {
         a.part = (float *)p->workspace;
-        a.part_db = a.part + 2 * (int64_t)expert_grad_teams(p->n, p->in, p->out) * p->out * pad4(p->in);
+        a.part_db = a.part + 2 * (int64_t)expert_grad_teams(p->n, p->n_experts, p->in, p->out) * p->out * pad4(p->in);
     }
     return launched(launch_expert_grad(a, (hipStream_t)stream), "expert_linear_grad launch");
 }

@@ -618,17 +618,20 @@ struct RowsTile {
 enum { BY_DIRECT, BY_REGISTERS, BY_VALUES };
 
 template <int OP, int WP, int WQ, int TP, int TQ, int BK, int NS, int D, int BY>
-__global__ __launch_bounds__(64 * WP * WQ, 2) void expert_rows_kernel(ExpertArgs a, int p_tiles)
-{
-    constexpr bool DIRECT = BY == BY_DIRECT, NARROW = BY == BY_VALUES;
+struct RowsShape {
+    static constexpr bool DIRECT = BY == BY_DIRECT, NARROW = BY == BY_VALUES;
     static_assert(DIRECT ? D == 1 : NS == 2, "stages");
     using T = RowsTile<OP, WP, WQ, TP, TQ, BK, D>;
-    constexpr int NT = T::NT, BP = T::BP, BQ = T::BQ;
-    constexpr int LDS = std::max(NS * T::STAGE, BQ * T::LDO * 2);
-    __shared__ __attribute__((aligned(1024))) char lds[LDS];
-    __shared__ int row_of[BQ];
-    __shared__ __attribute__((aligned(16))) float bias[OP == OP_FORWARD ? BP : 4];
-    const int id = xcd_order(blockIdx.x, gridDim.x);
+    static constexpr int NT = T::NT;
+    // LDS: the stages (the outputs at the end), the places' rows, the bias
+    static constexpr int ROWS_AT = std::max(NS * T::STAGE, T::BQ * T::LDO * 2), BIAS_AT = ROWS_AT + T::BQ * 4;
+    static constexpr int LDS = BIAS_AT + (OP == OP_FORWARD ? T::BP * 4 : 0);
+
+    __device__ __forceinline__ static void run(const ExpertArgs &a, int p_tiles, int id, char *lds)
+    {
+    constexpr int BP = T::BP, BQ = T::BQ;
+    int *row_of = (int *)(lds + ROWS_AT);
+    float *bias = (float *)(lds + BIAS_AT);
     const Piece pc = find_piece(a.offsets, a.E, a.n, id / p_tiles, BQ);
     if (pc.e < 0) return;
     const int p0 = id % p_tiles * BP;
@@ -765,19 +768,22 @@ __global__ __launch_bounds__(64 * WP * WQ, 2) void expert_rows_kernel(ExpertArgs
         } else {
             const int nk = (K + BK - 1) / BK;
             const std::integral_constant<bool, NARROW> narrow;
+            // the order of the direct loads: a last, shorter step first
+            const bool rest = K % BK != 0;
+            auto nth = [&](int i) { return rest && i < nk ? (i == 0 ? nk - 1 : i - 1) : i; };
 #pragma unroll
-            for (int d = 0; d < D; ++d) load(narrow, d, d);
+            for (int d = 0; d < D; ++d) load(narrow, d, nth(d));
             if (MASKED && whole) read_positive();
-            store(narrow, 0, 0, lds);
-            load(narrow, 0, D);
+            store(narrow, 0, nth(0), lds);
+            load(narrow, 0, nth(D));
             for (int k0 = 0; k0 < nk; k0 += D) {
 #pragma unroll
                 for (int d = 0; d < D; ++d) {
                     const int kt = k0 + d, next = (d + 1) % D;      // step, register set of the next one
                     if (kt >= nk) break;
                     meet();
-                    store(narrow, next, kt + 1, lds + (now ^ 1) * T::STAGE);
-                    load(narrow, next, kt + 1 + D);
+                    store(narrow, next, nth(kt + 1), lds + (now ^ 1) * T::STAGE);
+                    load(narrow, next, nth(kt + 1 + D));
                     multiply(NoCopies(), kt);
                 }
             }
@@ -868,6 +874,14 @@ __global__ __launch_bounds__(64 * WP * WQ, 2) void expert_rows_kernel(ExpertArgs
             store8_bits(to(r), nv, o);
         }
     }
+    }
+};
+
+template <typename S>
+__global__ __launch_bounds__(S::NT, 2) void expert_rows_kernel(ExpertArgs a, int p_tiles)
+{
+    __shared__ __attribute__((aligned(1024))) char lds[S::LDS];
+    S::run(a, p_tiles, xcd_order(blockIdx.x, gridDim.x), lds);
 }
 
 // ---------------------------------------------------------------------------
@@ -916,34 +930,33 @@ __device__ __forceinline__ int run_units(int all, int teams) { return max((all +
 // Places whose row indices are held in LDS ahead of their use, a power of two.
 constexpr int DW_ROWS = 512;
 
+// teams 0: a team for each expert instead, which takes its rows alone and writes dw and db
+// itself, zeros for none.
 template <int WP, int WQ, int TP, int TQ, int BK, int NS, int D, int BY, bool CK>
-__global__ __launch_bounds__(64 * WP * WQ, 2) void expert_dw_kernel(ExpertArgs a, int p_tiles, int q_tiles)
-{
-    constexpr bool DIRECT = BY == BY_DIRECT, NARROW = BY == BY_VALUES;
+struct DwShape {
+    static constexpr bool DIRECT = BY == BY_DIRECT, NARROW = BY == BY_VALUES;
     static_assert(DIRECT ? D == 1 : NS == 2, "stages");
     static_assert(DW_ROWS / BK > NS + 1 && DW_ROWS / BK > D + 2, "row indices are there a step before they are used");
-    constexpr int NT = 64 * WP * WQ, BP = 32 * WP * TP, BQ = 32 * WQ * TQ;
-    constexpr bool BYTES = DIRECT && CK;      // x's bytes by direct loads
+    static constexpr int NT = 64 * WP * WQ, BP = 32 * WP * TP, BQ = 32 * WQ * TQ;
+    static constexpr bool BYTES = DIRECT && CK;      // x's bytes by direct loads
     using P = std::conditional_t<CK && !DIRECT, AcrossCkpt<BP, NT, BK, D>, AcrossTile<BP, NT, BK, D>>;
     using Q = AcrossTile<BQ, NT, BK, D>;
     using R = CkptBytes<BP, NT, BK>;
     // direct loads of a step
-    constexpr int LP = BYTES ? R::U : P::U, L = (BYTES ? 2 * R::U : P::U) + Q::U;
+    static constexpr int LP = BYTES ? R::U : P::U, L = (BYTES ? 2 * R::U : P::U) + Q::U;
     // LDS: NS tiles of dy, of x (2 restored ones and NS of bytes), two sets of row indices
-    constexpr int PS = BYTES ? 2 : NS, P_AT = NS * Q::BYTES, R_AT = P_AT + PS * P::BYTES;
-    constexpr int ROWS_AT = R_AT + (BYTES ? NS * R::BYTES : 0);
-    __shared__ __attribute__((aligned(1024))) char lds[ROWS_AT + 2 * DW_ROWS * 4];
+    static constexpr int PS = BYTES ? 2 : NS, P_AT = NS * Q::BYTES, R_AT = P_AT + PS * P::BYTES;
+    static constexpr int ROWS_AT = R_AT + (BYTES ? NS * R::BYTES : 0), LDS = ROWS_AT + 2 * DW_ROWS * 4;
+
+    __device__ __forceinline__ static void run(const ExpertArgs &a, int p_tiles, int q_tiles, int teams, int id, char *lds)
+    {
     int *rows = (int *)(lds + ROWS_AT);
-    const int id = xcd_order(blockIdx.x, gridDim.x);
-    const int tiles = p_tiles * q_tiles, team = id / tiles, teams = gridDim.x / tiles;
+    const int team = id / (p_tiles * q_tiles);
     const int p0 = id % p_tiles * BP, q0 = id / p_tiles % q_tiles * BQ;
     const int lane = threadIdx.x & 63, wave = wave_id();
     const int wp = wave % WP * TP * 32, wq = wave / WP * TQ * 32;
     const bool with_db = a.db && p0 == 0;
     const int in4 = (a.in + 3) & ~3;
-
-    const int all = units_before(a, a.E), run = run_units(all, teams);
-    const int begin = min(team * run, all), end = min(begin + run, all);
 
     P tp;
     Q tq;
@@ -1073,10 +1086,55 @@ __global__ __launch_bounds__(64 * WP * WQ, 2) void expert_dw_kernel(ExpertArgs a
         meet();
     };
 
-    // the experts of the run; `u`: the units before expert e
-    int e = 0, u = 0;
-    {
-        // the last expert with begin at or after its first unit, 64 at a time
+    // the product to dw and db of expert e (slot < 0), or to a slot of the workspace
+    auto finish = [&](int e, int64_t slot) {
+        float *c = slot < 0 ? a.dw + (int64_t)e * a.out * a.ld_dw : a.part + slot * a.out * in4;
+        const int64_t ldc = slot < 0 ? a.ld_dw : in4;
+        if (with_db) {
+            float *red = (float *)lds;      // [NT / PAIRS][BQ]
+            red[threadIdx.x / PAIRS * BQ + threadIdx.x % PAIRS * 2] = db[0];
+            red[threadIdx.x / PAIRS * BQ + threadIdx.x % PAIRS * 2 + 1] = db[1];
+            __syncthreads();
+            float *d = slot < 0 ? a.db + (int64_t)e * a.out : a.part_db + slot * a.out;
+            for (int i = threadIdx.x; i < BQ && q0 + i < a.out; i += NT) {
+                float t = 0.0f;
+#pragma unroll
+                for (int r = 0; r < NT / PAIRS; ++r) t += red[r * BQ + i];
+                d[q0 + i] = t;
+            }
+            __syncthreads();
+        }
+        if (!a.dw) return;
+#pragma unroll
+        for (int j = 0; j < TQ; ++j) {
+            const int o = q0 + wq + 32 * j + (lane & 31);
+            if (o >= a.out) continue;
+#pragma unroll
+            for (int i = 0; i < TP; ++i)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int f = p0 + wp + 32 * i + 8 * g + 4 * (lane >> 5);
+                    const f32x4_r v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2],
+                                       acc[i][j][4 * g + 3]};
+                    if (f + 4 <= a.in) {
+                        *(f32x4_a4 *)(c + o * ldc + f) = v;
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (f + k < a.in) c[o * ldc + f + k] = v[k];
+                    }
+                }
+        }
+    };
+
+    // the experts of the run [begin, end) of units; `u`: the units before expert e
+    int begin = 0, end = 1, e = team, u = 0;
+    if (teams > 0) {
+        const int all = units_before(a, a.E), run = run_units(all, teams);
+        begin = min(team * run, all);
+        end = min(begin + run, all);
+        // the first expert that ends past `begin`, 64 at a time
+        e = a.E;
         int carry = 0;
         for (int e0 = 0; e0 < a.E; e0 += 64) {
             const int j = e0 + lane;
@@ -1099,52 +1157,40 @@ __global__ __launch_bounds__(64 * WP * WQ, 2) void expert_dw_kernel(ExpertArgs a
     }
     for (; u < end && e < a.E; ++e) {
         const Span sp = span_of(a, e);
-        if (sp.units == 0) continue;
-        const int ub = max(begin, u), ue = min(end, u + sp.units);
-        const int k0 = (ub - u) * DW_UNIT, k1 = min((ue - u) * DW_UNIT, sp.count);
-        product(__builtin_amdgcn_readfirstlane(sp.first + k0), __builtin_amdgcn_readfirstlane(k1 - k0));
-
-        const bool whole = u >= begin && u + sp.units <= end;
-        const int64_t slot = 2 * team + (u >= begin ? 1 : 0);
-        float *c = whole ? a.dw + (int64_t)e * a.out * a.ld_dw : a.part + slot * a.out * in4;
-        const int64_t ldc = whole ? a.ld_dw : in4;
-        if (with_db) {
-            float *red = (float *)lds;      // [NT / PAIRS][BQ]
-            red[threadIdx.x / PAIRS * BQ + threadIdx.x % PAIRS * 2] = db[0];
-            red[threadIdx.x / PAIRS * BQ + threadIdx.x % PAIRS * 2 + 1] = db[1];
-            __syncthreads();
-            float *d = whole ? a.db + (int64_t)e * a.out : a.part_db + slot * a.out;
-            for (int i = threadIdx.x; i < BQ && q0 + i < a.out; i += NT) {
-                float t = 0.0f;
-#pragma unroll
-                for (int r = 0; r < NT / PAIRS; ++r) t += red[r * BQ + i];
-                d[q0 + i] = t;
-            }
-            __syncthreads();
+        int k0 = 0, k1 = sp.count;
+        int64_t slot = -1;
+        if (teams > 0) {
+            if (sp.units == 0) continue;
+            k0 = (max(begin, u) - u) * DW_UNIT;
+            k1 = min((min(end, u + sp.units) - u) * DW_UNIT, sp.count);
+            if (u < begin || u + sp.units > end) slot = 2 * team + (u >= begin ? 1 : 0);
         }
-        if (a.dw)
-#pragma unroll
-            for (int j = 0; j < TQ; ++j) {
-                const int o = q0 + wq + 32 * j + (lane & 31);
-                if (o >= a.out) continue;
-#pragma unroll
-                for (int i = 0; i < TP; ++i)
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        const int f = p0 + wp + 32 * i + 8 * g + 4 * (lane >> 5);
-                        const f32x4_r v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2],
-                                           acc[i][j][4 * g + 3]};
-                        if (f + 4 <= a.in) {
-                            *(f32x4_a4 *)(c + o * ldc + f) = v;
-                        } else {
-#pragma unroll
-                            for (int k = 0; k < 4; ++k)
-                                if (f + k < a.in) c[o * ldc + f + k] = v[k];
-                        }
-                    }
-            }
+        product(__builtin_amdgcn_readfirstlane(sp.first + k0), __builtin_amdgcn_readfirstlane(k1 - k0));
+        finish(e, slot);
+        if (teams == 0) break;
         u += sp.units;
     }
+    }
+};
+
+template <typename S>
+__global__ __launch_bounds__(S::NT, 2) void expert_dw_kernel(ExpertArgs a, int p_tiles, int q_tiles, int teams)
+{
+    __shared__ __attribute__((aligned(1024))) char lds[S::LDS];
+    S::run(a, p_tiles, q_tiles, teams, xcd_order(blockIdx.x, gridDim.x), lds);
+}
+
+// Both gradients in one launch, the weights' blocks first: for few rows each of them is
+// latency, which the other's blocks fill.
+template <typename X, typename W>
+__global__ __launch_bounds__(X::NT, 2) void expert_grad_kernel(ExpertArgs a, int x_tiles, int p_tiles, int q_tiles,
+                                                               int teams, int w_blocks)
+{
+    static_assert(X::NT == W::NT, "one block size");
+    __shared__ __attribute__((aligned(1024))) char lds[std::max(X::LDS, W::LDS)];
+    const int b = blockIdx.x;
+    if (b < w_blocks) W::run(a, p_tiles, q_tiles, teams, xcd_order(b, w_blocks), lds);
+    else X::run(a, x_tiles, xcd_order(b - w_blocks, gridDim.x - w_blocks), lds);
 }
 
 // dw and db of the experts that no single team's run holds: the parts in the teams' order,
@@ -1186,21 +1232,9 @@ __global__ __launch_bounds__(256) void expert_dw_sum_kernel(ExpertArgs a, int te
     }
 }
 
-constexpr int64_t BIG_TILES = 512;
-constexpr int64_t DW_BIG_ROWS = 16384, DW_SMALL_BLOCKS = 1024, DW_RUN = 256;
-
 // Tiles of a launch over rows, for any group sizes: whole tiles, and a shorter one for
 // each expert and for the rest.
 static int64_t row_tiles(const ExpertArgs &a, int rows) { return a.n / rows + std::min<int64_t>(a.E + 1, a.n); }
-
-template <int OP, int WP, int WQ, int TP, int TQ, int BK, int NS, int D, int BY>
-static void rows_go(const ExpertArgs &a, hipStream_t s)
-{
-    using T = RowsTile<OP, WP, WQ, TP, TQ, BK, D>;
-    const int p_tiles = (int)ceil_div(OP == OP_FORWARD ? a.out : a.in, T::BP);
-    expert_rows_kernel<OP, WP, WQ, TP, TQ, BK, NS, D, BY>
-        <<<dim3((unsigned)(row_tiles(a, T::BQ) * p_tiles)), dim3(T::NT), 0, s>>>(a, p_tiles);
-}
 
 // Rows that direct loads can take: all at multiples of 16 bytes.
 static bool rows_aligned(const void *p, int64_t ld, int64_t size = 2)
@@ -1209,17 +1243,40 @@ static bool rows_aligned(const void *p, int64_t ld, int64_t size = 2)
 }
 
 template <int OP>
+using RowsBig = RowsShape<OP, 2, 2, 4, 2, 32, 3, 1, BY_DIRECT>;
+template <int OP>
+using RowsBigRegs = RowsShape<OP, 2, 2, 2, 2, 32, 2, 2, BY_REGISTERS>;
+template <int OP, int BY>
+using RowsSmall = RowsShape<OP, 2, 2, 1, 1, 64, BY == BY_DIRECT ? 4 : 2, BY == BY_REGISTERS ? 3 : 1, BY>;
+
+// From this many 256 x 128 tiles on they are used, below it 64 x 64 ones.
+constexpr int64_t BIG_TILES = 512;
+
+template <int OP>
+static bool rows_big(const ExpertArgs &a)
+{
+    const int np = OP == OP_FORWARD ? a.out : a.in;
+    return row_tiles(a, 128) * ceil_div(np, 256) >= BIG_TILES;
+}
+
+template <typename S, int OP>
+static void rows_go(const ExpertArgs &a, hipStream_t s)
+{
+    const int p_tiles = (int)ceil_div(OP == OP_FORWARD ? a.out : a.in, S::T::BP);
+    expert_rows_kernel<S><<<dim3((unsigned)(row_tiles(a, S::T::BQ) * p_tiles)), dim3(S::NT), 0, s>>>(a, p_tiles);
+}
+
+template <int OP>
 static void rows_launch(const ExpertArgs &a, bool direct, hipStream_t s)
 {
-    const int64_t big = row_tiles(a, 128) * ceil_div(OP == OP_FORWARD ? a.out : a.in, 256);
     const bool narrow = a.in < 8 || (OP != OP_FORWARD && a.out < 8);
-    if (big >= BIG_TILES && !narrow) {
-        if (direct) rows_go<OP, 2, 2, 4, 2, 32, 3, 1, BY_DIRECT>(a, s);
-        else rows_go<OP, 2, 2, 2, 2, 32, 2, 2, BY_REGISTERS>(a, s);
+    if (rows_big<OP>(a) && (direct || !narrow)) {
+        if (direct) rows_go<RowsBig<OP>, OP>(a, s);
+        else rows_go<RowsBigRegs<OP>, OP>(a, s);
     } else {
-        if (direct) rows_go<OP, 2, 2, 1, 1, 64, 4, 1, BY_DIRECT>(a, s);
-        else if (!narrow) rows_go<OP, 2, 2, 1, 1, 64, 2, 3, BY_REGISTERS>(a, s);
-        else rows_go<OP, 2, 2, 1, 1, 64, 2, 1, BY_VALUES>(a, s);
+        if (direct) rows_go<RowsSmall<OP, BY_DIRECT>, OP>(a, s);
+        else if (!narrow) rows_go<RowsSmall<OP, BY_REGISTERS>, OP>(a, s);
+        else rows_go<RowsSmall<OP, BY_VALUES>, OP>(a, s);
     }
 }
 
@@ -1229,57 +1286,99 @@ hipError_t launch_expert_linear(const ExpertArgs &a, hipStream_t s)
     return hipGetLastError();
 }
 
-// Tile of the weight gradient and its teams: 256 x 256 on the CUs' one block each where the
-// rows give every team at least DW_RUN of them, else 64 x 64.
-struct DwShape {
-    int tile, teams;
+template <int BY, bool CK>
+using DwBig = DwShape<2, 4, 4, 2, 32, BY == BY_DIRECT ? 4 : 2, 1, BY, CK>;
+template <int BY, bool CK>
+using DwSmall = DwShape<2, 2, 1, 1, 64, BY == BY_DIRECT ? 4 : 2, BY == BY_REGISTERS ? 3 : 1, BY, CK>;
+
+// The weight gradient's tile and teams: 256 x 256 tiles, a block on each CU, from
+// DW_BIG_ROWS rows on where both widths exceed half of one; else 64 x 64 ones, a team for
+// each expert up to DW_EXPERT_ROWS rows where that makes DW_EXPERT_BLOCKS blocks, or
+// DW_SMALL_BLOCKS blocks whose teams have at least DW_RUN rows.
+constexpr int64_t DW_BIG_ROWS = 16384, DW_EXPERT_ROWS = 8192, DW_EXPERT_BLOCKS = 128, DW_SMALL_BLOCKS = 1024,
+                  DW_RUN = 256;
+struct DwPlan {
+    int tile, teams;     // teams 0: the experts
 };
-static DwShape dw_shape(int64_t n, int in, int out)
+static DwPlan dw_plan(int64_t n, int n_experts, int in, int out)
 {
     const int64_t big = ceil_div(in, 256) * ceil_div(out, 256);
     if (n >= DW_BIG_ROWS && in > 128 && out > 128) return {256, (int)std::max<int64_t>(1, 256 / big)};
     const int64_t tiles = ceil_div(in, 64) * ceil_div(out, 64);
+    if (n <= DW_EXPERT_ROWS && tiles * n_experts >= DW_EXPERT_BLOCKS) return {64, 0};
     return {64, (int)std::max<int64_t>(1, std::min<int64_t>(DW_SMALL_BLOCKS / tiles, n / DW_RUN))};
 }
 
-int expert_grad_teams(int64_t n, int in, int out) { return dw_shape(n, in, out).teams; }
+int expert_grad_teams(int64_t n, int n_experts, int in, int out) { return dw_plan(n, n_experts, in, out).teams; }
 
-template <int BY, bool CK>
-static void dw_go(const ExpertArgs &a, const DwShape &d, hipStream_t s)
+struct DwGrid {
+    int p_tiles, q_tiles, blocks;
+};
+static DwGrid dw_grid(const ExpertArgs &a, const DwPlan &d)
 {
-    const int p_tiles = a.dw ? (int)ceil_div(a.in, d.tile) : 1, q_tiles = (int)ceil_div(a.out, d.tile);
-    const dim3 g((unsigned)(d.teams * p_tiles * q_tiles));
-    if constexpr (BY == BY_DIRECT) {
-        if (d.tile == 256) expert_dw_kernel<2, 4, 4, 2, 32, 4, 1, BY, CK><<<g, dim3(512), 0, s>>>(a, p_tiles, q_tiles);
-        else expert_dw_kernel<2, 2, 1, 1, 64, 4, 1, BY, CK><<<g, dim3(256), 0, s>>>(a, p_tiles, q_tiles);
-    } else if constexpr (BY == BY_REGISTERS) {
-        if (d.tile == 256) expert_dw_kernel<2, 4, 4, 2, 32, 2, 1, BY, CK><<<g, dim3(512), 0, s>>>(a, p_tiles, q_tiles);
-        else expert_dw_kernel<2, 2, 1, 1, 64, 2, 3, BY, CK><<<g, dim3(256), 0, s>>>(a, p_tiles, q_tiles);
-    } else {
-        expert_dw_kernel<2, 2, 1, 1, 64, 2, 1, BY, CK><<<g, dim3(256), 0, s>>>(a, p_tiles, q_tiles);
-    }
+    const int p = a.dw ? (int)ceil_div(a.in, d.tile) : 1, q = (int)ceil_div(a.out, d.tile);
+    return {p, q, (d.teams > 0 ? d.teams : a.E) * p * q};
+}
+
+template <typename S>
+static void dw_go(const ExpertArgs &a, const DwPlan &d, hipStream_t s)
+{
+    const DwGrid g = dw_grid(a, d);
+    expert_dw_kernel<S><<<dim3((unsigned)g.blocks), dim3(S::NT), 0, s>>>(a, g.p_tiles, g.q_tiles, d.teams);
+}
+
+template <bool CK>
+static void dw_launch(const ExpertArgs &a, const DwPlan &d, int by, hipStream_t s)
+{
+    if (d.tile == 256) by == BY_DIRECT ? dw_go<DwBig<BY_DIRECT, CK>>(a, d, s) : dw_go<DwBig<BY_REGISTERS, CK>>(a, d, s);
+    else if (by == BY_DIRECT) dw_go<DwSmall<BY_DIRECT, CK>>(a, d, s);
+    else if (by == BY_REGISTERS) dw_go<DwSmall<BY_REGISTERS, CK>>(a, d, s);
+    else dw_go<DwSmall<BY_VALUES, CK>>(a, d, s);
+}
+
+template <int OP, int BY, bool CK>
+static void grad_go(const ExpertArgs &a, const DwPlan &d, hipStream_t s)
+{
+    using X = RowsSmall<OP, BY>;
+    using W = DwSmall<BY, CK>;
+    const DwGrid g = dw_grid(a, d);
+    const int x_tiles = (int)ceil_div(a.in, X::T::BP);
+    expert_grad_kernel<X, W><<<dim3((unsigned)(g.blocks + row_tiles(a, X::T::BQ) * x_tiles)), dim3(X::NT), 0, s>>>(
+        a, x_tiles, g.p_tiles, g.q_tiles, d.teams, g.blocks);
+}
+
+template <int BY>
+static void grad_launch(const ExpertArgs &a, const DwPlan &d, bool ck, hipStream_t s)
+{
+    if (!a.relu) ck ? grad_go<OP_DX, BY, true>(a, d, s) : grad_go<OP_DX, BY, false>(a, d, s);
+    else ck ? grad_go<OP_DX_CKPT, BY, true>(a, d, s) : grad_go<OP_DX_X, BY, false>(a, d, s);
 }
 
 hipError_t launch_expert_grad(const ExpertArgs &a, hipStream_t s)
 {
-    const bool dy_ok = rows_aligned(a.dy, a.ld_dy);
-    if (a.dx && a.n > 0) {
-        const bool direct = dy_ok && rows_aligned(a.w, a.ld_w);
-        if (!a.relu) rows_launch<OP_DX>(a, direct, s);
-        else if (a.x) rows_launch<OP_DX_X>(a, direct, s);
-        else rows_launch<OP_DX_CKPT>(a, direct, s);
+    const bool with_dx = a.dx && a.n > 0, with_dw = a.dw || a.db;
+    const bool dy_ok = rows_aligned(a.dy, a.ld_dy), ck = a.dw && !a.x;
+    const bool x_ok = !a.dw || (ck ? rows_aligned(a.c.q, a.c.ld_q, 1) : rows_aligned(a.x, a.ld_x));
+    const bool dx_direct = dy_ok && rows_aligned(a.w, a.ld_w);
+    const bool wide = a.out >= 8 && (a.in >= 8 || !a.dw);
+    const int dw_by = dy_ok && x_ok ? BY_DIRECT : wide ? BY_REGISTERS : BY_VALUES;
+    const DwPlan d = dw_plan(a.n, a.E, a.in, a.out);
+    // one launch for both where both are small
+    const bool both = with_dx && with_dw && a.n > 0 && d.tile == 64 && !rows_big<OP_DX>(a) && a.in >= 8 && a.out >= 8;
+    if (both) {
+        if (dx_direct && dw_by == BY_DIRECT) grad_launch<BY_DIRECT>(a, d, ck, s);
+        else grad_launch<BY_REGISTERS>(a, d, ck, s);
+    } else if (with_dx) {
+        if (!a.relu) rows_launch<OP_DX>(a, dx_direct, s);
+        else if (a.x) rows_launch<OP_DX_X>(a, dx_direct, s);
+        else rows_launch<OP_DX_CKPT>(a, dx_direct, s);
     }
-    if (a.dw || a.db) {
-        const DwShape d = dw_shape(a.n, a.in, a.out);
-        if (a.n > 0) {
-            const bool ck = a.dw && !a.x;
-            const bool x_ok = !a.dw || (ck ? rows_aligned(a.c.q, a.c.ld_q, 1) : rows_aligned(a.x, a.ld_x));
-            if (dy_ok && x_ok) ck ? dw_go<BY_DIRECT, true>(a, d, s) : dw_go<BY_DIRECT, false>(a, d, s);
-            else if (a.out >= 8 && (a.in >= 8 || !a.dw)) ck ? dw_go<BY_REGISTERS, true>(a, d, s) : dw_go<BY_REGISTERS, false>(a, d, s);
-            else ck ? dw_go<BY_VALUES, true>(a, d, s) : dw_go<BY_VALUES, false>(a, d, s);
+    if (with_dw) {
+        if (!both && (a.n > 0 || d.teams == 0)) ck ? dw_launch<true>(a, d, dw_by, s) : dw_launch<false>(a, d, dw_by, s);
+        if (d.teams > 0) {
+            const int64_t work = (int64_t)a.out * ((a.in + 3) / 4) + a.out;
+            expert_dw_sum_kernel<<<dim3((unsigned)ceil_div(work, 256), a.E), dim3(256), 0, s>>>(a, d.teams);
         }
-        const int64_t work = (int64_t)a.out * ((a.in + 3) / 4) + a.out;
-        expert_dw_sum_kernel<<<dim3((unsigned)ceil_div(work, 256), a.E), dim3(256), 0, s>>>(a, d.teams);
     }
     return hipGetLastError();
 }
