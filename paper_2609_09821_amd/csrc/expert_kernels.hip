@@ -28,15 +28,19 @@ static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // first of them adds their count to the wavefront's counter of that expert, and
 // a lane's rank is the counter plus the matching lanes below it.  No two lanes
 // write a counter at a time, so the order is the rows' own, whatever the timing.
-// Blocks of GROUP_NT threads; one block alone up to GROUP_ONE rows (its counts
-// stay in LDS), else a counting launch leaves [block][expert] counts and every
-// block of the second launch adds up those before it.
+// Blocks of GROUP_NT threads; one block alone up to GROUP_ONE rows (its counts stay in
+// LDS), else a counting launch leaves [block][expert] counts and every block of the second
+// launch adds up those before it.
 // ---------------------------------------------------------------------------
 constexpr int GROUP_NT = 1024, GROUP_WAVES = GROUP_NT / 64;
-constexpr int64_t GROUP_BLOCKS = 256;
+constexpr int64_t GROUP_BLOCKS = 256, GROUP_ONE = 4096;
 
 // rows of a block, a multiple of GROUP_NT
-static int64_t group_rows_of(int64_t n) { return ceil_div(std::max<int64_t>(n, 1), GROUP_BLOCKS * GROUP_NT) * GROUP_NT; }
+static int64_t group_rows_of(int64_t n)
+{
+    const int64_t blocks = n <= GROUP_ONE ? 1 : GROUP_BLOCKS;
+    return ceil_div(std::max<int64_t>(n, 1), blocks * GROUP_NT) * GROUP_NT;
+}
 int64_t group_blocks(int64_t n) { return ceil_div(std::max<int64_t>(n, 1), group_rows_of(n)); }
 
 // The lanes with this lane's value v (< 2^bits).
@@ -120,26 +124,32 @@ __global__ __launch_bounds__(GROUP_NT) void group_count_kernel(GroupArgs g)
 template <bool MANY>
 __global__ __launch_bounds__(GROUP_NT) void group_place_kernel(GroupArgs g)
 {
-    extern __shared__ int cnt[];          // [GROUP_WAVES][E + 1], then [E + 2] starts
-    int *start = cnt + GROUP_WAVES * (g.E + 1);
+    extern __shared__ int cnt[];          // [GROUP_WAVES][E + 1], then of each expert:
+    int *start = cnt + GROUP_WAVES * (g.E + 1);      // the rows in all blocks, then the first place
+    int *before = start + g.E + 1;                   // the rows in the blocks before this one
     const int first = blockIdx.x * g.rows_block, last = min(first + g.rows_block, g.n);
+    for (int e = threadIdx.x; e <= g.E; e += GROUP_NT) start[e] = before[e] = 0;
     group_count(g, cnt, first, last);
-    // of each expert: the rows in all blocks (start) and in the blocks before this one
-    // (a thread's own experts: e = thread, E + 1 <= GROUP_NT + 1 of them)
-    int before[2] = {0, 0};
-    for (int e = threadIdx.x, k = 0; e <= g.E; e += GROUP_NT, ++k) {
-        int all = 0;
-        if constexpr (MANY) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    if constexpr (MANY) {
+        // wavefront w adds up blocks w, w + 16, .. (whole numbers: their order does not matter)
+        for (int e = lane; e <= g.E; e += 64) {
+            int all = 0, less = 0;
 #pragma unroll 8
-            for (int b = 0; b < (int)gridDim.x; ++b) {
+            for (int b = w; b < (int)gridDim.x; b += GROUP_WAVES) {
                 const int c = g.count[(int64_t)b * (g.E + 1) + e];
-                if (b == (int)blockIdx.x) before[k] = all;
                 all += c;
+                less += b < (int)blockIdx.x ? c : 0;
             }
-        } else {
-            for (int w = 0; w < GROUP_WAVES; ++w) all += cnt[w * (g.E + 1) + e];
+            atomicAdd(&start[e], all);
+            atomicAdd(&before[e], less);
         }
-        start[e] = all;
+    } else {
+        for (int e = threadIdx.x; e <= g.E; e += GROUP_NT) {
+            int all = 0;
+            for (int v = 0; v < GROUP_WAVES; ++v) all += cnt[v * (g.E + 1) + e];
+            start[e] = all;
+        }
     }
     __syncthreads();
     // exclusive sums over the experts, by the first wavefront
@@ -159,12 +169,12 @@ __global__ __launch_bounds__(GROUP_NT) void group_place_kernel(GroupArgs g)
         }
     }
     __syncthreads();
-    for (int e = threadIdx.x, k = 0; e <= g.E; e += GROUP_NT, ++k) {
+    for (int e = threadIdx.x; e <= g.E; e += GROUP_NT) {
         if (blockIdx.x == 0) g.offsets[e] = start[e];
-        int at = start[e] + before[k];
-        for (int w = 0; w < GROUP_WAVES; ++w) {
-            const int c = cnt[w * (g.E + 1) + e];
-            cnt[w * (g.E + 1) + e] = at;
+        int at = start[e] + before[e];
+        for (int v = 0; v < GROUP_WAVES; ++v) {
+            const int c = cnt[v * (g.E + 1) + e];
+            cnt[v * (g.E + 1) + e] = at;
             at += c;
         }
     }
@@ -185,7 +195,7 @@ hipError_t launch_group_rows(const int32_t *expert, int64_t n, int n_experts, in
     g.rows = rows;
     g.count = count;
     const unsigned blocks = (unsigned)group_blocks(n);
-    const size_t lds = ((size_t)GROUP_WAVES * (n_experts + 1) + n_experts + 1) * sizeof(int);
+    const size_t lds = (size_t)(GROUP_WAVES + 2) * (n_experts + 1) * sizeof(int);
     if (blocks > 1) {
         group_count_kernel<<<dim3(blocks), dim3(GROUP_NT), lds, s>>>(g);
         group_place_kernel<true><<<dim3(blocks), dim3(GROUP_NT), lds, s>>>(g);
@@ -1216,6 +1226,7 @@ __global__ __launch_bounds__(256) void expert_dw_sum_kernel(ExpertArgs a, int te
         if (!a.dw) return;
         const int o = (int)(t / q), f = (int)(t % q) * 4;
         f32x4_r s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
         for (int k = t0; k <= t1; ++k) {
             const int64_t slot = 2 * k + (u0 >= k * run ? 1 : 0);
             s += *(const f32x4_r *)(a.part + (slot * a.out + o) * in4 + f);
@@ -1249,14 +1260,15 @@ using RowsBigRegs = RowsShape<OP, 2, 2, 2, 2, 32, 2, 2, BY_REGISTERS>;
 template <int OP, int BY>
 using RowsSmall = RowsShape<OP, 2, 2, 1, 1, 64, BY == BY_DIRECT ? 4 : 2, BY == BY_REGISTERS ? 3 : 1, BY>;
 
-// From this many 256 x 128 tiles on they are used, below it 64 x 64 ones.
-constexpr int64_t BIG_TILES = 512;
+// From this many 256 x 128 tiles on they are used, below it 64 x 64 ones; for dx beside a
+// weight gradient of 64 x 64 tiles, with which it can share a launch, from GRAD_BIG_TILES on.
+constexpr int64_t BIG_TILES = 256, GRAD_BIG_TILES = 384;
 
 template <int OP>
-static bool rows_big(const ExpertArgs &a)
+static bool rows_big(const ExpertArgs &a, int64_t limit = BIG_TILES)
 {
     const int np = OP == OP_FORWARD ? a.out : a.in;
-    return row_tiles(a, 128) * ceil_div(np, 256) >= BIG_TILES;
+    return row_tiles(a, 128) * ceil_div(np, 256) >= limit;
 }
 
 template <typename S, int OP>
@@ -1295,7 +1307,7 @@ using DwSmall = DwShape<2, 2, 1, 1, 64, BY == BY_DIRECT ? 4 : 2, BY == BY_REGIST
 // DW_BIG_ROWS rows on where both widths exceed half of one; else 64 x 64 ones, a team for
 // each expert up to DW_EXPERT_ROWS rows where that makes DW_EXPERT_BLOCKS blocks, or
 // DW_SMALL_BLOCKS blocks whose teams have at least DW_RUN rows.
-constexpr int64_t DW_BIG_ROWS = 16384, DW_EXPERT_ROWS = 8192, DW_EXPERT_BLOCKS = 128, DW_SMALL_BLOCKS = 1024,
+constexpr int64_t DW_BIG_ROWS = 16384, DW_EXPERT_ROWS = 4096, DW_EXPERT_BLOCKS = 128, DW_SMALL_BLOCKS = 1024,
                   DW_RUN = 256;
 struct DwPlan {
     int tile, teams;     // teams 0: the experts
@@ -1364,7 +1376,8 @@ hipError_t launch_expert_grad(const ExpertArgs &a, hipStream_t s)
     const int dw_by = dy_ok && x_ok ? BY_DIRECT : wide ? BY_REGISTERS : BY_VALUES;
     const DwPlan d = dw_plan(a.n, a.E, a.in, a.out);
     // one launch for both where both are small
-    const bool both = with_dx && with_dw && a.n > 0 && d.tile == 64 && !rows_big<OP_DX>(a) && a.in >= 8 && a.out >= 8;
+    const bool both = with_dx && with_dw && a.n > 0 && d.tile == 64 && !rows_big<OP_DX>(a, GRAD_BIG_TILES) &&
+                      a.in >= 8 && a.out >= 8;
     if (both) {
         if (dx_direct && dw_by == BY_DIRECT) grad_launch<BY_DIRECT>(a, d, ck, s);
         else grad_launch<BY_REGISTERS>(a, d, ck, s);
