@@ -190,7 +190,10 @@ __global__ __launch_bounds__(NORM_NT) void norm_grad_kernel(NormGradArgs a)
         }
     }
     if (!a.part) return;
-    float *part = a.part + (int64_t)blockIdx.x * 2 * a.d;
+    // one block alone: its sums are the result
+    const bool alone = gridDim.x == 1;
+    float *sums[2] = {alone ? a.dgamma : a.part + (int64_t)blockIdx.x * 2 * a.d,
+                      alone ? a.dbeta : a.part + ((int64_t)blockIdx.x * 2 + 1) * a.d};
     if constexpr (T <= 64) {
         // teams of a wavefront, then the four wavefronts in order
 #pragma unroll
@@ -207,14 +210,15 @@ __global__ __launch_bounds__(NORM_NT) void norm_grad_kernel(NormGradArgs a)
                     if ((threadIdx.x & 63) < T) lds[(threadIdx.x >> 6) * W + (c * T + lane) * 8 + k] = t;
                 }
             __syncthreads();
-            for (int i = threadIdx.x; i < W && i < a.d; i += NORM_NT)
-                part[p * a.d + i] = (lds[i] + lds[W + i]) + (lds[2 * W + i] + lds[3 * W + i]);
+            if (sums[p])
+                for (int i = threadIdx.x; i < W && i < a.d; i += NORM_NT)
+                    sums[p][i] = (lds[i] + lds[W + i]) + (lds[2 * W + i] + lds[3 * W + i]);
         }
     } else {
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            store8(part + (c * T + lane) * 8, nv[c], dg[c]);
-            store8(part + a.d + (c * T + lane) * 8, nv[c], db[c]);
+            if (sums[0]) store8(sums[0] + (c * T + lane) * 8, nv[c], dg[c]);
+            if (sums[1]) store8(sums[1] + (c * T + lane) * 8, nv[c], db[c]);
         }
     }
 }
@@ -291,8 +295,12 @@ hipError_t launch_norm(const NormArgs &a, bool f32, hipStream_t s)
     return hipGetLastError();
 }
 
+// Few rows go to one block, which needs no second launch (4 us of the host): up to 8 passes.
+// Else four passes a block at least, and four blocks a CU at most (two: 262144 x 64 and
+// narrower stay as fast, 524288 x 512 takes 318 us for 262; eight: 302).
 int64_t norm_grad_blocks(int64_t n, int64_t d)
 {
+    if (n <= 8 * pass_rows(d)) return 1;
     return std::max<int64_t>(1, std::min<int64_t>(ceil_div(n, 4 * pass_rows(d)), 1024));
 }
 
@@ -311,7 +319,7 @@ hipError_t launch_norm_grad(const NormGradArgs &a, bool f32, hipStream_t s)
         }
     };
     by_width(a.d, go);
-    if (a.part)
+    if (a.part && blocks > 1)
         norm_grad_sum_kernel<<<dim3((unsigned)ceil_div(2 * a.d, 64)), dim3(64 * NORM_SUM_WAVES), 0, s>>>(
             a.part, (int)blocks, a.d, a.dgamma, a.dbeta);
     return hipGetLastError();
