@@ -1253,22 +1253,30 @@ static bool rows_aligned(const void *p, int64_t ld, int64_t size = 2)
     return ((uintptr_t)p & 15) == 0 && ld * size % 16 == 0;
 }
 
+// Tiles (outputs x places) by the number of 256 x 128 ones that there would be: those from
+// BIG_TILES on, 128 x 128 from MID_TILES, 128 x 64 from LOW_TILES, 64 x 64 below, each as long
+// as the larger one leaves CUs without work.  us with the larger and the smaller one:
+// 6000 rows 300x1000 of 10 experts (228) 16.7, 13.7 and with 128 x 64 16.9; 12000 rows 1024x256
+// (104) 17.7, 15.5; 2000 rows 1024x1024 of 4 (80) 17.0, 13.8 and with 64 x 64 16.9; 6000 rows
+// 1024x256 (57) 16.4, 10.5.  Rows of any alignment have the first (128 x 128) and the last.
 template <int OP>
 using RowsBig = RowsShape<OP, 2, 2, 4, 2, 32, 3, 1, BY_DIRECT>;
 template <int OP>
-using RowsBigRegs = RowsShape<OP, 2, 2, 2, 2, 32, 2, 2, BY_REGISTERS>;
+using RowsMid = RowsShape<OP, 2, 2, 2, 2, 64, 2, 1, BY_DIRECT>;
+template <int OP>
+using RowsLow = RowsShape<OP, 2, 2, 2, 1, 64, 3, 1, BY_DIRECT>;
 template <int OP, int BY>
 using RowsSmall = RowsShape<OP, 2, 2, 1, 1, 64, BY == BY_DIRECT ? 4 : 2, BY == BY_REGISTERS ? 3 : 1, BY>;
-
-// From this many 256 x 128 tiles on they are used, below it 64 x 64 ones; for dx beside a
-// weight gradient of 64 x 64 tiles, with which it can share a launch, from GRAD_BIG_TILES on.
-constexpr int64_t BIG_TILES = 256, GRAD_BIG_TILES = 384;
+template <int OP>
+using RowsBigRegs = RowsShape<OP, 2, 2, 2, 2, 32, 2, 2, BY_REGISTERS>;
+constexpr int64_t BIG_TILES = 256, MID_TILES = 150, LOW_TILES = 60;
+// dx beside a weight gradient of 64 x 64 tiles shares its launch below this many.
+constexpr int64_t GRAD_BIG_TILES = 384;
 
 template <int OP>
-static bool rows_big(const ExpertArgs &a, int64_t limit = BIG_TILES)
+static int64_t big_tiles(const ExpertArgs &a)
 {
-    const int np = OP == OP_FORWARD ? a.out : a.in;
-    return row_tiles(a, 128) * ceil_div(np, 256) >= limit;
+    return row_tiles(a, 128) * ceil_div(OP == OP_FORWARD ? a.out : a.in, 256);
 }
 
 template <typename S, int OP>
@@ -1281,14 +1289,17 @@ static void rows_go(const ExpertArgs &a, hipStream_t s)
 template <int OP>
 static void rows_launch(const ExpertArgs &a, bool direct, hipStream_t s)
 {
-    const bool narrow = a.in < 8 || (OP != OP_FORWARD && a.out < 8);
-    if (rows_big<OP>(a) && (direct || !narrow)) {
-        if (direct) rows_go<RowsBig<OP>, OP>(a, s);
-        else rows_go<RowsBigRegs<OP>, OP>(a, s);
+    const int64_t tiles = big_tiles<OP>(a);
+    if (direct) {
+        if (tiles >= BIG_TILES) rows_go<RowsBig<OP>, OP>(a, s);
+        else if (tiles >= MID_TILES) rows_go<RowsMid<OP>, OP>(a, s);
+        else if (tiles >= LOW_TILES) rows_go<RowsLow<OP>, OP>(a, s);
+        else rows_go<RowsSmall<OP, BY_DIRECT>, OP>(a, s);
+    } else if (a.in < 8 || (OP != OP_FORWARD && a.out < 8)) {
+        rows_go<RowsSmall<OP, BY_VALUES>, OP>(a, s);
     } else {
-        if (direct) rows_go<RowsSmall<OP, BY_DIRECT>, OP>(a, s);
-        else if (!narrow) rows_go<RowsSmall<OP, BY_REGISTERS>, OP>(a, s);
-        else rows_go<RowsSmall<OP, BY_VALUES>, OP>(a, s);
+        if (tiles >= BIG_TILES) rows_go<RowsBigRegs<OP>, OP>(a, s);
+        else rows_go<RowsSmall<OP, BY_REGISTERS>, OP>(a, s);
     }
 }
 
@@ -1376,7 +1387,7 @@ hipError_t launch_expert_grad(const ExpertArgs &a, hipStream_t s)
     const int dw_by = dy_ok && x_ok ? BY_DIRECT : wide ? BY_REGISTERS : BY_VALUES;
     const DwPlan d = dw_plan(a.n, a.E, a.in, a.out);
     // one launch for both where both are small
-    const bool both = with_dx && with_dw && a.n > 0 && d.tile == 64 && !rows_big<OP_DX>(a, GRAD_BIG_TILES) &&
+    const bool both = with_dx && with_dw && a.n > 0 && d.tile == 64 && big_tiles<OP_DX>(a) < GRAD_BIG_TILES &&
                       a.in >= 8 && a.out >= 8;
     if (both) {
         if (dx_direct && dw_by == BY_DIRECT) grad_launch<BY_DIRECT>(a, d, ck, s);

@@ -709,3 +709,36 @@ def test_large_tiles(n, E, din, dout, pad, form, kept):
     dw2, db2 = torch.zeros_like(dw), torch.zeros_like(db)
     im.expert_linear_grad(dy, src, w, off, rows, dw=dw2, db=db2)
     assert torch.equal(dw, dw2) and torch.equal(db, db2)
+
+
+@pytest.mark.parametrize("kept", [False, True])
+@pytest.mark.parametrize("n,E,din,dout,pad", [(5000, 3, 300, 1000, 4), (5000, 3, 1000, 300, 8),
+                                              (4900, 6, 1016, 1022, 2), (3000, 12, 520, 330, 6)])
+def test_middle_tiles(n, E, din, dout, pad, kept):
+    """Sizes of the tiles between the smallest and the largest; dx in a launch of its own."""
+    e, off, rows, x, w, b, g = _layer(n, E, din, dout, pad, n + dout, "holes")
+    x = _wide(x.clamp(min=0).contiguous(), pad)
+    wy = torch.zeros(n, -(-dout // 8) * 8, dtype=torch.bfloat16, device=DEV)
+    dy = wy[:, :dout]
+    dy.copy_(torch.randn(n, dout, device=DEV, generator=g))
+    y = _out(n, dout, pad, torch.bfloat16)
+    im.expert_linear(x, w, b, off, rows, y)
+    src, xin = x, x.double()
+    if kept:
+        src = im.Checkpoint.empty(n, din)
+        im.checkpoint_store(x, src)
+        xin = torch.from_numpy(_ckpt_ref(x)[2]).to(DEV)
+    dx, plain = _out(n, din, pad, torch.bfloat16), _out(n, din, pad, torch.bfloat16)
+    im.expert_linear_grad(dy, src, w, off, rows, dx=dx, relu_x=True)
+    im.expert_linear_grad(dy, None, w, off, rows, dx=plain)
+    none = torch.ones(n, dtype=torch.bool, device=DEV)
+    for k, r in enumerate(_by_expert(e, E)):
+        none[r] = False
+        v, d, wk = x[r].double(), dy[r].double(), w[k].double()
+        want = v @ wk.t() + b[k].double()
+        _within(y[r], want, 2 * (din + 1) * U * (v.abs() @ wk.abs().t() + b[k].double().abs()) + BF * want.abs(), "y")
+        want, size = d @ wk, d.abs() @ wk.abs()
+        _within(plain[r], want, 2 * dout * U * size + BF * want.abs(), "dx")
+        assert torch.equal(dx[r], torch.where(xin[r] > 0, plain[r], torch.zeros_like(plain[r])))
+    assert not y[none].any() and not dx[none].any()
+    _pad_kept(y), _pad_kept(dx)
