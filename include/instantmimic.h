@@ -644,7 +644,8 @@ im_status im_layer_norm_grad(const im_norm_grad *a, void *stream);
  *   x [n][in] bf16, w [n_experts][out][in] bf16 (row stride ld_w, expert stride
  *   out * ld_w), bias [n_experts][out] float or NULL, y [n][out] of y_dtype.
  * Products of bf16 values summed in fp32, one rounding at the end.  bf16 only
- * (dtype IM_DTYPE_F32: IM_ERR_UNSUPPORTED).  n <= 2^30, in and out <= 2^20.
+ * (dtype IM_DTYPE_F32: IM_ERR_UNSUPPORTED).  n <= 2^30, in and out <= 2^20, in * out
+ * <= 2^30, and (n / 128 + n_experts) times the larger width / 128 below 2^21.
  */
 typedef struct {
     int64_t n;

@@ -71,10 +71,9 @@ im_status check_layer(int64_t n, int32_t E, int32_t in, int32_t out, int32_t dty
     if (in > MAX_WIDTH || out > MAX_WIDTH || (int64_t)in * out > MAX_ROWS)
         return unsupported("in or out above 2^20, or in * out above 2^30");
     if (dtype != IM_DTYPE_BF16) return unsupported("expert layers are bf16 only");
-    // a launch has fewer than 2^32 threads
-    const int64_t tiles = n / 128 + E + 1;
-    if (tiles * (ceil_div(in, 128) > ceil_div(out, 128) ? ceil_div(in, 128) : ceil_div(out, 128)) >= (1 << 24))
-        return unsupported("more than 2^24 - 1 tiles of 128 rows and columns");
+    // a launch has fewer than 2^32 threads, in tiles of 64 x 64 at the least
+    const int64_t wide = ceil_div(in > out ? in : out, 128);
+    if ((n / 128 + E + 1) * wide >= (1 << 21)) return unsupported("more than 2^21 tiles of 128 rows and columns");
     if (!offsets) return invalid("NULL offsets");
     return IM_OK;
 }
@@ -233,6 +232,8 @@ im_status im_expert_linear_grad(const im_expert_layer_grad *p, void *stream)
     if (s != IM_OK) return s;
     const bool need_x = p->dw || (p->dx && p->relu_x), sums = p->dw || p->db;
     if (!p->dx && !sums) return invalid("no output asked for");
+    if (sums && p->n_experts * ceil_div(p->in, 64) * ceil_div(p->out, 64) >= (1 << 24))
+        return unsupported("more than 2^24 tiles of 64 x 64 in all experts' weights");
     if (p->ld_dy < p->out || (p->x && p->ld_x < p->in) || (p->dx && (p->ld_dx < p->in || p->ld_w < p->in)) ||
         (p->dw && p->ld_dw < p->in))
         return invalid("ld_dy must be >= out; ld_x, ld_w, ld_dx and ld_dw >= in");

@@ -357,11 +357,13 @@ __device__ __forceinline__ u32x2_r end_of_row(u32x2_r r, int nv)
 template <int R, int NT, int BK, int D>
 struct AlongTile {
     static constexpr int PITCH = BK * 2, SLOTS = BK / 8, U = R * PITCH / (NT * 16), BYTES = R * PITCH;
-    static constexpr int READS = 1;      // LDS reads of a fragment
     static_assert(U * NT * 16 == BYTES, "whole pieces");
     const uint16_t *p[U];
     u32x4_r v[D][U];
-    __device__ static int row(int u) { return (u * (NT / 64) + wave_id()) * (64 / SLOTS) + (threadIdx.x & 63) / SLOTS; }
+    __device__ static int row(int u)
+    {
+        return (u * (NT / 64) + wave_id()) * (64 / SLOTS) + (threadIdx.x & 63) / SLOTS;
+    }
     __device__ static int perm(int r) { return BK == 32 ? (r >> 2) & 3 : (r >> 1) & 7; }
     __device__ static int col() { return (((int)threadIdx.x & (SLOTS - 1)) ^ perm(row(0))) * 8; }
     // at(i): the address of row i of the tile (one that can be read, for all i < R)
@@ -411,7 +413,6 @@ struct AlongTile {
 template <int N, int NT, int BK, int D>
 struct AcrossTile {
     static constexpr int PITCH = N * 2, SLOTS = N / 8, U = BK * PITCH / (NT * 16), BYTES = BK * PITCH;
-    static constexpr int READS = 2;
     static_assert(U * NT * 16 == BYTES, "whole pieces");
     u32x4_r v[D][U];
     __device__ static int krow(int u) { return ((u * (NT / 64) + wave_id()) * 64 + (threadIdx.x & 63)) / SLOTS; }
@@ -526,12 +527,11 @@ struct CkptBytes {
     }
 };
 
-// One K step's products from a stage in LDS.  The fragments of a substep are read while
-// the one before is multiplied, and the next steps' direct loads (copy(u), u < COPIES) are
-// issued a few at a time: a read after each MFMA and a load now and then, held there by
-// the scheduler.  Left alone it reads a few fragments, waits for them and multiplies;
-// with all loads first, every wavefront stands at its loads before its first product.
-// last(): work for the vector units beside the last substep's products.
+// One K step's products from a stage in LDS.  The fragments of a substep are read before
+// the one before it is multiplied, and the next steps' direct loads (copy(u), u < COPIES)
+// are issued a few with each: with all loads first, every wavefront stands at its loads
+// before its first product (the weight gradient 167 us for 157).  last(): work for the
+// vector units beside the last substep's products.
 template <typename P, typename Q, int TP, int TQ, int BK, int COPIES, typename F, typename G>
 __device__ __forceinline__ void multiply_step(const char *ps, const char *qs, int wp, int wq, f32x16_t (&acc)[TP][TQ],
                                               F copy, G last)
@@ -548,7 +548,6 @@ __device__ __forceinline__ void multiply_step(const char *ps, const char *qs, in
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-        constexpr int READS = TP * P::READS + TQ * Q::READS, M = TP * TQ, EACH = (READS + M - 1) / M;
         const int c0 = COPIES * s / S, c1 = COPIES * (s + 1) / S;
         if (s + 1 < S) read(s + 1);
 #pragma unroll
@@ -559,12 +558,6 @@ __device__ __forceinline__ void multiply_step(const char *ps, const char *qs, in
 #pragma unroll
             for (int j = 0; j < TQ; ++j)
                 acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp[s & 1][i], fq[s & 1][j], acc[i][j], 0, 0, 0);
-#pragma unroll
-        for (int m = 0; m < M; ++m) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            if (s + 1 < S && m * EACH < READS) __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
-            if ((m + 1) * (c1 - c0) / M > m * (c1 - c0) / M) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
-        }
         __builtin_amdgcn_sched_barrier(0);
     }
 }
@@ -613,6 +606,11 @@ __device__ __forceinline__ void clear(f32x16_t (&acc)[TP][TQ])
 // ---------------------------------------------------------------------------
 // Forward and input gradient: C rows are places.  Blocks p-tile fastest, blocks of
 // one XCD consecutive: the tiles that read one set of rows share an L2.
+//
+// 65536 rows of 16 experts, unevenly drawn, 1024x1024: 180 us, 760 TFLOP/s.  Its parts alone:
+// products 90 us, loads from the L2 into LDS 117 (1.6 GB), and 47 more where the outputs
+// are stored.  Two blocks of 256 x 128 share a CU, so that one's loads and stores run beside
+// the other's products; 256 x 256 tiles load less but leave one block (206 us).
 // ---------------------------------------------------------------------------
 template <int OP, int WP, int WQ, int TP, int TQ, int BK, int D>
 struct RowsTile {
@@ -639,251 +637,255 @@ struct RowsShape {
 
     __device__ __forceinline__ static void run(const ExpertArgs &a, int p_tiles, int id, char *lds)
     {
-    constexpr int BP = T::BP, BQ = T::BQ;
-    int *row_of = (int *)(lds + ROWS_AT);
-    float *bias = (float *)(lds + BIAS_AT);
-    const Piece pc = find_piece(a.offsets, a.E, a.n, id / p_tiles, BQ);
-    if (pc.e < 0) return;
-    const int p0 = id % p_tiles * BP;
-    const int NP = OP == OP_FORWARD ? a.out : a.in, K = OP == OP_FORWARD ? a.in : a.out;
-    for (int i = threadIdx.x; i < BQ; i += NT) row_of[i] = i < pc.count ? row_at(a, pc.first + i) : -1;
-    if constexpr (OP == OP_FORWARD)
-        for (int i = threadIdx.x; i < BP; i += NT)
-            bias[i] = a.bias && pc.e < a.E && p0 + i < NP ? a.bias[(int64_t)pc.e * a.out + p0 + i] : 0.0f;
-    __syncthreads();
+        constexpr int BP = T::BP, BQ = T::BQ;
+        int *row_of = (int *)(lds + ROWS_AT);
+        float *bias = (float *)(lds + BIAS_AT);
+        const Piece pc = find_piece(a.offsets, a.E, a.n, id / p_tiles, BQ);
+        if (pc.e < 0) return;
+        const int p0 = id % p_tiles * BP;
+        const int NP = OP == OP_FORWARD ? a.out : a.in, K = OP == OP_FORWARD ? a.in : a.out;
+        for (int i = threadIdx.x; i < BQ; i += NT) row_of[i] = i < pc.count ? row_at(a, pc.first + i) : -1;
+        if constexpr (OP == OP_FORWARD)
+            for (int i = threadIdx.x; i < BP; i += NT)
+                bias[i] = a.bias && pc.e < a.E && p0 + i < NP ? a.bias[(int64_t)pc.e * a.out + p0 + i] : 0.0f;
+        __syncthreads();
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
-    const int wp = wave % WP * TP * 32, wq = wave / WP * TQ * 32;
-    // the pieces of C that this thread stores: features f.. of the places i0, i0 + NT / (BP / 8), ..
-    constexpr int PIECES = BQ * (BP / 8) / NT;
-    constexpr bool MASKED = OP == OP_DX_X || OP == OP_DX_CKPT;
-    const int i0 = tid / (BP / 8), f = tid % (BP / 8) * 8, nv = NP - p0 - f;
-    const bool whole = NP - p0 >= BP;
-    // Which inputs are positive: words of two, in their halves' sign bits, are shifted into one
-    // register for four pieces, and read while the first steps load (at the end it would be
-    // the whole latency of a row read at random).
-    uint32_t positive[(PIECES + 3) / 4];
-    auto read_positive = [&] {
-        constexpr int B = PIECES < 4 ? PIECES : 4;
+        const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
+        const int wp = wave % WP * TP * 32, wq = wave / WP * TQ * 32;
+        // the pieces of C that this thread stores: features f.. of the places i0, i0 + NT / (BP / 8), ..
+        constexpr int PIECES = BQ * (BP / 8) / NT;
+        constexpr bool MASKED = OP == OP_DX_X || OP == OP_DX_CKPT;
+        const int i0 = tid / (BP / 8), f = tid % (BP / 8) * 8, nv = NP - p0 - f;
+        const bool whole = NP - p0 >= BP;
+        // Which inputs are positive: words of two, in their halves' sign bits, are shifted into one
+        // register for four pieces, and read while the first steps load (at the end it would be
+        // the whole latency of a row read at random).
+        uint32_t positive[(PIECES + 3) / 4];
+        auto read_positive = [&] {
+            constexpr int B = PIECES < 4 ? PIECES : 4;
 #pragma unroll
-        for (int c0 = 0; c0 < PIECES; c0 += B) {
-            u32x4_r h[B];
-            u32x2_r q[B];
-            int scale[B];
+            for (int c0 = 0; c0 < PIECES; c0 += B) {
+                u32x4_r h[B];
+                u32x2_r q[B];
+                int scale[B];
 #pragma unroll
-            for (int c = 0; c < B; ++c) {
-                const int64_t r = max(row_of[i0 + (c0 + c) * (NT / (BP / 8))], 0);
-                if constexpr (OP == OP_DX_X) {
-                    h[c] = *(const u32x4_a2 *)(a.x + r * a.ld_x + p0 + f);
-                } else {
-                    q[c] = *(const u32x2_a1 *)(a.c.q + r * a.c.ld_q + p0 + f);
-                    scale[c] = a.c.scale[r * a.c.ld_scale + ((p0 + f) >> 5)];
+                for (int c = 0; c < B; ++c) {
+                    const int64_t r = max(row_of[i0 + (c0 + c) * (NT / (BP / 8))], 0);
+                    if constexpr (OP == OP_DX_X) {
+                        h[c] = *(const u32x4_a2 *)(a.x + r * a.ld_x + p0 + f);
+                    } else {
+                        q[c] = *(const u32x2_a1 *)(a.c.q + r * a.c.ld_q + p0 + f);
+                        scale[c] = a.c.scale[r * a.c.ld_scale + ((p0 + f) >> 5)];
+                    }
                 }
-            }
-            uint32_t m = 0;
+                uint32_t m = 0;
 #pragma unroll
-            for (int c = 0; c < B; ++c) {
-                if constexpr (OP == OP_DX_CKPT) h[c] = positive_bytes(q[c], scale[c]);
-                else h[c] = positive_bf16(h[c]);
+                for (int c = 0; c < B; ++c) {
+                    if constexpr (OP == OP_DX_CKPT) h[c] = positive_bytes(q[c], scale[c]);
+                    else h[c] = positive_bf16(h[c]);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) m = m >> 1 | h[c][k];
-            }
-            positive[c0 / 4] = m;
-        }
-    };
-    const bool has_expert = pc.e < a.E;      // else zeros are stored
-    f32x16_t acc[TP][TQ];
-    clear(acc);
-    if (has_expert) {
-        const uint16_t *q = OP == OP_FORWARD ? a.x : a.dy;
-        const int64_t ldq = OP == OP_FORWARD ? a.ld_x : a.ld_dy;
-        const uint16_t *w = a.w + (int64_t)pc.e * a.out * a.ld_w;
-        typename T::P tp;
-        typename T::Q tq;
-        // rows past the tile's last read row 0: their sums are not stored
-        tq.init([&](int i) { return q + (int64_t)max(row_of[i], 0) * ldq; });
-        const uint16_t *wcol = nullptr;
-        int nvp = 0;
-        if constexpr (OP == OP_FORWARD) {
-            tp.init([&](int i) { return w + (int64_t)min(p0 + i, NP - 1) * a.ld_w; });
-        } else {
-            nvp = NP - p0 - tp.col();
-            wcol = w + p0 + tp.col();
-        }
-        constexpr int L = T::P::U + T::Q::U;      // direct loads of a step
-        auto copy = [&](int u, int kt, char *st) {
-            if (u >= T::P::U) tq.copy(u - T::P::U, kt, st + T::P::BYTES);
-            else if constexpr (OP == OP_FORWARD) tp.copy(u, kt, st);
-            else tp.copy(u, nvp > 0 ? wcol + (int64_t)(kt * BK + tp.krow(u)) * a.ld_w : nullptr, st);
-        };
-        auto load = [&](auto narrow, int d, int kt) {
-            constexpr bool N = decltype(narrow)::value;
-            if constexpr (OP == OP_FORWARD)
-                tp.template load<N>(d, kt, K);
-            else
-                tp.template load<N>(d, [&](int u) -> const uint16_t * {
-                    const int k = kt * BK + tp.krow(u);
-                    return k < K ? wcol + (int64_t)k * a.ld_w : nullptr;
-                }, nvp);
-            tq.template load<N>(d, kt, K);
-        };
-        auto store = [&](auto narrow, int d, int kt, char *st) {
-            constexpr bool N = decltype(narrow)::value;
-            if constexpr (OP == OP_FORWARD) tp.template store<N>(d, kt, K, st);
-            else tp.template store<N>(d, nvp, NP - p0 >= BP, st);
-            tq.template store<N>(d, kt, K, st + T::P::BYTES);
-        };
-        int now = 0;     // stage of step kt
-        // a step's products, with `copies` direct loads of the step that comes NS - 1 later
-        auto multiply = [&](auto copies, int kt) {
-            const char *st = lds + now * T::STAGE;
-            char *ahead = lds + (now == 0 ? NS - 1 : now - 1) * T::STAGE;
-            multiply_step<typename T::P, typename T::Q, TP, TQ, BK, decltype(copies)::value>(
-                st, st + T::P::BYTES, wp, wq, acc, [&](int u) { copy(u, kt + NS - 1, ahead); }, [] {});
-            now = now + 1 == NS ? 0 : now + 1;
-        };
-        using NoCopies = std::integral_constant<int, 0>;
-        if constexpr (DIRECT) {
-            const int nk = K / BK;
-            // the last, shorter step comes first, through registers and the last stage
-            const bool rest = K % BK != 0;
-            const bool wide = K >= 8 && (OP == OP_FORWARD || NP >= 8);
-            if (rest && wide) load(std::false_type(), 0, nk);
-            for (int kt = 0; kt < NS - 1 && kt < nk; ++kt)
-#pragma unroll
-                for (int u = 0; u < L; ++u) copy(u, kt, lds + kt * T::STAGE);
-            if (MASKED && whole) read_positive();
-            if (rest) {
-                now = NS - 1;
-                if (wide) {
-                    store(std::false_type(), 0, nk, lds + now * T::STAGE);
-                } else {
-                    load(std::true_type(), 0, nk);
-                    store(std::true_type(), 0, nk, lds + now * T::STAGE);
+                    for (int k = 0; k < 4; ++k) m = m >> 1 | h[c][k];
                 }
-                meet();
-                multiply(NoCopies(), 0);
+                positive[c0 / 4] = m;
             }
-            int kt = 0;
-            for (; kt + NS - 1 < nk; ++kt) {
-                wait_loads<(NS - 2) * L>();
-                meet();
-                multiply(std::integral_constant<int, L>(), kt);
+        };
+        const bool has_expert = pc.e < a.E;      // else zeros are stored
+        f32x16_t acc[TP][TQ];
+        clear(acc);
+        if (has_expert) {
+            const uint16_t *q = OP == OP_FORWARD ? a.x : a.dy;
+            const int64_t ldq = OP == OP_FORWARD ? a.ld_x : a.ld_dy;
+            const uint16_t *w = a.w + (int64_t)pc.e * a.out * a.ld_w;
+            typename T::P tp;
+            typename T::Q tq;
+            // rows past the tile's last read row 0: their sums are not stored
+            tq.init([&](int i) { return q + (int64_t)max(row_of[i], 0) * ldq; });
+            const uint16_t *wcol = nullptr;
+            int nvp = 0;
+            if constexpr (OP == OP_FORWARD) {
+                tp.init([&](int i) { return w + (int64_t)min(p0 + i, NP - 1) * a.ld_w; });
+            } else {
+                nvp = NP - p0 - tp.col();
+                wcol = w + p0 + tp.col();
             }
-            for (; kt < nk; ++kt) {
-                wait_for_step<L, NS - 2>(nk - 1 - kt);
-                meet();
-                multiply(NoCopies(), kt);
-            }
-        } else {
-            const int nk = (K + BK - 1) / BK;
-            const std::integral_constant<bool, NARROW> narrow;
-            // the order of the direct loads: a last, shorter step first
-            const bool rest = K % BK != 0;
-            auto nth = [&](int i) { return rest && i < nk ? (i == 0 ? nk - 1 : i - 1) : i; };
+            constexpr int L = T::P::U + T::Q::U;      // direct loads of a step
+            auto copy = [&](int u, int kt, char *st) {
+                if (u >= T::P::U) tq.copy(u - T::P::U, kt, st + T::P::BYTES);
+                else if constexpr (OP == OP_FORWARD) tp.copy(u, kt, st);
+                else tp.copy(u, nvp > 0 ? wcol + (int64_t)(kt * BK + tp.krow(u)) * a.ld_w : nullptr, st);
+            };
+            auto load = [&](auto narrow, int d, int kt) {
+                constexpr bool N = decltype(narrow)::value;
+                if constexpr (OP == OP_FORWARD)
+                    tp.template load<N>(d, kt, K);
+                else
+                    tp.template load<N>(d, [&](int u) -> const uint16_t * {
+                        const int k = kt * BK + tp.krow(u);
+                        return k < K ? wcol + (int64_t)k * a.ld_w : nullptr;
+                    }, nvp);
+                tq.template load<N>(d, kt, K);
+            };
+            auto store = [&](auto narrow, int d, int kt, char *st) {
+                constexpr bool N = decltype(narrow)::value;
+                if constexpr (OP == OP_FORWARD) tp.template store<N>(d, kt, K, st);
+                else tp.template store<N>(d, nvp, NP - p0 >= BP, st);
+                tq.template store<N>(d, kt, K, st + T::P::BYTES);
+            };
+            int now = 0;     // stage of step kt
+            // a step's products, with `copies` direct loads of the step that comes NS - 1 later
+            auto multiply = [&](auto copies, int kt) {
+                const char *st = lds + now * T::STAGE;
+                char *ahead = lds + (now == 0 ? NS - 1 : now - 1) * T::STAGE;
+                multiply_step<typename T::P, typename T::Q, TP, TQ, BK, decltype(copies)::value>(
+                    st, st + T::P::BYTES, wp, wq, acc, [&](int u) { copy(u, kt + NS - 1, ahead); }, [] {});
+                now = now + 1 == NS ? 0 : now + 1;
+            };
+            using NoCopies = std::integral_constant<int, 0>;
+            if constexpr (DIRECT) {
+                const int nk = K / BK;
+                // the last, shorter step comes first, through registers and the last stage
+                const bool rest = K % BK != 0;
+                const bool wide = K >= 8 && (OP == OP_FORWARD || NP >= 8);
+                if (rest && wide) load(std::false_type(), 0, nk);
+                for (int kt = 0; kt < NS - 1 && kt < nk; ++kt)
 #pragma unroll
-            for (int d = 0; d < D; ++d) load(narrow, d, nth(d));
-            if (MASKED && whole) read_positive();
-            store(narrow, 0, nth(0), lds);
-            load(narrow, 0, nth(D));
-            for (int k0 = 0; k0 < nk; k0 += D) {
-#pragma unroll
-                for (int d = 0; d < D; ++d) {
-                    const int kt = k0 + d, next = (d + 1) % D;      // step, register set of the next one
-                    if (kt >= nk) break;
+                    for (int u = 0; u < L; ++u) copy(u, kt, lds + kt * T::STAGE);
+                if (MASKED && whole) read_positive();
+                if (rest) {
+                    now = NS - 1;
+                    if (wide) {
+                        store(std::false_type(), 0, nk, lds + now * T::STAGE);
+                    } else {
+                        load(std::true_type(), 0, nk);
+                        store(std::true_type(), 0, nk, lds + now * T::STAGE);
+                    }
                     meet();
-                    store(narrow, next, nth(kt + 1), lds + (now ^ 1) * T::STAGE);
-                    load(narrow, next, nth(kt + 1 + D));
+                    multiply(NoCopies(), 0);
+                }
+                int kt = 0;
+                for (; kt + NS - 1 < nk; ++kt) {
+                    wait_loads<(NS - 2) * L>();
+                    meet();
+                    multiply(std::integral_constant<int, L>(), kt);
+                }
+                for (; kt < nk; ++kt) {
+                    wait_for_step<L, NS - 2>(nk - 1 - kt);
+                    meet();
                     multiply(NoCopies(), kt);
                 }
+            } else {
+                const int nk = (K + BK - 1) / BK;
+                const std::integral_constant<bool, NARROW> narrow;
+                // the order of the direct loads: a last, shorter step first
+                const bool rest = K % BK != 0;
+                auto nth = [&](int i) { return rest && i < nk ? (i == 0 ? nk - 1 : i - 1) : i; };
+#pragma unroll
+                for (int d = 0; d < D; ++d) load(narrow, d, nth(d));
+                if (MASKED && whole) read_positive();
+                store(narrow, 0, nth(0), lds);
+                load(narrow, 0, nth(D));
+                for (int k0 = 0; k0 < nk; k0 += D) {
+#pragma unroll
+                    for (int d = 0; d < D; ++d) {
+                        const int kt = k0 + d, next = (d + 1) % D;      // step, register set of the next one
+                        if (kt >= nk) break;
+                        meet();
+                        store(narrow, next, nth(kt + 1), lds + (now ^ 1) * T::STAGE);
+                        load(narrow, next, nth(kt + 1 + D));
+                        multiply(NoCopies(), kt);
+                    }
+                }
             }
         }
-    }
-    meet();
+        meet();
 
-    // lane l: place wq + 32 j + l % 32, features wp + 32 i + 8 g + 4 (l / 32) + 0..3
-    // f: feature of the tile
-    auto finish = [&](int f, f32x4_r v) {
-        if constexpr (OP == OP_FORWARD) {
-            v += *(const f32x4_r *)(bias + f);
-            if (a.relu)
+        // lane l: place wq + 32 j + l % 32, features wp + 32 i + 8 g + 4 (l / 32) + 0..3
+        auto quad = [&](int i, int j, int g) {
+            return f32x4_r{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+        };
+        // f: feature of the tile
+        auto finish = [&](int f, f32x4_r v) {
+            if constexpr (OP == OP_FORWARD) {
+                v += *(const f32x4_r *)(bias + f);
+                if (a.relu)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) v[k] = v[k] < 0.0f ? 0.0f : v[k];   // NaN stays
+                    for (int k = 0; k < 4; ++k) v[k] = v[k] < 0.0f ? 0.0f : v[k];   // NaN stays
+            }
+            return v;
+        };
+        if (OP == OP_FORWARD && a.y_f32) {
+#pragma unroll
+            for (int j = 0; j < TQ; ++j) {
+                const int r = row_of[wq + 32 * j + (lane & 31)];
+                if (r < 0) continue;
+                float *y = (float *)a.y + (int64_t)r * a.ld_y;
+#pragma unroll
+                for (int i = 0; i < TP; ++i)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const int f = p0 + wp + 32 * i + 8 * g + 4 * (lane >> 5);
+                        const f32x4_r v = finish(f - p0, quad(i, j, g));
+                        if (f + 4 <= NP) {
+                            *(f32x4_a4 *)(y + f) = v;
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                if (f + k < NP) y[f + k] = v[k];
+                        }
+                    }
+            }
+            return;
         }
-        return v;
-    };
-    if (OP == OP_FORWARD && a.y_f32) {
+        // bf16 rows meet in LDS and leave in 16-byte pieces
+        uint16_t *out = (uint16_t *)lds;
 #pragma unroll
-        for (int j = 0; j < TQ; ++j) {
-            const int r = row_of[wq + 32 * j + (lane & 31)];
-            if (r < 0) continue;
-            float *y = (float *)a.y + (int64_t)r * a.ld_y;
+        for (int j = 0; j < TQ; ++j)
 #pragma unroll
             for (int i = 0; i < TP; ++i)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const int f = p0 + wp + 32 * i + 8 * g + 4 * (lane >> 5);
-                    const f32x4_r v = finish(f - p0, f32x4_r{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2],
-                                                        acc[i][j][4 * g + 3]});
-                    if (f + 4 <= NP) {
-                        *(f32x4_a4 *)(y + f) = v;
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            if (f + k < NP) y[f + k] = v[k];
-                    }
+                    const int f = wp + 32 * i + 8 * g + 4 * (lane >> 5);
+                    const f32x4_r v = finish(f, quad(i, j, g));
+                    const u32x2_r o = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+                    *(u32x2_r *)(out + (wq + 32 * j + (lane & 31)) * T::LDO + f) = o;
                 }
-        }
-        return;
-    }
-    // bf16 rows meet in LDS and leave in 16-byte pieces
-    uint16_t *out = (uint16_t *)lds;
+        __syncthreads();
+        auto to = [&](int r) -> uint16_t * {
+            return (OP == OP_FORWARD ? (uint16_t *)a.y + (int64_t)r * a.ld_y : a.dx + (int64_t)r * a.ld_dx) + p0 + f;
+        };
+        if (whole) {
 #pragma unroll
-    for (int j = 0; j < TQ; ++j)
+            for (int c = 0; c < PIECES; ++c) {
+                const int i = i0 + c * (NT / (BP / 8)), r = row_of[i];
+                u32x4_r o = *(const u32x4_r *)(out + i * T::LDO + f);
+                if constexpr (MASKED) {
+                    constexpr int B = PIECES < 4 ? PIECES : 4;
 #pragma unroll
-        for (int i = 0; i < TP; ++i)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int f = wp + 32 * i + 8 * g + 4 * (lane >> 5);
-                const f32x4_r v = finish(f, f32x4_r{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2],
-                                                         acc[i][j][4 * g + 3]});
-                const u32x2_r o = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-                *(u32x2_r *)(out + (wq + 32 * j + (lane & 31)) * T::LDO + f) = o;
+                    for (int k = 0; k < 4; ++k)
+                        o[k] &= half_signs(has_expert ? positive[c / 4] << (4 * B - 1 - (4 * (c % 4) + k)) : 0);
+                }
+                if (r >= 0) *(u32x4_a2 *)to(r) = o;
             }
-    __syncthreads();
-    auto to = [&](int r) -> uint16_t * {
-        return (OP == OP_FORWARD ? (uint16_t *)a.y + (int64_t)r * a.ld_y : a.dx + (int64_t)r * a.ld_dx) + p0 + f;
-    };
-    if (whole) {
-#pragma unroll
-        for (int c = 0; c < PIECES; ++c) {
-            const int i = i0 + c * (NT / (BP / 8)), r = row_of[i];
-            u32x4_r o = *(const u32x4_r *)(out + i * T::LDO + f);
-            if constexpr (MASKED) {
-                constexpr int B = PIECES < 4 ? PIECES : 4;
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    o[k] &= half_signs(has_expert ? positive[c / 4] << (4 * B - 1 - (4 * (c % 4) + k)) : 0);
-            }
-            if (r >= 0) *(u32x4_a2 *)to(r) = o;
-        }
-    } else if (nv > 0) {
+        } else if (nv > 0) {
 #pragma unroll 1
-        for (int c = 0; c < PIECES; ++c) {
-            const int i = i0 + c * (NT / (BP / 8)), r = row_of[i];
-            if (r < 0) continue;
-            u32x4_r o = *(const u32x4_r *)(out + i * T::LDO + f);
-            if constexpr (MASKED) {
-                u32x4_r h;
-                if constexpr (OP == OP_DX_X) h = positive_bf16(load8_bits(a.x + (int64_t)r * a.ld_x + p0 + f, nv));
-                else h = positive_bytes(load8_bytes(a.c.q + (int64_t)r * a.c.ld_q + p0 + f, nv),
-                                        a.c.scale[(int64_t)r * a.c.ld_scale + ((p0 + f) >> 5)]);
+            for (int c = 0; c < PIECES; ++c) {
+                const int i = i0 + c * (NT / (BP / 8)), r = row_of[i];
+                if (r < 0) continue;
+                u32x4_r o = *(const u32x4_r *)(out + i * T::LDO + f);
+                if constexpr (MASKED) {
+                    u32x4_r h;
+                    const int64_t at = r;
+                    if constexpr (OP == OP_DX_X)
+                        h = positive_bf16(load8_bits(a.x + at * a.ld_x + p0 + f, nv));
+                    else
+                        h = positive_bytes(load8_bytes(a.c.q + at * a.c.ld_q + p0 + f, nv),
+                                           a.c.scale[at * a.c.ld_scale + ((p0 + f) >> 5)]);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) o[k] &= half_signs(h[k]);
+                    for (int k = 0; k < 4; ++k) o[k] &= half_signs(h[k]);
+                }
+                store8_bits(to(r), nv, o);
             }
-            store8_bits(to(r), nv, o);
         }
-    }
     }
 };
 
@@ -895,16 +897,20 @@ __global__ __launch_bounds__(S::NT, 2) void expert_rows_kernel(ExpertArgs a, int
 }
 
 // ---------------------------------------------------------------------------
-// Weight gradient.  The blocks are TEAMS teams of one block for each tile (BQ outputs x
-// BP inputs).  The places with an expert are counted in units of 64 of one expert, and each
+// Weight gradient.  The blocks are teams of one block for each tile (BQ outputs x BP
+// inputs).  The places with an expert are counted in units of 64 of one expert, and each
 // team takes an equal run of the units, whatever the experts' sizes; its blocks, which
 // read the same rows, are neighbours in an L2.  Within its run a team forms one product for
 // each expert.  An expert that lies in one run is written to dw; one that spans several
-// leaves each team's part in the workspace: slot 2 t if team t's run began with it, slot
-// 2 t + 1 if it goes on past the run's end (so at most two parts a team), which
-// expert_dw_sum_kernel adds up in the teams' order.
-// The blocks of the first inputs also sum dy's columns for db, from the stages in LDS.
-// CK: x from its checkpoint; DIRECT: dy, and x where it is no checkpoint, by direct loads.
+// leaves each team's part in the workspace, in slot 2 t + 1 if it begins in team t's run,
+// else 2 t (a run has at most one of each), and expert_dw_sum_kernel adds the parts up in
+// the teams' order.  The blocks of the first inputs also sum dy's columns for db, from the
+// stages in LDS.  CK: x from its checkpoint, whose bytes each lane restores one step ahead.
+//
+// 65536 rows of 16 experts, 1024x512: 157 us with the sums of the parts (26 of them, and as
+// much to write the parts, 94 MB), 440 TFLOP/s; bound by latency, a barrier and the
+// restoring each 32 rows, as 256 x 256 tiles leave registers for two wavefronts a SIMD.
+// With an even number of pieces a run each instead (64 x 64 partial tiles): 430 us.
 // ---------------------------------------------------------------------------
 constexpr int DW_UNIT = 64;
 
@@ -958,228 +964,232 @@ struct DwShape {
     static constexpr int PS = BYTES ? 2 : NS, P_AT = NS * Q::BYTES, R_AT = P_AT + PS * P::BYTES;
     static constexpr int ROWS_AT = R_AT + (BYTES ? NS * R::BYTES : 0), LDS = ROWS_AT + 2 * DW_ROWS * 4;
 
-    __device__ __forceinline__ static void run(const ExpertArgs &a, int p_tiles, int q_tiles, int teams, int id, char *lds)
+    __device__ __forceinline__ static void run(const ExpertArgs &a, int p_tiles, int q_tiles, int teams, int id,
+                                               char *lds)
     {
-    int *rows = (int *)(lds + ROWS_AT);
-    const int team = id / (p_tiles * q_tiles);
-    const int p0 = id % p_tiles * BP, q0 = id / p_tiles % q_tiles * BQ;
-    const int lane = threadIdx.x & 63, wave = wave_id();
-    const int wp = wave % WP * TP * 32, wq = wave / WP * TQ * 32;
-    const bool with_db = a.db && p0 == 0;
-    const int in4 = (a.in + 3) & ~3;
+        int *rows = (int *)(lds + ROWS_AT);
+        const int team = id / (p_tiles * q_tiles);
+        const int p0 = id % p_tiles * BP, q0 = id / p_tiles % q_tiles * BQ;
+        const int lane = threadIdx.x & 63, wave = wave_id();
+        const int wp = wave % WP * TP * 32, wq = wave / WP * TQ * 32;
+        const bool with_db = a.db && p0 == 0;
+        const int in4 = (a.in + 3) & ~3;
 
-    P tp;
-    Q tq;
-    const int in = a.dw ? a.in : 0;      // db alone: x is not read
-    const int pcol = p0 + tp.col(), qcol = q0 + tq.col(), rcol = p0 + R::col() < in ? p0 + R::col() : -1;
-    const int nvp = in - pcol, nvq = a.out - qcol;
-    f32x16_t acc[TP][TQ];
-    float db[2];
-    // db: a thread sums two columns of DB_ROWS rows of each step
-    constexpr int PAIRS = BQ / 2, DB_ROWS = BK / (NT / PAIRS);
+        P tp;
+        Q tq;
+        const int in = a.dw ? a.in : 0;      // db alone: x is not read
+        const int pcol = p0 + tp.col(), qcol = q0 + tq.col(), rcol = p0 + R::col() < in ? p0 + R::col() : -1;
+        const int nvp = in - pcol, nvq = a.out - qcol;
+        f32x16_t acc[TP][TQ];
+        float db[2];
+        // db: a thread sums two columns of DB_ROWS rows of each step
+        constexpr int PAIRS = BQ / 2, DB_ROWS = BK / (NT / PAIRS);
 
-    // the product of K places from `first` on
-    auto product = [&](int first, int K) {
-        const int nk = (K + BK - 1) / BK;
-        // row indices of places c DW_ROWS .. of the product: set c % 2
-        constexpr int RU = DW_ROWS / NT;
-        int held[RU];
-        auto fetch = [&](int c) {
+        // the product of K places from `first` on
+        auto product = [&](int first, int K) {
+            const int nk = (K + BK - 1) / BK;
+            // row indices of places c DW_ROWS .. of the product: set c % 2
+            constexpr int RU = DW_ROWS / NT;
+            int held[RU];
+            auto fetch = [&](int c) {
 #pragma unroll
-            for (int u = 0; u < RU; ++u) {
-                const int k = c * DW_ROWS + u * NT + (int)threadIdx.x;
-                held[u] = k < K ? row_at(a, first + k) : -1;
-            }
-        };
-        auto keep = [&](int c) {
-#pragma unroll
-            for (int u = 0; u < RU; ++u) rows[(c & 1) * DW_ROWS + u * NT + threadIdx.x] = held[u];
-        };
-        auto row = [&](int kt, int k) { return rows[(kt * BK + k) & (2 * DW_ROWS - 1)]; };
-        fetch(0);
-        keep(0);
-        fetch(1);
-        keep(1);
-        fetch(2);
-        __syncthreads();
-
-        auto x_at = [&](int kt, int u) -> const uint16_t * {
-            const int r = row(kt, tp.krow(u));
-            return r >= 0 && in > 0 ? a.x + (int64_t)r * a.ld_x + pcol : nullptr;
-        };
-        auto dy_at = [&](int kt, int u) -> const uint16_t * {
-            const int r = row(kt, tq.krow(u));
-            return r >= 0 ? a.dy + (int64_t)r * a.ld_dy + qcol : nullptr;
-        };
-        // direct loads: dy of step kt, x of step kt (its bytes of step kt + 1)
-        auto copy = [&](int u, int kt) {
-            char *q = lds + kt % NS * Q::BYTES;
-            if (u >= LP) {
-                tq.copy(u - LP, nvq > 0 ? dy_at(kt, u - LP) : nullptr, q);
-            } else if constexpr (BYTES) {
-                R::copy(u, a.c, row(kt + 1, R::krow(u)), rcol, lds + R_AT + (kt + 1) % NS * R::BYTES);
-            } else {
-                tp.copy(u, nvp > 0 ? x_at(kt, u) : nullptr, lds + P_AT + kt % NS * P::BYTES);
-            }
-        };
-        // through register set d
-        auto load = [&](int d, int kt) {
-            tq.template load<NARROW>(d, [&](int u) { return dy_at(kt, u); }, nvq);
-            if constexpr (CK && !DIRECT)
-                tp.template load<NARROW>(d, a.c, [&](int u) { return in > 0 ? row(kt, tp.krow(u)) : -1; }, pcol, nvp);
-            else
-                tp.template load<NARROW>(d, [&](int u) { return x_at(kt, u); }, nvp);
-        };
-        auto store = [&](int d, int stage) {
-            tq.template store<NARROW>(d, nvq, a.out - q0 >= BQ, lds + stage * Q::BYTES);
-            tp.template store<NARROW>(d, nvp, in - p0 >= BP, lds + P_AT + stage * P::BYTES);
-        };
-        auto restore = [&](int kt) { R::restore(lds + R_AT + kt % NS * R::BYTES, lds + P_AT + (kt & 1) * P::BYTES); };
-        // a step after its loads: the next row indices now and then, db, the products
-        auto step = [&](int kt, auto copies) {
-            if (kt > 0 && kt * BK % DW_ROWS == 0) {
-                keep(kt * BK / DW_ROWS + 1);
-                fetch(kt * BK / DW_ROWS + 2);
-            }
-            const char *qs = lds + kt % NS * Q::BYTES, *ps = lds + P_AT + kt % PS * P::BYTES;
-            if (with_db) {
-                const int pair = threadIdx.x % PAIRS, k0 = threadIdx.x / PAIRS * DB_ROWS;
-#pragma unroll
-                for (int k = k0; k < k0 + DB_ROWS; ++k) {
-                    const uint32_t v = *(const uint32_t *)(qs + k * Q::PITCH + ((pair >> 2) ^ (Q::perm(k) << 2)) * 16 +
-                                                           (pair & 3) * 4);
-                    db[0] += __uint_as_float(v << 16);
-                    db[1] += __uint_as_float(v & 0xFFFF0000u);
+                for (int u = 0; u < RU; ++u) {
+                    const int k = c * DW_ROWS + u * NT + (int)threadIdx.x;
+                    held[u] = k < K ? row_at(a, first + k) : -1;
                 }
-            }
-            multiply_step<P, Q, TP, TQ, BK, decltype(copies)::value>(
-                ps, qs, wp, wq, acc, [&](int u) { copy(u, kt + NS - 1); },
-                [&] { if constexpr (BYTES) restore(kt + 1); });
-        };
-        clear(acc);
-        db[0] = db[1] = 0.0f;
-        if constexpr (DIRECT) {
-            // steps past the last have no rows: their loads bring zeros that nothing reads
-            if constexpr (BYTES)
+            };
+            auto keep = [&](int c) {
 #pragma unroll
-                for (int u = 0; u < R::U; ++u) R::copy(u, a.c, row(0, R::krow(u)), rcol, lds + R_AT);
-            for (int kt = 0; kt < NS - 1; ++kt)
-#pragma unroll
-                for (int u = 0; u < LP + Q::U; ++u) copy(u, kt);
-            if constexpr (BYTES) {
-                wait_loads<(NS - 1) * L>();
-                restore(0);
-            }
-            for (int kt = 0; kt < nk; ++kt) {
-                wait_loads<(NS - 2) * L>();
-                meet();
-                step(kt, std::integral_constant<int, LP + Q::U>());
-            }
-        } else {
-#pragma unroll
-            for (int d = 0; d < D; ++d) load(d, d);
-            store(0, 0);
-            load(0, D);
-            for (int k0 = 0; k0 < nk; k0 += D) {
-#pragma unroll
-                for (int d = 0; d < D; ++d) {
-                    const int kt = k0 + d, next = (d + 1) % D;
-                    if (kt >= nk) break;
-                    meet();
-                    store(next, (kt + 1) & 1);
-                    load(next, kt + 1 + D);
-                    step(kt, std::integral_constant<int, 0>());
-                }
-            }
-        }
-        wait_loads<0>();
-        meet();
-    };
+                for (int u = 0; u < RU; ++u) rows[(c & 1) * DW_ROWS + u * NT + threadIdx.x] = held[u];
+            };
+            auto row = [&](int kt, int k) { return rows[(kt * BK + k) & (2 * DW_ROWS - 1)]; };
+            fetch(0);
+            keep(0);
+            fetch(1);
+            keep(1);
+            fetch(2);
+            __syncthreads();
 
-    // the product to dw and db of expert e (slot < 0), or to a slot of the workspace
-    auto finish = [&](int e, int64_t slot) {
-        float *c = slot < 0 ? a.dw + (int64_t)e * a.out * a.ld_dw : a.part + slot * a.out * in4;
-        const int64_t ldc = slot < 0 ? a.ld_dw : in4;
-        if (with_db) {
-            float *red = (float *)lds;      // [NT / PAIRS][BQ]
-            red[threadIdx.x / PAIRS * BQ + threadIdx.x % PAIRS * 2] = db[0];
-            red[threadIdx.x / PAIRS * BQ + threadIdx.x % PAIRS * 2 + 1] = db[1];
-            __syncthreads();
-            float *d = slot < 0 ? a.db + (int64_t)e * a.out : a.part_db + slot * a.out;
-            for (int i = threadIdx.x; i < BQ && q0 + i < a.out; i += NT) {
-                float t = 0.0f;
+            auto x_at = [&](int kt, int u) -> const uint16_t * {
+                const int r = row(kt, tp.krow(u));
+                return r >= 0 && in > 0 ? a.x + (int64_t)r * a.ld_x + pcol : nullptr;
+            };
+            auto dy_at = [&](int kt, int u) -> const uint16_t * {
+                const int r = row(kt, tq.krow(u));
+                return r >= 0 ? a.dy + (int64_t)r * a.ld_dy + qcol : nullptr;
+            };
+            // direct loads: dy of step kt, x of step kt (its bytes of step kt + 1)
+            auto copy = [&](int u, int kt) {
+                char *q = lds + kt % NS * Q::BYTES;
+                if (u >= LP) {
+                    tq.copy(u - LP, nvq > 0 ? dy_at(kt, u - LP) : nullptr, q);
+                } else if constexpr (BYTES) {
+                    R::copy(u, a.c, row(kt + 1, R::krow(u)), rcol, lds + R_AT + (kt + 1) % NS * R::BYTES);
+                } else {
+                    tp.copy(u, nvp > 0 ? x_at(kt, u) : nullptr, lds + P_AT + kt % NS * P::BYTES);
+                }
+            };
+            // through register set d
+            auto load = [&](int d, int kt) {
+                tq.template load<NARROW>(d, [&](int u) { return dy_at(kt, u); }, nvq);
+                if constexpr (CK && !DIRECT)
+                    tp.template load<NARROW>(d, a.c, [&](int u) { return in > 0 ? row(kt, tp.krow(u)) : -1; }, pcol,
+                                             nvp);
+                else
+                    tp.template load<NARROW>(d, [&](int u) { return x_at(kt, u); }, nvp);
+            };
+            auto store = [&](int d, int stage) {
+                tq.template store<NARROW>(d, nvq, a.out - q0 >= BQ, lds + stage * Q::BYTES);
+                tp.template store<NARROW>(d, nvp, in - p0 >= BP, lds + P_AT + stage * P::BYTES);
+            };
+            auto restore = [&](int kt) {
+                R::restore(lds + R_AT + kt % NS * R::BYTES, lds + P_AT + (kt & 1) * P::BYTES);
+            };
+            // a step after its loads: the next row indices now and then, db, the products
+            auto step = [&](int kt, auto copies) {
+                if (kt > 0 && kt * BK % DW_ROWS == 0) {
+                    keep(kt * BK / DW_ROWS + 1);
+                    fetch(kt * BK / DW_ROWS + 2);
+                }
+                const char *qs = lds + kt % NS * Q::BYTES, *ps = lds + P_AT + kt % PS * P::BYTES;
+                if (with_db) {
+                    const int pair = threadIdx.x % PAIRS, k0 = threadIdx.x / PAIRS * DB_ROWS;
 #pragma unroll
-                for (int r = 0; r < NT / PAIRS; ++r) t += red[r * BQ + i];
-                d[q0 + i] = t;
-            }
-            __syncthreads();
-        }
-        if (!a.dw) return;
-#pragma unroll
-        for (int j = 0; j < TQ; ++j) {
-            const int o = q0 + wq + 32 * j + (lane & 31);
-            if (o >= a.out) continue;
-#pragma unroll
-            for (int i = 0; i < TP; ++i)
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const int f = p0 + wp + 32 * i + 8 * g + 4 * (lane >> 5);
-                    const f32x4_r v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2],
-                                       acc[i][j][4 * g + 3]};
-                    if (f + 4 <= a.in) {
-                        *(f32x4_a4 *)(c + o * ldc + f) = v;
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            if (f + k < a.in) c[o * ldc + f + k] = v[k];
+                    for (int k = k0; k < k0 + DB_ROWS; ++k) {
+                        const char *at = qs + k * Q::PITCH + ((pair >> 2) ^ (Q::perm(k) << 2)) * 16 + (pair & 3) * 4;
+                        const uint32_t v = *(const uint32_t *)at;
+                        db[0] += __uint_as_float(v << 16);
+                        db[1] += __uint_as_float(v & 0xFFFF0000u);
                     }
                 }
-        }
-    };
-
-    // the experts of the run [begin, end) of units; `u`: the units before expert e
-    int begin = 0, end = 1, e = team, u = 0;
-    if (teams > 0) {
-        const int all = units_before(a, a.E), run = run_units(all, teams);
-        begin = min(team * run, all);
-        end = min(begin + run, all);
-        // the first expert that ends past `begin`, 64 at a time
-        e = a.E;
-        int carry = 0;
-        for (int e0 = 0; e0 < a.E; e0 += 64) {
-            const int j = e0 + lane;
-            const int k = j < a.E ? span_of(a, j).units : 0;
-            int s = k;
+                multiply_step<P, Q, TP, TQ, BK, decltype(copies)::value>(
+                    ps, qs, wp, wq, acc, [&](int u) { copy(u, kt + NS - 1); },
+                    [&] { if constexpr (BYTES) restore(kt + 1); });
+            };
+            clear(acc);
+            db[0] = db[1] = 0.0f;
+            if constexpr (DIRECT) {
+                // steps past the last have no rows: their loads bring zeros that nothing reads
+                if constexpr (BYTES)
 #pragma unroll
-            for (int d = 1; d < 64; d *= 2) {
-                const int t = __shfl_up(s, d);
-                s += lane >= d ? t : 0;
+                    for (int u = 0; u < R::U; ++u) R::copy(u, a.c, row(0, R::krow(u)), rcol, lds + R_AT);
+                for (int kt = 0; kt < NS - 1; ++kt)
+#pragma unroll
+                    for (int u = 0; u < LP + Q::U; ++u) copy(u, kt);
+                if constexpr (BYTES) {
+                    wait_loads<(NS - 1) * L>();
+                    restore(0);
+                }
+                for (int kt = 0; kt < nk; ++kt) {
+                    wait_loads<(NS - 2) * L>();
+                    meet();
+                    step(kt, std::integral_constant<int, LP + Q::U>());
+                }
+            } else {
+#pragma unroll
+                for (int d = 0; d < D; ++d) load(d, d);
+                store(0, 0);
+                load(0, D);
+                for (int k0 = 0; k0 < nk; k0 += D) {
+#pragma unroll
+                    for (int d = 0; d < D; ++d) {
+                        const int kt = k0 + d, next = (d + 1) % D;
+                        if (kt >= nk) break;
+                        meet();
+                        store(next, (kt + 1) & 1);
+                        load(next, kt + 1 + D);
+                        step(kt, std::integral_constant<int, 0>());
+                    }
+                }
             }
-            const uint64_t hit = __ballot(carry + s > begin);
-            if (hit) {
-                const int l = __builtin_ctzll(hit);
-                e = e0 + l;
-                u = carry + __builtin_amdgcn_readlane(s, l) - __builtin_amdgcn_readlane(k, l);
-                break;
+            wait_loads<0>();
+            meet();
+        };
+
+        // the product to dw and db of expert e (slot < 0), or to a slot of the workspace
+        auto finish = [&](int e, int64_t slot) {
+            float *c = slot < 0 ? a.dw + (int64_t)e * a.out * a.ld_dw : a.part + slot * a.out * in4;
+            const int64_t ldc = slot < 0 ? a.ld_dw : in4;
+            if (with_db) {
+                float *red = (float *)lds;      // [NT / PAIRS][BQ]
+                red[threadIdx.x / PAIRS * BQ + threadIdx.x % PAIRS * 2] = db[0];
+                red[threadIdx.x / PAIRS * BQ + threadIdx.x % PAIRS * 2 + 1] = db[1];
+                __syncthreads();
+                float *d = slot < 0 ? a.db + (int64_t)e * a.out : a.part_db + slot * a.out;
+                for (int i = threadIdx.x; i < BQ && q0 + i < a.out; i += NT) {
+                    float t = 0.0f;
+#pragma unroll
+                    for (int r = 0; r < NT / PAIRS; ++r) t += red[r * BQ + i];
+                    d[q0 + i] = t;
+                }
+                __syncthreads();
             }
-            carry += __builtin_amdgcn_readlane(s, 63);
-        }
-    }
-    for (; u < end && e < a.E; ++e) {
-        const Span sp = span_of(a, e);
-        int k0 = 0, k1 = sp.count;
-        int64_t slot = -1;
+            if (!a.dw) return;
+#pragma unroll
+            for (int j = 0; j < TQ; ++j) {
+                const int o = q0 + wq + 32 * j + (lane & 31);
+                if (o >= a.out) continue;
+#pragma unroll
+                for (int i = 0; i < TP; ++i)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const int f = p0 + wp + 32 * i + 8 * g + 4 * (lane >> 5);
+                        const f32x4_r v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2],
+                                           acc[i][j][4 * g + 3]};
+                        if (f + 4 <= a.in) {
+                            *(f32x4_a4 *)(c + o * ldc + f) = v;
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                if (f + k < a.in) c[o * ldc + f + k] = v[k];
+                        }
+                    }
+            }
+        };
+
+        // the experts of the run [begin, end) of units; `u`: the units before expert e
+        int begin = 0, end = 1, e = team, u = 0;
         if (teams > 0) {
-            if (sp.units == 0) continue;
-            k0 = (max(begin, u) - u) * DW_UNIT;
-            k1 = min((min(end, u + sp.units) - u) * DW_UNIT, sp.count);
-            if (u < begin || u + sp.units > end) slot = 2 * team + (u >= begin ? 1 : 0);
+            const int all = units_before(a, a.E), run = run_units(all, teams);
+            begin = min(team * run, all);
+            end = min(begin + run, all);
+            // the first expert that ends past `begin`, 64 at a time
+            e = a.E;
+            int carry = 0;
+            for (int e0 = 0; e0 < a.E; e0 += 64) {
+                const int j = e0 + lane;
+                const int k = j < a.E ? span_of(a, j).units : 0;
+                int s = k;
+#pragma unroll
+                for (int d = 1; d < 64; d *= 2) {
+                    const int t = __shfl_up(s, d);
+                    s += lane >= d ? t : 0;
+                }
+                const uint64_t hit = __ballot(carry + s > begin);
+                if (hit) {
+                    const int l = __builtin_ctzll(hit);
+                    e = e0 + l;
+                    u = carry + __builtin_amdgcn_readlane(s, l) - __builtin_amdgcn_readlane(k, l);
+                    break;
+                }
+                carry += __builtin_amdgcn_readlane(s, 63);
+            }
         }
-        product(__builtin_amdgcn_readfirstlane(sp.first + k0), __builtin_amdgcn_readfirstlane(k1 - k0));
-        finish(e, slot);
-        if (teams == 0) break;
-        u += sp.units;
-    }
+        for (; u < end && e < a.E; ++e) {
+            const Span sp = span_of(a, e);
+            int k0 = 0, k1 = sp.count;
+            int64_t slot = -1;
+            if (teams > 0) {
+                if (sp.units == 0) continue;
+                k0 = (max(begin, u) - u) * DW_UNIT;
+                k1 = min((min(end, u + sp.units) - u) * DW_UNIT, sp.count);
+                if (u < begin || u + sp.units > end) slot = 2 * team + (u >= begin ? 1 : 0);
+            }
+            product(__builtin_amdgcn_readfirstlane(sp.first + k0), __builtin_amdgcn_readfirstlane(k1 - k0));
+            finish(e, slot);
+            if (teams == 0) break;
+            u += sp.units;
+        }
     }
 };
 
@@ -1259,8 +1269,12 @@ static bool rows_aligned(const void *p, int64_t ld, int64_t size = 2)
 // 6000 rows 300x1000 of 10 experts (228) 16.7, 13.7 and with 128 x 64 16.9; 12000 rows 1024x256
 // (104) 17.7, 15.5; 2000 rows 1024x1024 of 4 (80) 17.0, 13.8 and with 64 x 64 16.9; 6000 rows
 // 1024x256 (57) 16.4, 10.5.  Rows of any alignment have the first (128 x 128) and the last.
+// The largest runs on four wavefronts of 128 x 64 forward, on eight of 64 x 64 for dx (65536
+// rows of 16 experts: 1024x1024 forward 181 us, on eight 200; dx of 1024x512 with its mask 124
+// us, on four 133).
 template <int OP>
-using RowsBig = RowsShape<OP, 2, 2, 4, 2, 32, 3, 1, BY_DIRECT>;
+using RowsBig = std::conditional_t<OP == OP_FORWARD, RowsShape<OP, 2, 2, 4, 2, 32, 3, 1, BY_DIRECT>,
+                                   RowsShape<OP, 4, 2, 2, 2, 32, 3, 1, BY_DIRECT>>;
 template <int OP>
 using RowsMid = RowsShape<OP, 2, 2, 2, 2, 64, 2, 1, BY_DIRECT>;
 template <int OP>
@@ -1353,7 +1367,8 @@ static void dw_go(const ExpertArgs &a, const DwPlan &d, hipStream_t s)
 template <bool CK>
 static void dw_launch(const ExpertArgs &a, const DwPlan &d, int by, hipStream_t s)
 {
-    if (d.tile == 256) by == BY_DIRECT ? dw_go<DwBig<BY_DIRECT, CK>>(a, d, s) : dw_go<DwBig<BY_REGISTERS, CK>>(a, d, s);
+    if (d.tile == 256 && by == BY_DIRECT) dw_go<DwBig<BY_DIRECT, CK>>(a, d, s);
+    else if (d.tile == 256) dw_go<DwBig<BY_REGISTERS, CK>>(a, d, s);
     else if (by == BY_DIRECT) dw_go<DwSmall<BY_DIRECT, CK>>(a, d, s);
     else if (by == BY_REGISTERS) dw_go<DwSmall<BY_REGISTERS, CK>>(a, d, s);
     else dw_go<DwSmall<BY_VALUES, CK>>(a, d, s);
@@ -1398,7 +1413,10 @@ hipError_t launch_expert_grad(const ExpertArgs &a, hipStream_t s)
         else rows_launch<OP_DX_CKPT>(a, dx_direct, s);
     }
     if (with_dw) {
-        if (!both && (a.n > 0 || d.teams == 0)) ck ? dw_launch<true>(a, d, dw_by, s) : dw_launch<false>(a, d, dw_by, s);
+        if (!both && (a.n > 0 || d.teams == 0)) {
+            if (ck) dw_launch<true>(a, d, dw_by, s);
+            else dw_launch<false>(a, d, dw_by, s);
+        }
         if (d.teams > 0) {
             const int64_t work = (int64_t)a.out * ((a.in + 3) / 4) + a.out;
             expert_dw_sum_kernel<<<dim3((unsigned)ceil_div(work, 256), a.E), dim3(256), 0, s>>>(a, d.teams);
