@@ -1280,7 +1280,7 @@ using RowsMid = RowsShape<OP, 2, 2, 2, 2, 64, 2, 1, BY_DIRECT>;
 template <int OP>
 using RowsLow = RowsShape<OP, 2, 2, 2, 1, 64, 3, 1, BY_DIRECT>;
 template <int OP, int BY>
-using RowsSmall = RowsShape<OP, 2, 2, 1, 1, 64, BY == BY_DIRECT ? 4 : 2, BY == BY_REGISTERS ? 3 : 1, BY>;
+using RowsSmall = RowsShape<OP, 2, 2, 1, 1, 64, BY == BY_DIRECT ? 3 : 2, BY == BY_REGISTERS ? 2 : 1, BY>;
 template <int OP>
 using RowsBigRegs = RowsShape<OP, 2, 2, 2, 2, 32, 2, 2, BY_REGISTERS>;
 constexpr int64_t BIG_TILES = 256, MID_TILES = 150, LOW_TILES = 60;
@@ -1325,8 +1325,12 @@ hipError_t launch_expert_linear(const ExpertArgs &a, hipStream_t s)
 
 template <int BY, bool CK>
 using DwBig = DwShape<2, 4, 4, 2, 32, BY == BY_DIRECT ? 4 : 2, 1, BY, CK>;
+// Few stages and register sets for the smallest tiles: more blocks a CU are worth more than
+// steps loaded ahead (4095 rows 361x1024 of aligned rows 46.5 us with 4 stages, 37 with 2 and
+// 3; 3000 rows 1000x500 through 3 register sets 48, 2 sets 41, 1 set 40 but 300 rows 12.1 for
+// 11.7).
 template <int BY, bool CK>
-using DwSmall = DwShape<2, 2, 1, 1, 64, BY == BY_DIRECT ? 4 : 2, BY == BY_REGISTERS ? 3 : 1, BY, CK>;
+using DwSmall = DwShape<2, 2, 1, 1, 64, 2, BY == BY_REGISTERS ? 2 : 1, BY, CK>;
 
 // The weight gradient's tile and teams: 256 x 256 tiles, a block on each CU, from
 // DW_BIG_ROWS rows on where both widths exceed half of one; else 64 x 64 ones, a team for
