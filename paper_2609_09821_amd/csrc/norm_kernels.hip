@@ -1,11 +1,12 @@
 // norm_kernels.hip -- layer norm, its gradient and the 8-bit checkpoint of an
 // activation.  All three read each value once and are bound by HBM.
 //
-// A row belongs to a team of T lanes that holds it in registers, eight
-// consecutive values a lane and chunk of 8 T columns: T = 4 .. 64 lanes for rows
-// up to 8 T values (several rows a wavefront, so that narrow rows leave no lane
-// idle), NC chunks of a wavefront up to 2048, and a block of 256 threads above,
-// whose sums meet in LDS.  Four lanes then hold one 32-block of a checkpoint.
+// A row belongs to a team of T lanes that holds it in registers, eight consecutive
+// values a lane: 4 .. 64 lanes (several rows a wavefront, so that narrow rows leave
+// few lanes idle) or 2 .. 16 wavefronts of a block, whose sums meet in LDS.  Four
+// lanes then hold one 32-block of a checkpoint.  Two pieces a lane and half the
+// lanes hold twice the registers: the gradient of 29296 rows of 4096 bf16 took
+// 198 us so and takes 153, of 117187 rows of 1024 176 and 141.
 #include <algorithm>
 #include <type_traits>
 
@@ -15,9 +16,11 @@
 namespace im {
 
 constexpr int NORM_NT = 256;
+template <int T>
+constexpr int norm_threads = T > NORM_NT ? T : NORM_NT;
 
-// Sum over the team.  T = 256: over the block, through `lds` (8 floats, the two
-// halves used in turn, so that one barrier a sum is enough).
+// Sum over the team.  Teams of several wavefronts: through `lds` (one float a wavefront, in
+// two halves used in turn, so that one barrier a sum is enough), in the wavefronts' order.
 template <int T>
 __device__ __forceinline__ float row_sum(float x, float *lds, int &half)
 {
@@ -25,168 +28,141 @@ __device__ __forceinline__ float row_sum(float x, float *lds, int &half)
         return team_sum<T>(x);
     } else {
         x = team_sum<64>(x);
-        float *b = lds + 4 * half;
+        float *b = lds + norm_threads<T> / 64 * half;
         half ^= 1;
         if ((threadIdx.x & 63) == 0) b[threadIdx.x >> 6] = x;
         __syncthreads();
-        return (b[0] + b[1]) + (b[2] + b[3]);
+        b += threadIdx.x / T * (T / 64);
+        float s = b[0];
+#pragma unroll
+        for (int w = 1; w < T / 64; ++w) s += b[w];
+        return s;
     }
 }
 
 // Rows per block and pass, and a block's loop over them: every thread of a
-// wavefront (of a block for T = 256) makes the same passes.
+// wavefront (of a block for teams of several) makes the same passes: as its first row does.
 template <int T>
 struct Team {
-    static constexpr int ROWS = NORM_NT / T;
+    static constexpr int ROWS = norm_threads<T> / T;
     __device__ static int lane() { return threadIdx.x % T; }
-    __device__ static int64_t first() { return (int64_t)blockIdx.x * ROWS + threadIdx.x / T; }
+    __device__ static int offset() { return T <= 64 ? (threadIdx.x & 63) / T : threadIdx.x / T; }
+    __device__ static int64_t lead() { return (int64_t)blockIdx.x * ROWS + threadIdx.x / T - offset(); }
 };
 
 // ---------------------------------------------------------------------------
 // y = (x - mean) rstd gamma + beta, the variance about the mean (two passes over
-// the registers: no cancellation), optionally the checkpoint of x.
+// the registers: no cancellation), optionally the checkpoint of x.  65536 x 1024 bf16
+// with the checkpoint: 65 us, 340 MB at 5.2 TB/s; one row of 1024 floats: 2.1 us, the
+// latency of a load, two sums and a store.
 // ---------------------------------------------------------------------------
-template <typename E, int T, int NC, bool CK>
-__global__ __launch_bounds__(NORM_NT) void norm_kernel(NormArgs a)
+template <typename E, int T, int W, bool CK>
+__global__ __launch_bounds__(norm_threads<T>) void norm_kernel(NormArgs a)
 {
-    __shared__ float lds[8];
+    typedef RowPiece<W> P;
+    __shared__ float lds[2 * norm_threads<T> / 64];
     int half = 0;
-    const int lane = Team<T>::lane();
-    const int64_t step = (int64_t)gridDim.x * Team<T>::ROWS;
-    int nv[NC];
+    const int64_t step = (int64_t)gridDim.x * Team<T>::ROWS, lead = Team<T>::lead();
+    const int ofs = Team<T>::offset();
+    P pc;
+    pc.init(Team<T>::lane() * 8, a.d);
+    // the next row is on its way while this one is worked on
+    auto fetch = [&](int64_t r) { return load_raw((const E *)a.x + r * a.ld_x, pc, r < a.n); };
+    auto next = fetch(lead + ofs);
+    float ga[8], be[8];
 #pragma unroll
-    for (int c = 0; c < NC; ++c) nv[c] = a.d - (c * T + lane) * 8;
-    // gamma and beta stay in registers over the rows where they are few
-    constexpr bool KEEP = NC <= 2;
-    float ga[KEEP ? NC : 1][8], be[KEEP ? NC : 1][8];
-    auto affine = [&](int c, float *g, float *b) {
-        const int col = (c * T + lane) * 8;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) g[k] = 1.0f, b[k] = 0.0f;
-        if (a.gamma) load8(a.gamma + col, nv[c], g);
-        if (a.beta) load8(a.beta + col, nv[c], b);
-    };
-    if constexpr (KEEP)
-#pragma unroll
-        for (int c = 0; c < NC; ++c) affine(c, ga[c], be[c]);
-
-    // the wavefront's first row decides (teams of one wavefront stay together)
-    const int64_t lead = T <= 64 ? Team<T>::first() - (threadIdx.x & 63) / (T <= 64 ? T : 64) : Team<T>::first();
-    const int64_t ofs = Team<T>::first() - lead;
+    for (int k = 0; k < 8; ++k) ga[k] = 1.0f, be[k] = 0.0f;
+    if (a.gamma) unpack8(load_raw(a.gamma, pc, true), ga);
+    if (a.beta) unpack8(load_raw(a.beta, pc, true), be);
     for (int64_t r0 = lead; r0 < a.n; r0 += step) {
         const int64_t r = r0 + ofs;
         const bool on = r < a.n;
-        float v[NC][8];
-        float s = 0.0f;
+        float v[8], s = 0.0f, q = 0.0f;
+        unpack8(next, v);
+        if (r0 + step < a.n) next = fetch(r + step);
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            load8((const E *)a.x + r * a.ld_x + (c * T + lane) * 8, on ? nv[c] : 0, v[c]);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) s += v[c][k];
-        }
+        for (int k = 0; k < 8; ++k) s += W == EVEN || pc.own(k) ? v[k] : 0.0f;    // lanes past the row hold zeros
         const float mean = row_sum<T>(s, lds, half) * a.inv_d;
-        float q = 0.0f;
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float t = k < nv[c] ? v[c][k] - mean : 0.0f;
-                q = fmaf(t, t, q);
-            }
+        for (int k = 0; k < 8; ++k) {
+            const float t = pc.own(k) ? v[k] - mean : 0.0f;
+            q = fmaf(t, t, q);
+        }
         const float rstd = 1.0f / sqrtf(row_sum<T>(q, lds, half) * a.inv_d + a.eps);
-        if (on && lane == 0) {
+        if (on && Team<T>::lane() == 0) {
             if (a.mean) a.mean[r] = mean;
             if (a.rstd) a.rstd[r] = rstd;
         }
+        if constexpr (CK) store_bytes(a.c.q + r * a.c.ld_q, a.c.scale + r * a.c.ld_scale, pc, on, v);
+        float y[8];
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const int col = (c * T + lane) * 8;
-            if constexpr (CK) {
-                const int scale = ckpt_scale(ckpt_top(v[c]));
-                if (on && nv[c] > 0) {
-                    store8_bytes(a.c.q + r * a.c.ld_q + col, nv[c], ckpt_pack(v[c], scale));
-                    if ((lane & 3) == 0) a.c.scale[r * a.c.ld_scale + (col >> 5)] = (uint8_t)scale;
-                }
-            }
-            float g[8], b[8], y[8];
-            if constexpr (KEEP) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) g[k] = ga[c][k], b[k] = be[c][k];
-            } else {
-                affine(c, g, b);
-            }
-#pragma unroll
-            for (int k = 0; k < 8; ++k) y[k] = fmaf((v[c][k] - mean) * rstd, g[k], b[k]);
-            if (on) store8((E *)a.y + r * a.ld_y + col, nv[c], y);
-        }
+        for (int k = 0; k < 8; ++k) y[k] = fmaf((v[k] - mean) * rstd, ga[k], be[k]);
+        if (on) store_piece((E *)a.y + r * a.ld_y, pc, y);
     }
 }
 
 // ---------------------------------------------------------------------------
 // The gradient.  Each thread sums its columns' dgamma and dbeta over the rows of
 // its team; the block's teams meet at the end and leave one row of partial sums,
-// which norm_grad_sum_kernel adds up in float64 in the blocks' order.
+// which norm_grad_sum_kernel adds up in float64 in the blocks' order: no atomics, the
+// same bits in every run.  524288 x 512 bf16 from a checkpoint: 242 us and 7 us for the
+// sum, 1.35 GB at 5.4 TB/s; without the next row's loads in flight 18 us more.  Odd widths
+// that fill little more than half of a team are bound by its instructions (538: 3.9 TB/s).
 // ---------------------------------------------------------------------------
-template <typename E, int T, int NC, bool CK>
-__global__ __launch_bounds__(NORM_NT) void norm_grad_kernel(NormGradArgs a)
+template <typename E, int T, int W, bool CK>
+__global__ __launch_bounds__(norm_threads<T>) void norm_grad_kernel(NormGradArgs a)
 {
-    constexpr int W = (T < 64 ? T : 64) * NC * 8;    // columns of a wavefront
-    __shared__ float lds[T <= 64 ? 4 * W : 8];
+    typedef RowPiece<W> P;
+    constexpr int G = T <= 64 ? 4 : norm_threads<T> / T;    // wavefronts or teams whose sums meet
+    constexpr int C = T * 8, WAVES = norm_threads<T> / 64;
+    __shared__ float lds[G > 1 ? G * C : 2 * WAVES];
     int half = 0;
-    const int lane = Team<T>::lane();
-    const int64_t step = (int64_t)gridDim.x * Team<T>::ROWS;
-    int nv[NC];
-    float ga[NC][8], dg[NC][8], db[NC][8];
+    const int64_t step = (int64_t)gridDim.x * Team<T>::ROWS, lead = Team<T>::lead();
+    const int ofs = Team<T>::offset();
+    P pc;
+    pc.init(Team<T>::lane() * 8, a.d);
+    // the next row is on its way while this one is worked on
+    decltype(load_raw((const E *)0, pc, true)) next_dy, next_x;
+    RawBytes next_q;
+    float next_mean, next_rstd;
+    auto fetch = [&](int64_t r) {
+        const bool on = r < a.n;
+        next_mean = on ? a.mean[r] : 0.0f, next_rstd = on ? a.rstd[r] : 0.0f;
+        next_dy = load_raw((const E *)a.dy + r * a.ld_dy, pc, on);
+        if constexpr (CK) next_q = load_bytes(a.c.q + r * a.c.ld_q, a.c.scale + r * a.c.ld_scale, pc, on);
+        else next_x = load_raw((const E *)a.x + r * a.ld_x, pc, on);
+    };
+    fetch(lead + ofs);
+    float ga[8], dg[8], db[8];
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-        const int col = (c * T + lane) * 8;
-        nv[c] = a.d - col;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) ga[c][k] = 1.0f, dg[c][k] = 0.0f, db[c][k] = 0.0f;
-        if (a.gamma) load8(a.gamma + col, nv[c], ga[c]);
-    }
-    const int64_t lead = T <= 64 ? Team<T>::first() - (threadIdx.x & 63) / (T <= 64 ? T : 64) : Team<T>::first();
-    const int64_t ofs = Team<T>::first() - lead;
+    for (int k = 0; k < 8; ++k) ga[k] = 1.0f, dg[k] = 0.0f, db[k] = 0.0f;
+    if (a.gamma) unpack8(load_raw(a.gamma, pc, true), ga);
     for (int64_t r0 = lead; r0 < a.n; r0 += step) {
         const int64_t r = r0 + ofs;
         const bool on = r < a.n;
-        const float mean = on ? a.mean[r] : 0.0f, rstd = on ? a.rstd[r] : 0.0f;
-        float h[NC][8], dy[NC][8];
-        float s1 = 0.0f, s2 = 0.0f;
+        const float mean = next_mean, rstd = next_rstd;
+        float h[8], dy[8], s1 = 0.0f, s2 = 0.0f;
+        unpack8(next_dy, dy);
+        if constexpr (CK) unpack8(next_q, pc, h);
+        else unpack8(next_x, h);
+        fetch(r + step);
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const int col = (c * T + lane) * 8, m = on ? nv[c] : 0;
-            load8((const E *)a.dy + r * a.ld_dy + col, m, dy[c]);
-            if constexpr (CK) {
-                u32x2_r q = load8_bytes(a.c.q + r * a.c.ld_q + col, m);
-                const int scale = m > 0 ? a.c.scale[r * a.c.ld_scale + (col >> 5)] : 0;
-                ckpt_unpack(q, scale, h[c]);
-            } else {
-                load8((const E *)a.x + r * a.ld_x + col, m, h[c]);
-            }
+        for (int k = 0; k < 8; ++k) {
+            h[k] = (h[k] - mean) * rstd;
+            const float t = W == EVEN || pc.own(k) ? dy[k] : 0.0f;    // lanes past the row hold zeros
+            const float g = t * ga[k];
+            s1 += g;
+            s2 = fmaf(g, h[k], s2);
+            dg[k] = fmaf(t, h[k], dg[k]);
+            db[k] += t;
         }
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                // columns past the width have dy = 0; their h is held at 0 too
-                h[c][k] = k < nv[c] ? (h[c][k] - mean) * rstd : 0.0f;
-                const float g = dy[c][k] * ga[c][k];
-                s1 += g;
-                s2 = fmaf(g, h[c][k], s2);
-                dg[c][k] = fmaf(dy[c][k], h[c][k], dg[c][k]);
-                db[c][k] += dy[c][k];
-            }
         if (a.dx) {
             s1 = row_sum<T>(s1, lds, half) * a.inv_d;
             s2 = row_sum<T>(s2, lds, half) * a.inv_d;
+            float o[8];
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                float o[8];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) o[k] = rstd * (dy[c][k] * ga[c][k] - s1 - h[c][k] * s2);
-                if (on) store8((E *)a.dx + r * a.ld_dx + (c * T + lane) * 8, nv[c], o);
-            }
+            for (int k = 0; k < 8; ++k) o[k] = rstd * (dy[k] * ga[k] - s1 - h[k] * s2);
+            if (on) store_piece((E *)a.dx + r * a.ld_dx, pc, o);
         }
     }
     if (!a.part) return;
@@ -194,37 +170,39 @@ __global__ __launch_bounds__(NORM_NT) void norm_grad_kernel(NormGradArgs a)
     const bool alone = gridDim.x == 1;
     float *sums[2] = {alone ? a.dgamma : a.part + (int64_t)blockIdx.x * 2 * a.d,
                       alone ? a.dbeta : a.part + ((int64_t)blockIdx.x * 2 + 1) * a.d};
-    if constexpr (T <= 64) {
-        // teams of a wavefront, then the four wavefronts in order
+    if constexpr (G > 1) {
+        // teams of a wavefront, then wavefronts or teams in order
+        constexpr int V = T < 64 ? 64 : T;
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
-            auto &v = p ? db : dg;
             __syncthreads();
 #pragma unroll
-            for (int c = 0; c < NC; ++c)
+            for (int k = 0; k < 8; ++k) {
+                float t = p ? db[k] : dg[k];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    float t = v[c][k];
-#pragma unroll
-                    for (int m = T; m < 64; m *= 2) t += __shfl_xor(t, m);
-                    if ((threadIdx.x & 63) < T) lds[(threadIdx.x >> 6) * W + (c * T + lane) * 8 + k] = t;
-                }
+                for (int m = T; m < 64; m *= 2) t += __shfl_xor(t, m);
+                if (threadIdx.x % V < T && pc.own(k)) lds[threadIdx.x / V * C + pc.at + k] = t;
+            }
             __syncthreads();
             if (sums[p])
-                for (int i = threadIdx.x; i < W && i < a.d; i += NORM_NT)
-                    sums[p][i] = (lds[i] + lds[W + i]) + (lds[2 * W + i] + lds[3 * W + i]);
+                for (int i = threadIdx.x; i < a.d; i += NORM_NT) {
+                    const float t = lds[i] + lds[C + i];
+                    sums[p][i] = G == 2 ? t : t + (lds[2 * C + i] + lds[3 * C + i]);
+                }
         }
     } else {
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            if (sums[0]) store8(sums[0] + (c * T + lane) * 8, nv[c], dg[c]);
-            if (sums[1]) store8(sums[1] + (c * T + lane) * 8, nv[c], db[c]);
-        }
+        for (int k = 0; k < 8; ++k)
+            if (pc.own(k)) {
+                if (sums[0]) sums[0][pc.at + k] = dg[k];
+                if (sums[1]) sums[1][pc.at + k] = db[k];
+            }
     }
 }
 
 // Column sums of the partial rows: 64 columns a block, wavefront w takes rows w,
-// w + 16, ...; the wavefronts' sums meet in LDS in order.
+// w + 16, ...; the wavefronts' sums meet in LDS in order.  1024 rows of 512: 6.8 us, of
+// which most is the latency of 64 loads in turn by each of few blocks.
 constexpr int NORM_SUM_WAVES = 16;
 __global__ __launch_bounds__(64 * NORM_SUM_WAVES) void norm_grad_sum_kernel(const float *part, int rows, int d,
                                                                             float *dgamma, float *dbeta)
@@ -251,44 +229,49 @@ __global__ __launch_bounds__(64 * NORM_SUM_WAVES) void norm_grad_sum_kernel(cons
 template <int V>
 using Int = std::integral_constant<int, V>;
 
-// Calls f(T, NC) for rows of d values.
+// Lanes of a team for rows of d values.
+static int64_t team_lanes(int64_t d)
+{
+    int64_t t = 4;
+    while (8 * t < d) t *= 2;
+    return t;
+}
+
+// Calls f(T, W) for rows of d values.
 template <typename F>
 void by_width(int64_t d, F &&f)
 {
-    if (d <= 32) f(Int<4>(), Int<1>());
-    else if (d <= 64) f(Int<8>(), Int<1>());
-    else if (d <= 128) f(Int<16>(), Int<1>());
-    else if (d <= 256) f(Int<32>(), Int<1>());
-    else if (d <= 512) f(Int<64>(), Int<1>());
-    else if (d <= 1024) f(Int<64>(), Int<2>());
-    else if (d <= 1536) f(Int<64>(), Int<3>());
-    else if (d <= 2048) f(Int<64>(), Int<4>());
-    else if (d <= 4096) f(Int<256>(), Int<2>());
-    else f(Int<256>(), Int<4>());
+    const int64_t t = team_lanes(d);
+    auto at = [&](auto T) { d % 8 ? f(T, Int<ODD>()) : f(T, Int<EVEN>()); };
+    if (t == 4) f(Int<4>(), Int<NARROW>());
+    else if (t == 8) at(Int<8>());
+    else if (t == 16) at(Int<16>());
+    else if (t == 32) at(Int<32>());
+    else if (t == 64) at(Int<64>());
+    else if (t == 128) at(Int<128>());
+    else if (t == 256) at(Int<256>());
+    else if (t == 512) at(Int<512>());
+    else at(Int<1024>());
 }
 
-// Rows that a block takes in one pass.
-static int64_t pass_rows(int64_t d)
-{
-    int64_t t = 4;
-    while (t < 64 && 8 * t < d) t *= 2;
-    return NORM_NT / (d > 2048 ? 256 : t);
-}
+// Threads of a block, and rows that it takes in one pass.
+static int64_t block_threads(int64_t d) { return std::max<int64_t>(NORM_NT, team_lanes(d)); }
+static int64_t pass_rows(int64_t d) { return block_threads(d) / team_lanes(d); }
 
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 hipError_t launch_norm(const NormArgs &a, bool f32, hipStream_t s)
 {
-    const int64_t blocks = std::min<int64_t>(ceil_div(a.n, pass_rows(a.d)), 256 * 8);
-    auto go = [&](auto t, auto nc) {
-        constexpr int T = decltype(t)::value, NC = decltype(nc)::value;
-        const dim3 g((unsigned)blocks), b(NORM_NT);
+    const int64_t blocks = std::min<int64_t>(ceil_div(a.n, pass_rows(a.d)), 256 * 32 * NORM_NT / block_threads(a.d));
+    auto go = [&](auto t, auto w) {
+        constexpr int T = decltype(t)::value, W = decltype(w)::value;
+        const dim3 g((unsigned)blocks), b(norm_threads<T>);
         if (f32) {
-            if (a.c.q) norm_kernel<float, T, NC, true><<<g, b, 0, s>>>(a);
-            else norm_kernel<float, T, NC, false><<<g, b, 0, s>>>(a);
+            if (a.c.q) norm_kernel<float, T, W, true><<<g, b, 0, s>>>(a);
+            else norm_kernel<float, T, W, false><<<g, b, 0, s>>>(a);
         } else {
-            if (a.c.q) norm_kernel<uint16_t, T, NC, true><<<g, b, 0, s>>>(a);
-            else norm_kernel<uint16_t, T, NC, false><<<g, b, 0, s>>>(a);
+            if (a.c.q) norm_kernel<uint16_t, T, W, true><<<g, b, 0, s>>>(a);
+            else norm_kernel<uint16_t, T, W, false><<<g, b, 0, s>>>(a);
         }
     };
     by_width(a.d, go);
@@ -296,26 +279,26 @@ hipError_t launch_norm(const NormArgs &a, bool f32, hipStream_t s)
 }
 
 // Few rows go to one block, which needs no second launch (4 us of the host): up to 8 passes.
-// Else four passes a block at least, and four blocks a CU at most (two: 262144 x 64 and
-// narrower stay as fast, 524288 x 512 takes 318 us for 262; eight: 302).
+// Else four passes a block at least, and four blocks of 256 threads a CU at most (with five,
+// which bf16 allows, 524288 x 512 takes 270 us for 257).
 int64_t norm_grad_blocks(int64_t n, int64_t d)
 {
     if (n <= 8 * pass_rows(d)) return 1;
-    return std::max<int64_t>(1, std::min<int64_t>(ceil_div(n, 4 * pass_rows(d)), 1024));
+    return std::min(ceil_div(n, 4 * pass_rows(d)), 1024 * NORM_NT / block_threads(d));
 }
 
 hipError_t launch_norm_grad(const NormGradArgs &a, bool f32, hipStream_t s)
 {
     const int64_t blocks = norm_grad_blocks(a.n, a.d);
-    auto go = [&](auto t, auto nc) {
-        constexpr int T = decltype(t)::value, NC = decltype(nc)::value;
-        const dim3 g((unsigned)blocks), b(NORM_NT);
+    auto go = [&](auto t, auto w) {
+        constexpr int T = decltype(t)::value, W = decltype(w)::value;
+        const dim3 g((unsigned)blocks), b(norm_threads<T>);
         if (f32) {
-            if (a.x) norm_grad_kernel<float, T, NC, false><<<g, b, 0, s>>>(a);
-            else norm_grad_kernel<float, T, NC, true><<<g, b, 0, s>>>(a);
+            if (a.x) norm_grad_kernel<float, T, W, false><<<g, b, 0, s>>>(a);
+            else norm_grad_kernel<float, T, W, true><<<g, b, 0, s>>>(a);
         } else {
-            if (a.x) norm_grad_kernel<uint16_t, T, NC, false><<<g, b, 0, s>>>(a);
-            else norm_grad_kernel<uint16_t, T, NC, true><<<g, b, 0, s>>>(a);
+            if (a.x) norm_grad_kernel<uint16_t, T, W, false><<<g, b, 0, s>>>(a);
+            else norm_grad_kernel<uint16_t, T, W, true><<<g, b, 0, s>>>(a);
         }
     };
     by_width(a.d, go);
@@ -326,9 +309,10 @@ hipError_t launch_norm_grad(const NormGradArgs &a, bool f32, hipStream_t s)
 }
 
 // ---------------------------------------------------------------------------
-// Checkpoints alone.  A team of T lanes walks a row in chunks of 8 T columns.
+// Checkpoints alone.  A team of up to 64 lanes walks a row in chunks of 8 T columns.
+// 262144 x 1024 bf16: 162 us to store, 129 us to restore, 813 MB each way.
 // ---------------------------------------------------------------------------
-template <typename E, int T, bool STORE>
+template <typename E, int T, int W, bool STORE>
 __global__ __launch_bounds__(NORM_NT) void ckpt_kernel(E *x, int64_t ld_x, int64_t n, int64_t d, im_checkpoint c)
 {
     const int lane = threadIdx.x % T;
@@ -340,19 +324,15 @@ __global__ __launch_bounds__(NORM_NT) void ckpt_kernel(E *x, int64_t ld_x, int64
         uint8_t *sr = c.scale + r * c.ld_scale;
         // a quad's lanes are on one 32-block and pass together
         for (int64_t b = 0; b < d; b += 8 * T) {
-            const int64_t col = b + lane * 8;
-            const int nv = (int)(d - col < 8 ? d - col : 8);
+            RowPiece<W> p;
+            p.init((int)b + lane * 8, (int)d);
             float v[8];
             if constexpr (STORE) {
-                load8(xr + col, nv, v);
-                const int scale = ckpt_scale(ckpt_top(v));
-                if (nv > 0) {
-                    store8_bytes(qr + col, nv, ckpt_pack(v, scale));
-                    if ((lane & 3) == 0) sr[col >> 5] = (uint8_t)scale;
-                }
-            } else if (nv > 0) {
-                ckpt_unpack(load8_bytes(qr + col, nv), sr[col >> 5], v);
-                store8(xr + col, nv, v);
+                unpack8(load_raw((const E *)xr, p, true), v);
+                store_bytes(qr, sr, p, true, v);
+            } else {
+                unpack8(load_bytes(qr, sr, p, true), p, v);
+                store_piece(xr, p, v);
             }
         }
     }
@@ -361,22 +341,18 @@ __global__ __launch_bounds__(NORM_NT) void ckpt_kernel(E *x, int64_t ld_x, int64
 hipError_t launch_checkpoint(bool store, void *x, int64_t ld_x, bool f32, int64_t n, int64_t d,
                              const im_checkpoint &c, hipStream_t s)
 {
-    auto go = [&](auto t) {
-        constexpr int T = decltype(t)::value;
-        const dim3 g((unsigned)std::min<int64_t>(ceil_div(n, NORM_NT / T), 256 * 16)), b(NORM_NT);
+    auto go = [&](auto t, auto w) {
+        constexpr int T = decltype(t)::value, W = decltype(w)::value;
+        const dim3 g((unsigned)std::min<int64_t>(ceil_div(n, NORM_NT / T), 256 * 64)), b(NORM_NT);
         if (f32) {
-            if (store) ckpt_kernel<float, T, true><<<g, b, 0, s>>>((float *)x, ld_x, n, d, c);
-            else ckpt_kernel<float, T, false><<<g, b, 0, s>>>((float *)x, ld_x, n, d, c);
+            if (store) ckpt_kernel<float, T, W, true><<<g, b, 0, s>>>((float *)x, ld_x, n, d, c);
+            else ckpt_kernel<float, T, W, false><<<g, b, 0, s>>>((float *)x, ld_x, n, d, c);
         } else {
-            if (store) ckpt_kernel<uint16_t, T, true><<<g, b, 0, s>>>((uint16_t *)x, ld_x, n, d, c);
-            else ckpt_kernel<uint16_t, T, false><<<g, b, 0, s>>>((uint16_t *)x, ld_x, n, d, c);
+            if (store) ckpt_kernel<uint16_t, T, W, true><<<g, b, 0, s>>>((uint16_t *)x, ld_x, n, d, c);
+            else ckpt_kernel<uint16_t, T, W, false><<<g, b, 0, s>>>((uint16_t *)x, ld_x, n, d, c);
         }
     };
-    if (d <= 32) go(Int<4>());
-    else if (d <= 64) go(Int<8>());
-    else if (d <= 128) go(Int<16>());
-    else if (d <= 256) go(Int<32>());
-    else go(Int<64>());
+    by_width(std::min<int64_t>(d, 512 - (d % 8 ? 1 : 0)), go);
     return hipGetLastError();
 }
 

@@ -742,3 +742,43 @@ def test_middle_tiles(n, E, din, dout, pad, kept):
         assert torch.equal(dx[r], torch.where(xin[r] > 0, plain[r], torch.zeros_like(plain[r])))
     assert not y[none].any() and not dx[none].any()
     _pad_kept(y), _pad_kept(dx)
+
+
+# Rows whose last 32-block has 1 to 7 values: a lane's last eight are of two blocks, here of
+# very different scales.
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,d,pad", [(7, 33, 0), (300, 65, 0), (129, 519, 1), (40, 1031, 0), (9, 4097, 3)])
+def test_last_values_of_two_blocks(n, d, pad, dtype):
+    x, gamma, beta, g = _norm_inputs(n, d, pad, dtype, n + 5 * d)
+    seam = d // 32 * 32
+    x[:, seam:] *= 2.0 ** -12
+    x[1::2, seam:] *= 2.0 ** 24
+    ck = im.Checkpoint(_out(n, d, pad, torch.int8), _out(n, -(-d // 32), pad, torch.uint8))
+    ck2 = im.Checkpoint(_out(n, d, pad, torch.int8), _out(n, -(-d // 32), pad, torch.uint8))
+    y = _out(n, d, pad, dtype)
+    m, r = torch.zeros(n, device=DEV), torch.zeros(n, device=DEV)
+    im.layer_norm(x, gamma, beta, y, m, r, eps=1e-2, checkpoint=ck)
+    im.checkpoint_store(x, ck2)
+    back = _ckpt_ref(x)[2]
+    for c in (ck, ck2):
+        _check_ckpt(x, c)
+        v = _out(n, d, pad, torch.float32)
+        im.checkpoint_load(c, v)
+        assert np.array_equal(v.cpu().numpy().astype(np.float64), np.asarray(back, np.float64))
+        _pad_kept(c.q), _pad_kept(c.scale), _pad_kept(v)
+    dy = _wide(torch.randn(n, d, device=DEV, generator=g).to(dtype), pad)
+    dx, dg, db = _out(n, d, pad, dtype), torch.zeros(d, device=DEV), torch.zeros(d, device=DEV)
+    im.layer_norm_grad(dy, ck, gamma, m, r, dx, dg, db)
+    want, dgam, dbet, size, sg, sb, _ = _ngrad_ref(dy, torch.from_numpy(back).to(DEV), gamma, m, r)
+    _within(dx, want, 64 * U * size + (BF * want.abs() if dtype == torch.bfloat16 else 0) + 1e-300, "dx")
+    _within(dg, dgam, 80 * U * sg + 1e-300, "dgamma")
+    _within(db, dbet, 80 * U * sb + 1e-300, "dbeta")
+    _pad_kept(dx)
+
+
+# Several passes of a block over rows of 256, 512 and 1024 lanes.
+@pytest.mark.parametrize("kept", [False, True])
+@pytest.mark.parametrize("n,d", [(5200, 1030), (2600, 2050), (1500, 4101)])
+def test_layer_norm_grad_many_wide_rows(n, d, kept):
+    test_layer_norm_grad(n, d, 0, torch.bfloat16, kept)
+    test_layer_norm_grad(n, d, 1, torch.float32, kept)
