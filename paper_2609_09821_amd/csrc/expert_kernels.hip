@@ -1393,7 +1393,8 @@ template <int BY>
 static void grad_launch(const ExpertArgs &a, const DwPlan &d, bool ck, hipStream_t s)
 {
     if (!a.relu) ck ? grad_go<OP_DX, BY, true>(a, d, s) : grad_go<OP_DX, BY, false>(a, d, s);
-    else ck ? grad_go<OP_DX_CKPT, BY, true>(a, d, s) : grad_go<OP_DX_X, BY, false>(a, d, s);
+    // the mask reads x also where dw is not wanted
+    else a.x ? grad_go<OP_DX_X, BY, false>(a, d, s) : grad_go<OP_DX_CKPT, BY, true>(a, d, s);
 }
 
 hipError_t launch_expert_grad(const ExpertArgs &a, hipStream_t s)

@@ -782,3 +782,33 @@ def test_last_values_of_two_blocks(n, d, pad, dtype):
 def test_layer_norm_grad_many_wide_rows(n, d, kept):
     test_layer_norm_grad(n, d, 0, torch.bfloat16, kept)
     test_layer_norm_grad(n, d, 1, torch.float32, kept)
+
+
+@pytest.mark.parametrize("kept", [False, True])
+@pytest.mark.parametrize("n,E,din,dout,pad", [(300, 4, 64, 64, 0), (300, 4, 65, 40, 0), (40, 3, 6, 5, 0),
+                                              (5000, 4, 128, 64, 0)])
+def test_expert_linear_grad_pairs_of_outputs(n, E, din, dout, pad, kept):
+    """Any two of dx, dw and db, with and without the mask, the same bits as all three; without
+    dw and the mask x need not be given."""
+    e, off, rows, x, w, _, g = _layer(n, E, din, dout, pad, n + 3, "holes")
+    dy = _wide(torch.randn(n, dout, device=DEV, generator=g).bfloat16(), pad)
+    src = x
+    if kept:
+        src = im.Checkpoint.empty(n, din)
+        im.checkpoint_store(x, src)
+
+    def call(xin, relu, names):
+        o = dict(dx=torch.full((n, din), 5.0, dtype=torch.bfloat16, device=DEV),
+                 dw=torch.full((E, dout, din), 5.0, device=DEV), db=torch.full((E, dout), 5.0, device=DEV))
+        o = {k: o[k] for k in names}
+        im.expert_linear_grad(dy, xin, w, off, rows, relu_x=relu, **o)
+        return o
+
+    for relu in (False, True):
+        want = call(src, relu, ("dx", "dw", "db"))
+        for names in (("dx", "db"), ("dx", "dw"), ("dw", "db")):
+            for k, v in call(src, relu, names).items():
+                assert torch.equal(v, want[k]), (relu, names, k)
+        if not relu:
+            for k, v in call(None, False, ("dx", "db")).items():
+                assert torch.equal(v, want[k]), k
