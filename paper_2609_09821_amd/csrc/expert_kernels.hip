@@ -909,7 +909,10 @@ __global__ __launch_bounds__(S::NT, 2) void expert_rows_kernel(ExpertArgs a, int
 //
 // 65536 rows of 16 experts, 1024x512: 157 us with the sums of the parts (26 of them, and as
 // much to write the parts, 94 MB), 440 TFLOP/s; bound by latency, a barrier and the
-// restoring each 32 rows, as 256 x 256 tiles leave registers for two wavefronts a SIMD.
+// restoring each 32 rows, as 256 x 256 tiles leave registers for two wavefronts a SIMD: the
+// MFMA pipes are busy for 26% of the cycles, the LDS for 20, and wavefronts wait for 35% of
+// theirs.  128 x 256 tiles on four wavefronts, two blocks a CU, were slower (both gradients 303
+// us for 286), and addresses by 32-bit products brought nothing.
 // With an even number of pieces a run each instead (64 x 64 partial tiles): 430 us.
 // ---------------------------------------------------------------------------
 constexpr int DW_UNIT = 64;
