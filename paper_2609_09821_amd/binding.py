@@ -740,11 +740,14 @@ def _space(nbytes):
 
 
 def _workspace(given, need, stream):
-    """Pointer and size of a call's workspace: the given one, or one of its own."""
+    """Pointer and size of a call's workspace: the given one, or one of its own, which comes from
+    the memory of the stream that the call is on (another stream's may still be in use there)."""
     if given is None:
-        given = need()
-        if stream is not None:
-            given.record_stream(stream)
+        if stream is None:
+            given = need()
+        else:
+            with _torch.cuda.stream(stream):
+                given = need()
     elif not given.is_cuda or not given.is_contiguous():
         raise ValueError("a workspace is contiguous device memory")
     return given.data_ptr(), given.numel() * given.element_size()

@@ -1,0 +1,60 @@
+"""The layers of experts' binding without a GPU: the calls' scratch memory.  Tensors are on the
+CPU, the device -1 of the calls, and the C entries note what they are given."""
+from contextlib import contextmanager
+
+import pytest
+import torch
+
+from paper_2609_09821_amd import binding as im
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The three calls that need scratch memory, as functions of a stream and a workspace, and
+    what became of each: (torch's stream when its memory was allocated, addresses in use)."""
+    if not im._lib:
+        im.lib()
+    current, allocated, used = ["torch's own"], [], []
+
+    @contextmanager
+    def on(stream):
+        before, current[0] = current[0], stream
+        yield
+        current[0] = before
+
+    def space(nbytes):
+        t = torch.zeros(max(nbytes, 16), dtype=torch.uint8)
+        t.record_stream = lambda s: None
+        allocated.append((current[0], t))
+        return t
+
+    monkeypatch.setattr(im, "_torch", torch)
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(im, "_call_stream", lambda stream: (-1, 0))
+    monkeypatch.setattr(im, "_space", space)
+    monkeypatch.setattr(im, "im_group_rows", lambda *a: used.append(a[5]))
+    for f in ("im_layer_norm_grad", "im_expert_linear_grad"):
+        monkeypatch.setattr(im, f, lambda a, raw: used.append(a.workspace))
+
+    n, e, i, o = 6000, 4, 24, 40
+    idx = dict(dtype=torch.int32)
+    off, rows = torch.zeros(e + 1, **idx), torch.zeros(n, **idx)
+    x, dy = torch.zeros(n, i, dtype=torch.bfloat16), torch.zeros(n, o, dtype=torch.bfloat16)
+    w = torch.zeros(e, o, i, dtype=torch.bfloat16)
+    stat, dg = torch.zeros(n), torch.zeros(i)
+    return [
+        lambda **k: im.group_rows(torch.zeros(n, **idx), off, rows, **k),
+        lambda **k: im.layer_norm_grad(x, x, None, stat, stat, None, dg, **k),
+        lambda **k: im.expert_linear_grad(dy, x, w, off, rows, dw=torch.zeros(e, o, i), **k),
+    ], allocated, used
+
+
+def test_scratch_memory_is_of_the_calls_stream(calls):
+    """Memory of another stream's pool may still be in use by that stream's work."""
+    calls, allocated, used = calls
+    for stream, where in (("side", "side"), (None, "torch's own")):
+        for call in calls:
+            call(stream=stream)
+            at, t = allocated.pop()
+            assert at == where and not allocated
+            assert used.pop() == t.data_ptr()

@@ -812,3 +812,41 @@ def test_expert_linear_grad_pairs_of_outputs(n, E, din, dout, pad, kept):
         if not relu:
             for k, v in call(None, False, ("dx", "db")).items():
                 assert torch.equal(v, want[k]), k
+
+
+def test_scratch_memory_on_a_side_stream(monkeypatch):
+    """Calls on a side stream without workspaces, beside work of the current one: their memory is
+    allocated on the side stream, and the results are those of the current stream."""
+    n, E, d, o = 20000, 5, 96, 72
+    e, off, rows, x, w, b, g = _layer(n, E, d, o, 0, 41)
+    dy = torch.randn(n, o, device=DEV, generator=g).bfloat16()
+    m, r = torch.zeros(n, device=DEV), torch.zeros(n, device=DEV)
+    im.layer_norm(x, None, None, torch.zeros_like(x), m, r)
+    t = dict(off=torch.zeros_like(off), rows=torch.zeros_like(rows), dw=torch.zeros(E, o, d, device=DEV),
+             db=torch.zeros(E, o, device=DEV), dg=torch.zeros(d, device=DEV), dbt=torch.zeros(d, device=DEV))
+
+    def calls(stream=None):
+        im.group_rows(e, t["off"], t["rows"], stream=stream)
+        im.expert_linear_grad(dy, x, w, off, rows, dw=t["dw"], db=t["db"], stream=stream)
+        im.layer_norm_grad(x, x, None, m, r, dgamma=t["dg"], dbeta=t["dbt"], stream=stream)
+
+    calls()
+    ref = {k: v.clone() for k, v in t.items()}
+    for v in t.values():
+        v.zero_()
+    torch.cuda.synchronize()
+    side, seen, space = torch.cuda.Stream(), [], im._space
+
+    def noted(nbytes):
+        seen.append(torch.cuda.current_stream())
+        return space(nbytes)
+
+    monkeypatch.setattr(im, "_space", noted)
+    busy = torch.ones(1 << 24, device=DEV)
+    for k in range(8):
+        busy = busy * 1.5       # frees a temporary that the current stream still reads
+        calls(side)
+    torch.cuda.synchronize()
+    assert len(seen) == 24 and all(s == side for s in seen)
+    for k, v in t.items():
+        assert torch.equal(v, ref[k]), k
