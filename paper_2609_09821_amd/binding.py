@@ -740,8 +740,9 @@ def _space(nbytes):
 
 
 def _workspace(given, need, stream):
-    """Pointer and size of a call's workspace: the given one, or one of its own, which comes from
-    the memory of the stream that the call is on (another stream's may still be in use there)."""
+    """A call's workspace, its pointer and size: the given one, or one of its own, which comes from
+    the memory of the stream that the call is on (another stream's may still be in use there).
+    The call holds it until it has launched."""
     if given is None:
         if stream is None:
             given = need()
@@ -750,7 +751,7 @@ def _workspace(given, need, stream):
                 given = need()
     elif not given.is_cuda or not given.is_contiguous():
         raise ValueError("a workspace is contiguous device memory")
-    return given.data_ptr(), given.numel() * given.element_size()
+    return given, given.data_ptr(), given.numel() * given.element_size()
 
 
 class Checkpoint:
@@ -803,7 +804,7 @@ def group_rows(expert, offsets, rows, workspace=None, stream=None):
     dev, raw = _call_stream(stream)
     n, e = expert.numel(), offsets.numel() - 1
     i32 = _torch.int32
-    ws, nbytes = _workspace(workspace, lambda: group_rows_workspace(n, e), stream)
+    _held, ws, nbytes = _workspace(workspace, lambda: group_rows_workspace(n, e), stream)
     im_group_rows(_vec(expert, n, "expert", dev, i32), n, e,
                   _vec(offsets, e + 1, "offsets", dev, i32), _vec(rows, n, "rows", dev, i32),
                   ws, nbytes, raw)
@@ -836,7 +837,7 @@ def layer_norm_grad(dy, x, gamma, mean, rstd, dx=None, dgamma=None, dbeta=None, 
     f32 = _torch.float32
     ws, nbytes = None, 0
     if dgamma is not None or dbeta is not None:
-        ws, nbytes = _workspace(workspace, lambda: layer_norm_grad_workspace(n, d), stream)
+        _held, ws, nbytes = _workspace(workspace, lambda: layer_norm_grad_workspace(n, d), stream)
     if isinstance(x, Checkpoint):
         xp, ldx, ck = None, 0, C.pointer(x.struct(n, d, dev))
     else:
@@ -895,8 +896,8 @@ def expert_linear_grad(dy, x, w, offsets, rows, dx=None, dw=None, db=None, relu_
     i32, f32, bf16 = _torch.int32, _torch.float32, _torch.bfloat16
     ws, nbytes = None, 0
     if dw is not None or db is not None:
-        ws, nbytes = _workspace(workspace, lambda: expert_linear_grad_workspace(n, e, in_, out),
-                                stream)
+        _held, ws, nbytes = _workspace(
+            workspace, lambda: expert_linear_grad_workspace(n, e, in_, out), stream)
     xp, ldx, ck = None, 0, None
     if isinstance(x, Checkpoint):
         ck = C.pointer(x.struct(n, in_, dev))

@@ -1,5 +1,6 @@
 """The layers of experts' binding without a GPU: the calls' scratch memory.  Tensors are on the
 CPU, the device -1 of the calls, and the C entries note what they are given."""
+import weakref
 from contextlib import contextmanager
 
 import pytest
@@ -58,3 +59,23 @@ def test_scratch_memory_is_of_the_calls_stream(calls):
             at, t = allocated.pop()
             assert at == where and not allocated
             assert used.pop() == t.data_ptr()
+
+
+def test_scratch_memory_is_held_until_the_launch(calls, monkeypatch):
+    """Freed before, another thread could be given it between the two."""
+    calls, allocated, used = calls
+    refs, alive = [], []
+
+    def space(nbytes):
+        t = torch.zeros(max(nbytes, 16), dtype=torch.uint8)
+        refs.append(weakref.ref(t))
+        return t
+
+    monkeypatch.setattr(im, "_space", space)
+    for f in ("im_group_rows", "im_layer_norm_grad", "im_expert_linear_grad"):
+        monkeypatch.setattr(im, f, lambda *a: alive.append(refs[-1]() is not None))
+    for stream in ("side", None):
+        for call in calls:
+            call(stream=stream)
+    assert alive == [True] * 6
+    assert all(r() is None for r in refs)
