@@ -739,7 +739,7 @@ def _space(nbytes):
     return torch.empty(max(nbytes, 16), dtype=torch.uint8, device="cuda")
 
 
-def _workspace(given, need, stream):
+def _workspace(given, need, dev, stream):
     """A call's workspace, its pointer and size: the given one, or one of its own, which comes from
     the memory of the stream that the call is on (another stream's may still be in use there).
     The call holds it until it has launched."""
@@ -749,8 +749,8 @@ def _workspace(given, need, stream):
         else:
             with _torch.cuda.stream(stream):
                 given = need()
-    elif not given.is_cuda or not given.is_contiguous():
-        raise ValueError("a workspace is contiguous device memory")
+    elif given.get_device() != dev or not given.is_contiguous():
+        raise ValueError("a workspace is contiguous memory on the current device")
     return given, given.data_ptr(), given.numel() * given.element_size()
 
 
@@ -804,7 +804,7 @@ def group_rows(expert, offsets, rows, workspace=None, stream=None):
     dev, raw = _call_stream(stream)
     n, e = expert.numel(), offsets.numel() - 1
     i32 = _torch.int32
-    _held, ws, nbytes = _workspace(workspace, lambda: group_rows_workspace(n, e), stream)
+    _held, ws, nbytes = _workspace(workspace, lambda: group_rows_workspace(n, e), dev, stream)
     im_group_rows(_vec(expert, n, "expert", dev, i32), n, e,
                   _vec(offsets, e + 1, "offsets", dev, i32), _vec(rows, n, "rows", dev, i32),
                   ws, nbytes, raw)
@@ -837,7 +837,8 @@ def layer_norm_grad(dy, x, gamma, mean, rstd, dx=None, dgamma=None, dbeta=None, 
     f32 = _torch.float32
     ws, nbytes = None, 0
     if dgamma is not None or dbeta is not None:
-        _held, ws, nbytes = _workspace(workspace, lambda: layer_norm_grad_workspace(n, d), stream)
+        _held, ws, nbytes = _workspace(workspace, lambda: layer_norm_grad_workspace(n, d), dev,
+                                       stream)
     if isinstance(x, Checkpoint):
         xp, ldx, ck = None, 0, C.pointer(x.struct(n, d, dev))
     else:
@@ -897,7 +898,7 @@ def expert_linear_grad(dy, x, w, offsets, rows, dx=None, dw=None, db=None, relu_
     ws, nbytes = None, 0
     if dw is not None or db is not None:
         _held, ws, nbytes = _workspace(
-            workspace, lambda: expert_linear_grad_workspace(n, e, in_, out), stream)
+            workspace, lambda: expert_linear_grad_workspace(n, e, in_, out), dev, stream)
     xp, ldx, ck = None, 0, None
     if isinstance(x, Checkpoint):
         ck = C.pointer(x.struct(n, in_, dev))

@@ -79,3 +79,23 @@ def test_scratch_memory_is_held_until_the_launch(calls, monkeypatch):
             call(stream=stream)
     assert alive == [True] * 6
     assert all(r() is None for r in refs)
+
+
+class _OnDevice(torch.Tensor):
+    """Memory that says it is on device 1."""
+    is_cuda = True
+
+    def get_device(self):
+        return 1
+
+
+def test_a_workspace_of_another_device_is_refused(calls):
+    calls, _, used = calls
+    for call in calls:
+        with pytest.raises(ValueError, match="workspace"):
+            call(workspace=torch.zeros(1 << 20, dtype=torch.uint8).as_subclass(_OnDevice))
+        with pytest.raises(ValueError, match="workspace"):
+            call(workspace=torch.zeros(1 << 21, dtype=torch.uint8)[::2])
+        assert not used
+        call(workspace=torch.zeros(1 << 20, dtype=torch.uint8))
+        used.clear()
