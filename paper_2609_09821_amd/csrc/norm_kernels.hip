@@ -237,22 +237,16 @@ static int64_t team_lanes(int64_t d)
     return t;
 }
 
-// Calls f(T, W) for rows of d values.
-template <typename F>
+// Calls f(T, W) for rows of d values, T up to MOST lanes (which walk longer rows).
+template <int MOST, int T = 4, typename F>
 void by_width(int64_t d, F &&f)
 {
-    const int64_t t = team_lanes(d);
-    auto at = [&](auto T) { d % 8 ? f(T, Int<ODD>()) : f(T, Int<EVEN>()); };
-    if (t == 4) f(Int<4>(), Int<NARROW>());
-    else if (t == 8) at(Int<8>());
-    else if (t == 16) at(Int<16>());
-    else if (t == 32) at(Int<32>());
-    else if (t == 64) at(Int<64>());
-    else if (t == 128) at(Int<128>());
-    else if (t == 256) at(Int<256>());
-    else if (t == 512) at(Int<512>());
-    else at(Int<1024>());
+    if constexpr (T < MOST)
+        if (8 * T < d) return by_width<MOST, 2 * T>(d, f);
+    if constexpr (T == 4) f(Int<T>(), Int<NARROW>());
+    else d % 8 ? f(Int<T>(), Int<ODD>()) : f(Int<T>(), Int<EVEN>());
 }
+constexpr int NORM_LANES = IM_NORM_MAX_WIDTH / 8;
 
 // Threads of a block, and rows that it takes in one pass.
 static int64_t block_threads(int64_t d) { return std::max<int64_t>(NORM_NT, team_lanes(d)); }
@@ -274,7 +268,7 @@ hipError_t launch_norm(const NormArgs &a, bool f32, hipStream_t s)
             else norm_kernel<uint16_t, T, W, false><<<g, b, 0, s>>>(a);
         }
     };
-    by_width(a.d, go);
+    by_width<NORM_LANES>(a.d, go);
     return hipGetLastError();
 }
 
@@ -301,7 +295,7 @@ hipError_t launch_norm_grad(const NormGradArgs &a, bool f32, hipStream_t s)
             else norm_grad_kernel<uint16_t, T, W, true><<<g, b, 0, s>>>(a);
         }
     };
-    by_width(a.d, go);
+    by_width<NORM_LANES>(a.d, go);
     if (a.part && blocks > 1)
         norm_grad_sum_kernel<<<dim3((unsigned)ceil_div(2 * a.d, 64)), dim3(64 * NORM_SUM_WAVES), 0, s>>>(
             a.part, (int)blocks, a.d, a.dgamma, a.dbeta);
@@ -309,12 +303,14 @@ hipError_t launch_norm_grad(const NormGradArgs &a, bool f32, hipStream_t s)
 }
 
 // ---------------------------------------------------------------------------
-// Checkpoints alone.  A team of up to 64 lanes walks a row in chunks of 8 T columns.
+// Checkpoints alone.  A team of up to CKPT_LANES lanes walks a row in chunks of 8 T columns.
 // 262144 x 1024 bf16: 162 us to store, 129 us to restore, 813 MB each way.
 // ---------------------------------------------------------------------------
+constexpr int CKPT_LANES = 64;
 template <typename E, int T, int W, bool STORE>
 __global__ __launch_bounds__(NORM_NT) void ckpt_kernel(E *x, int64_t ld_x, int64_t n, int64_t d, im_checkpoint c)
 {
+    static_assert(T <= CKPT_LANES && NORM_NT % T == 0, "whole teams in a block, each in one wavefront");
     const int lane = threadIdx.x % T;
     const int64_t step = (int64_t)gridDim.x * (NORM_NT / T);
     const int64_t row0 = (int64_t)blockIdx.x * (NORM_NT / T) + threadIdx.x / T;
@@ -352,7 +348,7 @@ hipError_t launch_checkpoint(bool store, void *x, int64_t ld_x, bool f32, int64_
             else ckpt_kernel<uint16_t, T, W, false><<<g, b, 0, s>>>((uint16_t *)x, ld_x, n, d, c);
         }
     };
-    by_width(std::min<int64_t>(d, 512 - (d % 8 ? 1 : 0)), go);
+    by_width<CKPT_LANES>(d, go);
     return hipGetLastError();
 }
 
