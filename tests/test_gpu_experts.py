@@ -850,3 +850,94 @@ def test_scratch_memory_on_a_side_stream(monkeypatch):
     assert len(seen) == 24 and all(s == side for s in seen)
     for k, v in t.items():
         assert torch.equal(v, ref[k]), k
+
+
+# float32 outputs (a policy's head) and dx without a mask, on each size of tile
+@pytest.mark.parametrize("n,E,din,dout,pad,form", [
+    (17000, 5, 264, 1000, 0, "holes"), (16500, 3, 270, 1023, 1, "holes"),      # the largest, both ways of loading
+    (5000, 3, 300, 1000, 4, "holes"), (3000, 12, 520, 330, 0, "even"),         # 128 x 128 and 128 x 64
+])
+def test_fp32_outputs_of_large_tiles(n, E, din, dout, pad, form):
+    e, off, rows, x, w, b, g = _layer(n, E, din, dout, pad, n + dout, form)
+    for relu, bias in ((False, b), (True, None)):
+        y = _out(n, dout, 3, torch.float32)
+        y.fill_(5.0)
+        im.expert_linear(x, w, bias, off, rows, y, relu=relu)
+        none = torch.ones(n, dtype=torch.bool, device=DEV)
+        for k, r in enumerate(_by_expert(e, E)):
+            none[r] = False
+            v, wk = x[r].double(), w[k].double()
+            want, size = v @ wk.t(), v.abs() @ wk.abs().t()
+            if bias is not None:
+                want, size = want + b[k].double(), size + b[k].double().abs()
+            _within(y[r], want.clamp(min=0) if relu else want, 2 * (din + 1) * U * size, "y")
+        assert not y[none].any()
+        _pad_kept(y)
+
+
+@pytest.mark.parametrize("n,E,din,dout,pad", [(17000, 5, 1000, 264, 0), (16500, 3, 1023, 270, 1)])
+def test_unmasked_dx_of_large_tiles(n, E, din, dout, pad):
+    e, off, rows, _, w, _, g = _layer(n, E, din, dout, pad, n + dout, "holes")
+    dy = _wide(torch.randn(n, dout, device=DEV, generator=g).bfloat16(), pad)
+    dx = _out(n, din, pad, torch.bfloat16)
+    dx.fill_(5.0)
+    im.expert_linear_grad(dy, None, w, off, rows, dx=dx)
+    none = torch.ones(n, dtype=torch.bool, device=DEV)
+    for k, r in enumerate(_by_expert(e, E)):
+        none[r] = False
+        d, wk = dy[r].double(), w[k].double()
+        want = d @ wk
+        _within(dx[r], want, 2 * dout * U * (d.abs() @ wk.abs()) + BF * want.abs(), "dx")
+    assert not dx[none].any()
+    _pad_kept(dx)
+
+
+# More experts than a wavefront has lanes, their rows divided among teams of blocks: of 64 x 64
+# tiles and of 256 x 256 ones, of aligned and of odd rows.
+@pytest.mark.parametrize("kept", [False, True])
+@pytest.mark.parametrize("n,E,din,dout,pad", [
+    (3000, 70, 64, 64, 0), (6000, 70, 64, 104, 0), (9000, 200, 41, 72, 0),
+    (20000, 70, 264, 200, 0), (20000, 200, 137, 264, 2),
+])
+def test_weight_gradient_of_many_experts(n, E, din, dout, pad, kept):
+    g = _gen(n + E)
+    # uneven, with long and empty ones on both sides of number 64
+    share = 0.1 + torch.rand(E, device=DEV, generator=g)
+    share[torch.tensor([5, 62, 66, E - 3])] = 0.08 * E
+    share[torch.tensor([0, 7, 63, 64, 65, E - 1])] = 0.0
+    e = torch.multinomial(share, n, replacement=True, generator=g).to(torch.int32)
+    e[::50] = -1
+    off, rows = torch.zeros(E + 1, dtype=torch.int32, device=DEV), torch.zeros(n, dtype=torch.int32, device=DEV)
+    im.group_rows(e, off, rows)
+    x = _wide(torch.randn(n, din, device=DEV, generator=g).bfloat16(), pad)
+    dy = _wide(torch.randn(n, dout, device=DEV, generator=g).bfloat16(), pad)
+    w = torch.zeros(E, dout, din, dtype=torch.bfloat16, device=DEV)
+    src, xin = x, x.double()
+    if kept:
+        src = im.Checkpoint(_out(n, din, pad, torch.int8), _out(n, -(-din // 32), pad, torch.uint8))
+        im.checkpoint_store(x, src)
+        xin = torch.from_numpy(_ckpt_ref(x)[2]).to(DEV)
+    dw, db = torch.full((E, dout, din), 5.0, device=DEV), torch.full((E, dout), 5.0, device=DEV)
+    im.expert_linear_grad(dy, src, w, off, rows, dw=dw, db=db)
+    for k, r in enumerate(_by_expert(e, E)):
+        d, m = dy[r].double(), xin[r]
+        _within(dw[k], d.t() @ m, 2 * len(r) * U * (d.abs().t() @ m.abs()), "dw %d" % k)
+        _within(db[k], d.sum(0), 2 * len(r) * U * d.abs().sum(0), "db %d" % k)
+
+
+def test_mask_of_a_checkpoint():
+    """From a checkpoint the ReLU's mask is that of the restored values: it differs from the mask
+    of the activations at positive ones of half a step or less, and nowhere else."""
+    n, E, din, dout = 700, 3, 200, 72
+    e, off, rows, x, w, b, g = _layer(n, E, din, dout, 0, 55)
+    h = x.clamp(min=0)
+    dy = torch.randn(n, dout, device=DEV, generator=g).bfloat16()
+    ck = im.Checkpoint.empty(n, din)
+    im.checkpoint_store(h, ck)
+    dx, exact = (torch.zeros(n, din, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    im.expert_linear_grad(dy, h, w, off, rows, dx=exact, relu_x=True)
+    im.expert_linear_grad(dy, ck, w, off, rows, dx=dx, relu_x=True)
+    step = torch.exp2(ck.scale.double() - 133).repeat_interleave(32, dim=1)[:, :din]
+    lost = (h > 0) & (h.double() <= step / 2)
+    assert 0 < int(lost.sum()) < 0.02 * int((h > 0).sum())
+    assert torch.equal(dx, torch.where(lost, torch.zeros_like(exact), exact))
