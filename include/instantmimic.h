@@ -666,7 +666,12 @@ im_status im_expert_linear(const im_expert_layer *a, void *stream);
  * Its gradients, dy [n][out] bf16 the loss's gradient before any ReLU of y:
  *   dx[r] = W_e^T dy[r] bf16, with relu_x zero where not x[r] > 0 (x is a ReLU's
  *           output: dx is then the gradient before that ReLU); zero for rows
- *           without an expert
+ *           without an expert.  From a checkpoint the mask goes by the restored
+ *           values: positive ones that were at most half a step (1/127.5 of their
+ *           block's largest at most; about 1% of the positive values of rectified
+ *           normal ones, 5% where their scales are log-normal besides, sigma 1)
+ *           count as zero: their dx is lost, not rounded.  So does a whole block
+ *           with a NaN or an infinity.  With x itself the mask is exact.
  *   dw_e  = sum over e's rows of dy[r] x[r]^T, float [n_experts][out][in] (row
  *           stride ld_dw), db_e = sum of dy[r], float [n_experts][out]; an expert
  *           without rows gets zeros

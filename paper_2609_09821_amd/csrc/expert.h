@@ -52,7 +52,8 @@ hipError_t launch_norm_grad(const NormGradArgs &a, bool f32, hipStream_t s);
 hipError_t launch_checkpoint(bool store, void *x, int64_t ld_x, bool f32, int64_t n, int64_t d,
                              const im_checkpoint &c, hipStream_t s);
 
-// Rows by expert: blocks of GROUP_ROWS(n) rows, their counts in `count`.
+// Rows by expert: blocks of a launch over n rows; where there are several, their counts are
+// left in `count`, [blocks][n_experts + 1].
 int64_t group_blocks(int64_t n);
 hipError_t launch_group_rows(const int32_t *expert, int64_t n, int n_experts, int32_t *offsets,
                              int32_t *rows, int32_t *count, hipStream_t s);

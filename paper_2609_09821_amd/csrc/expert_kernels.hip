@@ -30,7 +30,10 @@ static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // write a counter at a time, so the order is the rows' own, whatever the timing.
 // Blocks of GROUP_NT threads; one block alone up to GROUP_ONE rows (its counts stay in
 // LDS), else a counting launch leaves [block][expert] counts and every block of the second
-// launch adds up those before it.
+// launch adds up those before it.  us in one launch and in two, replayed from a graph: 2048
+// rows of 64 experts 6.0, 7.4; 4096 rows 9.0, 7.5 (of 1024 experts 16.7, 20.2); 6000 rows 11.9,
+// 7.7.  The bound counts the 4 us that a second launch costs the host where there is no graph.
+// 262144 rows of 64 experts: 3.5 us to count, 7.6 to place.
 // ---------------------------------------------------------------------------
 constexpr int GROUP_NT = 1024, GROUP_WAVES = GROUP_NT / 64;
 constexpr int64_t GROUP_BLOCKS = 256, GROUP_ONE = 4096;
@@ -607,7 +610,7 @@ __device__ __forceinline__ void clear(f32x16_t (&acc)[TP][TQ])
 // Forward and input gradient: C rows are places.  Blocks p-tile fastest, blocks of
 // one XCD consecutive: the tiles that read one set of rows share an L2.
 //
-// 65536 rows of 16 experts, unevenly drawn, 1024x1024: 180 us, 760 TFLOP/s.  Its parts alone:
+// 65536 rows of 16 experts, unevenly drawn, 1024x1024: 179 us, 768 TFLOP/s.  Its parts alone:
 // products 90 us, loads from the L2 into LDS 117 (1.6 GB), and 47 more where the outputs
 // are stored.  Two blocks of 256 x 128 share a CU, so that one's loads and stores run beside
 // the other's products; 256 x 256 tiles load less but leave one block (206 us).
@@ -813,6 +816,8 @@ struct RowsShape {
             }
             return v;
         };
+        // fp32 rows leave from the registers, 32 bytes of 32 rows at a time: 65536 rows 1024x1024
+        // 213 us for 179 in bf16, with 134 MB more to write
         if (OP == OP_FORWARD && a.y_f32) {
 #pragma unroll
             for (int j = 0; j < TQ; ++j) {
@@ -907,8 +912,8 @@ __global__ __launch_bounds__(S::NT, 2) void expert_rows_kernel(ExpertArgs a, int
 // the teams' order.  The blocks of the first inputs also sum dy's columns for db, from the
 // stages in LDS.  CK: x from its checkpoint, whose bytes each lane restores one step ahead.
 //
-// 65536 rows of 16 experts, 1024x512: 157 us with the sums of the parts (26 of them, and as
-// much to write the parts, 94 MB), 440 TFLOP/s; bound by latency, a barrier and the
+// 65536 rows of 16 experts, 1024x512: 152 us with the sums of the parts (28 of them, and as
+// much to write the parts, 94 MB), 450 TFLOP/s; bound by latency, a barrier and the
 // restoring each 32 rows, as 256 x 256 tiles leave registers for two wavefronts a SIMD: the
 // MFMA pipes are busy for 26% of the cycles, the LDS for 20, and wavefronts wait for 35% of
 // theirs.  128 x 256 tiles on four wavefronts, two blocks a CU, were slower (both gradients 303
@@ -1287,7 +1292,12 @@ using RowsSmall = RowsShape<OP, 2, 2, 1, 1, 64, BY == BY_DIRECT ? 3 : 2, BY == B
 template <int OP>
 using RowsBigRegs = RowsShape<OP, 2, 2, 2, 2, 32, 2, 2, BY_REGISTERS>;
 constexpr int64_t BIG_TILES = 256, MID_TILES = 150, LOW_TILES = 60;
-// dx beside a weight gradient of 64 x 64 tiles shares its launch below this many.
+// dx beside a weight gradient of 64 x 64 tiles shares its launch below this many: all blocks of
+// the launch are of dx's smallest tiles then.  us of the whole gradient in one launch and in
+// two, 8 experts: 500 rows 361x1024 (22 tiles) 18.2, 21.0; 4000 rows (80) 35.1, 42.5; 8000 rows
+// (142) 75.1, 71.0; 4000 rows 1024x1024 (160) 74.5, 66.8; 8000 rows 1024x512 (284) 83.4, 71.7;
+// 12000 rows (408) 113, 86; but 16000 rows 256x256 of 16 (142) 35.0, 40.6.  So the bound leaves
+// up to 30% where wide layers have between 140 and 384 tiles, and gains 15% where narrow ones do.
 constexpr int64_t GRAD_BIG_TILES = 384;
 
 template <int OP>
@@ -1338,7 +1348,23 @@ using DwSmall = DwShape<2, 2, 1, 1, 64, 2, BY == BY_REGISTERS ? 2 : 1, BY, CK>;
 // The weight gradient's tile and teams: 256 x 256 tiles, a block on each CU, from
 // DW_BIG_ROWS rows on where both widths exceed half of one; else 64 x 64 ones, a team for
 // each expert up to DW_EXPERT_ROWS rows where that makes DW_EXPERT_BLOCKS blocks, or
-// DW_SMALL_BLOCKS blocks whose teams have at least DW_RUN rows.
+// DW_SMALL_BLOCKS blocks whose teams have at least DW_RUN rows.  Both sides of each, us of dw and
+// db with the sums of parts, replayed from a graph, even experts:
+//   256 x 256 and 64 x 64 tiles: 361x1024 of 8 experts, 8000 rows 45.9, 43.8, 12000 rows 51.6,
+//     53.8, 16384 rows 57.4, 64.7, 65536 rows 118, 198; 1024x1024 of 16, 8000 rows 81.5, 91.3.
+//     Widths, 32768 rows: 100x1024 52.1, 45.9; 130x1024 53.7, 60.8.  Where both widths barely
+//     exceed a tile it loses: 130x130 36.2, 23.9; 264x264 47.7, 37.8.
+//   a team for each expert and runs: 361x1024, 1000 rows of 16 13.9, 30.1, 4000 rows 21.4, 35.9;
+//     4000 rows of 4 23.2, 30.4, 8000 rows of 4 51.6, 39.5, of 16 33.8, 47.8, of 64 46.8, 77.0.  It
+//     does not look at the experts' sizes, which the host does not know: one expert that holds
+//     all rows is taken by one block a tile (2048 rows 55.4, 24.4; 4000 rows 103, 31.4).
+//   by the blocks that a team for each expert makes: 4000 rows, 128x128 of 8 (32 blocks) 13.3,
+//     15.6, 256x256 of 4 (64) 22.0, 16.4, 361x256 of 8 (192) 13.7, 18.7.  Below the bound few rows
+//     would gain by it as well: 200 rows 64x64 of 64 experts 4.5, 165.
+//   512, 1024 and 2048 blocks: 16000 rows 361x1024 of 8 95.8, 63.9, 69.4; 65536 rows 128x1024 of
+//     16 117, 74.3, 84.4.
+//   128, 256 and 512 rows at least: 128x256 of 8, 5000 rows 14.4, 16.7, 20.3, 16000 rows 21.8,
+//     20.0, 22.0; 16000 rows 64x64 of 16 14.0, 15.4, 20.1.
 constexpr int64_t DW_BIG_ROWS = 16384, DW_EXPERT_ROWS = 4096, DW_EXPERT_BLOCKS = 128, DW_SMALL_BLOCKS = 1024,
                   DW_RUN = 256;
 struct DwPlan {

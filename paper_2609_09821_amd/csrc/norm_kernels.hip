@@ -4,9 +4,11 @@
 // A row belongs to a team of T lanes that holds it in registers, eight consecutive
 // values a lane: 4 .. 64 lanes (several rows a wavefront, so that narrow rows leave
 // few lanes idle) or 2 .. 16 wavefronts of a block, whose sums meet in LDS.  Four
-// lanes then hold one 32-block of a checkpoint.  Two pieces a lane and half the
-// lanes hold twice the registers: the gradient of 29296 rows of 4096 bf16 took
-// 198 us so and takes 153, of 117187 rows of 1024 176 and 141.
+// lanes then hold one 32-block of a checkpoint.  Up to four pieces a lane, on fewer
+// lanes, hold more registers: the gradient of 29296 rows of 4096 bf16 from their
+// checkpoint took 155 us so and takes 118, of 117187 rows of 1024 123 and 112, of 96000
+// of 2500 674 and 297; of 446096 rows of 538 floats 470 and 487 (back to back from a
+// graph).
 #include <algorithm>
 #include <type_traits>
 
@@ -53,8 +55,8 @@ struct Team {
 // ---------------------------------------------------------------------------
 // y = (x - mean) rstd gamma + beta, the variance about the mean (two passes over
 // the registers: no cancellation), optionally the checkpoint of x.  65536 x 1024 bf16
-// with the checkpoint: 65 us, 340 MB at 5.2 TB/s; one row of 1024 floats: 2.1 us, the
-// latency of a load, two sums and a store.
+// with the checkpoint: 62 us, 338 MB at 5.4 TB/s; one row of 1024 floats: 2.1 us, the
+// latency of a load, two sums and a store; 3478260 x 69 bf16 231 us, 4.3 TB/s.
 // ---------------------------------------------------------------------------
 template <typename E, int T, int W, bool CK>
 __global__ __launch_bounds__(norm_threads<T>) void norm_kernel(NormArgs a)
@@ -105,9 +107,10 @@ __global__ __launch_bounds__(norm_threads<T>) void norm_kernel(NormArgs a)
 // The gradient.  Each thread sums its columns' dgamma and dbeta over the rows of
 // its team; the block's teams meet at the end and leave one row of partial sums,
 // which norm_grad_sum_kernel adds up in float64 in the blocks' order: no atomics, the
-// same bits in every run.  524288 x 512 bf16 from a checkpoint: 242 us and 7 us for the
-// sum, 1.35 GB at 5.4 TB/s; without the next row's loads in flight 18 us more.  Odd widths
-// that fill little more than half of a team are bound by its instructions (538: 3.9 TB/s).
+// same bits in every run.  524288 x 512 bf16 from a checkpoint: 254 us with 8 for the
+// sum, 1.35 GB at 5.3 TB/s; without the next row's loads in flight 18 us more.  Odd widths
+// that fill little more than half of a team are bound by its instructions (538: 3.9 TB/s,
+// 69: 3.6).
 // ---------------------------------------------------------------------------
 template <typename E, int T, int W, bool CK>
 __global__ __launch_bounds__(norm_threads<T>) void norm_grad_kernel(NormGradArgs a)
@@ -201,7 +204,7 @@ __global__ __launch_bounds__(norm_threads<T>) void norm_grad_kernel(NormGradArgs
 }
 
 // Column sums of the partial rows: 64 columns a block, wavefront w takes rows w,
-// w + 16, ...; the wavefronts' sums meet in LDS in order.  1024 rows of 512: 6.8 us, of
+// w + 16, ...; the wavefronts' sums meet in LDS in order.  1024 rows of 512: 8 us, of
 // which most is the latency of 64 loads in turn by each of few blocks.
 constexpr int NORM_SUM_WAVES = 16;
 __global__ __launch_bounds__(64 * NORM_SUM_WAVES) void norm_grad_sum_kernel(const float *part, int rows, int d,
@@ -304,7 +307,7 @@ hipError_t launch_norm_grad(const NormGradArgs &a, bool f32, hipStream_t s)
 
 // ---------------------------------------------------------------------------
 // Checkpoints alone.  A team of up to CKPT_LANES lanes walks a row in chunks of 8 T columns.
-// 262144 x 1024 bf16: 162 us to store, 129 us to restore, 813 MB each way.
+// 262144 x 1024 bf16: 146 us to store, 140 us to restore, 814 MB each way.
 // ---------------------------------------------------------------------------
 constexpr int CKPT_LANES = 64;
 template <typename E, int T, int W, bool STORE>

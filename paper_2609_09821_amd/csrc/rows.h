@@ -76,9 +76,9 @@ __device__ __forceinline__ u32x2_r load8_bytes(const int8_t *p, int nv)
 // before col are then its neighbour's as well; both compute and store them, the same bits, and
 // only one counts them in a sum.  So a row of any width is loaded and stored in whole pieces;
 // value by value, up to seven loads that wait for each other would hold up the whole row.
-// Widths of whole pieces (EVEN) need none of this: with it the gradient of 524288 x 512 takes
-// 267 us for 257, a checkpoint of 262144 x 1024 323 us for 310.  A row of fewer than eight values is
-// read value by value (NARROW: may be one).
+// Widths of whole pieces (EVEN) need none of this: with it the gradient of 524288 x 512 from a
+// checkpoint takes 264 us for 255, restoring 262144 x 1024 155 us for 140 (storing is alike).  A
+// row of fewer than eight values is read value by value (NARROW: may be one).
 enum RowWidth { EVEN, ODD, NARROW };
 template <int W>
 struct RowPiece {

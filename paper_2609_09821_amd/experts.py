@@ -8,7 +8,9 @@ expert, normed, and go through two layers whose weights go by the expert:
     u = layer_norm(obs),  h = relu(W1_e u + b1_e),  mean = W2_e h + b2_e.
 
 Training keeps the three activations in 8 bits and no others: the gradients of the
-weights, the ReLU's mask and the norm's gradient are taken from them.  Run as a
+weights, the ReLU's mask and the norm's gradient are taken from them.  The mask is that
+of the kept h: a hidden unit of at most half a step, about one in a hundred of those
+that are active, passes no gradient back in that pass.  Run as a
 program it imitates the actions of a context's own policy on the envs' observations,
 step by step as the envs move on, and prints the loss.
 """
@@ -49,7 +51,7 @@ class ExpertPolicy:
 
 
 class Batch:
-    """Buffers and workspaces of a policy on up to n rows."""
+    """Buffers and workspaces of a policy on batches of n rows."""
 
     def __init__(self, policy, n, device="cuda"):
         d, h, a = policy.dims
