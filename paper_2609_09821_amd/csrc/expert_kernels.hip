@@ -1294,7 +1294,7 @@ using RowsBigRegs = RowsShape<OP, 2, 2, 2, 2, 32, 2, 2, BY_REGISTERS>;
 constexpr int64_t BIG_TILES = 256, MID_TILES = 150, LOW_TILES = 60;
 // dx beside a weight gradient of 64 x 64 tiles shares its launch below this many: all blocks of
 // the launch are of dx's smallest tiles then.  us of the whole gradient in one launch and in
-// two, 8 experts: 500 rows 361x1024 (22 tiles) 18.2, 21.0; 4000 rows (80) 35.1, 42.5; 8000 rows
+// two, 8 experts: 500 rows 361x1024 (24 tiles) 18.2, 21.0; 4000 rows (80) 35.1, 42.5; 8000 rows
 // (142) 75.1, 71.0; 4000 rows 1024x1024 (160) 74.5, 66.8; 8000 rows 1024x512 (284) 83.4, 71.7;
 // 12000 rows (408) 113, 86; but 16000 rows 256x256 of 16 (142) 35.0, 40.6.  So the bound leaves
 // up to 30% where wide layers have between 140 and 384 tiles, and gains 15% where narrow ones do.
