@@ -163,7 +163,7 @@ im_status im_layer_norm_grad(const im_norm_grad *p, void *stream)
     if (p->n > 0 && (!p->dy || !p->mean || !p->rstd || (!p->x && !p->checkpoint)))
         return invalid("NULL dy, mean, rstd, or neither x nor a checkpoint");
     const bool sums = p->dgamma || p->dbeta;
-    if (!p->dx && !sums) return invalid("no output asked for");
+    if (!p->dx && !sums && p->n > 0) return invalid("no output asked for");
     s = check_workspace(p->workspace, p->workspace_bytes, sums ? im_layer_norm_grad_workspace(p->n, p->d) : 0, 4);
     if (s != IM_OK) return s;
     if (p->n == 0 && !sums) return IM_OK;
@@ -231,7 +231,7 @@ im_status im_expert_linear_grad(const im_expert_layer_grad *p, void *stream)
     im_status s = check_layer(p->n, p->n_experts, p->in, p->out, p->dtype, p->offsets);
     if (s != IM_OK) return s;
     const bool need_x = p->dw || (p->dx && p->relu_x), sums = p->dw || p->db;
-    if (!p->dx && !sums) return invalid("no output asked for");
+    if (!p->dx && !sums && p->n > 0) return invalid("no output asked for");
     if (sums && p->n_experts * ceil_div(p->in, 64) * ceil_div(p->out, 64) >= (1 << 24))
         return unsupported("more than 2^24 tiles of 64 x 64 in all experts' weights");
     if (p->ld_dy < p->out || (p->x && p->ld_x < p->in) || (p->dx && (p->ld_dx < p->in || p->ld_w < p->in)) ||

@@ -99,3 +99,21 @@ def test_a_workspace_of_another_device_is_refused(calls):
         assert not used
         call(workspace=torch.zeros(1 << 20, dtype=torch.uint8))
         used.clear()
+
+
+def test_calls_on_no_rows(monkeypatch):
+    """An empty batch is done, whichever of the rows' outputs is asked for."""
+    im.lib()
+    monkeypatch.setattr(im, "_torch", torch)
+    monkeypatch.setattr(im, "_call_stream", lambda stream: (-1, 0))
+    x, y = (torch.zeros(0, d, dtype=torch.bfloat16) for d in (24, 40))
+    w, off = torch.zeros(4, 40, 24, dtype=torch.bfloat16), torch.zeros(5, dtype=torch.int32)
+    stat, ck = torch.zeros(0), im.Checkpoint.empty(0, 24, "cpu")
+    im.checkpoint_store(x, ck)
+    im.checkpoint_load(ck, x)
+    im.layer_norm(x, None, None, x, stat, stat, checkpoint=ck)
+    im.expert_linear(x, w, None, off, None, y)
+    for src in (x, ck):
+        im.layer_norm_grad(x, src, None, stat, stat, dx=x)
+        im.expert_linear_grad(y, src, w, off, None, dx=x)
+        im.expert_linear_grad(y, src, w, off, off[:0], dx=x, relu_x=True)
