@@ -703,6 +703,222 @@ typedef struct {
 int64_t im_expert_linear_grad_workspace(int64_t n, int32_t n_experts, int32_t in, int32_t out);
 im_status im_expert_linear_grad(const im_expert_layer_grad *a, void *stream);
 
+/*
+ * Blocks of a recurrent policy.  A policy that remembers has blocks of a
+ * root-mean-square norm of the residual stream, products in 8-bit floating
+ * point and a gated linear recurrence over the rollout's steps.  What is said
+ * above of the layers of experts (memory, workspaces, streams, graphs, strides,
+ * fixed sums, overlaps) holds for these calls too.
+ */
+
+/*
+ * A matrix [n][d] in 8-bit floating point.  A block of 128 consecutive values of a
+ * row (the last one of a row may be shorter), or of 128 rows x 128 columns, shares a
+ * power of two: value = q 2^(scale - 127), q in e4m3 (4 exponent bits, 3 of the
+ * mantissa, at most 448).  The scale is the least that takes the block's largest
+ * magnitude to at most 448 (0, the smallest, if any would), and q is rounded to
+ * nearest even: off by at most 1/16 of the value, or 2^-10 2^(scale - 127) where that
+ * is more.  A block that holds a NaN or an infinity has scale 255, is NaN throughout
+ * when restored and makes every sum of a product NaN that it enters; a block of zeros
+ * has scale 0 and q 0.  Restored values are exact in fp32, and in bf16 from scale 3 on.
+ *   q [n][ld_q] e4m3 bytes: 16-byte aligned, ld_q a multiple of 16 and at least
+ *     IM_BLOCK8_PAD(d) = d rounded up to whole blocks; the columns from d on hold zeros
+ *     (the calls that write q write them)
+ *   scale [ceil(n / rows)][ld_scale] uint8, ld_scale >= ceil(d / 128)
+ *   rows: 1, or 128 for square blocks (weights: their transpose has the same blocks)
+ */
+#define IM_BLOCK8 128
+#define IM_BLOCK8_PAD(d) (((int64_t)(d) + IM_BLOCK8 - 1) / IM_BLOCK8 * IM_BLOCK8)
+typedef struct {
+    uint8_t *q, *scale;
+    int64_t ld_q, ld_scale;
+    int32_t rows;
+} im_block8;
+
+/*
+ * x [n][d] (float, or bf16 bit patterns: dtype) in 8 bits: as it lies into c, and
+ * transposed into t (a matrix [d][n], its blocks along x's columns), from one read;
+ * either may be NULL.  Where both are given they have the same `rows`.  im_block_load
+ * restores c's values.  n <= 2^30, d <= 2^20 (IM_ERR_UNSUPPORTED above).
+ */
+im_status im_block_store(const void *x, int64_t ld_x, int32_t dtype, int64_t n, int64_t d,
+                          const im_block8 *c, const im_block8 *t, void *stream);
+im_status im_block_load(const im_block8 *c, int64_t n, int64_t d, void *x, int64_t ld_x,
+                         int32_t dtype, void *stream);
+
+/*
+ * Root-mean-square norm over the rows of h = x + residual (residual NULL: of x):
+ * rstd = 1 / sqrt(sum h^2 / d + eps), y = h rstd gamma, in fp32 and of the sum before
+ * it is rounded; x, residual, h, y of `dtype`.  gamma [d] float (NULL: 1).  Outputs,
+ * each may be NULL (not wanted): h (h and y may be x or residual), y, y8 (y in 8 bits,
+ * of the values before their rounding to dtype; rows 1), rstd [n] float.
+ * 0 <= n, 1 <= d <= IM_NORM_MAX_WIDTH (IM_ERR_UNSUPPORTED above), eps >= 0.
+ */
+typedef struct {
+    int64_t n, d;
+    int32_t dtype;
+    float eps;
+    const void *x;
+    int64_t ld_x;
+    const void *residual;
+    int64_t ld_residual;
+    const float *gamma;
+    void *h;
+    int64_t ld_h;
+    void *y;
+    int64_t ld_y;
+    const im_block8 *y8;
+    float *rstd;
+} im_rms;
+im_status im_rms_norm(const im_rms *a, void *stream);
+
+/*
+ * Its gradient, with the forward's h and rstd: u = h rstd, g = dy gamma,
+ *   dx = dh + rstd (g - u sum (g u) / d),  dgamma = sum_rows dy u,
+ * dh the gradient that reaches h past the norm (NULL: none); dx is the gradient of x
+ * and of the residual alike.  dy, h, dh, dx of `dtype`; dx may be dy, h or dh (or
+ * NULL: not wanted); dgamma [d] float (NULL: not wanted), overwritten (zero for n = 0).
+ * workspace: im_rms_norm_grad_workspace(n, d) bytes, 4-byte aligned (not needed
+ * without dgamma).
+ */
+typedef struct {
+    int64_t n, d;
+    int32_t dtype;
+    const void *dy;
+    int64_t ld_dy;
+    const void *h;
+    int64_t ld_h;
+    const void *dh;
+    int64_t ld_dh;
+    const float *gamma, *rstd;
+    void *dx;
+    int64_t ld_dx;
+    float *dgamma;
+    void *workspace;
+    int64_t workspace_bytes;
+} im_rms_grad;
+int64_t im_rms_norm_grad_workspace(int64_t n, int64_t d);
+im_status im_rms_norm_grad(const im_rms_grad *a, void *stream);
+
+/*
+ * Linear layer in 8 bits: y = x w^T + bias (then max(., 0) with relu; NaN stays), x
+ * [n][in] and w [out][in] in 8 bits, each with blocks of either kind, bias [out] float
+ * or NULL.  One rounding at the end: to y [n][out] of y_dtype, and to y8 [n][out] in 8
+ * bits (rows 1), of the values before y's rounding; either may be NULL.  The restored
+ * values' products are exact and summed in fp32; values below 2^-126, and products whose
+ * scales' product is, may count as 0.  Where y in bf16 is the only output, the matrix
+ * cores add eight products of neighbouring k at a time to a unit of 2^-13 of the largest
+ * one's power of two before the fp32 sum: that is 1.4e-5 of the norm of sums of normal
+ * values, a hundredth of bf16's rounding, and at most 2^-10 of the sum of magnitudes.
+ * n <= 2^30, in and out <= 2^20 (IM_ERR_UNSUPPORTED above).
+ */
+typedef struct {
+    int64_t n, in, out;
+    int32_t y_dtype, relu;
+    const im_block8 *x, *w;
+    const float *bias;
+    void *y;
+    int64_t ld_y;
+    const im_block8 *y8;
+} im_layer8;
+im_status im_block_linear(const im_layer8 *a, void *stream);
+
+/*
+ * Its gradients for dy [n][out] of `dtype`.  With y (NULL: no ReLU), the layer's output
+ * of the same dtype, dy counts as zero where not y > 0.  dy is then stored in 8 bits, in
+ * blocks along its rows for dx and along its columns for dw:
+ *   dx = dy w  [n][in] of `dtype`;  dw = dy^T x  float [out][in];
+ *   db = sum_rows dy  float [out] (of dy itself)
+ * wt: w^T [in][out] and xt: x^T [in][n] in 8 bits, as im_block_store's t (needed for dx
+ * and dw).  dx in bf16 is summed as im_block_linear's y in bf16 is, dw in fp32 throughout.
+ * dx, dw and db may each be NULL: not wanted; dw and db are zero for n = 0.
+ * workspace: im_block_linear_grad_workspace(...) bytes, 16-byte aligned.
+ */
+typedef struct {
+    int64_t n, in, out;
+    int32_t dtype;
+    const void *dy;
+    int64_t ld_dy;
+    const void *y;
+    int64_t ld_y;
+    const im_block8 *xt, *wt;
+    void *dx;
+    int64_t ld_dx;
+    float *dw;
+    int64_t ld_dw;
+    float *db;
+    void *workspace;
+    int64_t workspace_bytes;
+} im_layer8_grad;
+int64_t im_block_linear_grad_workspace(int64_t n, int64_t in, int64_t out);
+im_status im_block_linear_grad(const im_layer8_grad *a, void *stream);
+
+/*
+ * Gated linear recurrence of n envs over T steps, each of d values by itself:
+ *   a_t = 1 / (1 + exp(-gate_t)),  h_t = a_t c_(t-1) + (1 - a_t) x_t,
+ *   c_t = h_t, or 0 where the env's episode ends with step t (terminated or truncated:
+ *         uint8 [T][ld_flags] as the rollout stores them, each may be NULL: none),
+ * from c_(-1) = state (float [n][d], NULL: 0).  gate, x, h: [T][n][d] of `dtype` with
+ * strides of a step (st_) and of a row (ld_) in elements, in either order; a row's values
+ * lie together.  state_out (float [n][d], NULL: not wanted; may be state) = c_(T-1); with
+ * T = 1 the call is one step of a rollout.  keep (float [ceil(T / IM_SCAN_KEEP)][n][d],
+ * NULL: not wanted): c before the steps 0, IM_SCAN_KEEP, .., for the gradient.  The sums
+ * and the state are fp32.  0 <= T, n <= 2^30, 1 <= d, n d <= 2^31 (IM_ERR_UNSUPPORTED
+ * above).
+ * workspace: im_gated_scan_workspace(T, n, d) bytes, 16-byte aligned (0 where the steps of
+ * all envs are walked one after the other).
+ */
+#define IM_SCAN_KEEP 16
+typedef struct {
+    int64_t T, n, d;
+    int32_t dtype;
+    const void *gate;
+    int64_t st_gate, ld_gate;
+    const void *x;
+    int64_t st_x, ld_x;
+    const uint8_t *terminated, *truncated;
+    int64_t ld_flags;
+    const float *state;
+    void *h;
+    int64_t st_h, ld_h;
+    float *state_out, *keep;
+    void *workspace;
+    int64_t workspace_bytes;
+} im_scan;
+int64_t im_gated_scan_workspace(int64_t T, int64_t n, int64_t d);
+im_status im_gated_scan(const im_scan *a, void *stream);
+
+/*
+ * Its gradients, from keep (c at the other steps is formed again): with G_t = dh_t +
+ * (0 where the episode ends with t, else a_(t+1) G_(t+1); dstate after the last step)
+ *   dx_t = (1 - a_t) G_t,  dgate_t = a_t (1 - a_t) (c_(t-1) - x_t) G_t  (of `dtype`),
+ *   dstate_out = a_0 G_0: the gradient of state (float [n][d], NULL: not wanted; for T = 0
+ *   it is dstate).
+ * dstate: the gradient of state_out (float [n][d], NULL: 0; dstate_out may be it).
+ * workspace: as the forward's.
+ */
+typedef struct {
+    int64_t T, n, d;
+    int32_t dtype;
+    const void *dh;
+    int64_t st_dh, ld_dh;
+    const void *gate;
+    int64_t st_gate, ld_gate;
+    const void *x;
+    int64_t st_x, ld_x;
+    const uint8_t *terminated, *truncated;
+    int64_t ld_flags;
+    const float *keep, *dstate;
+    void *dgate;
+    int64_t st_dgate, ld_dgate;
+    void *dx;
+    int64_t st_dx, ld_dx;
+    float *dstate_out;
+    void *workspace;
+    int64_t workspace_bytes;
+} im_scan_grad;
+im_status im_gated_scan_grad(const im_scan_grad *a, void *stream);
+
 const char *im_status_str(im_status s);
 const char *im_last_error(void);
 

@@ -22,6 +22,7 @@ IM_OK, IM_ERR_INVALID_ARG, IM_ERR_UNSUPPORTED, IM_ERR_OOM, IM_ERR_HIP = range(5)
 IM_DTYPE_F32, IM_DTYPE_BF16 = 0, 1
 IM_GAE_NOALLOC_MAX_ENVS = 1 << 20   # im_gae_noalloc scratch limit
 IM_JOINT_FREE, IM_JOINT_SPHERICAL, IM_JOINT_REVOLUTE, IM_JOINT_FIXED = range(4)
+IM_BLOCK8, IM_SCAN_KEEP = 128, 16
 IM_SPLIT_AUTO, IM_SPLIT_ONE, IM_SPLIT_HALVES, IM_SPLIT_PATHS = range(4)
 
 
@@ -138,6 +139,64 @@ class ImExpertLayerGrad(C.Structure):
                 ("workspace_bytes", C.c_int64)]
 
 
+class ImBlock8(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("scale", C.c_void_p), ("ld_q", C.c_int64),
+                ("ld_scale", C.c_int64), ("rows", C.c_int32)]
+
+
+class ImRms(C.Structure):
+    _fields_ = [("n", C.c_int64), ("d", C.c_int64), ("dtype", C.c_int32), ("eps", C.c_float),
+                ("x", C.c_void_p), ("ld_x", C.c_int64), ("residual", C.c_void_p),
+                ("ld_residual", C.c_int64), ("gamma", C.c_void_p), ("h", C.c_void_p),
+                ("ld_h", C.c_int64), ("y", C.c_void_p), ("ld_y", C.c_int64),
+                ("y8", C.POINTER(ImBlock8)), ("rstd", C.c_void_p)]
+
+
+class ImRmsGrad(C.Structure):
+    _fields_ = [("n", C.c_int64), ("d", C.c_int64), ("dtype", C.c_int32), ("dy", C.c_void_p),
+                ("ld_dy", C.c_int64), ("h", C.c_void_p), ("ld_h", C.c_int64), ("dh", C.c_void_p),
+                ("ld_dh", C.c_int64), ("gamma", C.c_void_p), ("rstd", C.c_void_p),
+                ("dx", C.c_void_p), ("ld_dx", C.c_int64), ("dgamma", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
+
+
+class ImLayer8(C.Structure):
+    _fields_ = [("n", C.c_int64), ("in_", C.c_int64), ("out", C.c_int64), ("y_dtype", C.c_int32),
+                ("relu", C.c_int32), ("x", C.POINTER(ImBlock8)), ("w", C.POINTER(ImBlock8)),
+                ("bias", C.c_void_p), ("y", C.c_void_p), ("ld_y", C.c_int64),
+                ("y8", C.POINTER(ImBlock8))]
+
+
+class ImLayer8Grad(C.Structure):
+    _fields_ = [("n", C.c_int64), ("in_", C.c_int64), ("out", C.c_int64), ("dtype", C.c_int32),
+                ("dy", C.c_void_p), ("ld_dy", C.c_int64), ("y", C.c_void_p), ("ld_y", C.c_int64),
+                ("xt", C.POINTER(ImBlock8)), ("wt", C.POINTER(ImBlock8)), ("dx", C.c_void_p),
+                ("ld_dx", C.c_int64), ("dw", C.c_void_p), ("ld_dw", C.c_int64), ("db", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
+
+
+class ImScan(C.Structure):
+    _fields_ = [("T", C.c_int64), ("n", C.c_int64), ("d", C.c_int64), ("dtype", C.c_int32),
+                ("gate", C.c_void_p), ("st_gate", C.c_int64), ("ld_gate", C.c_int64),
+                ("x", C.c_void_p), ("st_x", C.c_int64), ("ld_x", C.c_int64),
+                ("terminated", C.c_void_p), ("truncated", C.c_void_p), ("ld_flags", C.c_int64),
+                ("state", C.c_void_p), ("h", C.c_void_p), ("st_h", C.c_int64), ("ld_h", C.c_int64),
+                ("state_out", C.c_void_p), ("keep", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_int64)]
+
+
+class ImScanGrad(C.Structure):
+    _fields_ = [("T", C.c_int64), ("n", C.c_int64), ("d", C.c_int64), ("dtype", C.c_int32),
+                ("dh", C.c_void_p), ("st_dh", C.c_int64), ("ld_dh", C.c_int64),
+                ("gate", C.c_void_p), ("st_gate", C.c_int64), ("ld_gate", C.c_int64),
+                ("x", C.c_void_p), ("st_x", C.c_int64), ("ld_x", C.c_int64),
+                ("terminated", C.c_void_p), ("truncated", C.c_void_p), ("ld_flags", C.c_int64),
+                ("keep", C.c_void_p), ("dstate", C.c_void_p), ("dgate", C.c_void_p),
+                ("st_dgate", C.c_int64), ("ld_dgate", C.c_int64), ("dx", C.c_void_p),
+                ("st_dx", C.c_int64), ("ld_dx", C.c_int64), ("dstate_out", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
+
+
 class ImInfo(C.Structure):
     _fields_ = [("n_bodies", C.c_int32), ("obs_dim", C.c_int32), ("action_dim", C.c_int32),
                 ("n_clips", C.c_int32), ("n_layers", C.c_int32), ("policy_dtype", C.c_int32),
@@ -151,7 +210,10 @@ EXPORTED = ["im_create", "im_destroy", "im_get_info", "im_env_step_fused", "im_p
             "im_ppo_read", "im_group_rows_workspace", "im_group_rows", "im_checkpoint_store",
             "im_checkpoint_load", "im_layer_norm", "im_layer_norm_grad_workspace",
             "im_layer_norm_grad", "im_expert_linear", "im_expert_linear_grad_workspace",
-            "im_expert_linear_grad", "im_status_str", "im_last_error"]
+            "im_expert_linear_grad", "im_block_store", "im_block_load", "im_rms_norm",
+            "im_rms_norm_grad_workspace", "im_rms_norm_grad", "im_block_linear",
+            "im_block_linear_grad_workspace", "im_block_linear_grad", "im_gated_scan_workspace",
+            "im_gated_scan", "im_gated_scan_grad", "im_status_str", "im_last_error"]
 # measurement probes of the GPU (include/instantmimic_calib.h), not the method
 CALIB_EXPORTED = ["im_calib_mfma", "im_calib_lds", "im_calib_read"]
 IM_CALIB_MFMA_BF16, IM_CALIB_MFMA_F32 = 0, 1
@@ -232,6 +294,30 @@ def lib():
     L.im_expert_linear_grad_workspace.restype = C.c_int64
     L.im_expert_linear_grad.argtypes = [C.POINTER(ImExpertLayerGrad), C.c_void_p]
     L.im_expert_linear_grad.restype = st
+    L.im_block_store.argtypes = [C.c_void_p, C.c_int64, C.c_int32, C.c_int64, C.c_int64,
+                                  C.POINTER(ImBlock8), C.POINTER(ImBlock8), C.c_void_p]
+    L.im_block_store.restype = st
+    L.im_block_load.argtypes = [C.POINTER(ImBlock8), C.c_int64, C.c_int64, C.c_void_p, C.c_int64,
+                                 C.c_int32, C.c_void_p]
+    L.im_block_load.restype = st
+    L.im_rms_norm.argtypes = [C.POINTER(ImRms), C.c_void_p]
+    L.im_rms_norm.restype = st
+    L.im_rms_norm_grad_workspace.argtypes = [C.c_int64, C.c_int64]
+    L.im_rms_norm_grad_workspace.restype = C.c_int64
+    L.im_rms_norm_grad.argtypes = [C.POINTER(ImRmsGrad), C.c_void_p]
+    L.im_rms_norm_grad.restype = st
+    L.im_block_linear.argtypes = [C.POINTER(ImLayer8), C.c_void_p]
+    L.im_block_linear.restype = st
+    L.im_block_linear_grad_workspace.argtypes = [C.c_int64, C.c_int64, C.c_int64]
+    L.im_block_linear_grad_workspace.restype = C.c_int64
+    L.im_block_linear_grad.argtypes = [C.POINTER(ImLayer8Grad), C.c_void_p]
+    L.im_block_linear_grad.restype = st
+    L.im_gated_scan_workspace.argtypes = [C.c_int64, C.c_int64, C.c_int64]
+    L.im_gated_scan_workspace.restype = C.c_int64
+    L.im_gated_scan.argtypes = [C.POINTER(ImScan), C.c_void_p]
+    L.im_gated_scan.restype = st
+    L.im_gated_scan_grad.argtypes = [C.POINTER(ImScanGrad), C.c_void_p]
+    L.im_gated_scan_grad.restype = st
     L.im_status_str.argtypes = [C.c_int]
     L.im_status_str.restype = C.c_char_p
     L.im_last_error.argtypes = []
@@ -387,6 +473,38 @@ def im_expert_linear(args, stream=None):
 
 def im_expert_linear_grad(args, stream=None):
     _check(lib().im_expert_linear_grad(C.byref(args), stream))
+
+
+def im_block_store(x_ptr, ld_x, dtype, n, d, c, t, stream=None):
+    _check(lib().im_block_store(x_ptr, ld_x, dtype, n, d, c, t, stream))
+
+
+def im_block_load(c, n, d, x_ptr, ld_x, dtype, stream=None):
+    _check(lib().im_block_load(c, n, d, x_ptr, ld_x, dtype, stream))
+
+
+def im_rms_norm(args, stream=None):
+    _check(lib().im_rms_norm(C.byref(args), stream))
+
+
+def im_rms_norm_grad(args, stream=None):
+    _check(lib().im_rms_norm_grad(C.byref(args), stream))
+
+
+def im_block_linear(args, stream=None):
+    _check(lib().im_block_linear(C.byref(args), stream))
+
+
+def im_block_linear_grad(args, stream=None):
+    _check(lib().im_block_linear_grad(C.byref(args), stream))
+
+
+def im_gated_scan(args, stream=None):
+    _check(lib().im_gated_scan(C.byref(args), stream))
+
+
+def im_gated_scan_grad(args, stream=None):
+    _check(lib().im_gated_scan_grad(C.byref(args), stream))
 
 
 # ------------------------------------------------------------- conveniences
@@ -913,3 +1031,228 @@ def expert_linear_grad(dy, x, w, offsets, rows, dx=None, dw=None, db=None, relu_
                           0 if dx is None else _ld(dx, n, in_, "dx", dev, bf16), _dptr(dw),
                           0 if dw is None else _expert_ld(dw, e, out, in_, "dw", dev, f32),
                           _vec(db, e * out, "db", dev, f32), ws, nbytes), raw)
+
+
+# ------------------------------------------------- blocks of a recurrent policy
+class Block8:
+    """A matrix [n][d] in 8 bits: q float8_e4m3fn [n][d rounded up to 128] (columns from d
+    on zero) and scale uint8 [ceil(n / rows)][ceil(d / 128)] tensors; rows 1, or 128 for
+    square blocks.  Rows may be strided, q's by multiples of 16."""
+
+    def __init__(self, q, scale, d, rows=1):
+        self.q, self.scale, self.d, self.rows = q, scale, d, rows
+
+    @classmethod
+    def empty(cls, n, d, rows=1, device="cuda"):
+        import torch
+        blocks = -(-d // IM_BLOCK8)
+        return cls(torch.zeros((n, blocks * IM_BLOCK8), dtype=torch.float8_e4m3fn, device=device),
+                   torch.zeros((-(-n // rows), blocks), dtype=torch.uint8, device=device), d, rows)
+
+    @property
+    def shape(self):
+        return self.q.shape[0], self.d
+
+    def struct(self, n, d, dev, name):
+        if self.d != d:
+            raise ValueError("%s holds rows of %d values, not of %d" % (name, self.d, d))
+        if self.rows != 1 and self.rows != IM_BLOCK8:
+            raise ValueError("%s: rows must be 1 or 128" % name)
+        blocks = -(-d // IM_BLOCK8)
+        return ImBlock8(self.q.data_ptr(), self.scale.data_ptr(),
+                        _ld(self.q, n, blocks * IM_BLOCK8, name + ".q", dev, _torch.float8_e4m3fn),
+                        _ld(self.scale, -(-n // self.rows), blocks, name + ".scale", dev,
+                            _torch.uint8), self.rows)
+
+
+def _block8(b, n, d, dev, name):
+    return None if b is None else C.pointer(b.struct(n, d, dev, name))
+
+
+def block8_store(x, c=None, t=None, stream=None):
+    """x (float32 or bfloat16 [n][d]) in 8 bits: as it lies into the Block8 c, transposed
+    into the Block8 t (of [d][n]); either may be None."""
+    dev, raw = _call_stream(stream)
+    n, d = x.shape
+    im_block_store(x.data_ptr(), _ld(x, n, d, "x", dev), _dtype(x), n, d,
+                    _block8(c, n, d, dev, "c"), _block8(t, d, n, dev, "t"), raw)
+
+
+def block8_load(c, x, stream=None):
+    """The Block8's values into x (float32 or bfloat16 [n][d])."""
+    dev, raw = _call_stream(stream)
+    n, d = x.shape
+    im_block_load(_block8(c, n, d, dev, "c"), n, d, x.data_ptr(), _ld(x, n, d, "x", dev),
+                   _dtype(x), raw)
+
+
+def _opt(t, n, d, name, dev, dtype):
+    """Pointer and row stride of a matrix that may be None."""
+    return (None, 0) if t is None else (t.data_ptr(), _ld(t, n, d, name, dev, dtype))
+
+
+def rms_norm(x, gamma, y=None, rstd=None, eps=1e-6, residual=None, h=None, y8=None, stream=None):
+    """Root-mean-square norm of the rows of h = x + residual ([n][d], float32 or bfloat16):
+    y = h / sqrt(mean h^2 + eps) gamma, each output if it is given: the sum h, y, y in 8 bits
+    (the Block8 y8), the row statistic rstd [n]."""
+    dev, raw = _call_stream(stream)
+    n, d = x.shape
+    f32 = _torch.float32
+    im_rms_norm(ImRms(n, d, _dtype(x), eps, x.data_ptr(), _ld(x, n, d, "x", dev),
+                      *_opt(residual, n, d, "residual", dev, x.dtype),
+                      _vec(gamma, d, "gamma", dev, f32), *_opt(h, n, d, "h", dev, x.dtype),
+                      *_opt(y, n, d, "y", dev, x.dtype), _block8(y8, n, d, dev, "y8"),
+                      _vec(rstd, n, "rstd", dev, f32)), raw)
+
+
+def rms_norm_grad_workspace(n, d):
+    """A workspace tensor for rms_norm_grad."""
+    return _space(lib().im_rms_norm_grad_workspace(n, d))
+
+
+def rms_norm_grad(dy, h, gamma, rstd, dx=None, dgamma=None, dh=None, workspace=None, stream=None):
+    """Gradient of rms_norm from its h (x, where nothing was added) and rstd; dh: the gradient
+    that reaches h past the norm, added to dx."""
+    dev, raw = _call_stream(stream)
+    n, d = dy.shape
+    f32 = _torch.float32
+    ws, nbytes = None, 0
+    if dgamma is not None:
+        _held, ws, nbytes = _workspace(workspace, lambda: rms_norm_grad_workspace(n, d), dev, stream)
+    im_rms_norm_grad(
+        ImRmsGrad(n, d, _dtype(dy), dy.data_ptr(), _ld(dy, n, d, "dy", dev), h.data_ptr(),
+                  _ld(h, n, d, "h", dev, dy.dtype), *_opt(dh, n, d, "dh", dev, dy.dtype),
+                  _vec(gamma, d, "gamma", dev, f32), _vec(rstd, n, "rstd", dev, f32),
+                  *_opt(dx, n, d, "dx", dev, dy.dtype), _vec(dgamma, d, "dgamma", dev, f32),
+                  ws, nbytes), raw)
+
+
+def linear8(x, w, bias, y=None, y8=None, relu=False, stream=None):
+    """y = x w^T + bias (ReLU with relu) of the Block8s x [n][in] and w [out][in]; bias [out]
+    float32 or None; y [n][out] float32 or bfloat16, and the Block8 y8: each if it is given."""
+    dev, raw = _call_stream(stream)
+    (n, in_), out = x.shape, w.shape[0]
+    yp, ldy = (None, 0) if y is None else (y.data_ptr(), _ld(y, n, out, "y", dev))
+    im_block_linear(ImLayer8(n, in_, out, IM_DTYPE_BF16 if y is None else _dtype(y), 1 if relu else 0,
+                        _block8(x, n, in_, dev, "x"), _block8(w, out, in_, dev, "w"),
+                        _vec(bias, out, "bias", dev, _torch.float32), yp, ldy,
+                        _block8(y8, n, out, dev, "y8")), raw)
+
+
+def linear8_grad_workspace(n, in_, out):
+    """A workspace tensor for linear8_grad."""
+    return _space(lib().im_block_linear_grad_workspace(n, in_, out))
+
+
+def linear8_grad(dy, xt, wt, dx=None, dw=None, db=None, y=None, workspace=None, stream=None):
+    """Gradients of linear8 for dy [n][out] (float32 or bfloat16): dx [n][in] of dy's type, dw
+    [out][in] and db [out] float32 (each may be None).  xt, wt: the Block8s of the transposed
+    input [in][n] (None without dw) and weights [in][out] (None without dx); y: the layer's
+    output where it had a ReLU."""
+    dev, raw = _call_stream(stream)
+    n, out = dy.shape
+    if dx is not None:
+        in_ = dx.shape[1]
+    elif dw is not None:
+        in_ = dw.shape[1]
+    else:
+        in_ = 1
+    f32 = _torch.float32
+    ws, nbytes = None, 0
+    if n:
+        _held, ws, nbytes = _workspace(workspace, lambda: linear8_grad_workspace(n, in_, out), dev,
+                                       stream)
+    im_block_linear_grad(
+        ImLayer8Grad(n, in_, out, _dtype(dy), dy.data_ptr(), _ld(dy, n, out, "dy", dev),
+                     *_opt(y, n, out, "y", dev, dy.dtype),
+                     None if dw is None else _block8(xt, in_, n, dev, "xt"),
+                     None if dx is None else _block8(wt, in_, out, dev, "wt"),
+                     *_opt(dx, n, in_, "dx", dev, dy.dtype), *_opt(dw, out, in_, "dw", dev, f32),
+                     _vec(db, out, "db", dev, f32), ws, nbytes), raw)
+
+
+def _strides(t, T, n, d, name, dev, dtype):
+    """Strides of a step and of a row of an argument [T][n][d]."""
+    if tuple(t.shape) != (T, n, d) or t.dtype is not dtype or t.get_device() != dev:
+        raise ValueError("%s must be [%d][%d][%d] of %s on the current device, got %s %s" % (
+            name, T, n, d, dtype, list(t.shape), t.dtype))
+    st, ld, one = t.stride()
+    if one != 1 and d > 1:
+        raise ValueError("%s: the values of a row must lie together" % name)
+    return st if T > 1 else 0, ld if n > 1 else 0
+
+
+def _flags(terminated, truncated, T, n, dev):
+    """Pointers of the two flags [T][n] (uint8 or bool; either None) and their row stride."""
+    out, ld = [], None
+    for t, name in ((terminated, "terminated"), (truncated, "truncated")):
+        if t is None:
+            out.append(None)
+            continue
+        if t.dtype is not _torch.uint8 and t.dtype is not _torch.bool:
+            raise ValueError("%s must be uint8 or bool, got %s" % (name, t.dtype))
+        k = _ld(t, T, n, name, dev)
+        if ld is not None and k != ld:
+            raise ValueError("terminated and truncated must have the same row stride")
+        ld = k
+        out.append(t.data_ptr())
+    return out[0], out[1], ld or 0
+
+
+def _state(t, n, d, name, dev):
+    if t is not None and t.shape[-2:] != (n, d):
+        raise ValueError("%s must be [%d][%d], got %s" % (name, n, d, list(t.shape)))
+    return _vec(t, n * d, name, dev, _torch.float32)
+
+
+def gated_scan_workspace(T, n, d):
+    """A workspace tensor for gated_scan and gated_scan_grad."""
+    return _space(lib().im_gated_scan_workspace(T, n, d))
+
+
+def gated_scan(gate, x, h, state=None, state_out=None, keep=None, terminated=None, truncated=None,
+               workspace=None, stream=None):
+    """h_t = a_t c_(t-1) + (1 - a_t) x_t with a = sigmoid(gate) over the steps of gate, x, h
+    ([T][n][d], float32 or bfloat16), c_t = h_t or, where an env's episode ends with step t
+    (terminated or truncated [T][n]), 0; from c_(-1) = state [n][d] float32 (None: 0) to
+    state_out [n][d] (may be state).  keep: float32 [ceil(T / 16)][n][d], the states that
+    gated_scan_grad starts from.  T = 1: one step of a rollout."""
+    dev, raw = _call_stream(stream)
+    T, n, d = x.shape
+    dt = x.dtype
+    need = lib().im_gated_scan_workspace(T, n, d)
+    ws, nbytes = None, 0
+    if need:
+        _held, ws, nbytes = _workspace(workspace, lambda: _space(need), dev, stream)
+    im_gated_scan(
+        ImScan(T, n, d, _dtype(x), gate.data_ptr(), *_strides(gate, T, n, d, "gate", dev, dt),
+               x.data_ptr(), *_strides(x, T, n, d, "x", dev, dt),
+               *_flags(terminated, truncated, T, n, dev), _state(state, n, d, "state", dev),
+               h.data_ptr(), *_strides(h, T, n, d, "h", dev, dt),
+               _state(state_out, n, d, "state_out", dev),
+               _vec(keep, -(-T // IM_SCAN_KEEP) * n * d, "keep", dev, _torch.float32), ws, nbytes),
+        raw)
+
+
+def gated_scan_grad(dh, gate, x, keep, dgate, dx, dstate=None, dstate_out=None, terminated=None,
+                    truncated=None, workspace=None, stream=None):
+    """Gradients of gated_scan from the states that it kept: dgate, dx ([T][n][d] of dh's type)
+    and dstate_out [n][d] float32 (None: not wanted), the gradient of its state; dstate: the
+    gradient of its state_out (None: 0)."""
+    dev, raw = _call_stream(stream)
+    T, n, d = dh.shape
+    dt = dh.dtype
+    need = lib().im_gated_scan_workspace(T, n, d)
+    ws, nbytes = None, 0
+    if need:
+        _held, ws, nbytes = _workspace(workspace, lambda: _space(need), dev, stream)
+    im_gated_scan_grad(
+        ImScanGrad(T, n, d, _dtype(dh), dh.data_ptr(), *_strides(dh, T, n, d, "dh", dev, dt),
+                   gate.data_ptr(), *_strides(gate, T, n, d, "gate", dev, dt),
+                   x.data_ptr(), *_strides(x, T, n, d, "x", dev, dt),
+                   *_flags(terminated, truncated, T, n, dev),
+                   _vec(keep, -(-T // IM_SCAN_KEEP) * n * d, "keep", dev, _torch.float32),
+                   _state(dstate, n, d, "dstate", dev), dgate.data_ptr(),
+                   *_strides(dgate, T, n, d, "dgate", dev, dt), dx.data_ptr(),
+                   *_strides(dx, T, n, d, "dx", dev, dt),
+                   _state(dstate_out, n, d, "dstate_out", dev), ws, nbytes), raw)

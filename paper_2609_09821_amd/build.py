@@ -18,7 +18,8 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libinstantmimic.so")
 SOURCES = ["api.hip", "env_kernels.hip", "policy_kernels.hip", "layer_kernels.hip",
            "rollout_kernels.hip", "train_kernels.hip", "calib_kernels.hip", "expert_kernels.hip",
-           "norm_kernels.hip", "expert_api.hip"]
+           "norm_kernels.hip", "expert_api.hip", "block8_kernels.hip", "linear8_kernels.hip",
+           "rms_kernels.hip", "scan_kernels.hip", "recurrent_api.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

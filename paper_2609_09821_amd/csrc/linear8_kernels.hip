@@ -1,0 +1,364 @@
+// linear8_kernels.hip -- products of matrices in 8 bits on MFMA: C[q][p] = sum_k Q[q][k] P[p][k].
+//   forward  q = row,    p = output, k = input    Q = x, P = w
+//   dx       q = row,    p = input,  k = output   Q = dy, P = w^T
+//   dw       q = output, p = input,  k = row      Q = dy^T, P = x^T
+// All three read both operands along k, in whole blocks of 128 (rows are padded with
+// zeros).  MFMA accumulators give a lane one q and four consecutive p per register group.
+//
+// Outputs in bf16: v_mfma_scale_f32_32x32x64_f8f6f4, which multiplies each operand's
+// row by its own power of two, so that scales cost no instruction besides their load.  It adds
+// the products of eight neighbouring k to 14 bits from the largest one's exponent down, and only
+// these sums in fp32 (found by adding one small product to a large one; v_mfma_f32_32x32x16_fp8_fp8
+// gives the same bits): sums of normal values are off by 1.4e-5 of their norm, a hundredth of
+// what an output in bf16 loses.  Outputs in fp32 would lose by it, and in 8 bits values next to the
+// middle of two steps would go to the other one (8.9e-4 of the norm): there the bytes become bf16
+// with their block's scale (exact) and are multiplied by v_mfma_f32_32x32x16_bf16, at half the rate.
+#include <algorithm>
+#include <type_traits>
+
+#include "block8.h"
+#include "recurrent.h"
+
+namespace im {
+
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef int i32x8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+#define IM_LDS3 __attribute__((address_space(3)))
+
+static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
+// Copies 16 bytes a lane to LDS at `to` (the same in every lane) + 16 lane.
+__device__ __forceinline__ void copy_to_lds(const void *from, char *to)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)from,
+                                     (IM_LDS3 uint32_t *)to, 16, 0, 0);
+}
+
+// Copies a byte a lane, as a word, to `to` + 4 lane.
+__device__ __forceinline__ void copy_byte_to_lds(const void *from, char *to)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)from,
+                                     (IM_LDS3 uint32_t *)to, 1, 0, 0);
+}
+
+// All but the wavefront's N last loads are done, and its LDS accesses.
+template <int N>
+__device__ __forceinline__ void wait_loads()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+}
+
+// Waits for a step that `later` steps of L loads each follow (M of them at most).
+template <int L, int M>
+__device__ __forceinline__ void wait_for_step(int later)
+{
+    if constexpr (M > 0) {
+        if (later >= M) wait_loads<M * L>();
+        else wait_for_step<L, M - 1>(later);
+    } else {
+        wait_loads<0>();
+    }
+}
+
+// The block meets; LDS accesses stay on their side.
+__device__ __forceinline__ void meet()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// acc += (a 2^(sa - 127)) (b 2^(sb - 127)) over 64 k.  A lane holds 32 bytes of one row of each
+// operand, its k by the half of the wavefront; both operands are read alike, so that which k is
+// of no matter, and a row has one scale over all 128 k of a block.
+__device__ __forceinline__ f32x16_t mfma8(i32x8_t a, i32x8_t b, f32x16_t acc, int sa, int sb)
+{
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc, 0, 0, 0, sa, 0, sb);
+}
+
+// Eight e4m3 values times the scale's power of two as bf16: exact, but for values below 2^-126.
+__device__ __forceinline__ bf16x8_t widen8(uint32_t lo, uint32_t hi, float scale)
+{
+    const bf16x2_t v[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false),
+                           __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true),
+                           __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false),
+                           __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true)};
+    return __builtin_bit_cast(bf16x8_t, v);
+}
+
+// Last steps of every kernel: eight consecutive values of a row, from `col` of `wide` columns
+// on, get their bias, the ReLU, and leave.  All 16 lanes of 128 columns call together.
+__device__ __forceinline__ void finish8(const Linear8Args &a, int64_t row, int64_t col, bool on, float (&v)[8])
+{
+    const int nv = (int)min((int64_t)8, a.out - col);
+    if (a.bias) {
+        float b[8];
+        load8(a.bias + col, nv, b);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] += b[k];
+    }
+    if (a.relu)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = v[k] < 0.0f ? 0.0f : v[k];      // NaN stays
+    if (a.y8.q) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) top = max(top, k < nv ? magnitude(v[k]) : 0);
+        const int s = block8_scale(lanes_max<16>(top));
+        if (on) {
+            *(u32x2_r *)(a.y8.q + row * a.y8.ld_q + col) = block8_pack(v, s, nv);
+            if ((col & 127) == 0) a.y8.scale[row * a.y8.ld_scale + col / 128] = (uint8_t)s;
+        }
+    }
+    if (!on || nv <= 0 || !a.y) return;
+    if (a.y_f32) store8((float *)a.y + row * a.ld_y + col, nv, v);
+    else store8((uint16_t *)a.y + row * a.ld_y + col, nv, v);
+}
+
+// ---------------------------------------------------------------------------
+// Tiles.  A block of WP x WQ wavefronts forms BP x BQ of C, a wavefront TP x TQ MFMA tiles.
+// K steps of 128 bytes go through a ring of NS stages in LDS by direct loads, NS - 1 steps
+// ahead, their scales as a word a row after them; a step has one barrier.  Direct loads write
+// 64 consecutive 16-byte pieces, so a stage has no padding: piece c of row r lies at
+// c ^ (r / 2 mod 8), and 16 rows' pieces of one k cover all banks.
+// ---------------------------------------------------------------------------
+template <int WP_, int WQ_, int TP_, int TQ_, int NS_>
+struct TileShape {
+    static constexpr int WP = WP_, WQ = WQ_, TP = TP_, TQ = TQ_, NS = NS_;
+    static constexpr int NT = 64 * WP * WQ, WAVES = WP * WQ, BP = 32 * WP * TP, BQ = 32 * WQ * TQ;
+    static_assert(BP % 128 == 0, "whole blocks of y8");
+    static constexpr int UP = BP * 8 / NT, UQ = BQ * 8 / NT;             // 16-byte pieces of a thread
+    static constexpr int US = ((BP + BQ) / 64 + WAVES - 1) / WAVES;      // scales of a thread
+    static constexpr int L = UP + UQ + US;                               // direct loads of a step
+    static constexpr int Q_AT = BP * 128, S_AT = Q_AT + BQ * 128, STAGE = S_AT + US * WAVES * 256;
+    static constexpr int LDO = BP + 4;                                   // floats of an epilogue row
+    static constexpr int OUT_ROWS = 32 * WQ, LDS = std::max(NS * STAGE, OUT_ROWS * LDO * 4);
+    static_assert(UP * NT == BP * 8 && UQ * NT == BQ * 8 && (BP + BQ) % 64 == 0, "whole pieces");
+};
+
+template <typename S, bool WIDE>
+__global__ __launch_bounds__(S::NT, 2) void linear8_tile_kernel(Linear8Args a, int p_tiles, int tiles)
+{
+    __shared__ __attribute__((aligned(1024))) char lds[S::LDS];
+    constexpr int TP = S::TP, TQ = S::TQ, BP = S::BP, BQ = S::BQ, NS = S::NS;
+    const int lane = threadIdx.x & 63, wave = wave_id();
+    const int id = xcd_order(blockIdx.x, gridDim.x);
+    const int split = id / tiles, tile = id % tiles;
+    const int64_t p0 = (int64_t)(tile % p_tiles) * BP, q0 = (int64_t)(tile / p_tiles) * BQ;
+    const int wp = wave % S::WP * TP * 32, wq = wave / S::WP * TQ * 32;
+    const int64_t k0 = a.steps * split / a.splits;
+    const int nk = (int)(a.steps * (split + 1) / a.splits - k0);
+
+    // Addresses of this thread's pieces and scales.  Rows past the last read the last one: their
+    // sums are not stored.
+    const uint8_t *from[S::UP + S::UQ], *sfrom[S::US];
+#pragma unroll
+    for (int u = 0; u < S::UP + S::UQ; ++u) {
+        const bool q = u >= S::UP;
+        const int r = ((q ? u - S::UP : u) * S::WAVES + wave) * 8 + lane / 8;
+        const int c = (lane & 7) ^ (r >> 1 & 7);
+        const Mat8 &m = q ? a.q : a.p;
+        const int64_t row = min((q ? q0 : p0) + r, (q ? a.n : a.out) - 1);
+        from[u] = m.q + row * m.ld_q + k0 * 128 + c * 16;
+    }
+#pragma unroll
+    for (int u = 0; u < S::US; ++u) {
+        const int r = (u * S::WAVES + wave) * 64 + lane;
+        const bool q = r >= BP;
+        const Mat8 &m = q ? a.q : a.p;
+        const int64_t row = min(q ? q0 + min(r - BP, BQ - 1) : p0 + r, (q ? a.n : a.out) - 1);
+        sfrom[u] = m.scale + (row >> m.shift) * m.ld_scale + k0;
+    }
+    auto copy = [&](int u, int kt, char *st) {
+        if (u < S::UP + S::UQ) copy_to_lds(from[u] + kt * 128, st + (u * S::WAVES + wave) * 1024);
+        else copy_byte_to_lds(sfrom[u - S::UP - S::UQ] + kt,
+                              st + S::S_AT + ((u - S::UP - S::UQ) * S::WAVES + wave) * 256);
+    };
+    // 16 bytes of one of 32 rows: half h of the wavefront takes piece 2 s + h
+    auto piece = [&](const char *at, int row, int s) {
+        const int r = row + (lane & 31), perm = (r >> 1 & 7) << 4;
+        return *(const u32x4_r *)(at + r * 128 + (((2 * s + (lane >> 5)) << 4) ^ perm));
+    };
+    auto frag = [&](const char *at, int row, int s) {
+        const u32x4_r lo = piece(at, row, 2 * s), hi = piece(at, row, 2 * s + 1);
+        return i32x8_t{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+    };
+    f32x16_t acc[TP][TQ];
+#pragma unroll
+    for (int i = 0; i < TP; ++i)
+#pragma unroll
+        for (int j = 0; j < TQ; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+    auto multiply = [&](int kt, bool more) {
+        const char *st = lds + kt % NS * S::STAGE;
+        char *ahead = lds + (kt + NS - 1) % NS * S::STAGE;
+        const int *sc = (const int *)(st + S::S_AT);
+        int sp[TP], sq[TQ];
+#pragma unroll
+        for (int i = 0; i < TP; ++i) sp[i] = sc[wp + 32 * i + (lane & 31)];
+#pragma unroll
+        for (int j = 0; j < TQ; ++j) sq[j] = sc[BP + wq + 32 * j + (lane & 31)];
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                u32x4_r bp[TP], bq[TQ];
+#pragma unroll
+                for (int i = 0; i < TP; ++i) bp[i] = piece(st, wp + 32 * i, s);
+#pragma unroll
+                for (int j = 0; j < TQ; ++j) bq[j] = piece(st + S::Q_AT, wq + 32 * j, s);
+                if (more)
+#pragma unroll
+                    for (int u = S::L * s / 4; u < S::L * (s + 1) / 4; ++u) copy(u, kt + NS - 1, ahead);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    bf16x8_t fp[TP], fq[TQ];
+#pragma unroll
+                    for (int i = 0; i < TP; ++i)
+                        fp[i] = widen8(bp[i][2 * h], bp[i][2 * h + 1], __uint_as_float((uint32_t)sp[i] << 23));
+#pragma unroll
+                    for (int j = 0; j < TQ; ++j)
+                        fq[j] = widen8(bq[j][2 * h], bq[j][2 * h + 1], __uint_as_float((uint32_t)sq[j] << 23));
+#pragma unroll
+                    for (int i = 0; i < TP; ++i)
+#pragma unroll
+                        for (int j = 0; j < TQ; ++j)
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp[i], fq[j], acc[i][j], 0, 0, 0);
+                }
+            }
+            return;
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            i32x8_t fp[TP], fq[TQ];
+#pragma unroll
+            for (int i = 0; i < TP; ++i) fp[i] = frag(st, wp + 32 * i, s);
+#pragma unroll
+            for (int j = 0; j < TQ; ++j) fq[j] = frag(st + S::Q_AT, wq + 32 * j, s);
+            if (more)
+#pragma unroll
+                for (int u = S::L * s / 2; u < S::L * (s + 1) / 2; ++u) copy(u, kt + NS - 1, ahead);
+#pragma unroll
+            for (int i = 0; i < TP; ++i)
+#pragma unroll
+                for (int j = 0; j < TQ; ++j) acc[i][j] = mfma8(fp[i], fq[j], acc[i][j], sp[i], sq[j]);
+        }
+    };
+    for (int kt = 0; kt < NS - 1 && kt < nk; ++kt)
+#pragma unroll
+        for (int u = 0; u < S::L; ++u) copy(u, kt, lds + kt * S::STAGE);
+    int kt = 0;
+    for (; kt + NS - 1 < nk; ++kt) {
+        wait_loads<(NS - 2) * S::L>();
+        meet();
+        multiply(kt, true);
+    }
+    for (; kt < nk; ++kt) {
+        wait_for_step<S::L, NS - 2>(nk - 1 - kt);
+        meet();
+        multiply(kt, false);
+    }
+
+    // rows leave through LDS, 32 of each wavefront at a time: lane l holds q = wq + 32 j + l % 32,
+    // p = wp + 32 i + 8 g + 4 (l / 32) + 0..3
+    float *out = (float *)lds;
+    constexpr int PIECES = S::OUT_ROWS * (BP / 8) / S::NT;
+#pragma unroll
+    for (int j = 0; j < TQ; ++j) {
+        meet();
+#pragma unroll
+        for (int i = 0; i < TP; ++i)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x4_r v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+                *(f32x4_r *)(out + (wave / S::WP * 32 + (lane & 31)) * S::LDO + wp + 32 * i + 8 * g +
+                             4 * (lane >> 5)) = v;
+            }
+        meet();
+#pragma unroll
+        for (int c = 0; c < PIECES; ++c) {
+            const int at = c * S::NT + threadIdx.x, r = at / (BP / 8), f = at % (BP / 8) * 8;
+            const int64_t row = q0 + r / 32 * TQ * 32 + 32 * j + r % 32, col = p0 + f;
+            float v[8];
+            const f32x4_r lo = *(const f32x4_r *)(out + r * S::LDO + f), hi = *(const f32x4_r *)(out + r * S::LDO + f + 4);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = lo[k], v[4 + k] = hi[k];
+            if (a.part) {
+                const int64_t ld = (a.out + 3) / 4 * 4;
+                const int nv = (int)min((int64_t)8, a.out - col);
+                if (row < a.n && nv > 0) store8(a.part + ((int64_t)split * a.n + row) * ld + col, nv, v);
+            } else {
+                finish8(a, row, col, row < a.n, v);
+            }
+        }
+    }
+}
+
+// Parts of a product to y, in their order.
+__global__ __launch_bounds__(256) void linear8_join_kernel(Linear8Args a)
+{
+    const int64_t ld = (a.out + 3) / 4 * 4, quads = ld / 4, all = a.n * quads;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / quads, col = (i - row * quads) * 4;
+        const float *p = a.part + row * ld + col;
+        f32x4_r s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 8
+        for (int k = 0; k < a.splits; ++k) s += *(const f32x4_r *)(p + (int64_t)k * a.n * ld);
+        float *y = (float *)a.y + row * a.ld_y + col;
+        if (col + 4 <= a.out) {
+            *(f32x4_a4 *)y = s;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (col + k < a.out) y[k] = s[k];
+        }
+    }
+}
+
+typedef TileShape<2, 2, 2, 2, 2> Tile128;
+
+int linear8_splits(int64_t n, int64_t out, int64_t steps)
+{
+    const int64_t tiles = ceil_div(n, 128) * ceil_div(out, 128);
+    return (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, steps / 4));
+}
+
+// Products in bf16, summed in fp32 throughout.
+static bool wide(const Linear8Args &a) { return (a.y && a.y_f32) || a.y8.q; }
+
+template <typename S>
+static void tile_by(const Linear8Args &a, hipStream_t s)
+{
+    const int64_t p_tiles = ceil_div(a.out, S::BP), tiles = p_tiles * ceil_div(a.n, S::BQ);
+    const dim3 g((unsigned)(tiles * a.splits)), b(S::NT);
+    if (wide(a)) linear8_tile_kernel<S, true><<<g, b, 0, s>>>(a, (int)p_tiles, (int)tiles);
+    else linear8_tile_kernel<S, false><<<g, b, 0, s>>>(a, (int)p_tiles, (int)tiles);
+}
+
+hipError_t launch_linear8(const Linear8Args &a, hipStream_t s)
+{
+    if (a.part) {
+        tile_by<Tile128>(a, s);
+        linear8_join_kernel<<<dim3((unsigned)std::min<int64_t>(ceil_div(a.n * ceil_div(a.out, 4), 256), 256 * 16)),
+                              dim3(256), 0, s>>>(a);
+        return hipGetLastError();
+    }
+    // parts of rows with fewer than 2^21 tiles of 128 x 128
+    const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 20) / ceil_div(a.out, 128)) * 128;
+    for (int64_t r = 0; r < a.n; r += most) {
+        Linear8Args b = a;
+        b.n = std::min(most, a.n - r);
+        b.q.q += r * a.q.ld_q;
+        b.q.scale += (r >> a.q.shift) * a.q.ld_scale;
+        if (a.y) b.y = (char *)a.y + r * a.ld_y * (a.y_f32 ? 4 : 2);
+        if (a.y8.q) b.y8.q += r * a.y8.ld_q, b.y8.scale += r * a.y8.ld_scale;
+        tile_by<Tile128>(b, s);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace im

@@ -1,0 +1,224 @@
+"""The C ABI of a recurrent policy's blocks without a GPU: what the calls refuse before they
+touch the device, and the workspace sizes."""
+import ctypes as C
+import os
+
+import pytest
+
+from paper_2609_09821_amd import binding as im
+
+P = 1 << 20      # stands for a device address that no refused call reads
+BAD, UNS = im.IM_ERR_INVALID_ARG, im.IM_ERR_UNSUPPORTED
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(im.LIB_PATH):
+        from paper_2609_09821_amd import build
+        build.build()
+    return im.lib()
+
+
+def _refused(lib, status, code, words):
+    assert status == code, (status, lib.im_last_error())
+    assert words in lib.im_last_error().decode(), lib.im_last_error()
+
+
+def _b8(d=8, n=4, rows=1, **over):
+    b = im.ImBlock8(P, P, -(-d // 128) * 128, -(-d // 128), rows)
+    for k, v in over.items():
+        setattr(b, k, v)
+    return b
+
+
+BAD_BLOCKS = [
+    (dict(rows=2), "rows must"), (dict(rows=0), "rows must"), (dict(ld_q=112), "ld_q"),
+    (dict(ld_q=136), "ld_q"), (dict(ld_scale=0), "ld_scale"), (dict(q=None), "NULL block8"),
+    (dict(scale=None), "NULL block8"), (dict(q=P + 8), "aligned"),
+]
+
+
+@pytest.mark.parametrize("over,words", BAD_BLOCKS)
+def test_block8_arguments(lib, over, words):
+    b = _b8(**over)
+    for status in (lib.im_block_store(P, 8, 0, 4, 8, C.byref(b), None, None),
+                   lib.im_block_store(P, 4, 0, 8, 4, None, C.byref(b), None),
+                   lib.im_block_load(C.byref(b), 4, 8, P, 8, 0, None),
+                   lib.im_rms_norm(C.byref(_rms(y8=C.pointer(b))), None),
+                   lib.im_block_linear(C.byref(_layer(x=C.pointer(b))), None),
+                   lib.im_block_linear(C.byref(_layer(w=C.pointer(b))), None),
+                   lib.im_block_linear(C.byref(_layer(out=8, ld_y=8, y8=C.pointer(b))), None),
+                   lib.im_block_linear_grad(C.byref(_layer_grad(xt=C.pointer(b))), None),
+                   lib.im_block_linear_grad(C.byref(_layer_grad(wt=C.pointer(b))), None)):
+        _refused(lib, status, BAD, words)
+
+
+@pytest.mark.parametrize("x,ld,dtype,n,d,c,t,code,words", [
+    (P, 8, 0, -1, 8, _b8(), None, BAD, "n must"),
+    (P, 8, 0, 4, 0, _b8(), None, BAD, "width"),
+    (P, 8, 2, 4, 8, _b8(), None, BAD, "dtype"),
+    (P, 7, 0, 4, 8, _b8(), None, BAD, "ld_x"),
+    (None, 8, 0, 4, 8, _b8(), None, BAD, "NULL x"),
+    (P, 8, 0, 4, 8, None, None, BAD, "neither"),
+    (P, 8, 0, 4, 8, _b8(), _b8(4, rows=128), BAD, "same rows"),
+    (P, 8, 0, (1 << 30) + 1, 8, _b8(), None, UNS, "2^30"),
+    (P, 1 << 21, 0, 4, (1 << 20) + 1, _b8((1 << 20) + 1), None, UNS, "2^20"),
+])
+def test_block8_store_refuses(lib, x, ld, dtype, n, d, c, t, code, words):
+    ref = [b and C.byref(b) for b in (c, t)]
+    _refused(lib, lib.im_block_store(x, ld, dtype, n, d, *ref, None), code, words)
+    if c and not t:
+        _refused(lib, lib.im_block_load(ref[0], n, d, x, ld, dtype, None), code, words)
+
+
+def test_null_arguments(lib):
+    for f in (lib.im_rms_norm, lib.im_rms_norm_grad, lib.im_block_linear, lib.im_block_linear_grad,
+              lib.im_gated_scan, lib.im_gated_scan_grad):
+        _refused(lib, f(None, None), BAD, "NULL im_")
+    _refused(lib, lib.im_block_load(None, 4, 8, P, 8, 0, None), BAD, "NULL block8")
+
+
+def _set(a, over):
+    for k, v in over.items():
+        setattr(a, k, v)
+    return a
+
+
+def _rms(**over):
+    return _set(im.ImRms(4, 8, 0, 1e-6, P, 8, P, 8, P, 2 * P, 8, 3 * P, 8, None, P), over)
+
+
+@pytest.mark.parametrize("over,code,words", [
+    (dict(n=-1), BAD, "n must"), (dict(d=0), BAD, "width"), (dict(eps=-1.0), BAD, "eps"),
+    (dict(d=8193, ld_x=9000, ld_residual=9000, ld_h=9000, ld_y=9000), UNS, "WIDTH"),
+    (dict(eps=float("nan")), BAD, "eps"), (dict(dtype=7), BAD, "dtype"), (dict(ld_x=7), BAD, "ld_x"),
+    (dict(ld_residual=7), BAD, "ld_"), (dict(ld_h=7), BAD, "ld_"), (dict(ld_y=7), BAD, "ld_"),
+    (dict(x=None), BAD, "NULL x"), (dict(h=None, y=None, rstd=None), BAD, "no output"),
+    (dict(h=3 * P), BAD, "one array"), (dict(y8=C.pointer(_b8(rows=128))), BAD, "rows must be 1"),
+])
+def test_rms_norm_refuses(lib, over, code, words):
+    _refused(lib, lib.im_rms_norm(C.byref(_rms(**over)), None), code, words)
+
+
+def _rms_grad(**over):
+    return _set(im.ImRmsGrad(4, 8, 0, P, 8, P, 8, P, 8, P, P, P, 8, P, P, 1 << 20), over)
+
+
+@pytest.mark.parametrize("over,code,words", [
+    (dict(n=-1), BAD, "n must"), (dict(d=0), BAD, "width"), (dict(dtype=3), BAD, "dtype"),
+    (dict(ld_dy=7), BAD, "ld_dy"), (dict(ld_h=7), BAD, "ld_"), (dict(ld_dh=7), BAD, "ld_"),
+    (dict(ld_dx=7), BAD, "ld_"), (dict(dy=None), BAD, "NULL"), (dict(h=None), BAD, "NULL"),
+    (dict(rstd=None), BAD, "NULL"), (dict(dx=None, dgamma=None), BAD, "no output"),
+    (dict(workspace=None), BAD, "workspace"), (dict(workspace_bytes=4), BAD, "workspace"),
+    (dict(workspace=P + 2), BAD, "aligned"),
+])
+def test_rms_norm_grad_refuses(lib, over, code, words):
+    _refused(lib, lib.im_rms_norm_grad(C.byref(_rms_grad(**over)), None), code, words)
+
+
+def _layer(**over):
+    return _set(im.ImLayer8(4, 8, 16, 0, 1, C.pointer(_b8(8)), C.pointer(_b8(8, 16, 128)), P, P, 16, None), over)
+
+
+@pytest.mark.parametrize("over,code,words", [
+    (dict(n=-1), BAD, "n must"), (dict(in_=0), BAD, "width"), (dict(out=0), BAD, "out must"),
+    (dict(y_dtype=5), BAD, "dtype"), (dict(ld_y=15), BAD, "ld_y"), (dict(y=None), BAD, "no output"),
+    (dict(x=None), BAD, "NULL block8"), (dict(w=None), BAD, "NULL block8"),
+    (dict(in_=129), BAD, "ld_q"), (dict(in_=(1 << 20) + 1), UNS, "2^20"), (dict(out=(1 << 20) + 1), UNS, "2^20"),
+    (dict(n=(1 << 30) + 1), UNS, "2^30"), (dict(y8=C.pointer(_b8(16, rows=128))), BAD, "rows must be 1"),
+])
+def test_linear8_refuses(lib, over, code, words):
+    _refused(lib, lib.im_block_linear(C.byref(_layer(**over)), None), code, words)
+
+
+def _layer_grad(**over):
+    return _set(im.ImLayer8Grad(4, 8, 16, 0, P, 16, P, 16, C.pointer(_b8(4)), C.pointer(_b8(16, rows=128)),
+                                P, 8, P, 8, P, P, 1 << 30), over)
+
+
+@pytest.mark.parametrize("over,code,words", [
+    (dict(n=-1), BAD, "n must"), (dict(in_=0), BAD, "width"), (dict(out=0), BAD, "out must"),
+    (dict(dtype=5), BAD, "dtype"), (dict(ld_dy=15), BAD, "ld_dy"), (dict(ld_y=15), BAD, "ld_"),
+    (dict(ld_dx=7), BAD, "ld_"), (dict(ld_dw=7), BAD, "ld_"), (dict(dy=None), BAD, "NULL dy"),
+    (dict(xt=None), BAD, "xt"), (dict(wt=None), BAD, "wt"),
+    (dict(dx=None, dw=None, db=None), BAD, "no output"), (dict(workspace=None), BAD, "workspace"),
+    (dict(workspace_bytes=16), BAD, "workspace"), (dict(workspace=P + 8), BAD, "aligned"),
+])
+def test_linear8_grad_refuses(lib, over, code, words):
+    _refused(lib, lib.im_block_linear_grad(C.byref(_layer_grad(**over)), None), code, words)
+
+
+def _scan(**over):
+    return _set(im.ImScan(6, 4, 8, 0, P, 32, 8, P, 32, 8, P, P, 4, P, P, 32, 8, P, P, P, 1 << 30), over)
+
+
+def _scan_grad(**over):
+    return _set(im.ImScanGrad(6, 4, 8, 0, P, 32, 8, P, 32, 8, P, 32, 8, P, P, 4, P, P, P, 32, 8, P, 32, 8, P,
+                              P, 1 << 30), over)
+
+
+BOTH = [
+    (dict(T=-1), BAD, "T and n"), (dict(n=-1), BAD, "T and n"), (dict(d=0), BAD, "T and n"),
+    (dict(dtype=2), BAD, "dtype"), (dict(ld_flags=3), BAD, "ld_flags"), (dict(gate=None), BAD, "NULL gate"),
+    (dict(x=None), BAD, "NULL"), (dict(st_x=-32), BAD, "negative"), (dict(ld_gate=-8), BAD, "negative"),
+    (dict(T=(1 << 30) + 1), UNS, "2^30"), (dict(n=1 << 20, d=1 << 12), UNS, "2^31"),
+]
+
+
+@pytest.mark.parametrize("over,code,words", BOTH + [
+    (dict(h=None), BAD, "NULL"), (dict(st_h=31), BAD, "overlap"), (dict(ld_h=7), BAD, "overlap"),
+    (dict(st_h=0), BAD, "overlap"), (dict(st_h=8, ld_h=40), BAD, "overlap"), (dict(st_h=-32), BAD, "overlap"),
+])
+def test_gated_scan_refuses(lib, over, code, words):
+    over = dict(over)
+    if over.get("gate", P) is None:
+        words = "NULL"
+    _refused(lib, lib.im_gated_scan(C.byref(_scan(**over)), None), code, words)
+
+
+@pytest.mark.parametrize("over,code,words", [(o, c, "NULL" if "NULL" in w else w) for o, c, w in BOTH] + [
+    (dict(dh=None), BAD, "NULL"), (dict(keep=None), BAD, "NULL"), (dict(dgate=None), BAD, "NULL"),
+    (dict(dx=None), BAD, "NULL"), (dict(st_dx=31), BAD, "overlap"), (dict(ld_dgate=7), BAD, "overlap"),
+    (dict(st_dh=-1), BAD, "negative"),
+])
+def test_gated_scan_grad_refuses(lib, over, code, words):
+    _refused(lib, lib.im_gated_scan_grad(C.byref(_scan_grad(**over)), None), code, words)
+
+
+def test_scan_workspace_is_asked_for(lib):
+    need = lib.im_gated_scan_workspace(100000, 1, 8)
+    assert need > 0
+    big = dict(T=100000, n=1, st_gate=8, st_x=8, st_h=8, st_dh=8, st_dgate=8, st_dx=8)
+    for over in (dict(workspace=None), dict(workspace_bytes=need - 1), dict(workspace=P + 4)):
+        for f, a in ((lib.im_gated_scan, _scan), (lib.im_gated_scan_grad, _scan_grad)):
+            s = a()
+            _set(s, {k: v for k, v in dict(big, **over).items() if hasattr(s, k)})
+            _refused(lib, f(C.byref(s), None), BAD, "workspace")
+
+
+def test_workspace_sizes(lib):
+    assert lib.im_rms_norm_grad_workspace(-1, 8) == lib.im_rms_norm_grad_workspace(4, 0) == -1
+    assert lib.im_rms_norm_grad_workspace(4, 8193) == -1 and lib.im_rms_norm_grad_workspace(1 << 20, 512) > 0
+    for a in ((-1, 8, 8), (4, 0, 8), (4, 8, 0), ((1 << 30) + 1, 8, 8), (4, 1 << 21, 8)):
+        assert lib.im_block_linear_grad_workspace(*a) == -1
+    # dy in 8 bits, twice, with its scales
+    assert lib.im_block_linear_grad_workspace(65536, 1024, 512) >= 2 * 65536 * 516
+    for a in ((-1, 4, 8), (4, -1, 8), (4, 4, 0), ((1 << 30) + 1, 1, 1), (4, 1 << 20, 1 << 12)):
+        assert lib.im_gated_scan_workspace(*a) == -1
+    for a in ((0, 0, 1), (1, 65536, 1024), (32, 16384, 256)):
+        assert lib.im_gated_scan_workspace(*a) == 0
+
+
+def test_calls_on_nothing(lib):
+    """Empty batches are done without a look at the arrays."""
+    none = dict(n=0, x=None, residual=None, gamma=None, h=None, y=None, rstd=None)
+    assert lib.im_rms_norm(C.byref(_rms(**none)), None) == im.IM_OK
+    assert lib.im_rms_norm_grad(C.byref(_rms_grad(n=0, dy=None, h=None, rstd=None, dgamma=None)), None) == im.IM_OK
+    empty = _b8(q=None, scale=None)
+    assert lib.im_block_store(None, 8, 0, 0, 8, C.byref(empty), None, None) == im.IM_OK
+    assert lib.im_block_load(C.byref(empty), 0, 8, None, 8, 0, None) == im.IM_OK
+    assert lib.im_block_linear(C.byref(_layer(n=0, x=C.pointer(empty), y=None)), None) == im.IM_OK
+    assert lib.im_block_linear_grad(C.byref(_layer_grad(n=0, dy=None, dw=None, db=None)), None) == im.IM_OK
+    assert lib.im_gated_scan(C.byref(_scan(n=0, gate=None, x=None, h=None)), None) == im.IM_OK
+    assert lib.im_gated_scan(C.byref(_scan(T=0, gate=None, x=None, h=None, state_out=None)), None) == im.IM_OK
+    assert lib.im_gated_scan_grad(C.byref(_scan_grad(n=0, dh=None)), None) == im.IM_OK
