@@ -25,9 +25,9 @@ constexpr int KEEP = IM_SCAN_KEEP;
 template <typename E, int V>
 struct StepPiece {
     static constexpr int BYTES = sizeof(E) * V;
-    typedef uint32_t word_t __attribute__((ext_vector_type(BYTES >= 4 ? BYTES / 4 : 1)));
+    typedef uint32_t word_t __attribute__((ext_vector_type(BYTES / 4)));
     typedef word_t at_t __attribute__((aligned(sizeof(E))));
-    static_assert(BYTES >= 4 || V == 1, "whole words, or one value");
+    static_assert(BYTES % 4 == 0, "whole words");
     int at, lo, hi;      // first column; the values lo .. hi - 1 are this piece's own
     __device__ __forceinline__ void init(int64_t piece, int64_t d)
     {
@@ -36,23 +36,18 @@ struct StepPiece {
         lo = col - at;
         hi = min(V, (int)d);
     }
-    __device__ __forceinline__ word_t load(const E *row) const
+    // p: the address of column `at`
+    __device__ __forceinline__ word_t load(const E *p) const
     {
-        if constexpr (V == 1) {
-            word_t r;
-            r[0] = sizeof(E) == 2 ? (uint32_t)((const uint16_t *)row)[at] : ((const uint32_t *)row)[at];
-            return r;
-        } else {
-            if (hi == V) return *(const at_t *)(row + at);
-            word_t r = {};
+        if (hi == V) return *(const at_t *)p;
+        word_t r = {};
 #pragma unroll
-            for (int k = 0; k < V; ++k)
-                if (k < hi) {
-                    if constexpr (sizeof(E) == 2) r[k / 2] |= (uint32_t)row[k] << (16 * (k & 1));
-                    else r[k] = ((const uint32_t *)row)[k];
-                }
-            return r;
-        }
+        for (int k = 0; k < V; ++k)
+            if (k < hi) {
+                if constexpr (sizeof(E) == 2) r[k / 2] |= (uint32_t)p[k] << (16 * (k & 1));
+                else r[k] = ((const uint32_t *)p)[k];
+            }
+        return r;
     }
     __device__ __forceinline__ static void unpack(word_t w, float (&v)[V])
     {
@@ -62,29 +57,44 @@ struct StepPiece {
             else v[k] = __uint_as_float(k & 1 ? w[k / 2] & 0xFFFF0000u : w[k / 2] << 16);
         }
     }
-    __device__ __forceinline__ void store(E *row, const float (&v)[V]) const
+    __device__ __forceinline__ void store(E *p, const float (&v)[V]) const
     {
         word_t w;
         if constexpr (sizeof(E) == 4) {
 #pragma unroll
             for (int k = 0; k < V; ++k) w[k] = __float_as_uint(v[k]);
-        } else if constexpr (V == 1) {
-            w[0] = pack_bf16x2(v[0], 0.0f);
         } else {
 #pragma unroll
             for (int k = 0; k < V / 2; ++k) w[k] = pack_bf16x2(v[2 * k], v[2 * k + 1]);
         }
-        if (V > 1 && lo == 0 && hi == V) {
-            *(at_t *)(row + at) = w;
+        if (lo == 0 && hi == V) {
+            *(at_t *)p = w;
         } else {
 #pragma unroll
             for (int k = 0; k < V; ++k)
                 if (k >= lo && k < hi) {
-                    if constexpr (sizeof(E) == 4) ((uint32_t *)row)[at + k] = w[k];
-                    else row[at + k] = (E)(w[k / 2] >> (16 * (k & 1)));
+                    if constexpr (sizeof(E) == 4) ((uint32_t *)p)[k] = w[k];
+                    else p[k] = (E)(w[k / 2] >> (16 * (k & 1)));
                 }
         }
     }
+};
+
+// An array's values of this thread: step t at base + t st, the same in all lanes, and a lane's
+// own offset from its wavefront's first env, so that the steps' addresses take no vector
+// registers (the gradient's five arrays of 16 steps would take them all).  O: the offset's type.
+template <typename E, typename O>
+struct Steps {
+    E *base;
+    int64_t st;
+    O off;
+    __device__ __forceinline__ void init(const void *p, int64_t st_, int64_t ld, int64_t env, int first, int at)
+    {
+        base = (E *)p + first * ld;
+        st = st_;
+        off = (O)(((env - first) * ld + at) * (int64_t)sizeof(E));
+    }
+    __device__ __forceinline__ E *operator[](int64_t t) const { return (E *)((char *)(base + t * st) + off); }
 };
 
 // a = 1 / (1 + exp(-g)) and b = 1 - a = 1 / (1 + exp(g)), neither by a difference.  exp2's
@@ -96,33 +106,70 @@ __device__ __forceinline__ void gates(float g, float &a, float &b)
     const float n = -fabsf(g), t = n * L;
     const float rest = fmaf(n, L2, fmaf(n, L, -t));
     float e = __builtin_amdgcn_exp2f(t);
-    e = g == g && t > -150.0f ? fmaf(e * 0x1.62e43p-1f, rest, e) : e;      // infinities stay out of the products
+    e = t > -150.0f ? fmaf(e * 0x1.62e43p-1f, rest, e) : e;      // infinities stay out of the products
     const float r = __builtin_amdgcn_rcpf(1.0f + e);
     const float s = e * r;
     a = g < 0.0f ? s : r;
     b = g < 0.0f ? r : s;
 }
 
+// Whether an env's episode ends with each of KEEP steps, a bit a step.
+struct Ends {
+    const uint8_t *f1, *f2;      // null: none do
+    int64_t ld, env;
+    bool one;                    // all lanes have the same env
+    __device__ __forceinline__ void init(const ScanArgs &a, int64_t e)
+    {
+        f1 = a.term ? a.term : a.trunc, f2 = a.trunc ? a.trunc : a.term;
+        ld = a.ld_flags, env = e;
+        const int lo = __builtin_amdgcn_readfirstlane((int)e);
+        one = __ballot((int)e != lo) == 0 && __ballot(true) == ~0ull;
+    }
+    // Steps t .. t + KEEP - 1 (of the last ones some may not exist).  Where a wavefront has one env,
+    // its lanes take a byte each, the steps' first flags and their second ones.
+    __device__ __forceinline__ uint32_t load(int64_t t, int64_t t1) const
+    {
+        if (!f1) return 0;
+        if (one) {
+            const int lane = threadIdx.x & 63;
+            const int64_t q = min(t + (lane & (KEEP - 1)), t1 - 1);
+            const uint64_t m = __ballot(lane < 2 * KEEP && (lane < KEEP ? f1 : f2)[q * ld + env] != 0);
+            return (uint32_t)(m | m >> KEEP) & ((1u << KEEP) - 1);
+        }
+        uint32_t m[KEEP], e = 0;
+#pragma unroll
+        for (int u = 0; u < KEEP; ++u) {
+            const int64_t q = min(t + u, t1 - 1) * ld + env;
+            m[u] = f1[q] | f2[q];
+        }
+#pragma unroll
+        for (int u = 0; u < KEEP; ++u) e |= m[u] ? 1u << u : 0;
+        return e;
+    }
+};
+
 // ---------------------------------------------------------------------------
 // A chunk's steps forward.  MAP: its map alone, from gate and x.
 // ---------------------------------------------------------------------------
-template <typename E, int V, bool MAP>
+template <typename E, int V, typename O, bool MAP>
 __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, int64_t pieces)
 {
     typedef StepPiece<E, V> P;
     constexpr int U = KEEP / 2;      // steps whose loads are in flight together
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t id = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
     if (id >= a.n * pieces) return;
     const int64_t env = id / pieces, chunk = blockIdx.y;
     P pc;
     pc.init(id - env * pieces, a.d);
     const int64_t t0 = chunk * a.chunk, t1 = min(t0 + a.chunk, a.T);
-    const E *gate = (const E *)a.gate + env * a.ld_gate + t0 * a.st_gate;
-    const E *x = (const E *)a.x + env * a.ld_x + t0 * a.st_x;
-    E *h = MAP ? nullptr : (E *)a.h + env * a.ld_h + t0 * a.st_h;
+    const int first = __builtin_amdgcn_readfirstlane((int)env);
+    Steps<E, O> gate, x, h;
+    gate.init(a.gate, a.st_gate, a.ld_gate, env, first, pc.at);
+    x.init(a.x, a.st_x, a.ld_x, env, first, pc.at);
+    h.init(a.h, a.st_h, a.ld_h, env, first, pc.at);
     const int64_t row = env * a.d;                 // of the states
-    const bool has_flags = a.term || a.trunc;
-    const uint8_t *f1 = a.term ? a.term : a.trunc, *f2 = a.trunc ? a.trunc : a.term;
+    Ends ends;
+    ends.init(a, env);
 
     float c[V], p[V];
 #pragma unroll
@@ -135,30 +182,19 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, int64_t pieces)
                 if (k < pc.hi) c[k] = from[row + pc.at + k];
     }
     typename P::word_t wg[2][U], wx[2][U];
-    uint32_t end[2];                               // of each step: the episode ends
+    // steps past the last: the last once more
     auto fetch = [&](int s, int64_t t) {
-        uint32_t m[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t q = min(t + u, t1 - 1) - t0;      // steps past the last: the last once more
-            wg[s][u] = pc.load(gate + q * a.st_gate);
-            wx[s][u] = pc.load(x + q * a.st_x);
-            m[u] = has_flags ? f1[(t0 + q) * a.ld_flags + env] | f2[(t0 + q) * a.ld_flags + env] : 0;
+            const int64_t q = min(t + u, t1 - 1);
+            wg[s][u] = pc.load(gate[q]);
+            wx[s][u] = pc.load(x[q]);
         }
-        uint32_t e = 0;
-#pragma unroll
-        for (int u = 0; u < U; ++u) e |= m[u] ? 1u << u : 0;
-        end[s] = e;
     };
-    auto walk = [&](int s, int64_t t) {
+    auto walk = [&](int s, int64_t t, uint32_t end) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (t + u >= t1) break;
-            if (!MAP && u == 0 && a.keep && t % KEEP == 0) {
-#pragma unroll
-                for (int k = 0; k < V; ++k)
-                    if (k >= pc.lo && k < pc.hi) a.keep[t / KEEP * a.n * a.d + row + pc.at + k] = c[k];
-            }
             float g[V], v[V];
             P::unpack(wg[s][u], g);
             P::unpack(wx[s][u], v);
@@ -169,19 +205,33 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, int64_t pieces)
                 c[k] = fmaf(ga, c[k], gb * v[k]);
                 if constexpr (MAP) p[k] = p[k] < 0.0f ? p[k] : p[k] * ga;
             }
-            if constexpr (!MAP) pc.store(h + (t + u - t0) * a.st_h, c);
-            if (end[s] >> u & 1)
+            if constexpr (!MAP) pc.store(h[t + u], c);
 #pragma unroll
-                for (int k = 0; k < V; ++k) c[k] = 0.0f, p[k] = -1.0f;
+            for (int k = 0; k < V; ++k) {
+                c[k] = end >> u & 1 ? 0.0f : c[k];
+                if constexpr (MAP) p[k] = end >> u & 1 ? -1.0f : p[k];
+            }
         }
     };
-    if (t0 < t1) fetch(0, t0);
-    for (int64_t t = t0; t < t1; t += 2 * U) {
+    uint32_t next = 0;
+    if (t0 < t1) {
+        fetch(0, t0);
+        next = ends.load(t0, t1);
+    }
+    for (int64_t t = t0; t < t1; t += KEEP) {
+        const uint32_t end = next;
         if (t + U < t1) fetch(1, t + U);
-        walk(0, t);
+        if (!MAP && a.keep)
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                if (k >= pc.lo && k < pc.hi) a.keep[t / KEEP * a.n * a.d + row + pc.at + k] = c[k];
+        walk(0, t, end);
         if (t + U >= t1) break;
-        if (t + 2 * U < t1) fetch(0, t + 2 * U);
-        walk(1, t + U);
+        if (t + KEEP < t1) {
+            fetch(0, t + KEEP);
+            next = ends.load(t + KEEP, t1);
+        }
+        walk(1, t + U, end >> U);
     }
     if constexpr (MAP) {
         float *m = a.maps + chunk * 2 * a.n * a.d + row;
@@ -198,24 +248,29 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, int64_t pieces)
 // ---------------------------------------------------------------------------
 // Backwards: D, the gradient of the state that passes on from a step, starts from dstate;
 // at each step G = dh + live D, D = a G.  The states within 16 steps are formed again from the
-// kept one.  MAP: the chunk's map of D alone, from gate and dh.
+// kept one, and with them what G is multiplied by, which takes the place of gate and x in
+// registers.  MAP: the chunk's map of D alone, from gate and dh.
 // ---------------------------------------------------------------------------
-template <typename E, int V, bool MAP>
+template <typename E, int V, typename O, bool MAP>
 __global__ __launch_bounds__(256) void scan_grad_kernel(ScanArgs a, int64_t pieces)
 {
     typedef StepPiece<E, V> P;
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t id = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
     if (id >= a.n * pieces) return;
     const int64_t env = id / pieces, chunk = blockIdx.y;
     P pc;
     pc.init(id - env * pieces, a.d);
     const int64_t t0 = chunk * a.chunk, t1 = min(t0 + a.chunk, a.T);
-    const E *gate = (const E *)a.gate + env * a.ld_gate, *x = (const E *)a.x + env * a.ld_x;
-    const E *dh = (const E *)a.dh + env * a.ld_dh;
-    E *dgate = (E *)a.dgate + env * a.ld_dgate, *dx = (E *)a.dx + env * a.ld_dx;
+    const int first = __builtin_amdgcn_readfirstlane((int)env);
+    Steps<E, O> gate, x, dh, dgate, dx;
+    gate.init(a.gate, a.st_gate, a.ld_gate, env, first, pc.at);
+    x.init(a.x, a.st_x, a.ld_x, env, first, pc.at);
+    dh.init(a.dh, a.st_dh, a.ld_dh, env, first, pc.at);
+    dgate.init(a.dgate, a.st_dgate, a.ld_dgate, env, first, pc.at);
+    dx.init(a.dx, a.st_dx, a.ld_dx, env, first, pc.at);
     const int64_t row = env * a.d;
-    const bool has_flags = a.term || a.trunc;
-    const uint8_t *f1 = a.term ? a.term : a.trunc, *f2 = a.trunc ? a.trunc : a.term;
+    Ends ends;
+    ends.init(a, env);
 
     float D[V], p[V];
 #pragma unroll
@@ -230,57 +285,53 @@ __global__ __launch_bounds__(256) void scan_grad_kernel(ScanArgs a, int64_t piec
     for (int64_t t = t0 + (t1 - 1 - t0) / KEEP * KEEP; t >= t0 && t < t1; t -= KEEP) {
         const int steps = (int)min((int64_t)KEEP, t1 - t);
         typename P::word_t wg[KEEP], wx[KEEP], wd[KEEP];
-        uint32_t m[KEEP];
 #pragma unroll
         for (int u = 0; u < KEEP; ++u) {
             const int64_t q = t + min(u, steps - 1);
-            wg[u] = pc.load(gate + q * a.st_gate);
-            if constexpr (!MAP) wx[u] = pc.load(x + q * a.st_x);
-            wd[u] = pc.load(dh + q * a.st_dh);
-            m[u] = has_flags ? f1[q * a.ld_flags + env] | f2[q * a.ld_flags + env] : 0;
+            wg[u] = pc.load(gate[q]);
+            if constexpr (!MAP) wx[u] = pc.load(x[q]);
         }
-        float before[KEEP][V];
-        if constexpr (!MAP) {
-            float c[V];
 #pragma unroll
-            for (int k = 0; k < V; ++k) c[k] = k < pc.hi ? a.keep[t / KEEP * a.n * a.d + row + pc.at + k] : 0.0f;
+        for (int u = 0; u < KEEP; ++u) wd[u] = pc.load(dh[t + min(u, steps - 1)]);
+        const uint32_t end = ends.load(t, t1);
+        float ga[KEEP][V], gb[KEEP][V], diff[KEEP][V];
+        float c[V];
 #pragma unroll
-            for (int u = 0; u < KEEP; ++u) {
-                float g[V], v[V];
-                P::unpack(wg[u], g);
-                P::unpack(wx[u], v);
+        for (int k = 0; k < V; ++k)
+            c[k] = !MAP && k < pc.hi ? a.keep[t / KEEP * a.n * a.d + row + pc.at + k] : 0.0f;
 #pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    before[u][k] = c[k];
-                    float ga, gb;
-                    gates(g[k], ga, gb);
-                    c[k] = m[u] ? 0.0f : fmaf(ga, c[k], gb * v[k]);
+        for (int u = 0; u < KEEP; ++u) {
+            float g[V], v[V];
+            P::unpack(wg[u], g);
+            if constexpr (!MAP) P::unpack(wx[u], v);
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                gates(g[k], ga[u][k], gb[u][k]);
+                if constexpr (!MAP) {
+                    diff[u][k] = c[k] - v[k];
+                    c[k] = end >> u & 1 ? 0.0f : fmaf(ga[u][k], c[k], gb[u][k] * v[k]);
                 }
             }
         }
 #pragma unroll
         for (int u = KEEP - 1; u >= 0; --u) {
             if (u >= steps) continue;
-            float g[V], v[V], d[V], og[V], ox[V];
-            P::unpack(wg[u], g);
+            float d[V], og[V], ox[V];
             P::unpack(wd[u], d);
-            if constexpr (!MAP) P::unpack(wx[u], v);
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-                float ga, gb;
-                gates(g[k], ga, gb);
-                const float G = d[k] + (m[u] ? 0.0f : D[k]);
-                D[k] = ga * G;
+                const float G = d[k] + (end >> u & 1 ? 0.0f : D[k]);
+                D[k] = ga[u][k] * G;
                 if constexpr (MAP) {
-                    p[k] = m[u] || p[k] < 0.0f ? -1.0f : ga * p[k];
+                    p[k] = end >> u & 1 || p[k] < 0.0f ? -1.0f : ga[u][k] * p[k];
                 } else {
-                    ox[k] = gb * G;
-                    og[k] = ga * (before[u][k] - v[k]) * ox[k];
+                    ox[k] = gb[u][k] * G;
+                    og[k] = ga[u][k] * diff[u][k] * ox[k];
                 }
             }
             if constexpr (!MAP) {
-                pc.store(dgate + (t + u) * a.st_dgate, og);
-                pc.store(dx + (t + u) * a.st_dx, ox);
+                pc.store(dgate[t + u], og);
+                pc.store(dx[t + u], ox);
             }
         }
     }
@@ -347,31 +398,36 @@ int64_t scan_chunk(int64_t T, int64_t n, int64_t d)
     return std::max<int64_t>(chunk, ceil_div(ceil_div(T, 65535), KEEP) * KEEP);
 }
 
-template <typename E, int V>
+// V: values of a thread forward, W: backward.
+template <typename E, int V, int W, typename O>
 static void scan_by(const ScanArgs &a, bool grad, hipStream_t s)
 {
-    const int64_t pieces = ceil_div(a.d, V);
-    const dim3 g((unsigned)ceil_div(a.n * pieces, 256), (unsigned)a.chunks), b(256);
+    const int64_t pieces = ceil_div(a.d, grad ? W : V);
+    // chunks of few envs leave less of a small block idle
+    const dim3 b(a.chunks > 1 ? 64 : 256), g((unsigned)ceil_div(a.n * pieces, b.x), (unsigned)a.chunks);
     const dim3 gc((unsigned)ceil_div(a.n * a.d, 64)), bc(64 * COMPOSE_WAVES);
     if (grad) {
         if (a.chunks > 1) {
-            scan_grad_kernel<E, V, true><<<g, b, 0, s>>>(a, pieces);
+            scan_grad_kernel<E, W, O, true><<<g, b, 0, s>>>(a, pieces);
             compose_kernel<true><<<gc, bc, 0, s>>>(a);
         }
-        scan_grad_kernel<E, V, false><<<g, b, 0, s>>>(a, pieces);
+        scan_grad_kernel<E, W, O, false><<<g, b, 0, s>>>(a, pieces);
     } else {
         if (a.chunks > 1) {
-            scan_kernel<E, V, true><<<g, b, 0, s>>>(a, pieces);
+            scan_kernel<E, V, O, true><<<g, b, 0, s>>>(a, pieces);
             compose_kernel<false><<<gc, bc, 0, s>>>(a);
         }
-        scan_kernel<E, V, false><<<g, b, 0, s>>>(a, pieces);
+        scan_kernel<E, V, O, false><<<g, b, 0, s>>>(a, pieces);
     }
 }
 
 hipError_t launch_scan(const ScanArgs &a, bool grad, bool f32, hipStream_t s)
 {
-    if (f32) scan_by<float, 2>(a, grad, s);
-    else scan_by<uint16_t, 4>(a, grad, s);
+    // a wavefront's envs, at most 64, from its first one on
+    const int64_t ld = std::max({a.ld_gate, a.ld_x, a.ld_h, a.ld_dh, a.ld_dgate, a.ld_dx});
+    const bool near = (63 * ld + a.d) * 4 < ((int64_t)1 << 32);
+    if (f32) near ? scan_by<float, 2, 2, uint32_t>(a, grad, s) : scan_by<float, 2, 2, int64_t>(a, grad, s);
+    else near ? scan_by<uint16_t, 4, 2, uint32_t>(a, grad, s) : scan_by<uint16_t, 4, 2, int64_t>(a, grad, s);
     return hipGetLastError();
 }
 

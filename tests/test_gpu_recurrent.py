@@ -1,5 +1,7 @@
 """The blocks of a recurrent policy on the GPU: 8-bit matrices, root-mean-square norm, products
 in 8 bits, gated scan and their gradients, against plain forms in 64 bits."""
+import zlib
+
 import numpy as np
 import pytest
 
@@ -15,7 +17,7 @@ DT = {"f32": torch.float32, "bf16": torch.bfloat16}
 
 def _gen(*key):
     g = torch.Generator()
-    g.manual_seed(abs(hash(key)) % (1 << 31))
+    g.manual_seed(zlib.crc32(repr(key).encode()))
     return g
 
 
