@@ -22,6 +22,7 @@
 namespace im {
 
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
@@ -72,12 +73,24 @@ __device__ __forceinline__ void meet()
     asm volatile("" ::: "memory");
 }
 
+__device__ __forceinline__ i32x8_t join(u32x4_r lo, u32x4_r hi)
+{
+    return i32x8_t{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+}
+
 // acc += (a 2^(sa - 127)) (b 2^(sb - 127)) over 64 k.  A lane holds 32 bytes of one row of each
 // operand, its k by the half of the wavefront; both operands are read alike, so that which k is
 // of no matter, and a row has one scale over all 128 k of a block.
 __device__ __forceinline__ f32x16_t mfma8(i32x8_t a, i32x8_t b, f32x16_t acc, int sa, int sb)
 {
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc, 0, 0, 0, sa, 0, sb);
+}
+
+// The same of 16 rows each and 128 k, 32 bytes of a row in each of its four lanes; sa in byte A.
+template <int A>
+__device__ __forceinline__ f32x4_t mfma8_16(i32x8_t a, i32x8_t b, f32x4_t acc, int sa, int sb)
+{
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 0, 0, A, sa, 0, sb);
 }
 
 // Eight e4m3 values times the scale's power of two as bf16: exact, but for values below 2^-126.
@@ -184,8 +197,7 @@ __global__ __launch_bounds__(S::NT, 2) void linear8_tile_kernel(Linear8Args a, i
         return *(const u32x4_r *)(at + r * 128 + (((2 * s + (lane >> 5)) << 4) ^ perm));
     };
     auto frag = [&](const char *at, int row, int s) {
-        const u32x4_r lo = piece(at, row, 2 * s), hi = piece(at, row, 2 * s + 1);
-        return i32x8_t{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+        return join(piece(at, row, 2 * s), piece(at, row, 2 * s + 1));
     };
     f32x16_t acc[TP][TQ];
 #pragma unroll
@@ -298,6 +310,234 @@ __global__ __launch_bounds__(S::NT, 2) void linear8_tile_kernel(Linear8Args a, i
     }
 }
 
+// ---------------------------------------------------------------------------
+// Panels.  With many rows and a k that fits, a block keeps 128 columns of P, all their k, in LDS
+// and its wavefronts walk over the rows of Q by themselves, 64 at a time, without a barrier: Q's
+// fragments come straight into registers, a step of 128 k ahead, also across the end of a tile, so
+// that one wavefront's outputs leave while others multiply.  A block for each CU; the panels
+// of one run of rows are neighbours in an L2.  Bias is where the sums start.
+//
+// A wavefront's tile is 128 p x 64 q in MFMA tiles of 16 x 16 (v_mfma_scale_f32_16x16x128_f8f6f4,
+// v_mfma_f32_16x16x32_bf16): four lanes then hold one row of Q, and a load takes 64 bytes of each
+// of 16 rows.
+// ---------------------------------------------------------------------------
+constexpr int PANEL_STEPS = 9, PANEL_WAVES = 8, PANEL_ROWS = 64;
+template <bool WIDE>
+__global__ __launch_bounds__(64 * PANEL_WAVES, 1) void linear8_panel_kernel(Linear8Args a, int panels, int streams)
+{
+    constexpr int TP = 8, TQ = PANEL_ROWS / 16, SETS = 2;
+    __shared__ __attribute__((aligned(1024))) char lds[PANEL_STEPS * 16384];
+    __shared__ int pscale[PANEL_STEPS][16][2];      // byte i % 4 of word i / 4: row 16 i + lane's
+    __shared__ float bias[128];
+    const int lane = threadIdx.x & 63, wave = wave_id(), l16 = lane & 15, grp = lane >> 4;
+    const int place = blockIdx.x >> 3, panel = place % panels;
+    const int stream = place / panels * 8 + (blockIdx.x & 7);
+    if (place / panels * 8 >= streams) return;
+    const int64_t p0 = (int64_t)panel * 128;
+    const int steps = (int)a.steps;
+    for (int u = wave; u < steps * 16; u += PANEL_WAVES) {
+        const int r = (u & 15) * 8 + lane / 8, c = (lane & 7) ^ (r >> 1 & 7);
+        const int64_t row = min(p0 + r, a.out - 1);
+        copy_to_lds(a.p.q + row * a.p.ld_q + (u >> 4) * 128 + c * 16, lds + u * 1024);
+    }
+    for (int u = threadIdx.x; u < steps * 32; u += 64 * PANEL_WAVES) {
+        int v = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t row = min(p0 + 64 * (u & 1) + 16 * i + (u >> 1 & 15), a.out - 1);
+            v |= a.p.scale[(row >> a.p.shift) * a.p.ld_scale + (u >> 5)] << (8 * i);
+        }
+        pscale[u >> 5][u >> 1 & 15][u & 1] = v;
+    }
+    // columns past the last are copies of it, which leave their rows' largest magnitudes as they are
+    if (threadIdx.x < 128) bias[threadIdx.x] = a.bias ? a.bias[min(p0 + threadIdx.x, a.out - 1)] : 0.0f;
+    wait_loads<0>();
+    __syncthreads();
+
+    const int64_t tiles = (a.n + PANEL_ROWS - 1) / PANEL_ROWS, stride = (int64_t)streams * PANEL_WAVES;
+    int64_t tile = (int64_t)stream * PANEL_WAVES + wave;
+    if (tile >= tiles) return;
+    // Q: bytes 32 grp .. 32 grp + 31 of a step of the rows 16 j + l16, and the row's scale
+    u32x4_r bq[SETS][TQ][2];
+    int sq[SETS];                  // of row `lane`
+    // part j of step kt of tile t; rows past the last read the last one: their sums are not stored
+    auto fetch = [&](int set, int64_t t, int kt, int j) {
+        const int64_t q0 = t * PANEL_ROWS;
+        const int last = (int)min((int64_t)PANEL_ROWS, a.n - q0) - 1;
+        const uint8_t *base = a.q.q + q0 * a.q.ld_q + kt * 128;
+        const uint32_t off = (uint32_t)min(16 * j + l16, last) * (uint32_t)a.q.ld_q + grp * 32;
+        bq[set][j][0] = *(const u32x4_r *)(base + off);
+        bq[set][j][1] = *(const u32x4_r *)(base + off + 16);
+        if (j == 0) sq[set] = a.q.scale[((q0 + min(lane, last)) >> a.q.shift) * a.q.ld_scale + kt];
+    };
+    f32x4_t acc[TP][TQ];
+    auto start = [&] {
+#pragma unroll
+        for (int i = 0; i < TP; ++i) {
+            const f32x4_t b = *(const f32x4_t *)(bias + 16 * i + 4 * grp);
+#pragma unroll
+            for (int j = 0; j < TQ; ++j) acc[i][j] = b;
+        }
+    };
+    // a step's products; more(i): work beside those of the i-th tile of P
+    auto multiply = [&](int set, int kt, auto more) {
+        const char *st = lds + kt * 16384;
+        const int sp[2] = {pscale[kt][l16][0], pscale[kt][l16][1]};
+        // the scale of row 16 j + l16 in all four lanes of the row
+        const auto x = __builtin_amdgcn_permlane16_swap(sq[set], sq[set], false, false);
+        const auto even = __builtin_amdgcn_permlane32_swap(x[0], x[0], false, false);
+        const auto odd = __builtin_amdgcn_permlane32_swap(x[1], x[1], false, false);
+        const int s4[4] = {(int)even[0], (int)odd[0], (int)even[1], (int)odd[1]};
+        // piece c of a row at c ^ (row / 2 mod 8)
+        auto piece = [&](int i, int k) {
+            return *(const u32x4_r *)(st + (16 * i + l16) * 128 + (((2 * grp + k) ^ (l16 >> 1)) << 4));
+        };
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {      // eight bytes of each of a row's four lanes
+                bf16x8_t fq[TQ];
+#pragma unroll
+                for (int j = 0; j < TQ; ++j)
+                    fq[j] = widen8(bq[set][j][k / 2][k % 2 * 2], bq[set][j][k / 2][k % 2 * 2 + 1],
+                                   __uint_as_float((uint32_t)s4[j] << 23));
+#pragma unroll
+                for (int i = 0; i < TP; ++i) {
+                    const u32x2_r b = *(const u32x2_r *)(st + (16 * i + l16) * 128 +
+                                                         (((2 * grp + k / 2) ^ (l16 >> 1)) << 4) + k % 2 * 8);
+                    const bf16x8_t fp = widen8(b[0], b[1], __uint_as_float((uint32_t)(sp[i / 4] >> (8 * (i % 4)) & 255) << 23));
+                    if (k == 3) more(i);
+#pragma unroll
+                    for (int j = 0; j < TQ; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp, fq[j], acc[i][j], 0, 0, 0);
+                    if (i % 2) __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < TP; ++i) {
+                const i32x8_t fp = join(piece(i, 0), piece(i, 1));
+                more(i);
+#pragma unroll
+                for (int j = 0; j < TQ; ++j) {
+                    const i32x8_t fq = join(bq[set][j][0], bq[set][j][1]);
+                    if (i % 4 == 0) acc[i][j] = mfma8_16<0>(fp, fq, acc[i][j], sp[i / 4], s4[j]);
+                    if (i % 4 == 1) acc[i][j] = mfma8_16<1>(fp, fq, acc[i][j], sp[i / 4], s4[j]);
+                    if (i % 4 == 2) acc[i][j] = mfma8_16<2>(fp, fq, acc[i][j], sp[i / 4], s4[j]);
+                    if (i % 4 == 3) acc[i][j] = mfma8_16<3>(fp, fq, acc[i][j], sp[i / 4], s4[j]);
+                }
+            }
+        }
+    };
+    // A lane's sums of a 16 x 16 tile are p = 4 grp + 0..3 of one q.  Lanes of a row exchange theirs
+    // across tiles, so that each has 16 bytes of neighbouring p to store, 64 a row.
+    auto store = [&](int64_t t) {
+#pragma unroll
+        for (int j = 0; j < TQ; ++j) {
+            const int64_t row = t * PANEL_ROWS + 16 * j + l16;
+            const bool on = row < a.n;
+            if (a.relu)
+#pragma unroll
+                for (int i = 0; i < TP; ++i)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) acc[i][j][k] = acc[i][j][k] < 0.0f ? 0.0f : acc[i][j][k];   // NaN stays
+            if (WIDE && a.y8.q) {
+                uint32_t top = 0;
+#pragma unroll
+                for (int i = 0; i < TP; ++i)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) top = max(top, magnitude(acc[i][j][k]));
+                top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+                top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+                const int s = block8_scale(top);
+                if (on && grp == 0) a.y8.scale[row * a.y8.ld_scale + panel] = (uint8_t)s;
+#pragma unroll
+                for (int i = 0; i < TP; i += 4) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int h = 0; h < 4; h += 2) {
+                        float v[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) v[k] = acc[i + h + k / 4][j][k % 4];
+                        const u32x2_r b = block8_pack(v, s, 8);
+                        w[h] = b[0], w[h + 1] = b[1];
+                    }
+                    const auto x0 = __builtin_amdgcn_permlane16_swap(w[0], w[1], false, false);
+                    const auto x1 = __builtin_amdgcn_permlane16_swap(w[2], w[3], false, false);
+                    const auto y0 = __builtin_amdgcn_permlane32_swap(x0[0], x1[0], false, false);
+                    const auto y1 = __builtin_amdgcn_permlane32_swap(x0[1], x1[1], false, false);
+                    u32x4_r b = {y0[0], y1[0], y0[1], y1[1]};
+                    const int64_t col = p0 + 16 * i + 16 * grp;
+                    // columns past the last are zeros
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int nv = (int)min((int64_t)4, a.out - col - 4 * k);
+                        b[k] = nv >= 4 ? b[k] : nv <= 0 ? 0 : b[k] & ((1u << (8 * nv)) - 1);
+                    }
+                    if (on) *(u32x4_r *)(a.y8.q + row * a.y8.ld_q + col) = b;
+                }
+            }
+            if (!a.y) continue;
+            if (WIDE && a.y_f32) {
+#pragma unroll
+                for (int i = 0; i < TP; ++i) {
+                    const int64_t col = p0 + 16 * i + 4 * grp;
+                    float *y = (float *)a.y + row * a.ld_y + col;
+                    if (on && col + 4 <= a.out) {
+                        *(f32x4_a4 *)y = acc[i][j];
+                    } else if (on) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (col + k < a.out) y[k] = acc[i][j][k];
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < TP; i += 2) {
+                    uint32_t w[2][2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) w[h][k] = pack_bf16x2(acc[i + h][j][2 * k], acc[i + h][j][2 * k + 1]);
+                    const auto x0 = __builtin_amdgcn_permlane16_swap(w[0][0], w[1][0], false, false);
+                    const auto x1 = __builtin_amdgcn_permlane16_swap(w[0][1], w[1][1], false, false);
+                    const int64_t col = p0 + 16 * i + (grp & 1) * 16 + (grp >> 1) * 8;
+                    if (on) store8_bits((uint16_t *)a.y + row * a.ld_y + col, (int)min((int64_t)8, a.out - col),
+                                        u32x4_r{x0[0], x1[0], x0[1], x1[1]});
+                }
+            }
+        }
+    };
+    // the step that is fetched next, SETS - 1 ahead
+    int kt = 0, next_kt = 0;
+    int64_t next_tile = tile;
+    auto advance = [&] {
+        if (++next_kt == steps) next_kt = 0, next_tile += stride;
+        if (next_tile >= tiles) next_tile = tile;      // after the last step: read again, not used
+    };
+#pragma unroll
+    for (int set = 0; set < SETS - 1; ++set) {
+#pragma unroll
+        for (int j = 0; j < TQ; ++j) fetch(set, next_tile, next_kt, j);
+        advance();
+    }
+    while (true) {
+#pragma unroll
+        for (int set = 0; set < SETS; ++set) {
+            if (kt == 0) start();
+            multiply(set, kt, [&](int i) {
+                if (i < TQ) fetch((set + SETS - 1) % SETS, next_tile, next_kt, i);
+            });
+            advance();
+            if (++kt == steps) {
+                store(tile);
+                kt = 0;
+                tile += stride;
+                if (tile >= tiles) return;
+            }
+        }
+    }
+}
+
 // Parts of a product to y, in their order.
 __global__ __launch_bounds__(256) void linear8_join_kernel(Linear8Args a)
 {
@@ -345,6 +585,14 @@ hipError_t launch_linear8(const Linear8Args &a, hipStream_t s)
         tile_by<Tile128>(a, s);
         linear8_join_kernel<<<dim3((unsigned)std::min<int64_t>(ceil_div(a.n * ceil_div(a.out, 4), 256), 256 * 16)),
                               dim3(256), 0, s>>>(a);
+        return hipGetLastError();
+    }
+    const int64_t panels = ceil_div(a.out, 128);
+    if (a.n >= 16384 && a.steps <= PANEL_STEPS && panels <= 32 && a.q.ld_q < (1 << 24)) {
+        const int streams = 8 * (int)(32 / panels);
+        const dim3 g(256), b(64 * PANEL_WAVES);
+        if (wide(a)) linear8_panel_kernel<true><<<g, b, 0, s>>>(a, (int)panels, streams);
+        else linear8_panel_kernel<false><<<g, b, 0, s>>>(a, (int)panels, streams);
         return hipGetLastError();
     }
     // parts of rows with fewer than 2^21 tiles of 128 x 128

@@ -18,11 +18,22 @@ namespace im {
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 constexpr int KEEP = IM_SCAN_KEEP;
+constexpr int64_t INFINITY_CACHE = 256 << 20;
+
+// Values of a thread.  bf16 32 x 16384 x 256 forward with 8, 4, 2: 195, 212, 181 us; fp32 32 x 8192 x
+// 256 with 4, 2: 208, 182 us; the gradients' registers hold 16 steps of 2 values.
+constexpr int SCAN_V = 2;
 
 // V values of a row as words, at any address of their element's alignment.  The last piece of a
 // row whose width is no multiple of V takes the last V values of the row: `lo` of them belong
 // to the piece before, which alone stores them.  Rows of fewer than V values: value by value.
-template <typename E, int V>
+// What a launch does: a chunk's map alone; a chunk's steps; all steps, arrays that no cache holds
+// (their loads and stores are marked as such: 32 x 16384 x 256 bf16 forward 181 -> 165 us, the
+// gradient 330 -> 290; the chunks' second launch reads what the first one left in the caches, and
+// takes 108 us for 95 if marked).
+enum { MAP, STEPS, STREAM };
+
+template <typename E, int V, int MODE>
 struct StepPiece {
     static constexpr int BYTES = sizeof(E) * V;
     typedef uint32_t word_t __attribute__((ext_vector_type(BYTES / 4)));
@@ -39,7 +50,7 @@ struct StepPiece {
     // p: the address of column `at`
     __device__ __forceinline__ word_t load(const E *p) const
     {
-        if (hi == V) return *(const at_t *)p;
+        if (hi == V) return MODE == STREAM ? __builtin_nontemporal_load((const at_t *)p) : *(const at_t *)p;
         word_t r = {};
 #pragma unroll
         for (int k = 0; k < V; ++k)
@@ -68,7 +79,8 @@ struct StepPiece {
             for (int k = 0; k < V / 2; ++k) w[k] = pack_bf16x2(v[2 * k], v[2 * k + 1]);
         }
         if (lo == 0 && hi == V) {
-            *(at_t *)p = w;
+            if constexpr (MODE == STREAM) __builtin_nontemporal_store(w, (at_t *)p);
+            else *(at_t *)p = w;
         } else {
 #pragma unroll
             for (int k = 0; k < V; ++k)
@@ -151,10 +163,10 @@ struct Ends {
 // ---------------------------------------------------------------------------
 // A chunk's steps forward.  MAP: its map alone, from gate and x.
 // ---------------------------------------------------------------------------
-template <typename E, int V, typename O, bool MAP>
+template <typename E, int V, typename O, int MODE>
 __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, int64_t pieces)
 {
-    typedef StepPiece<E, V> P;
+    typedef StepPiece<E, V, MODE> P;
     constexpr int U = KEEP / 2;      // steps whose loads are in flight together
     const int64_t id = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
     if (id >= a.n * pieces) return;
@@ -174,7 +186,7 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, int64_t pieces)
     float c[V], p[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) c[k] = 0.0f, p[k] = 1.0f;
-    if constexpr (!MAP) {
+    if constexpr (MODE != MAP) {
         const float *from = a.chunks > 1 ? a.maps + chunk * 2 * a.n * a.d : a.state;
         if (from)
 #pragma unroll
@@ -203,13 +215,13 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, int64_t pieces)
                 float ga, gb;
                 gates(g[k], ga, gb);
                 c[k] = fmaf(ga, c[k], gb * v[k]);
-                if constexpr (MAP) p[k] = p[k] < 0.0f ? p[k] : p[k] * ga;
+                if constexpr (MODE == MAP) p[k] = p[k] < 0.0f ? p[k] : p[k] * ga;
             }
-            if constexpr (!MAP) pc.store(h[t + u], c);
+            if constexpr (MODE != MAP) pc.store(h[t + u], c);
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 c[k] = end >> u & 1 ? 0.0f : c[k];
-                if constexpr (MAP) p[k] = end >> u & 1 ? -1.0f : p[k];
+                if constexpr (MODE == MAP) p[k] = end >> u & 1 ? -1.0f : p[k];
             }
         }
     };
@@ -221,7 +233,7 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, int64_t pieces)
     for (int64_t t = t0; t < t1; t += KEEP) {
         const uint32_t end = next;
         if (t + U < t1) fetch(1, t + U);
-        if (!MAP && a.keep)
+        if (MODE != MAP && a.keep)
 #pragma unroll
             for (int k = 0; k < V; ++k)
                 if (k >= pc.lo && k < pc.hi) a.keep[t / KEEP * a.n * a.d + row + pc.at + k] = c[k];
@@ -233,7 +245,7 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, int64_t pieces)
         }
         walk(1, t + U, end >> U);
     }
-    if constexpr (MAP) {
+    if constexpr (MODE == MAP) {
         float *m = a.maps + chunk * 2 * a.n * a.d + row;
 #pragma unroll
         for (int k = 0; k < V; ++k)
@@ -251,10 +263,10 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, int64_t pieces)
 // kept one, and with them what G is multiplied by, which takes the place of gate and x in
 // registers.  MAP: the chunk's map of D alone, from gate and dh.
 // ---------------------------------------------------------------------------
-template <typename E, int V, typename O, bool MAP>
-__global__ __launch_bounds__(256) void scan_grad_kernel(ScanArgs a, int64_t pieces)
+template <typename E, int V, typename O, int MODE>
+__global__ __launch_bounds__(256, sizeof(E) == 2 ? 3 : 2) void scan_grad_kernel(ScanArgs a, int64_t pieces)
 {
-    typedef StepPiece<E, V> P;
+    typedef StepPiece<E, V, MODE> P;
     const int64_t id = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
     if (id >= a.n * pieces) return;
     const int64_t env = id / pieces, chunk = blockIdx.y;
@@ -275,7 +287,7 @@ __global__ __launch_bounds__(256) void scan_grad_kernel(ScanArgs a, int64_t piec
     float D[V], p[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) D[k] = 0.0f, p[k] = 1.0f;
-    if constexpr (!MAP) {
+    if constexpr (MODE != MAP) {
         const float *from = a.chunks > 1 ? a.maps + chunk * 2 * a.n * a.d : a.state;
         if (from)
 #pragma unroll
@@ -289,7 +301,7 @@ __global__ __launch_bounds__(256) void scan_grad_kernel(ScanArgs a, int64_t piec
         for (int u = 0; u < KEEP; ++u) {
             const int64_t q = t + min(u, steps - 1);
             wg[u] = pc.load(gate[q]);
-            if constexpr (!MAP) wx[u] = pc.load(x[q]);
+            if constexpr (MODE != MAP) wx[u] = pc.load(x[q]);
         }
 #pragma unroll
         for (int u = 0; u < KEEP; ++u) wd[u] = pc.load(dh[t + min(u, steps - 1)]);
@@ -298,16 +310,16 @@ __global__ __launch_bounds__(256) void scan_grad_kernel(ScanArgs a, int64_t piec
         float c[V];
 #pragma unroll
         for (int k = 0; k < V; ++k)
-            c[k] = !MAP && k < pc.hi ? a.keep[t / KEEP * a.n * a.d + row + pc.at + k] : 0.0f;
+            c[k] = MODE != MAP && k < pc.hi ? a.keep[t / KEEP * a.n * a.d + row + pc.at + k] : 0.0f;
 #pragma unroll
         for (int u = 0; u < KEEP; ++u) {
             float g[V], v[V];
             P::unpack(wg[u], g);
-            if constexpr (!MAP) P::unpack(wx[u], v);
+            if constexpr (MODE != MAP) P::unpack(wx[u], v);
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 gates(g[k], ga[u][k], gb[u][k]);
-                if constexpr (!MAP) {
+                if constexpr (MODE != MAP) {
                     diff[u][k] = c[k] - v[k];
                     c[k] = end >> u & 1 ? 0.0f : fmaf(ga[u][k], c[k], gb[u][k] * v[k]);
                 }
@@ -322,20 +334,20 @@ __global__ __launch_bounds__(256) void scan_grad_kernel(ScanArgs a, int64_t piec
             for (int k = 0; k < V; ++k) {
                 const float G = d[k] + (end >> u & 1 ? 0.0f : D[k]);
                 D[k] = ga[u][k] * G;
-                if constexpr (MAP) {
+                if constexpr (MODE == MAP) {
                     p[k] = end >> u & 1 || p[k] < 0.0f ? -1.0f : ga[u][k] * p[k];
                 } else {
                     ox[k] = gb[u][k] * G;
                     og[k] = ga[u][k] * diff[u][k] * ox[k];
                 }
             }
-            if constexpr (!MAP) {
+            if constexpr (MODE != MAP) {
                 pc.store(dgate[t + u], og);
                 pc.store(dx[t + u], ox);
             }
         }
     }
-    if constexpr (MAP) {
+    if constexpr (MODE == MAP) {
         float *m = a.maps + chunk * 2 * a.n * a.d + row;
 #pragma unroll
         for (int k = 0; k < V; ++k)
@@ -349,18 +361,20 @@ __global__ __launch_bounds__(256) void scan_grad_kernel(ScanArgs a, int64_t piec
 
 // ---------------------------------------------------------------------------
 // From the chunks' maps the state before each chunk (BACK: the gradient after it), left in the
-// place of the maps' P: 64 values a block, wavefront w composes a sixteenth of the chunks, the
-// wavefronts' maps meet in LDS, and each then walks its own chunks.
+// place of the maps' P.  A block has 16 values; each 16 lanes compose a 64th of the chunks, the
+// maps of a wavefront's four parts meet by shuffles, those of the wavefronts in LDS, and each part
+// then walks its own chunks.  512 chunks of 722 values: 64 values a block and a part for each
+// wavefront took 11.5 us, 17.6 with a part's maps held in registers.
 // ---------------------------------------------------------------------------
-constexpr int COMPOSE_WAVES = 16;
+constexpr int COMPOSE_WAVES = 16, COMPOSE_VALUES = 16;
 template <bool BACK>
 __global__ __launch_bounds__(64 * COMPOSE_WAVES) void compose_kernel(ScanArgs a)
 {
-    __shared__ float lp[COMPOSE_WAVES][64], ls[COMPOSE_WAVES][64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t all = a.n * a.d, v = (int64_t)blockIdx.x * 64 + lane;
-    const int64_t per = (a.chunks + COMPOSE_WAVES - 1) / COMPOSE_WAVES;
-    const int64_t first = min(w * per, a.chunks), last = min(first + per, a.chunks);
+    __shared__ float lp[COMPOSE_WAVES][COMPOSE_VALUES], ls[COMPOSE_WAVES][COMPOSE_VALUES];
+    const int at = threadIdx.x & 15, part = threadIdx.x >> 4, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int64_t all = a.n * a.d, v = (int64_t)blockIdx.x * COMPOSE_VALUES + at;
+    const int64_t per = (a.chunks + 4 * COMPOSE_WAVES - 1) / (4 * COMPOSE_WAVES);
+    const int64_t first = min(part * per, a.chunks), last = min(first + per, a.chunks);
     const bool on = v < all;
     auto apply = [](float mp, float ms, float c) { return mp < 0.0f ? ms : fmaf(mp, c, ms); };
     auto map = [&](int64_t i) { return a.maps + (BACK ? a.chunks - 1 - i : i) * 2 * all + v; };
@@ -373,11 +387,22 @@ __global__ __launch_bounds__(64 * COMPOSE_WAVES) void compose_kernel(ScanArgs a)
             s = apply(mp, ms, s);
             p = mp < 0.0f || p < 0.0f ? -1.0f : p * mp;
         }
-    lp[w][lane] = p;
-    ls[w][lane] = s;
+    // of this part and those before it in the wavefront
+#pragma unroll
+    for (int d = 16; d < 64; d *= 2) {
+        const float bp = __shfl_up(p, d), bs = __shfl_up(s, d);
+        if (lane >= d) {
+            s = apply(p, s, bs);
+            p = p < 0.0f || bp < 0.0f ? -1.0f : p * bp;
+        }
+    }
+    if (lane >= 48) lp[w][at] = p, ls[w][at] = s;
     __syncthreads();
     float c = on && a.state ? a.state[v] : 0.0f;
-    for (int k = 0; k < w; ++k) c = apply(lp[k][lane], ls[k][lane], c);
+    for (int k = 0; k < w; ++k) c = apply(lp[k][at], ls[k][at], c);
+    // the parts before this one
+    const float bp = __shfl_up(p, 16), bs = __shfl_up(s, 16);
+    if (lane >= 16) c = apply(bp, bs, c);
     if (on)
 #pragma unroll 8
         for (int64_t i = first; i < last; ++i) {
@@ -398,27 +423,28 @@ int64_t scan_chunk(int64_t T, int64_t n, int64_t d)
     return std::max<int64_t>(chunk, ceil_div(ceil_div(T, 65535), KEEP) * KEEP);
 }
 
-// V: values of a thread forward, W: backward.
-template <typename E, int V, int W, typename O>
+template <typename E, typename O, int MODE>
+static void scan_launch(const ScanArgs &a, bool grad, dim3 g, dim3 b, int64_t pieces, hipStream_t s)
+{
+    if (grad) scan_grad_kernel<E, SCAN_V, O, MODE><<<g, b, 0, s>>>(a, pieces);
+    else scan_kernel<E, SCAN_V, O, MODE><<<g, b, 0, s>>>(a, pieces);
+}
+
+template <typename E, typename O>
 static void scan_by(const ScanArgs &a, bool grad, hipStream_t s)
 {
-    const int64_t pieces = ceil_div(a.d, grad ? W : V);
+    const int64_t pieces = ceil_div(a.d, SCAN_V);
     // chunks of few envs leave less of a small block idle
     const dim3 b(a.chunks > 1 ? 64 : 256), g((unsigned)ceil_div(a.n * pieces, b.x), (unsigned)a.chunks);
-    const dim3 gc((unsigned)ceil_div(a.n * a.d, 64)), bc(64 * COMPOSE_WAVES);
-    if (grad) {
-        if (a.chunks > 1) {
-            scan_grad_kernel<E, W, O, true><<<g, b, 0, s>>>(a, pieces);
-            compose_kernel<true><<<gc, bc, 0, s>>>(a);
-        }
-        scan_grad_kernel<E, W, O, false><<<g, b, 0, s>>>(a, pieces);
-    } else {
-        if (a.chunks > 1) {
-            scan_kernel<E, V, O, true><<<g, b, 0, s>>>(a, pieces);
-            compose_kernel<false><<<gc, bc, 0, s>>>(a);
-        }
-        scan_kernel<E, V, O, false><<<g, b, 0, s>>>(a, pieces);
+    if (a.chunks > 1) {
+        const dim3 gc((unsigned)ceil_div(a.n * a.d, COMPOSE_VALUES)), bc(64 * COMPOSE_WAVES);
+        scan_launch<E, O, MAP>(a, grad, g, b, pieces, s);
+        if (grad) compose_kernel<true><<<gc, bc, 0, s>>>(a);
+        else compose_kernel<false><<<gc, bc, 0, s>>>(a);
     }
+    const int64_t bytes = a.T * a.n * a.d * (int64_t)sizeof(E) * (grad ? 5 : 3);
+    if (a.chunks == 1 && bytes > INFINITY_CACHE) scan_launch<E, O, STREAM>(a, grad, g, b, pieces, s);
+    else scan_launch<E, O, STEPS>(a, grad, g, b, pieces, s);
 }
 
 hipError_t launch_scan(const ScanArgs &a, bool grad, bool f32, hipStream_t s)
@@ -426,8 +452,8 @@ hipError_t launch_scan(const ScanArgs &a, bool grad, bool f32, hipStream_t s)
     // a wavefront's envs, at most 64, from its first one on
     const int64_t ld = std::max({a.ld_gate, a.ld_x, a.ld_h, a.ld_dh, a.ld_dgate, a.ld_dx});
     const bool near = (63 * ld + a.d) * 4 < ((int64_t)1 << 32);
-    if (f32) near ? scan_by<float, 2, 2, uint32_t>(a, grad, s) : scan_by<float, 2, 2, int64_t>(a, grad, s);
-    else near ? scan_by<uint16_t, 4, 2, uint32_t>(a, grad, s) : scan_by<uint16_t, 4, 2, int64_t>(a, grad, s);
+    if (f32) near ? scan_by<float, uint32_t>(a, grad, s) : scan_by<float, int64_t>(a, grad, s);
+    else near ? scan_by<uint16_t, uint32_t>(a, grad, s) : scan_by<uint16_t, int64_t>(a, grad, s);
     return hipGetLastError();
 }
 

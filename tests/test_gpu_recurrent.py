@@ -224,7 +224,8 @@ def _pair(x, rows, **k):
 
 
 SIZES = [(1, 1, 1), (1, 361, 1024), (3, 128, 5), (33, 129, 69), (64, 512, 130), (128, 256, 128), (129, 640, 127),
-         (300, 77, 260), (513, 1024, 384), (1000, 1100, 200), (31, 2500, 33)]
+         (300, 77, 260), (513, 1024, 384), (1000, 1100, 200), (31, 2500, 33),
+         (16384, 40, 300), (17001, 1100, 69)]
 
 
 @pytest.mark.parametrize("n,i,o", SIZES)
