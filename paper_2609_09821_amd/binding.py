@@ -149,7 +149,7 @@ class ImRms(C.Structure):
                 ("x", C.c_void_p), ("ld_x", C.c_int64), ("residual", C.c_void_p),
                 ("ld_residual", C.c_int64), ("gamma", C.c_void_p), ("h", C.c_void_p),
                 ("ld_h", C.c_int64), ("y", C.c_void_p), ("ld_y", C.c_int64),
-                ("y8", C.POINTER(ImBlock8)), ("rstd", C.c_void_p)]
+                ("y8", C.c_void_p), ("rstd", C.c_void_p)]
 
 
 class ImRmsGrad(C.Structure):
@@ -162,15 +162,15 @@ class ImRmsGrad(C.Structure):
 
 class ImLayer8(C.Structure):
     _fields_ = [("n", C.c_int64), ("in_", C.c_int64), ("out", C.c_int64), ("y_dtype", C.c_int32),
-                ("relu", C.c_int32), ("x", C.POINTER(ImBlock8)), ("w", C.POINTER(ImBlock8)),
+                ("relu", C.c_int32), ("x", C.c_void_p), ("w", C.c_void_p),
                 ("bias", C.c_void_p), ("y", C.c_void_p), ("ld_y", C.c_int64),
-                ("y8", C.POINTER(ImBlock8))]
+                ("y8", C.c_void_p)]
 
 
 class ImLayer8Grad(C.Structure):
     _fields_ = [("n", C.c_int64), ("in_", C.c_int64), ("out", C.c_int64), ("dtype", C.c_int32),
                 ("dy", C.c_void_p), ("ld_dy", C.c_int64), ("y", C.c_void_p), ("ld_y", C.c_int64),
-                ("xt", C.POINTER(ImBlock8)), ("wt", C.POINTER(ImBlock8)), ("dx", C.c_void_p),
+                ("xt", C.c_void_p), ("wt", C.c_void_p), ("dx", C.c_void_p),
                 ("ld_dx", C.c_int64), ("dw", C.c_void_p), ("ld_dw", C.c_int64), ("db", C.c_void_p),
                 ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
 
@@ -1054,19 +1054,27 @@ class Block8:
         return self.q.shape[0], self.d
 
     def struct(self, n, d, dev, name):
+        q, scale, rows, blocks = self.q, self.scale, self.rows, (d + IM_BLOCK8 - 1) // IM_BLOCK8
         if self.d != d:
             raise ValueError("%s holds rows of %d values, not of %d" % (name, self.d, d))
-        if self.rows != 1 and self.rows != IM_BLOCK8:
+        if rows != 1 and rows != IM_BLOCK8:
             raise ValueError("%s: rows must be 1 or 128" % name)
-        blocks = -(-d // IM_BLOCK8)
-        return ImBlock8(self.q.data_ptr(), self.scale.data_ptr(),
-                        _ld(self.q, n, blocks * IM_BLOCK8, name + ".q", dev, _torch.float8_e4m3fn),
-                        _ld(self.scale, -(-n // self.rows), blocks, name + ".scale", dev,
-                            _torch.uint8), self.rows)
+        return ImBlock8(q.data_ptr(), scale.data_ptr(),
+                        _row(q, n, blocks * IM_BLOCK8, name + ".q", dev, _torch.float8_e4m3fn),
+                        _row(scale, n if rows == 1 else -(-n // rows), blocks, name + ".scale", dev,
+                             _torch.uint8), rows)
 
 
-def _block8(b, n, d, dev, name):
-    return None if b is None else C.pointer(b.struct(n, d, dev, name))
+def _row(t, n, d, name, dev, dtype):
+    """_ld, with the usual case decided by few calls into torch."""
+    if t.dtype is dtype and t.shape == (n, d) and t.is_contiguous() and t.get_device() == dev:
+        return d
+    return _ld(t, n, d, name, dev, dtype)
+
+
+def _at(struct):
+    """A struct's address for the call that holds it."""
+    return None if struct is None else C.addressof(struct)
 
 
 def block8_store(x, c=None, t=None, stream=None):
@@ -1074,21 +1082,22 @@ def block8_store(x, c=None, t=None, stream=None):
     into the Block8 t (of [d][n]); either may be None."""
     dev, raw = _call_stream(stream)
     n, d = x.shape
-    im_block_store(x.data_ptr(), _ld(x, n, d, "x", dev), _dtype(x), n, d,
-                    _block8(c, n, d, dev, "c"), _block8(t, d, n, dev, "t"), raw)
+    im_block_store(x.data_ptr(), _row(x, n, d, "x", dev, x.dtype), _dtype(x), n, d,
+                   None if c is None else C.byref(c.struct(n, d, dev, "c")),
+                   None if t is None else C.byref(t.struct(d, n, dev, "t")), raw)
 
 
 def block8_load(c, x, stream=None):
     """The Block8's values into x (float32 or bfloat16 [n][d])."""
     dev, raw = _call_stream(stream)
     n, d = x.shape
-    im_block_load(_block8(c, n, d, dev, "c"), n, d, x.data_ptr(), _ld(x, n, d, "x", dev),
-                   _dtype(x), raw)
+    im_block_load(C.byref(c.struct(n, d, dev, "c")), n, d, x.data_ptr(),
+                  _row(x, n, d, "x", dev, x.dtype), _dtype(x), raw)
 
 
 def _opt(t, n, d, name, dev, dtype):
     """Pointer and row stride of a matrix that may be None."""
-    return (None, 0) if t is None else (t.data_ptr(), _ld(t, n, d, name, dev, dtype))
+    return (None, 0) if t is None else (t.data_ptr(), _row(t, n, d, name, dev, dtype))
 
 
 def rms_norm(x, gamma, y=None, rstd=None, eps=1e-6, residual=None, h=None, y8=None, stream=None):
@@ -1098,10 +1107,11 @@ def rms_norm(x, gamma, y=None, rstd=None, eps=1e-6, residual=None, h=None, y8=No
     dev, raw = _call_stream(stream)
     n, d = x.shape
     f32 = _torch.float32
-    im_rms_norm(ImRms(n, d, _dtype(x), eps, x.data_ptr(), _ld(x, n, d, "x", dev),
+    b8 = None if y8 is None else y8.struct(n, d, dev, "y8")
+    im_rms_norm(ImRms(n, d, _dtype(x), eps, x.data_ptr(), _row(x, n, d, "x", dev, x.dtype),
                       *_opt(residual, n, d, "residual", dev, x.dtype),
                       _vec(gamma, d, "gamma", dev, f32), *_opt(h, n, d, "h", dev, x.dtype),
-                      *_opt(y, n, d, "y", dev, x.dtype), _block8(y8, n, d, dev, "y8"),
+                      *_opt(y, n, d, "y", dev, x.dtype), _at(b8),
                       _vec(rstd, n, "rstd", dev, f32)), raw)
 
 
@@ -1132,11 +1142,12 @@ def linear8(x, w, bias, y=None, y8=None, relu=False, stream=None):
     float32 or None; y [n][out] float32 or bfloat16, and the Block8 y8: each if it is given."""
     dev, raw = _call_stream(stream)
     (n, in_), out = x.shape, w.shape[0]
-    yp, ldy = (None, 0) if y is None else (y.data_ptr(), _ld(y, n, out, "y", dev))
-    im_block_linear(ImLayer8(n, in_, out, IM_DTYPE_BF16 if y is None else _dtype(y), 1 if relu else 0,
-                        _block8(x, n, in_, dev, "x"), _block8(w, out, in_, dev, "w"),
-                        _vec(bias, out, "bias", dev, _torch.float32), yp, ldy,
-                        _block8(y8, n, out, dev, "y8")), raw)
+    yp, ldy = (None, 0) if y is None else (y.data_ptr(), _row(y, n, out, "y", dev, y.dtype))
+    sx, sw = x.struct(n, in_, dev, "x"), w.struct(out, in_, dev, "w")
+    b8 = None if y8 is None else y8.struct(n, out, dev, "y8")
+    im_block_linear(ImLayer8(n, in_, out, IM_DTYPE_BF16 if y is None else _dtype(y),
+                             1 if relu else 0, C.addressof(sx), C.addressof(sw),
+                             _vec(bias, out, "bias", dev, _torch.float32), yp, ldy, _at(b8)), raw)
 
 
 def linear8_grad_workspace(n, in_, out):
@@ -1162,18 +1173,21 @@ def linear8_grad(dy, xt, wt, dx=None, dw=None, db=None, y=None, workspace=None, 
     if n:
         _held, ws, nbytes = _workspace(workspace, lambda: linear8_grad_workspace(n, in_, out), dev,
                                        stream)
+    sx = None if dw is None or xt is None else xt.struct(in_, n, dev, "xt")
+    sw = None if dx is None or wt is None else wt.struct(in_, out, dev, "wt")
     im_block_linear_grad(
-        ImLayer8Grad(n, in_, out, _dtype(dy), dy.data_ptr(), _ld(dy, n, out, "dy", dev),
-                     *_opt(y, n, out, "y", dev, dy.dtype),
-                     None if dw is None else _block8(xt, in_, n, dev, "xt"),
-                     None if dx is None else _block8(wt, in_, out, dev, "wt"),
+        ImLayer8Grad(n, in_, out, _dtype(dy), dy.data_ptr(),
+                     _row(dy, n, out, "dy", dev, dy.dtype), *_opt(y, n, out, "y", dev, dy.dtype),
+                     _at(sx), _at(sw),
                      *_opt(dx, n, in_, "dx", dev, dy.dtype), *_opt(dw, out, in_, "dw", dev, f32),
                      _vec(db, out, "db", dev, f32), ws, nbytes), raw)
 
 
 def _strides(t, T, n, d, name, dev, dtype):
     """Strides of a step and of a row of an argument [T][n][d]."""
-    if tuple(t.shape) != (T, n, d) or t.dtype is not dtype or t.get_device() != dev:
+    if t.dtype is dtype and t.shape == (T, n, d) and t.is_contiguous() and t.get_device() == dev:
+        return (n * d if T > 1 else 0), (d if n > 1 else 0)
+    if t.shape != (T, n, d) or t.dtype is not dtype or t.get_device() != dev:
         raise ValueError("%s must be [%d][%d][%d] of %s on the current device, got %s %s" % (
             name, T, n, d, dtype, list(t.shape), t.dtype))
     st, ld, one = t.stride()
@@ -1182,27 +1196,34 @@ def _strides(t, T, n, d, name, dev, dtype):
     return st if T > 1 else 0, ld if n > 1 else 0
 
 
+def _flag(t, T, n, name, dev):
+    if t.dtype is not _torch.uint8 and t.dtype is not _torch.bool:
+        raise ValueError("%s must be uint8 or bool, got %s" % (name, t.dtype))
+    return _row(t, T, n, name, dev, t.dtype)
+
+
 def _flags(terminated, truncated, T, n, dev):
     """Pointers of the two flags [T][n] (uint8 or bool; either None) and their row stride."""
-    out, ld = [], None
-    for t, name in ((terminated, "terminated"), (truncated, "truncated")):
-        if t is None:
-            out.append(None)
-            continue
-        if t.dtype is not _torch.uint8 and t.dtype is not _torch.bool:
-            raise ValueError("%s must be uint8 or bool, got %s" % (name, t.dtype))
-        k = _ld(t, T, n, name, dev)
-        if ld is not None and k != ld:
-            raise ValueError("terminated and truncated must have the same row stride")
-        ld = k
-        out.append(t.data_ptr())
-    return out[0], out[1], ld or 0
+    if terminated is None:
+        if truncated is None:
+            return None, None, 0
+        return None, truncated.data_ptr(), _flag(truncated, T, n, "truncated", dev)
+    ld = _flag(terminated, T, n, "terminated", dev)
+    if truncated is None:
+        return terminated.data_ptr(), None, ld
+    if _flag(truncated, T, n, "truncated", dev) != ld:
+        raise ValueError("terminated and truncated must have the same row stride")
+    return terminated.data_ptr(), truncated.data_ptr(), ld
 
 
 def _state(t, n, d, name, dev):
-    if t is not None and t.shape[-2:] != (n, d):
-        raise ValueError("%s must be [%d][%d], got %s" % (name, n, d, list(t.shape)))
-    return _vec(t, n * d, name, dev, _torch.float32)
+    if t is None:
+        return None
+    if (t.dtype is not _torch.float32 or t.shape[-2:] != (n, d) or t.numel() != n * d
+            or t.get_device() != dev or not t.is_contiguous()):
+        raise ValueError("%s must be [%d][%d] contiguous float32 values on the current device, "
+                         "got %s %s" % (name, n, d, list(t.shape), t.dtype))
+    return t.data_ptr()
 
 
 def gated_scan_workspace(T, n, d):
@@ -1220,7 +1241,8 @@ def gated_scan(gate, x, h, state=None, state_out=None, keep=None, terminated=Non
     dev, raw = _call_stream(stream)
     T, n, d = x.shape
     dt = x.dtype
-    need = lib().im_gated_scan_workspace(T, n, d)
+    # one step needs none
+    need = lib().im_gated_scan_workspace(T, n, d) if T > 1 else 0
     ws, nbytes = None, 0
     if need:
         _held, ws, nbytes = _workspace(workspace, lambda: _space(need), dev, stream)
@@ -1242,7 +1264,8 @@ def gated_scan_grad(dh, gate, x, keep, dgate, dx, dstate=None, dstate_out=None, 
     dev, raw = _call_stream(stream)
     T, n, d = dh.shape
     dt = dh.dtype
-    need = lib().im_gated_scan_workspace(T, n, d)
+    # one step needs none
+    need = lib().im_gated_scan_workspace(T, n, d) if T > 1 else 0
     ws, nbytes = None, 0
     if need:
         _held, ws, nbytes = _workspace(workspace, lambda: _space(need), dev, stream)

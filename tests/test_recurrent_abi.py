@@ -31,6 +31,16 @@ def _b8(d=8, n=4, rows=1, **over):
     return b
 
 
+_HOLD = []
+
+
+def _held(*a, **k):
+    """Address of a matrix in 8 bits that lives as long as the tests."""
+    _HOLD.append(_b8(*a, **k))
+    return C.addressof(_HOLD[-1])
+
+
+_SQUARE, _SQUARE16 = _held(rows=128), _held(16, rows=128)
 BAD_BLOCKS = [
     (dict(rows=2), "rows must"), (dict(rows=0), "rows must"), (dict(ld_q=112), "ld_q"),
     (dict(ld_q=136), "ld_q"), (dict(ld_scale=0), "ld_scale"), (dict(q=None), "NULL block8"),
@@ -44,12 +54,12 @@ def test_block8_arguments(lib, over, words):
     for status in (lib.im_block_store(P, 8, 0, 4, 8, C.byref(b), None, None),
                    lib.im_block_store(P, 4, 0, 8, 4, None, C.byref(b), None),
                    lib.im_block_load(C.byref(b), 4, 8, P, 8, 0, None),
-                   lib.im_rms_norm(C.byref(_rms(y8=C.pointer(b))), None),
-                   lib.im_block_linear(C.byref(_layer(x=C.pointer(b))), None),
-                   lib.im_block_linear(C.byref(_layer(w=C.pointer(b))), None),
-                   lib.im_block_linear(C.byref(_layer(out=8, ld_y=8, y8=C.pointer(b))), None),
-                   lib.im_block_linear_grad(C.byref(_layer_grad(xt=C.pointer(b))), None),
-                   lib.im_block_linear_grad(C.byref(_layer_grad(wt=C.pointer(b))), None)):
+                   lib.im_rms_norm(C.byref(_rms(y8=C.addressof(b))), None),
+                   lib.im_block_linear(C.byref(_layer(x=C.addressof(b))), None),
+                   lib.im_block_linear(C.byref(_layer(w=C.addressof(b))), None),
+                   lib.im_block_linear(C.byref(_layer(out=8, ld_y=8, y8=C.addressof(b))), None),
+                   lib.im_block_linear_grad(C.byref(_layer_grad(xt=C.addressof(b))), None),
+                   lib.im_block_linear_grad(C.byref(_layer_grad(wt=C.addressof(b))), None)):
         _refused(lib, status, BAD, words)
 
 
@@ -94,7 +104,7 @@ def _rms(**over):
     (dict(eps=float("nan")), BAD, "eps"), (dict(dtype=7), BAD, "dtype"), (dict(ld_x=7), BAD, "ld_x"),
     (dict(ld_residual=7), BAD, "ld_"), (dict(ld_h=7), BAD, "ld_"), (dict(ld_y=7), BAD, "ld_"),
     (dict(x=None), BAD, "NULL x"), (dict(h=None, y=None, rstd=None), BAD, "no output"),
-    (dict(h=3 * P), BAD, "one array"), (dict(y8=C.pointer(_b8(rows=128))), BAD, "rows must be 1"),
+    (dict(h=3 * P), BAD, "one array"), (dict(y8=_SQUARE), BAD, "rows must be 1"),
 ])
 def test_rms_norm_refuses(lib, over, code, words):
     _refused(lib, lib.im_rms_norm(C.byref(_rms(**over)), None), code, words)
@@ -117,7 +127,7 @@ def test_rms_norm_grad_refuses(lib, over, code, words):
 
 
 def _layer(**over):
-    return _set(im.ImLayer8(4, 8, 16, 0, 1, C.pointer(_b8(8)), C.pointer(_b8(8, 16, 128)), P, P, 16, None), over)
+    return _set(im.ImLayer8(4, 8, 16, 0, 1, _held(8), _held(8, 16, 128), P, P, 16, None), over)
 
 
 @pytest.mark.parametrize("over,code,words", [
@@ -125,14 +135,14 @@ def _layer(**over):
     (dict(y_dtype=5), BAD, "dtype"), (dict(ld_y=15), BAD, "ld_y"), (dict(y=None), BAD, "no output"),
     (dict(x=None), BAD, "NULL block8"), (dict(w=None), BAD, "NULL block8"),
     (dict(in_=129), BAD, "ld_q"), (dict(in_=(1 << 20) + 1), UNS, "2^20"), (dict(out=(1 << 20) + 1), UNS, "2^20"),
-    (dict(n=(1 << 30) + 1), UNS, "2^30"), (dict(y8=C.pointer(_b8(16, rows=128))), BAD, "rows must be 1"),
+    (dict(n=(1 << 30) + 1), UNS, "2^30"), (dict(y8=_SQUARE16), BAD, "rows must be 1"),
 ])
 def test_linear8_refuses(lib, over, code, words):
     _refused(lib, lib.im_block_linear(C.byref(_layer(**over)), None), code, words)
 
 
 def _layer_grad(**over):
-    return _set(im.ImLayer8Grad(4, 8, 16, 0, P, 16, P, 16, C.pointer(_b8(4)), C.pointer(_b8(16, rows=128)),
+    return _set(im.ImLayer8Grad(4, 8, 16, 0, P, 16, P, 16, _held(4), _held(16, rows=128),
                                 P, 8, P, 8, P, P, 1 << 30), over)
 
 
@@ -217,7 +227,7 @@ def test_calls_on_nothing(lib):
     empty = _b8(q=None, scale=None)
     assert lib.im_block_store(None, 8, 0, 0, 8, C.byref(empty), None, None) == im.IM_OK
     assert lib.im_block_load(C.byref(empty), 0, 8, None, 8, 0, None) == im.IM_OK
-    assert lib.im_block_linear(C.byref(_layer(n=0, x=C.pointer(empty), y=None)), None) == im.IM_OK
+    assert lib.im_block_linear(C.byref(_layer(n=0, x=C.addressof(empty), y=None)), None) == im.IM_OK
     assert lib.im_block_linear_grad(C.byref(_layer_grad(n=0, dy=None, dw=None, db=None)), None) == im.IM_OK
     assert lib.im_gated_scan(C.byref(_scan(n=0, gate=None, x=None, h=None)), None) == im.IM_OK
     assert lib.im_gated_scan(C.byref(_scan(T=0, gate=None, x=None, h=None, state_out=None)), None) == im.IM_OK
