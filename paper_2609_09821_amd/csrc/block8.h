@@ -49,27 +49,22 @@ __device__ __forceinline__ int block8_scale(uint32_t top)
 // 2^(127 - scale) for the scales 0 .. 247 of finite blocks.
 __device__ __forceinline__ float block8_inverse(int scale) { return __uint_as_float((uint32_t)(254 - scale) << 23); }
 
-// Eight values as e4m3 at a block's scale: the product is exact or far below e4m3's smallest
+// Four values as e4m3 at a block's scale: the product is exact or far below e4m3's smallest
 // value, so that the conversion's rounding to nearest even is the only one.  nv: values that
-// exist; zeros after them.
+// exist, may be none; zeros after them.
+__device__ __forceinline__ uint32_t block8_pack4(const float *v, int scale, int nv)
+{
+    uint32_t w = 0x7F7F7F7Fu;
+    if (scale != 255) {
+        const float s = block8_inverse(scale);
+        const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[0] * s, v[1] * s, 0, false);
+        w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[2] * s, v[3] * s, lo, true);
+    }
+    return nv >= 4 ? w : nv <= 0 ? 0 : w & ((1u << (8 * nv)) - 1);
+}
 __device__ __forceinline__ u32x2_r block8_pack(const float *v, int scale, int nv)
 {
-    u32x2_r r;
-    if (scale == 255) {
-        r = u32x2_r{0x7F7F7F7Fu, 0x7F7F7F7Fu};
-    } else {
-        const float s = block8_inverse(scale);
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            int w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * k] * s, v[4 * k + 1] * s, 0, false);
-            r[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[4 * k + 2] * s, v[4 * k + 3] * s, w, true);
-        }
-    }
-    if (nv < 8) {
-        const uint64_t w = nv <= 0 ? 0 : (r[0] | (uint64_t)r[1] << 32) << (64 - 8 * nv) >> (64 - 8 * nv);
-        r = u32x2_r{(uint32_t)w, (uint32_t)(w >> 32)};
-    }
-    return r;
+    return u32x2_r{block8_pack4(v, scale, nv), block8_pack4(v + 4, scale, nv - 4)};
 }
 
 // Eight restored values.  The scale's power of two is subnormal for scale 0.
@@ -95,6 +90,26 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t x)
     if constexpr (T >= 8) x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xF, 0xF, true));
     if constexpr (T >= 16) x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xF, 0xF, true));
     return x;
+}
+
+// Column sums of partial rows by a block of 1024: 64 columns, wavefront w takes rows w, w + 16, ..;
+// the wavefronts' sums meet in LDS in order.
+constexpr int COLUMN_SUM_WAVES = 16;
+__device__ __forceinline__ void column_sums(const float *part, int64_t rows, int64_t d, float *sums, int64_t block,
+                                            double (*lds)[64])
+{
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int64_t col = block * 64 + lane;
+    double s = 0.0;
+    if (col < d)
+#pragma unroll 8
+        for (int64_t r = w; r < rows; r += COLUMN_SUM_WAVES) s += (double)part[r * d + col];
+    lds[w][lane] = s;
+    __syncthreads();
+    if (w == 0 && col < d) {
+        for (int k = 1; k < COLUMN_SUM_WAVES; ++k) s += lds[k][lane];
+        sums[col] = (float)s;
+    }
 }
 
 }  // namespace im

@@ -11,89 +11,117 @@ namespace im {
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // ---------------------------------------------------------------------------
-// Stores.  A block of 256 threads takes 128 rows x 128 columns: thread (g, l) = (t / 16,
-// t % 16) holds eight values of each of the rows 8 g .. 8 g + 7, columns 8 l .. 8 l + 7, in
-// registers.  A row's block is 16 neighbouring lanes; a column's meets in LDS, as does the
-// whole tile's where it has one scale.  The transposed bytes are put together from a thread's
-// eight rows and pass through LDS, so that both outputs leave in whole 128-byte blocks.
+// Stores.  A block takes 128 rows x 128 columns: thread (g, l) = (t / 16, t % 16) holds eight
+// values of each of the rows 4 g .. 4 g + 3, columns 8 l .. 8 l + 7, in registers.  A row's block
+// is 16 neighbouring lanes; a column's meets in LDS, as does the whole tile's where it has one scale.
+// The transposed bytes are put together from a thread's four rows and pass through LDS, so that
+// both outputs leave in whole 128-byte blocks.
 // C, TR: which outputs; SQUARE: one scale a tile; MASK: x counts as 0 where not y > 0.
 // ---------------------------------------------------------------------------
+constexpr int ST_NT = 512, ST_ROWS = 4, ST_GROUPS = ST_NT / 16;
 constexpr int ST_PITCH = 128 + 16;      // bytes of a transposed column in LDS
+constexpr int ST_WORDS = 128 + 2;       // words of a row group's columns
+// A column's place in LDS: the lanes of a row group, which hold each eighth column, are neighbours
+// (column by column they meet in few banks: 4095 x 1024 bf16 both ways 11.4 us for 10.2).
+__device__ __forceinline__ int column_of(int place) { return (place & 15) * 8 + (place >> 4); }
+static_assert(ST_ROWS * ST_GROUPS == 128, "whole tiles");
 template <typename E, bool C, bool TR, bool SQUARE, bool MASK>
-__global__ __launch_bounds__(256) void block8_store_kernel(StoreArgs a, int64_t col_tiles, int64_t tiles)
+__global__ __launch_bounds__(ST_NT) void block8_store_kernel(StoreArgs a, int64_t col_tiles, int64_t tiles)
 {
     __shared__ __attribute__((aligned(16))) uint8_t bytes[TR ? 128 * ST_PITCH : 16];
-    __shared__ uint32_t tops[16][128];
-    __shared__ float sums[16][128];
+    __shared__ uint32_t tops[TR || SQUARE ? ST_GROUPS : 1][ST_WORDS];
+    __shared__ float sums[ST_GROUPS][ST_WORDS];
     const int g = threadIdx.x >> 4, l = threadIdx.x & 15;
     for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         const int64_t r0 = tile / col_tiles * 128, c0 = tile % col_tiles * 128;
         const int64_t col = c0 + 8 * l;
         const int nv = (int)min((int64_t)8, a.d - col);      // columns, may be none
         const int rows = (int)min((int64_t)128, a.n - r0);
-        float v[8][8];
+        float v[ST_ROWS][8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int r = 8 * g + k;
-            const int have = r < rows ? nv : 0;
-            load8((const E *)a.x + (r0 + r) * a.ld_x + col, have, v[k]);
-            if constexpr (MASK) {
-                float y[8];
-                load8((const E *)a.y + (r0 + r) * a.ld_y + col, have, y);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[k][j] = y[j] > 0.0f ? v[k][j] : 0.0f;
-            }
+        for (int k = 0; k < ST_ROWS; ++k) {
+            const int r = ST_ROWS * g + k;
+            load8((const E *)a.x + (r0 + r) * a.ld_x + col, r < rows ? nv : 0, v[k]);
         }
-        // largest magnitudes of the rows, of the columns
-        uint32_t across[8], down[8];
+        if constexpr (MASK) {
+            float y[ST_ROWS][8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) across[k] = down[k] = 0;
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t m = magnitude(v[k][j]);
-                across[k] = max(across[k], m);
-                down[j] = max(down[j], m);
+            for (int k = 0; k < ST_ROWS; ++k) {
+                const int r = ST_ROWS * g + k;
+                load8((const E *)a.y + (r0 + r) * a.ld_y + col, r < rows ? nv : 0, y[k]);
             }
-        if (a.sums) {
+#pragma unroll
+            for (int k = 0; k < ST_ROWS; ++k)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[k][j] = y[k][j] > 0.0f ? v[k][j] : 0.0f;
+        }
+        // largest magnitudes and sums of the thread's part of each column
+        if (TR || SQUARE || a.sums) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
+                uint32_t top = 0;
                 float s = 0.0f;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) s += v[k][j];
-                sums[g][8 * l + j] = s;
+                for (int k = 0; k < ST_ROWS; ++k) top = max(top, magnitude(v[k][j])), s += v[k][j];
+                if constexpr (TR || SQUARE) tops[g][16 * j + l] = top;
+                if (a.sums) sums[g][16 * j + l] = s;
             }
+            __syncthreads();
         }
-        if constexpr (TR || SQUARE) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) tops[g][8 * l + j] = down[j];
-        }
-        if (TR || SQUARE || a.sums) __syncthreads();
-        if (a.sums && threadIdx.x < 128 && c0 + threadIdx.x < a.d) {
+        // of whole columns, by four threads each; a magnitude goes in the first of its column's words
+        const int place = threadIdx.x >> 2, part = threadIdx.x & 3;
+        const int64_t own = c0 + column_of(place);
+        if (a.sums) {
             float s = 0.0f;
 #pragma unroll
-            for (int k = 0; k < 16; ++k) s += sums[k][threadIdx.x];
-            a.sums[r0 / 128 * a.d + c0 + threadIdx.x] = s;
+            for (int k = 0; k < ST_GROUPS / 4; ++k) s += sums[part * (ST_GROUPS / 4) + k][place];
+            s = team_sum<4>(s);
+            if (part == 0 && own < a.d) a.sums[r0 / 128 * a.d + own] = s;
+        }
+        if constexpr (TR || SQUARE) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int k = 0; k < ST_GROUPS / 4; ++k) m = max(m, tops[part * (ST_GROUPS / 4) + k][place]);
+            m = quad_max(m);
+            if constexpr (SQUARE) {
+#pragma unroll
+                for (int b = 4; b < 64; b *= 2) m = max(m, (uint32_t)__shfl_xor((int)m, b));
+            } else if (part == 0 && own < a.d) {
+                a.t.scale[own * a.t.ld_scale + r0 / 128] = (uint8_t)block8_scale(m);
+            }
+            __syncthreads();
+            if (SQUARE ? (threadIdx.x & 63) == 0 : part == 0) tops[0][SQUARE ? threadIdx.x >> 6 : place] = m;
+            __syncthreads();
         }
         int whole = 0;
         if constexpr (SQUARE) {
             uint32_t m = 0;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) m = max(m, tops[k][threadIdx.x & 127]), m = max(m, tops[k + 8][threadIdx.x & 127]);
+            for (int k = 0; k < ST_NT / 64; ++k) m = max(m, tops[0][k]);
+            whole = block8_scale(m);
+        }
+        if constexpr (TR) {
 #pragma unroll
-            for (int b = 1; b < 64; b *= 2) m = max(m, (uint32_t)__shfl_xor((int)m, b));
-            // the wavefronts' two halves of the columns
-            __syncthreads();
-            if ((threadIdx.x & 63) == 0) tops[0][threadIdx.x >> 6] = m;
-            __syncthreads();
-            whole = block8_scale(max(tops[0][0], tops[0][1]));
+            for (int j = 0; j < 8; ++j) {
+                const int s = SQUARE ? whole : block8_scale(tops[0][16 * j + l]);
+                float w[ST_ROWS];
+#pragma unroll
+                for (int k = 0; k < ST_ROWS; ++k) w[k] = v[k][j];
+                *(uint32_t *)(bytes + (16 * j + l) * ST_PITCH + ST_ROWS * g) = block8_pack4(w, s, rows - ST_ROWS * g);
+            }
+            if (SQUARE && threadIdx.x == 0) a.t.scale[c0 / 128 * a.t.ld_scale + r0 / 128] = (uint8_t)whole;
         }
         if constexpr (C) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const int r = 8 * g + k;
-                const int s = SQUARE ? whole : block8_scale(lanes_max<16>(across[k]));
+            for (int k = 0; k < ST_ROWS; ++k) {
+                const int r = ST_ROWS * g + k;
+                int s = whole;
+                if constexpr (!SQUARE) {
+                    uint32_t top = 0;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) top = max(top, magnitude(v[k][j]));
+                    s = block8_scale(lanes_max<16>(top));
+                }
                 if (r >= rows) continue;
                 *(u32x2_r *)(a.c.q + (r0 + r) * a.c.ld_q + col) = block8_pack(v[k], s, nv);
                 if (!SQUARE && l == 0) a.c.scale[(r0 + r) * a.c.ld_scale + c0 / 128] = (uint8_t)s;
@@ -101,28 +129,13 @@ __global__ __launch_bounds__(256) void block8_store_kernel(StoreArgs a, int64_t 
             if (SQUARE && threadIdx.x == 0) a.c.scale[r0 / 128 * a.c.ld_scale + c0 / 128] = (uint8_t)whole;
         }
         if constexpr (TR) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                int s = whole;
-                if constexpr (!SQUARE) {
-                    uint32_t m = 0;
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) m = max(m, tops[k][8 * l + j]);
-                    s = block8_scale(m);
-                    if (g == 0 && j < nv) a.t.scale[(col + j) * a.t.ld_scale + r0 / 128] = (uint8_t)s;
-                }
-                float w[8];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) w[k] = v[k][j];
-                *(u32x2_r *)(bytes + (8 * l + j) * ST_PITCH + 8 * g) = block8_pack(w, s, min(max(rows - 8 * g, 0), 8));
-            }
-            if (SQUARE && threadIdx.x == 0) a.t.scale[c0 / 128 * a.t.ld_scale + r0 / 128] = (uint8_t)whole;
             __syncthreads();
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int c = u * 32 + (threadIdx.x >> 3), at = threadIdx.x % 8 * 16;
-                if (c0 + c < a.d)
-                    *(u32x4_r *)(a.t.q + (c0 + c) * a.t.ld_q + r0 + at) = *(const u32x4_r *)(bytes + c * ST_PITCH + at);
+            for (int u = 0; u < 128 * 8 / ST_NT; ++u) {
+                const int c = u * (ST_NT / 8) + (threadIdx.x >> 3), at = threadIdx.x % 8 * 16;
+                const int64_t to = c0 + column_of(c);
+                if (to < a.d)
+                    *(u32x4_r *)(a.t.q + to * a.t.ld_q + r0 + at) = *(const u32x4_r *)(bytes + c * ST_PITCH + at);
             }
         }
         if (tile + gridDim.x < tiles) __syncthreads();
@@ -138,17 +151,17 @@ static void store_by(const StoreArgs &a, int64_t cols, int64_t tiles, hipStream_
     auto go = [&](auto c, auto t) {
         constexpr bool C = decltype(c)::value, T = decltype(t)::value;
         // only a gradient is masked, and its blocks lie along rows
-        if (square) block8_store_kernel<E, C, T, true, false><<<g, dim3(256), 0, s>>>(a, cols, tiles);
-        else if (mask) block8_store_kernel<E, C, T, false, true><<<g, dim3(256), 0, s>>>(a, cols, tiles);
-        else block8_store_kernel<E, C, T, false, false><<<g, dim3(256), 0, s>>>(a, cols, tiles);
+        if (square) block8_store_kernel<E, C, T, true, false><<<g, dim3(ST_NT), 0, s>>>(a, cols, tiles);
+        else if (mask) block8_store_kernel<E, C, T, false, true><<<g, dim3(ST_NT), 0, s>>>(a, cols, tiles);
+        else block8_store_kernel<E, C, T, false, false><<<g, dim3(ST_NT), 0, s>>>(a, cols, tiles);
     };
     const std::true_type yes;
     const std::false_type no;
     if (a.c.q && a.t.q) go(yes, yes);
     else if (a.c.q) go(yes, no);
     else if (a.t.q) go(no, yes);
-    else if (mask) block8_store_kernel<E, false, false, false, true><<<g, dim3(256), 0, s>>>(a, cols, tiles);
-    else block8_store_kernel<E, false, false, false, false><<<g, dim3(256), 0, s>>>(a, cols, tiles);
+    else if (mask) block8_store_kernel<E, false, false, false, true><<<g, dim3(ST_NT), 0, s>>>(a, cols, tiles);
+    else block8_store_kernel<E, false, false, false, false><<<g, dim3(ST_NT), 0, s>>>(a, cols, tiles);
 }
 
 hipError_t launch_block8_store(const StoreArgs &a, bool f32, hipStream_t s)
@@ -187,32 +200,15 @@ hipError_t launch_block8_load(const Mat8 &c, int64_t n, int64_t d, void *x, int6
     return hipGetLastError();
 }
 
-// ---------------------------------------------------------------------------
-// Column sums of partial rows: 64 columns a block, wavefront w takes rows w, w + 16, ..;
-// the wavefronts' sums meet in LDS in order.
-// ---------------------------------------------------------------------------
-constexpr int SUM_WAVES = 16;
-__global__ __launch_bounds__(64 * SUM_WAVES) void column_sums_kernel(const float *part, int64_t rows, int64_t d,
-                                                                     float *sums)
+__global__ __launch_bounds__(64 * COLUMN_SUM_WAVES) void column_sums_kernel(ColumnSums c)
 {
-    __shared__ double lds[SUM_WAVES][64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t col = (int64_t)blockIdx.x * 64 + lane;
-    double s = 0.0;
-    if (col < d)
-#pragma unroll 8
-        for (int64_t r = w; r < rows; r += SUM_WAVES) s += (double)part[r * d + col];
-    lds[w][lane] = s;
-    __syncthreads();
-    if (w == 0 && col < d) {
-        for (int k = 1; k < SUM_WAVES; ++k) s += lds[k][lane];
-        sums[col] = (float)s;
-    }
+    __shared__ double lds[COLUMN_SUM_WAVES][64];
+    column_sums(c.part, c.rows, c.d, c.sums, blockIdx.x, lds);
 }
 
-hipError_t launch_column_sums(const float *part, int64_t rows, int64_t d, float *sums, hipStream_t s)
+hipError_t launch_column_sums(const ColumnSums &c, hipStream_t s)
 {
-    column_sums_kernel<<<dim3((unsigned)ceil_div(d, 64)), dim3(64 * SUM_WAVES), 0, s>>>(part, rows, d, sums);
+    column_sums_kernel<<<dim3((unsigned)ceil_div(c.d, 64)), dim3(64 * COLUMN_SUM_WAVES), 0, s>>>(c);
     return hipGetLastError();
 }
 

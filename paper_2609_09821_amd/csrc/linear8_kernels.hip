@@ -143,23 +143,20 @@ template <int WP_, int WQ_, int TP_, int TQ_, int NS_>
 struct TileShape {
     static constexpr int WP = WP_, WQ = WQ_, TP = TP_, TQ = TQ_, NS = NS_;
     static constexpr int NT = 64 * WP * WQ, WAVES = WP * WQ, BP = 32 * WP * TP, BQ = 32 * WQ * TQ;
-    static_assert(BP % 128 == 0, "whole blocks of y8");
     static constexpr int UP = BP * 8 / NT, UQ = BQ * 8 / NT;             // 16-byte pieces of a thread
-    static constexpr int US = ((BP + BQ) / 64 + WAVES - 1) / WAVES;      // scales of a thread
+    static constexpr int US = ((BP + BQ + 63) / 64 + WAVES - 1) / WAVES;      // scales of a thread
     static constexpr int L = UP + UQ + US;                               // direct loads of a step
     static constexpr int Q_AT = BP * 128, S_AT = Q_AT + BQ * 128, STAGE = S_AT + US * WAVES * 256;
     static constexpr int LDO = BP + 4;                                   // floats of an epilogue row
     static constexpr int OUT_ROWS = 32 * WQ, LDS = std::max(NS * STAGE, OUT_ROWS * LDO * 4);
-    static_assert(UP * NT == BP * 8 && UQ * NT == BQ * 8 && (BP + BQ) % 64 == 0, "whole pieces");
+    static_assert(UP * NT == BP * 8 && UQ * NT == BQ * 8, "whole pieces");
 };
 
 template <typename S, bool WIDE>
-__global__ __launch_bounds__(S::NT, 2) void linear8_tile_kernel(Linear8Args a, int p_tiles, int tiles)
+__device__ __forceinline__ void tile_run(const Linear8Args &a, int p_tiles, int tiles, int id, char *lds)
 {
-    __shared__ __attribute__((aligned(1024))) char lds[S::LDS];
     constexpr int TP = S::TP, TQ = S::TQ, BP = S::BP, BQ = S::BQ, NS = S::NS;
     const int lane = threadIdx.x & 63, wave = wave_id();
-    const int id = xcd_order(blockIdx.x, gridDim.x);
     const int split = id / tiles, tile = id % tiles;
     const int64_t p0 = (int64_t)(tile % p_tiles) * BP, q0 = (int64_t)(tile / p_tiles) * BQ;
     const int wp = wave % S::WP * TP * 32, wq = wave / S::WP * TQ * 32;
@@ -308,6 +305,24 @@ __global__ __launch_bounds__(S::NT, 2) void linear8_tile_kernel(Linear8Args a, i
             }
         }
     }
+}
+
+template <typename S, bool WIDE>
+__global__ __launch_bounds__(S::NT, 2) void linear8_tile_kernel(Linear8Args a, int p_tiles, int tiles)
+{
+    __shared__ __attribute__((aligned(1024))) char lds[S::LDS];
+    tile_run<S, WIDE>(a, p_tiles, tiles, xcd_order(blockIdx.x, gridDim.x), lds);
+}
+
+// Two products side by side in one launch, a layer's gradients: the second one is wide.
+template <typename S, bool WIDE>
+__global__ __launch_bounds__(S::NT, 2) void linear8_two_kernel(Linear8Args a, int a_tiles, int a_blocks, Linear8Args b,
+                                                              int b_p_tiles, int b_tiles)
+{
+    __shared__ __attribute__((aligned(1024))) char lds[S::LDS];
+    const int id = xcd_order(blockIdx.x, gridDim.x);
+    if (id < a_blocks) tile_run<S, WIDE>(a, a_tiles, a_blocks, id, lds);
+    else tile_run<S, true>(b, b_p_tiles, b_tiles, id - a_blocks, lds);
 }
 
 // ---------------------------------------------------------------------------
@@ -538,11 +553,18 @@ __global__ __launch_bounds__(64 * PANEL_WAVES, 1) void linear8_panel_kernel(Line
     }
 }
 
-// Parts of a product to y, in their order.
-__global__ __launch_bounds__(256) void linear8_join_kernel(Linear8Args a)
+// Parts of a product to y, in their order.  The blocks after the first `blocks` add up column
+// sums instead (column_sums: 64 columns a block).
+__global__ __launch_bounds__(1024) void linear8_join_kernel(Linear8Args a, int blocks, const float *part, int64_t rows,
+                                                            int64_t d, float *sums)
 {
+    __shared__ double lds[COLUMN_SUM_WAVES][64];
+    if ((int)blockIdx.x >= blocks) {
+        column_sums(part, rows, d, sums, blockIdx.x - blocks, lds);
+        return;
+    }
     const int64_t ld = (a.out + 3) / 4 * 4, quads = ld / 4, all = a.n * quads;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    for (int64_t i = (int64_t)blockIdx.x * 1024 + threadIdx.x; i < all; i += (int64_t)blocks * 1024) {
         const int64_t row = i / quads, col = (i - row * quads) * 4;
         const float *p = a.part + row * ld + col;
         f32x4_r s = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -559,16 +581,24 @@ __global__ __launch_bounds__(256) void linear8_join_kernel(Linear8Args a)
     }
 }
 
-typedef TileShape<2, 2, 2, 2, 2> Tile128;
-
-int linear8_splits(int64_t n, int64_t out, int64_t steps)
-{
-    const int64_t tiles = ceil_div(n, 128) * ceil_div(out, 128);
-    return (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, steps / 4));
-}
+typedef TileShape<2, 2, 2, 2, 2> Tile128;     // 128 x 128, two blocks a CU
+typedef TileShape<2, 2, 1, 1, 4> Tile64;      // 64 x 64, three steps ahead
+typedef TileShape<4, 1, 1, 1, 3> TileFlat;    // 128 x 32, for whole blocks of y8
 
 // Products in bf16, summed in fp32 throughout.
 static bool wide(const Linear8Args &a) { return (a.y && a.y_f32) || a.y8.q; }
+
+static int64_t tiles_of(int64_t n, int64_t out, int side) { return ceil_div(n, side) * ceil_div(out, side); }
+
+// Few tiles of 128 x 128 leave CUs without one.
+static bool few_tiles(int64_t n, int64_t out, int64_t splits) { return tiles_of(n, out, 128) * splits < 256; }
+
+int linear8_splits(int64_t n, int64_t out, int64_t steps)
+{
+    const int64_t big = std::max<int64_t>(1, std::min<int64_t>(512 / tiles_of(n, out, 128), steps / 4));
+    if (!few_tiles(n, out, big)) return (int)big;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles_of(n, out, 64), steps / 4));
+}
 
 template <typename S>
 static void tile_by(const Linear8Args &a, hipStream_t s)
@@ -579,23 +609,28 @@ static void tile_by(const Linear8Args &a, hipStream_t s)
     else linear8_tile_kernel<S, false><<<g, b, 0, s>>>(a, (int)p_tiles, (int)tiles);
 }
 
+static void join(const Linear8Args &a, const ColumnSums &c, hipStream_t s)
+{
+    const int64_t blocks = std::min<int64_t>(ceil_div(a.n * ceil_div(a.out, 4), 1024), 256 * 4);
+    linear8_join_kernel<<<dim3((unsigned)(blocks + (c.sums ? ceil_div(c.d, 64) : 0))), dim3(1024), 0, s>>>(
+        a, (int)blocks, c.part, c.rows, c.d, c.sums);
+}
+
 hipError_t launch_linear8(const Linear8Args &a, hipStream_t s)
 {
-    if (a.part) {
-        tile_by<Tile128>(a, s);
-        linear8_join_kernel<<<dim3((unsigned)std::min<int64_t>(ceil_div(a.n * ceil_div(a.out, 4), 256), 256 * 16)),
-                              dim3(256), 0, s>>>(a);
-        return hipGetLastError();
-    }
-    const int64_t panels = ceil_div(a.out, 128);
-    if (a.n >= 16384 && a.steps <= PANEL_STEPS && panels <= 32 && a.q.ld_q < (1 << 24)) {
-        const int streams = 8 * (int)(32 / panels);
+    if (a.n >= 16384 && a.steps <= PANEL_STEPS && ceil_div(a.out, 128) <= 32 && a.q.ld_q < (1 << 24)) {
+        const int panels = (int)ceil_div(a.out, 128), streams = 8 * (32 / panels);
         const dim3 g(256), b(64 * PANEL_WAVES);
-        if (wide(a)) linear8_panel_kernel<true><<<g, b, 0, s>>>(a, (int)panels, streams);
-        else linear8_panel_kernel<false><<<g, b, 0, s>>>(a, (int)panels, streams);
+        if (wide(a)) linear8_panel_kernel<true><<<g, b, 0, s>>>(a, panels, streams);
+        else linear8_panel_kernel<false><<<g, b, 0, s>>>(a, panels, streams);
         return hipGetLastError();
     }
-    // parts of rows with fewer than 2^21 tiles of 128 x 128
+    if (few_tiles(a.n, a.out, 1)) {
+        if (a.y8.q) tile_by<TileFlat>(a, s);
+        else tile_by<Tile64>(a, s);
+        return hipGetLastError();
+    }
+    // parts of rows with fewer than 2^21 tiles
     const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 20) / ceil_div(a.out, 128)) * 128;
     for (int64_t r = 0; r < a.n; r += most) {
         Linear8Args b = a;
@@ -607,6 +642,35 @@ hipError_t launch_linear8(const Linear8Args &a, hipStream_t s)
         tile_by<Tile128>(b, s);
     }
     return hipGetLastError();
+}
+
+// dx (y null: not wanted), then dw's parts joined beside the column sums.
+hipError_t launch_linear8_grad(const Linear8Args &dx, const Linear8Args &dw, const ColumnSums &c, hipStream_t s)
+{
+    hipError_t e = hipSuccess;
+    const bool with_dx = dx.y != nullptr, small = dw.y && few_tiles(dw.n, dw.out, dw.splits);
+    if (with_dx && small && few_tiles(dx.n, dx.out, 1)) {
+        typedef Tile64 S;
+        const int64_t ap = ceil_div(dx.out, S::BP), at = ap * ceil_div(dx.n, S::BQ);
+        const int64_t bp = ceil_div(dw.out, S::BP), bt = bp * ceil_div(dw.n, S::BQ);
+        const dim3 g((unsigned)(at + bt * dw.splits)), b(S::NT);
+        if (wide(dx)) linear8_two_kernel<S, true><<<g, b, 0, s>>>(dx, (int)ap, (int)at, dw, (int)bp, (int)bt);
+        else linear8_two_kernel<S, false><<<g, b, 0, s>>>(dx, (int)ap, (int)at, dw, (int)bp, (int)bt);
+        e = hipGetLastError();
+    } else {
+        if (with_dx) e = launch_linear8(dx, s);
+        if (e == hipSuccess && dw.y) {
+            if (small) tile_by<Tile64>(dw, s);
+            else tile_by<Tile128>(dw, s);
+            e = hipGetLastError();
+        }
+    }
+    if (e != hipSuccess) return e;
+    if (dw.y && dw.part) {
+        join(dw, c, s);
+        return hipGetLastError();
+    }
+    return c.sums ? launch_column_sums(c, s) : e;
 }
 
 }  // namespace im

@@ -76,8 +76,13 @@ struct RmsGradArgs {
 int64_t rms_grad_blocks(int64_t n, int64_t d);
 hipError_t launch_rms_grad(const RmsGradArgs &a, bool f32, hipStream_t s);
 
-// sums[col] = the sum of part[row][col] over the rows, in float64 in their order.
-hipError_t launch_column_sums(const float *part, int64_t rows, int64_t d, float *sums, hipStream_t s);
+// sums[col] = the sum of part[row][col] over the rows, in float64 in a fixed order.
+struct ColumnSums {
+    const float *part;
+    int64_t rows, d;
+    float *sums;             // null: not wanted
+};
+hipError_t launch_column_sums(const ColumnSums &c, hipStream_t s);
 
 // C[q][p] = sum_k Q[q][k] P[p][k]: rows of Q are y's rows, rows of P its columns.
 struct Linear8Args {
@@ -96,6 +101,8 @@ struct Linear8Args {
 // `splits` parts of k pay for a float y of few tiles and a long k.
 int linear8_splits(int64_t n, int64_t out, int64_t steps);
 hipError_t launch_linear8(const Linear8Args &a, hipStream_t s);
+// A layer's gradients: dx and dw (y null: not wanted; dw in its splits) and db's column sums.
+hipError_t launch_linear8_grad(const Linear8Args &dx, const Linear8Args &dw, const ColumnSums &c, hipStream_t s);
 
 struct ScanArgs {
     int64_t T, n, d;

@@ -300,34 +300,32 @@ im_status im_block_linear_grad(const im_layer8_grad *p, void *stream)
     if (p->db) a.sums = (float *)(ws + g.sums);
     hipError_t e = hipSuccess;
     if (p->n > 0) e = launch_block8_store(a, f32, st);
-    if (e == hipSuccess && p->db) e = launch_column_sums(a.sums, ceil_div(p->n, IM_BLOCK8), p->out, p->db, st);
-    if (e == hipSuccess && p->dx && p->n > 0) {
-        Linear8Args l{};
-        l.n = p->n;
-        l.out = p->in;
-        l.steps = ceil_div(p->out, IM_BLOCK8);
-        l.q = a.c;
-        l.p = mat8(p->wt);
-        l.y = p->dx;
-        l.ld_y = p->ld_dx;
-        l.y_f32 = f32;
-        l.splits = 1;
-        e = launch_linear8(l, st);
+    Linear8Args dx{}, dw{};
+    if (p->dx && p->n > 0) {
+        dx.n = p->n;
+        dx.out = p->in;
+        dx.steps = ceil_div(p->out, IM_BLOCK8);
+        dx.q = a.c;
+        dx.p = mat8(p->wt);
+        dx.y = p->dx;
+        dx.ld_y = p->ld_dx;
+        dx.y_f32 = f32;
+        dx.splits = 1;
     }
-    if (e == hipSuccess && p->dw) {
-        Linear8Args l{};
-        l.n = p->out;
-        l.out = p->in;
-        l.steps = ceil_div(p->n, IM_BLOCK8);
-        l.q = a.t;
-        if (p->n > 0) l.p = mat8(p->xt);
-        l.y = p->dw;
-        l.ld_y = p->ld_dw;
-        l.y_f32 = 1;
-        l.splits = g.splits;
-        if (g.splits > 1) l.part = (float *)(ws + g.part);
-        e = launch_linear8(l, st);
+    if (p->dw) {
+        dw.n = p->out;
+        dw.out = p->in;
+        dw.steps = ceil_div(p->n, IM_BLOCK8);
+        dw.q = a.t;
+        if (p->n > 0) dw.p = mat8(p->xt);
+        dw.y = p->dw;
+        dw.ld_y = p->ld_dw;
+        dw.y_f32 = 1;
+        dw.splits = g.splits;
+        if (g.splits > 1) dw.part = (float *)(ws + g.part);
     }
+    if (e == hipSuccess)
+        e = launch_linear8_grad(dx, dw, ColumnSums{a.sums, ceil_div(p->n, IM_BLOCK8), p->out, p->db}, st);
     return launched(e, "block_linear_grad launch");
 }
 

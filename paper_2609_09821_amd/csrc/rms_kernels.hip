@@ -221,7 +221,7 @@ hipError_t launch_rms_grad(const RmsGradArgs &a, bool f32, hipStream_t s)
         }
     };
     by_width<NORM_LANES>(a.d, go);
-    if (a.part && blocks > 1) return launch_column_sums(a.part, blocks, a.d, a.dgamma, s);
+    if (a.part && blocks > 1) return launch_column_sums(ColumnSums{a.part, blocks, a.d, a.dgamma}, s);
     return hipGetLastError();
 }
 
