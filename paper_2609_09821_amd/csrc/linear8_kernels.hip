@@ -30,6 +30,9 @@ typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+template <int V>
+using Int = std::integral_constant<int, V>;
+
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
 // Copies 16 bytes a lane to LDS at `to` (the same in every lane) + 16 lane.
@@ -103,53 +106,34 @@ __device__ __forceinline__ bf16x8_t widen8(uint32_t lo, uint32_t hi, float scale
     return __builtin_bit_cast(bf16x8_t, v);
 }
 
-// Last steps of every kernel: eight consecutive values of a row, from `col` of `wide` columns
-// on, get their bias, the ReLU, and leave.  All 16 lanes of 128 columns call together.
-__device__ __forceinline__ void finish8(const Linear8Args &a, int64_t row, int64_t col, bool on, float (&v)[8])
+// Bits of four values as a vector.
+__device__ __forceinline__ u32x4_r bits4(const f32x16_t &a, int g)
 {
-    const int nv = (int)min((int64_t)8, a.out - col);
-    if (a.bias) {
-        float b[8];
-        load8(a.bias + col, nv, b);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] += b[k];
-    }
-    if (a.relu)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = v[k] < 0.0f ? 0.0f : v[k];      // NaN stays
-    if (a.y8.q) {
-        uint32_t top = 0;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) top = max(top, k < nv ? magnitude(v[k]) : 0);
-        const int s = block8_scale(lanes_max<16>(top));
-        if (on) {
-            *(u32x2_r *)(a.y8.q + row * a.y8.ld_q + col) = block8_pack(v, s, nv);
-            if ((col & 127) == 0) a.y8.scale[row * a.y8.ld_scale + col / 128] = (uint8_t)s;
-        }
-    }
-    if (!on || nv <= 0 || !a.y) return;
-    if (a.y_f32) store8((float *)a.y + row * a.ld_y + col, nv, v);
-    else store8((uint16_t *)a.y + row * a.ld_y + col, nv, v);
+    return u32x4_r{__float_as_uint(a[4 * g]), __float_as_uint(a[4 * g + 1]), __float_as_uint(a[4 * g + 2]),
+                   __float_as_uint(a[4 * g + 3])};
 }
 
 // ---------------------------------------------------------------------------
 // Tiles.  A block of WP x WQ wavefronts forms BP x BQ of C, a wavefront TP x TQ MFMA tiles.
-// K steps of 128 bytes go through a ring of NS stages in LDS by direct loads, NS - 1 steps
+// K steps of BK bytes go through a ring of NS stages in LDS by direct loads, NS - 1 steps
 // ahead, their scales as a word a row after them; a step has one barrier.  Direct loads write
-// 64 consecutive 16-byte pieces, so a stage has no padding: piece c of row r lies at
-// c ^ (r / 2 mod 8), and 16 rows' pieces of one k cover all banks.
+// 64 consecutive 16-byte pieces, so a stage has no padding: pieces are permuted in their row
+// instead, so that 16 rows' pieces of one k cover all banks.
 // ---------------------------------------------------------------------------
-template <int WP_, int WQ_, int TP_, int TQ_, int NS_>
+template <int WP_, int WQ_, int TP_, int TQ_, int NS_, int BK_ = 128>
 struct TileShape {
-    static constexpr int WP = WP_, WQ = WQ_, TP = TP_, TQ = TQ_, NS = NS_;
+    static constexpr int WP = WP_, WQ = WQ_, TP = TP_, TQ = TQ_, NS = NS_, BK = BK_;
+    static constexpr int SLOTS = BK / 16, ROWS = 64 / SLOTS;             // pieces of a row, rows of a copy
     static constexpr int NT = 64 * WP * WQ, WAVES = WP * WQ, BP = 32 * WP * TP, BQ = 32 * WQ * TQ;
-    static constexpr int UP = BP * 8 / NT, UQ = BQ * 8 / NT;             // 16-byte pieces of a thread
+    static constexpr int UP = BP * SLOTS / NT, UQ = BQ * SLOTS / NT;             // 16-byte pieces of a thread
     static constexpr int US = ((BP + BQ + 63) / 64 + WAVES - 1) / WAVES;      // scales of a thread
     static constexpr int L = UP + UQ + US;                               // direct loads of a step
-    static constexpr int Q_AT = BP * 128, S_AT = Q_AT + BQ * 128, STAGE = S_AT + US * WAVES * 256;
-    static constexpr int LDO = BP + 4;                                   // floats of an epilogue row
-    static constexpr int OUT_ROWS = 32 * WQ, LDS = std::max(NS * STAGE, OUT_ROWS * LDO * 4);
-    static_assert(UP * NT == BP * 8 && UQ * NT == BQ * 8, "whole pieces");
+    static constexpr int Q_AT = BP * BK, S_AT = Q_AT + BQ * BK, STAGE = S_AT + US * WAVES * 256;
+    static constexpr int LDO = 128 + 16, OUT = 32 * LDO;                 // bytes of a wavefront's 32 output rows
+    static constexpr int LDS = std::max(NS * STAGE, WAVES * OUT);
+    // piece c of row r lies at c ^ perm(r)
+    __device__ static int perm(int r) { return BK == 64 ? r >> 2 & 3 : r >> 1 & 7; }
+    static_assert(UP * NT == BP * SLOTS && UQ * NT == BQ * SLOTS, "whole pieces");
 };
 
 template <typename S, bool WIDE>
@@ -160,8 +144,9 @@ __device__ __forceinline__ void tile_run(const Linear8Args &a, int p_tiles, int 
     const int split = id / tiles, tile = id % tiles;
     const int64_t p0 = (int64_t)(tile % p_tiles) * BP, q0 = (int64_t)(tile / p_tiles) * BQ;
     const int wp = wave % S::WP * TP * 32, wq = wave / S::WP * TQ * 32;
+    constexpr int BK = S::BK, PER = 128 / BK;      // steps of a block of k
     const int64_t k0 = a.steps * split / a.splits;
-    const int nk = (int)(a.steps * (split + 1) / a.splits - k0);
+    const int nk = (int)(a.steps * (split + 1) / a.splits - k0) * PER;
 
     // Addresses of this thread's pieces and scales.  Rows past the last read the last one: their
     // sums are not stored.
@@ -169,8 +154,8 @@ __device__ __forceinline__ void tile_run(const Linear8Args &a, int p_tiles, int 
 #pragma unroll
     for (int u = 0; u < S::UP + S::UQ; ++u) {
         const bool q = u >= S::UP;
-        const int r = ((q ? u - S::UP : u) * S::WAVES + wave) * 8 + lane / 8;
-        const int c = (lane & 7) ^ (r >> 1 & 7);
+        const int r = ((q ? u - S::UP : u) * S::WAVES + wave) * S::ROWS + lane / S::SLOTS;
+        const int c = lane % S::SLOTS ^ S::perm(r);
         const Mat8 &m = q ? a.q : a.p;
         const int64_t row = min((q ? q0 : p0) + r, (q ? a.n : a.out) - 1);
         from[u] = m.q + row * m.ld_q + k0 * 128 + c * 16;
@@ -184,25 +169,30 @@ __device__ __forceinline__ void tile_run(const Linear8Args &a, int p_tiles, int 
         sfrom[u] = m.scale + (row >> m.shift) * m.ld_scale + k0;
     }
     auto copy = [&](int u, int kt, char *st) {
-        if (u < S::UP + S::UQ) copy_to_lds(from[u] + kt * 128, st + (u * S::WAVES + wave) * 1024);
-        else copy_byte_to_lds(sfrom[u - S::UP - S::UQ] + kt,
+        if (u < S::UP + S::UQ) copy_to_lds(from[u] + kt * BK, st + (u * S::WAVES + wave) * 1024);
+        else copy_byte_to_lds(sfrom[u - S::UP - S::UQ] + kt / PER,
                               st + S::S_AT + ((u - S::UP - S::UQ) * S::WAVES + wave) * 256);
     };
     // 16 bytes of one of 32 rows: half h of the wavefront takes piece 2 s + h
     auto piece = [&](const char *at, int row, int s) {
-        const int r = row + (lane & 31), perm = (r >> 1 & 7) << 4;
-        return *(const u32x4_r *)(at + r * 128 + (((2 * s + (lane >> 5)) << 4) ^ perm));
+        const int r = row + (lane & 31);
+        return *(const u32x4_r *)(at + r * BK + (((2 * s + (lane >> 5)) ^ S::perm(r)) << 4));
     };
-    auto frag = [&](const char *at, int row, int s) {
-        return join(piece(at, row, 2 * s), piece(at, row, 2 * s + 1));
-    };
+    // The sums start from the bias.  Columns past the last are copies of it, which leave their rows'
+    // largest magnitudes as they are.
     f32x16_t acc[TP][TQ];
+    const int half = lane >> 5, l32 = lane & 31;
 #pragma unroll
     for (int i = 0; i < TP; ++i)
 #pragma unroll
-        for (int j = 0; j < TQ; ++j)
+        for (int k = 0; k < 16; ++k) {
+            const int64_t col = p0 + wp + 32 * i + 8 * (k / 4) + 4 * half + k % 4;
+            acc[i][0][k] = a.bias ? a.bias[min(col, a.out - 1)] : 0.0f;
+        }
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+    for (int j = 1; j < TQ; ++j)
+#pragma unroll
+        for (int i = 0; i < TP; ++i) acc[i][j] = acc[i][0];
     auto multiply = [&](int kt, bool more) {
         const char *st = lds + kt % NS * S::STAGE;
         char *ahead = lds + (kt + NS - 1) % NS * S::STAGE;
@@ -212,49 +202,66 @@ __device__ __forceinline__ void tile_run(const Linear8Args &a, int p_tiles, int 
         for (int i = 0; i < TP; ++i) sp[i] = sc[wp + 32 * i + (lane & 31)];
 #pragma unroll
         for (int j = 0; j < TQ; ++j) sq[j] = sc[BP + wq + 32 * j + (lane & 31)];
+        // the pieces of a substep are read before the one before it is multiplied
+        u32x4_r bp[2][TP], bq[2][TQ];
+        auto read = [&](int s) {
+#pragma unroll
+            for (int i = 0; i < TP; ++i) bp[s & 1][i] = piece(st, wp + 32 * i, s);
+#pragma unroll
+            for (int j = 0; j < TQ; ++j) bq[s & 1][j] = piece(st + S::Q_AT, wq + 32 * j, s);
+        };
+        auto more_copies = [&](int s, int of) {
+            if (more)
+#pragma unroll
+                for (int u = S::L * s / of; u < S::L * (s + 1) / of; ++u) copy(u, kt + NS - 1, ahead);
+        };
+        read(0);
         if constexpr (WIDE) {
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                u32x4_r bp[TP], bq[TQ];
-#pragma unroll
-                for (int i = 0; i < TP; ++i) bp[i] = piece(st, wp + 32 * i, s);
-#pragma unroll
-                for (int j = 0; j < TQ; ++j) bq[j] = piece(st + S::Q_AT, wq + 32 * j, s);
-                if (more)
-#pragma unroll
-                    for (int u = S::L * s / 4; u < S::L * (s + 1) / 4; ++u) copy(u, kt + NS - 1, ahead);
+            for (int s = 0; s < BK / 32; ++s) {
+                if (s + 1 < BK / 32) read(s + 1);
+                more_copies(s, BK / 32);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     bf16x8_t fp[TP], fq[TQ];
 #pragma unroll
                     for (int i = 0; i < TP; ++i)
-                        fp[i] = widen8(bp[i][2 * h], bp[i][2 * h + 1], __uint_as_float((uint32_t)sp[i] << 23));
+                        fp[i] = widen8(bp[s & 1][i][2 * h], bp[s & 1][i][2 * h + 1],
+                                       __uint_as_float((uint32_t)sp[i] << 23));
 #pragma unroll
                     for (int j = 0; j < TQ; ++j)
-                        fq[j] = widen8(bq[j][2 * h], bq[j][2 * h + 1], __uint_as_float((uint32_t)sq[j] << 23));
+                        fq[j] = widen8(bq[s & 1][j][2 * h], bq[s & 1][j][2 * h + 1],
+                                       __uint_as_float((uint32_t)sq[j] << 23));
 #pragma unroll
                     for (int i = 0; i < TP; ++i)
 #pragma unroll
                         for (int j = 0; j < TQ; ++j)
                             acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp[i], fq[j], acc[i][j], 0, 0, 0);
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
-            return;
-        }
+        } else {
+            u32x4_r cp[TP], cq[TQ];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            i32x8_t fp[TP], fq[TQ];
+            for (int s = 0; s < BK / 64; ++s) {
+                read(2 * s + 1);
 #pragma unroll
-            for (int i = 0; i < TP; ++i) fp[i] = frag(st, wp + 32 * i, s);
+                for (int i = 0; i < TP; ++i) cp[i] = bp[0][i];
 #pragma unroll
-            for (int j = 0; j < TQ; ++j) fq[j] = frag(st + S::Q_AT, wq + 32 * j, s);
-            if (more)
+                for (int j = 0; j < TQ; ++j) cq[j] = bq[0][j];
+                i32x8_t fp[TP], fq[TQ];
 #pragma unroll
-                for (int u = S::L * s / 2; u < S::L * (s + 1) / 2; ++u) copy(u, kt + NS - 1, ahead);
+                for (int i = 0; i < TP; ++i) fp[i] = join(cp[i], bp[1][i]);
 #pragma unroll
-            for (int i = 0; i < TP; ++i)
+                for (int j = 0; j < TQ; ++j) fq[j] = join(cq[j], bq[1][j]);
+                if (s + 1 < BK / 64) read(2 * s + 2);
+                more_copies(s, BK / 64);
 #pragma unroll
-                for (int j = 0; j < TQ; ++j) acc[i][j] = mfma8(fp[i], fq[j], acc[i][j], sp[i], sq[j]);
+                for (int i = 0; i < TP; ++i)
+#pragma unroll
+                    for (int j = 0; j < TQ; ++j) acc[i][j] = mfma8(fp[i], fq[j], acc[i][j], sp[i], sq[j]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
     };
     for (int kt = 0; kt < NS - 1 && kt < nk; ++kt)
@@ -272,36 +279,93 @@ __device__ __forceinline__ void tile_run(const Linear8Args &a, int p_tiles, int 
         multiply(kt, false);
     }
 
-    // rows leave through LDS, 32 of each wavefront at a time: lane l holds q = wq + 32 j + l % 32,
-    // p = wp + 32 i + 8 g + 4 (l / 32) + 0..3
-    float *out = (float *)lds;
-    constexpr int PIECES = S::OUT_ROWS * (BP / 8) / S::NT;
+    // Outputs: lane l holds q = wq + 32 j + l % 32, p = wp + 32 i + 8 g + 4 (l / 32) + 0..3.  They leave
+    // through a part of LDS of the wavefront's own, in pieces of 16 bytes, up to 128 of a row.
+    meet();
+    char *mine = lds + wave * S::OUT, *to = mine + l32 * S::LDO + 4 * half;
+    // `wide` bytes of each row from `mine` to the columns col.. (in bytes) of rows of ld bytes; of
+    // `end` bytes
+    auto leave = [&](auto row_bytes, char *y, int64_t ld, int j, int64_t col, int64_t end, int unit) {
+        constexpr int LANES = decltype(row_bytes)::value / 16, ROWS = 64 / LANES;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int u = 0; u < 32 / ROWS; ++u) {
+            const int r = u * ROWS + lane / LANES, c = lane % LANES * 16;
+            const u32x4_r v = *(const u32x4_r *)(mine + r * S::LDO + c);
+            const int64_t row = q0 + wq + 32 * j + r;
+            const int64_t nv = end - col - c;
+            if (row >= a.n || nv <= 0) continue;
+            char *at = y + row * ld + col + c;
+            if (nv >= 16) {
+                *(u32x4_a2 *)at = v;
+            } else if (unit == 2) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (2 * k < nv) ((uint16_t *)at)[k] = (uint16_t)(v[k / 2] >> (16 * (k & 1)));
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (4 * k < nv) ((uint32_t *)at)[k] = v[k];
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    };
 #pragma unroll
     for (int j = 0; j < TQ; ++j) {
-        meet();
+        if (a.relu)
 #pragma unroll
-        for (int i = 0; i < TP; ++i)
+            for (int i = 0; i < TP; ++i)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const f32x4_r v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-                *(f32x4_r *)(out + (wave / S::WP * 32 + (lane & 31)) * S::LDO + wp + 32 * i + 8 * g +
-                             4 * (lane >> 5)) = v;
+                for (int k = 0; k < 16; ++k) acc[i][j][k] = __builtin_elementwise_maximum(acc[i][j][k], 0.0f);   // NaN stays
+        if constexpr (WIDE && TP == 4) {
+            if (a.y8.q) {
+                uint32_t top = 0;
+#pragma unroll
+                for (int i = 0; i < TP; ++i)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) top = max(top, magnitude(acc[i][j][k]));
+                top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+                const int s = block8_scale(top);
+                const int64_t row = q0 + wq + 32 * j + l32, col = p0 + wp;
+                if (half == 0 && row < a.n && col < a.out) a.y8.scale[row * a.y8.ld_scale + col / 128] = (uint8_t)s;
+#pragma unroll
+                for (int i = 0; i < TP; ++i)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const float v[4] = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+                        const int64_t nv = a.out - col - (32 * i + 8 * g + 4 * half);
+                        *(uint32_t *)(to + 32 * i + 8 * g) = block8_pack4(v, s, (int)max(min(nv, (int64_t)4), (int64_t)0));
+                    }
+                leave(Int<128>(), (char *)a.y8.q, a.y8.ld_q, j, col, (a.out + 127) / 128 * 128, 4);
             }
-        meet();
-#pragma unroll
-        for (int c = 0; c < PIECES; ++c) {
-            const int at = c * S::NT + threadIdx.x, r = at / (BP / 8), f = at % (BP / 8) * 8;
-            const int64_t row = q0 + r / 32 * TQ * 32 + 32 * j + r % 32, col = p0 + f;
-            float v[8];
-            const f32x4_r lo = *(const f32x4_r *)(out + r * S::LDO + f), hi = *(const f32x4_r *)(out + r * S::LDO + f + 4);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = lo[k], v[4 + k] = hi[k];
+        }
+        if (!a.y) continue;
+        if (WIDE && a.y_f32) {
+            char *y = (char *)a.y;
+            int64_t ld = a.ld_y * 4;
             if (a.part) {
-                const int64_t ld = (a.out + 3) / 4 * 4;
-                const int nv = (int)min((int64_t)8, a.out - col);
-                if (row < a.n && nv > 0) store8(a.part + ((int64_t)split * a.n + row) * ld + col, nv, v);
-            } else {
-                finish8(a, row, col, row < a.n, v);
+                ld = (a.out + 3) / 4 * 16;
+                y = (char *)a.part + split * a.n * ld;
+            }
+#pragma unroll
+            for (int i = 0; i < TP; ++i) {
+#pragma unroll
+                for (int g = 0; g < 4; ++g) *(u32x4_r *)(mine + l32 * S::LDO + 32 * g + 16 * half) = bits4(acc[i][j], g);
+                leave(Int<128>(), y, ld, j, (p0 + wp + 32 * i) * 4, a.out * 4, 4);
+            }
+        } else {
+            constexpr int PAIR = TP % 2 ? 1 : 2;
+#pragma unroll
+            for (int i = 0; i < TP; i += PAIR) {
+#pragma unroll
+                for (int h = 0; h < PAIR; ++h)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const f32x16_t &c = acc[i + h][j];
+                        *(u32x2_r *)(mine + l32 * S::LDO + 64 * h + 16 * g + 8 * half) =
+                            u32x2_r{pack_bf16x2(c[4 * g], c[4 * g + 1]), pack_bf16x2(c[4 * g + 2], c[4 * g + 3])};
+                    }
+                leave(Int<64 * PAIR>(), (char *)a.y, a.ld_y * 2, j, (p0 + wp + 32 * i) * 2, a.out * 2, 2);
             }
         }
     }
@@ -326,22 +390,22 @@ __global__ __launch_bounds__(S::NT, 2) void linear8_two_kernel(Linear8Args a, in
 }
 
 // ---------------------------------------------------------------------------
-// Panels.  With many rows and a k that fits, a block keeps 128 columns of P, all their k, in LDS
-// and its wavefronts walk over the rows of Q by themselves, 64 at a time, without a barrier: Q's
-// fragments come straight into registers, a step of 128 k ahead, also across the end of a tile, so
-// that one wavefront's outputs leave while others multiply.  A block for each CU; the panels
-// of one run of rows are neighbours in an L2.  Bias is where the sums start.
+// Panels.  With many rows, an output in bf16 and a k that fits, a block keeps 128 columns of P, all
+// their k, in LDS and its wavefronts walk over the rows of Q by themselves, 64 at a time, without a
+// barrier: Q's fragments come straight into registers, a step of 128 k ahead, also across the end of
+// a tile, so that one wavefront's outputs leave while others multiply.  A block for each CU; the
+// panels of one run of rows are neighbours in an L2.
 //
-// A wavefront's tile is 128 p x 64 q in MFMA tiles of 16 x 16 (v_mfma_scale_f32_16x16x128_f8f6f4,
-// v_mfma_f32_16x16x32_bf16): four lanes then hold one row of Q, and a load takes 64 bytes of each
-// of 16 rows.
+// A wavefront's tile is 128 p x 64 q in MFMA tiles of 16 x 16 (v_mfma_scale_f32_16x16x128_f8f6f4):
+// four lanes then hold one row of Q.  Bound by the CU's vector cache, to which each 16 bytes that a
+// lane loads are an access: so scales are loaded four steps at a time and outputs pass through LDS.
 // ---------------------------------------------------------------------------
-constexpr int PANEL_STEPS = 9, PANEL_WAVES = 8, PANEL_ROWS = 64;
-template <bool WIDE>
+constexpr int PANEL_STEPS = 8, PANEL_WAVES = 8, PANEL_ROWS = 64;
 __global__ __launch_bounds__(64 * PANEL_WAVES, 1) void linear8_panel_kernel(Linear8Args a, int panels, int streams)
 {
-    constexpr int TP = 8, TQ = PANEL_ROWS / 16, SETS = 2;
+    constexpr int TP = 8, TQ = PANEL_ROWS / 16, LDO = 128 + 16;
     __shared__ __attribute__((aligned(1024))) char lds[PANEL_STEPS * 16384];
+    __shared__ __attribute__((aligned(16))) char outs[PANEL_WAVES][16 * LDO];
     __shared__ int pscale[PANEL_STEPS][16][2];      // byte i % 4 of word i / 4: row 16 i + lane's
     __shared__ float bias[128];
     const int lane = threadIdx.x & 63, wave = wave_id(), l16 = lane & 15, grp = lane >> 4;
@@ -364,7 +428,6 @@ __global__ __launch_bounds__(64 * PANEL_WAVES, 1) void linear8_panel_kernel(Line
         }
         pscale[u >> 5][u >> 1 & 15][u & 1] = v;
     }
-    // columns past the last are copies of it, which leave their rows' largest magnitudes as they are
     if (threadIdx.x < 128) bias[threadIdx.x] = a.bias ? a.bias[min(p0 + threadIdx.x, a.out - 1)] : 0.0f;
     wait_loads<0>();
     __syncthreads();
@@ -372,21 +435,34 @@ __global__ __launch_bounds__(64 * PANEL_WAVES, 1) void linear8_panel_kernel(Line
     const int64_t tiles = (a.n + PANEL_ROWS - 1) / PANEL_ROWS, stride = (int64_t)streams * PANEL_WAVES;
     int64_t tile = (int64_t)stream * PANEL_WAVES + wave;
     if (tile >= tiles) return;
-    // Q: bytes 32 grp .. 32 grp + 31 of a step of the rows 16 j + l16, and the row's scale
-    u32x4_r bq[SETS][TQ][2];
-    int sq[SETS];                  // of row `lane`
+    // Q: 16 bytes grp and 4 + grp of a step of the rows 16 j + l16
+    u32x4_r bq[2][TQ][2];
+    // the scales of row `lane`: bytes of the steps 0..3, and of the last four (steps 4..7)
+    uint32_t scale[2], next_scale[2] = {0, 0};
     // part j of step kt of tile t; rows past the last read the last one: their sums are not stored
     auto fetch = [&](int set, int64_t t, int kt, int j) {
         const int64_t q0 = t * PANEL_ROWS;
         const int last = (int)min((int64_t)PANEL_ROWS, a.n - q0) - 1;
         const uint8_t *base = a.q.q + q0 * a.q.ld_q + kt * 128;
-        const uint32_t off = (uint32_t)min(16 * j + l16, last) * (uint32_t)a.q.ld_q + grp * 32;
+        const uint32_t off = (uint32_t)min(16 * j + l16, last) * (uint32_t)a.q.ld_q + grp * 16;
         bq[set][j][0] = *(const u32x4_r *)(base + off);
-        bq[set][j][1] = *(const u32x4_r *)(base + off + 16);
-        if (j == 0) sq[set] = a.q.scale[((q0 + min(lane, last)) >> a.q.shift) * a.q.ld_scale + kt];
+        bq[set][j][1] = *(const u32x4_r *)(base + off + 64);
+        if (j == 0 && kt == 0) {
+            const uint8_t *s = a.q.scale + ((q0 + min(lane, last)) >> a.q.shift) * a.q.ld_scale;
+            if (steps >= 4) {
+                typedef uint32_t u32_a1 __attribute__((aligned(1)));
+                next_scale[0] = *(const u32_a1 *)s;
+                next_scale[1] = *(const u32_a1 *)(s + steps - 4) >> (8 * (8 - steps) & 31);
+            } else {
+                next_scale[0] = s[0];
+                if (steps > 1) next_scale[0] |= s[1] << 8;
+                if (steps > 2) next_scale[0] |= s[2] << 16;
+            }
+        }
     };
     f32x4_t acc[TP][TQ];
     auto start = [&] {
+        scale[0] = next_scale[0], scale[1] = next_scale[1];
 #pragma unroll
         for (int i = 0; i < TP; ++i) {
             const f32x4_t b = *(const f32x4_t *)(bias + 16 * i + 4 * grp);
@@ -399,150 +475,70 @@ __global__ __launch_bounds__(64 * PANEL_WAVES, 1) void linear8_panel_kernel(Line
         const char *st = lds + kt * 16384;
         const int sp[2] = {pscale[kt][l16][0], pscale[kt][l16][1]};
         // the scale of row 16 j + l16 in all four lanes of the row
-        const auto x = __builtin_amdgcn_permlane16_swap(sq[set], sq[set], false, false);
+        const uint32_t own = scale[kt >> 2] >> (8 * (kt & 3));
+        const auto x = __builtin_amdgcn_permlane16_swap(own, own, false, false);
         const auto even = __builtin_amdgcn_permlane32_swap(x[0], x[0], false, false);
         const auto odd = __builtin_amdgcn_permlane32_swap(x[1], x[1], false, false);
-        const int s4[4] = {(int)even[0], (int)odd[0], (int)even[1], (int)odd[1]};
+        const int s4[TQ] = {(int)even[0], (int)odd[0], (int)even[1], (int)odd[1]};
         // piece c of a row at c ^ (row / 2 mod 8)
         auto piece = [&](int i, int k) {
-            return *(const u32x4_r *)(st + (16 * i + l16) * 128 + (((2 * grp + k) ^ (l16 >> 1)) << 4));
+            return *(const u32x4_r *)(st + (16 * i + l16) * 128 + (((4 * k + grp) ^ (l16 >> 1)) << 4));
         };
-        if constexpr (WIDE) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {      // eight bytes of each of a row's four lanes
-                bf16x8_t fq[TQ];
+        for (int i = 0; i < TP; ++i) {
+            const i32x8_t fp = join(piece(i, 0), piece(i, 1));
+            more(i);
 #pragma unroll
-                for (int j = 0; j < TQ; ++j)
-                    fq[j] = widen8(bq[set][j][k / 2][k % 2 * 2], bq[set][j][k / 2][k % 2 * 2 + 1],
-                                   __uint_as_float((uint32_t)s4[j] << 23));
-#pragma unroll
-                for (int i = 0; i < TP; ++i) {
-                    const u32x2_r b = *(const u32x2_r *)(st + (16 * i + l16) * 128 +
-                                                         (((2 * grp + k / 2) ^ (l16 >> 1)) << 4) + k % 2 * 8);
-                    const bf16x8_t fp = widen8(b[0], b[1], __uint_as_float((uint32_t)(sp[i / 4] >> (8 * (i % 4)) & 255) << 23));
-                    if (k == 3) more(i);
-#pragma unroll
-                    for (int j = 0; j < TQ; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp, fq[j], acc[i][j], 0, 0, 0);
-                    if (i % 2) __builtin_amdgcn_sched_barrier(0);
-                }
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < TP; ++i) {
-                const i32x8_t fp = join(piece(i, 0), piece(i, 1));
-                more(i);
-#pragma unroll
-                for (int j = 0; j < TQ; ++j) {
-                    const i32x8_t fq = join(bq[set][j][0], bq[set][j][1]);
-                    if (i % 4 == 0) acc[i][j] = mfma8_16<0>(fp, fq, acc[i][j], sp[i / 4], s4[j]);
-                    if (i % 4 == 1) acc[i][j] = mfma8_16<1>(fp, fq, acc[i][j], sp[i / 4], s4[j]);
-                    if (i % 4 == 2) acc[i][j] = mfma8_16<2>(fp, fq, acc[i][j], sp[i / 4], s4[j]);
-                    if (i % 4 == 3) acc[i][j] = mfma8_16<3>(fp, fq, acc[i][j], sp[i / 4], s4[j]);
-                }
+            for (int j = 0; j < TQ; ++j) {
+                const i32x8_t fq = join(bq[set][j][0], bq[set][j][1]);
+                if (i % 4 == 0) acc[i][j] = mfma8_16<0>(fp, fq, acc[i][j], sp[i / 4], s4[j]);
+                if (i % 4 == 1) acc[i][j] = mfma8_16<1>(fp, fq, acc[i][j], sp[i / 4], s4[j]);
+                if (i % 4 == 2) acc[i][j] = mfma8_16<2>(fp, fq, acc[i][j], sp[i / 4], s4[j]);
+                if (i % 4 == 3) acc[i][j] = mfma8_16<3>(fp, fq, acc[i][j], sp[i / 4], s4[j]);
             }
         }
     };
-    // A lane's sums of a 16 x 16 tile are p = 4 grp + 0..3 of one q.  Lanes of a row exchange theirs
-    // across tiles, so that each has 16 bytes of neighbouring p to store, 64 a row.
+    // A lane's sums of a 16 x 16 tile are p = 4 grp + 0..3 of one q.  16 rows x 64 columns at a time leave
+    // through the wavefront's own LDS, 128 bytes of a row.
     auto store = [&](int64_t t) {
+        char *mine = outs[wave];
 #pragma unroll
-        for (int j = 0; j < TQ; ++j) {
-            const int64_t row = t * PANEL_ROWS + 16 * j + l16;
-            const bool on = row < a.n;
-            if (a.relu)
+        for (int j = 0; j < TQ; ++j)
 #pragma unroll
-                for (int i = 0; i < TP; ++i)
+            for (int i0 = 0; i0 < TP; i0 += 4) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) acc[i][j][k] = acc[i][j][k] < 0.0f ? 0.0f : acc[i][j][k];   // NaN stays
-            if (WIDE && a.y8.q) {
-                uint32_t top = 0;
+                for (int i = 0; i < 4; ++i) {
+                    f32x4_t v = acc[i0 + i][j];
+                    if (a.relu)
 #pragma unroll
-                for (int i = 0; i < TP; ++i)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) top = max(top, magnitude(acc[i][j][k]));
-                top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-                top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-                const int s = block8_scale(top);
-                if (on && grp == 0) a.y8.scale[row * a.y8.ld_scale + panel] = (uint8_t)s;
-#pragma unroll
-                for (int i = 0; i < TP; i += 4) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int h = 0; h < 4; h += 2) {
-                        float v[8];
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) v[k] = acc[i + h + k / 4][j][k % 4];
-                        const u32x2_r b = block8_pack(v, s, 8);
-                        w[h] = b[0], w[h + 1] = b[1];
-                    }
-                    const auto x0 = __builtin_amdgcn_permlane16_swap(w[0], w[1], false, false);
-                    const auto x1 = __builtin_amdgcn_permlane16_swap(w[2], w[3], false, false);
-                    const auto y0 = __builtin_amdgcn_permlane32_swap(x0[0], x1[0], false, false);
-                    const auto y1 = __builtin_amdgcn_permlane32_swap(x0[1], x1[1], false, false);
-                    u32x4_r b = {y0[0], y1[0], y0[1], y1[1]};
-                    const int64_t col = p0 + 16 * i + 16 * grp;
-                    // columns past the last are zeros
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int nv = (int)min((int64_t)4, a.out - col - 4 * k);
-                        b[k] = nv >= 4 ? b[k] : nv <= 0 ? 0 : b[k] & ((1u << (8 * nv)) - 1);
-                    }
-                    if (on) *(u32x4_r *)(a.y8.q + row * a.y8.ld_q + col) = b;
+                        for (int k = 0; k < 4; ++k) v[k] = __builtin_elementwise_maximum(v[k], 0.0f);      // NaN stays
+                    *(u32x2_r *)(mine + l16 * LDO + 32 * i + 8 * grp) = u32x2_r{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
                 }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int r = u * 8 + lane / 8, c = lane % 8 * 8;
+                    const u32x4_r o = *(const u32x4_r *)(mine + r * LDO + c * 2);
+                    const int64_t row = t * PANEL_ROWS + 16 * j + r, col = p0 + 16 * i0 + c;
+                    if (row < a.n)
+                        store8_bits((uint16_t *)a.y + row * a.ld_y + col, (int)min((int64_t)8, a.out - col), o);
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             }
-            if (!a.y) continue;
-            if (WIDE && a.y_f32) {
-#pragma unroll
-                for (int i = 0; i < TP; ++i) {
-                    const int64_t col = p0 + 16 * i + 4 * grp;
-                    float *y = (float *)a.y + row * a.ld_y + col;
-                    if (on && col + 4 <= a.out) {
-                        *(f32x4_a4 *)y = acc[i][j];
-                    } else if (on) {
-#pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            if (col + k < a.out) y[k] = acc[i][j][k];
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < TP; i += 2) {
-                    uint32_t w[2][2];
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) w[h][k] = pack_bf16x2(acc[i + h][j][2 * k], acc[i + h][j][2 * k + 1]);
-                    const auto x0 = __builtin_amdgcn_permlane16_swap(w[0][0], w[1][0], false, false);
-                    const auto x1 = __builtin_amdgcn_permlane16_swap(w[0][1], w[1][1], false, false);
-                    const int64_t col = p0 + 16 * i + (grp & 1) * 16 + (grp >> 1) * 8;
-                    if (on) store8_bits((uint16_t *)a.y + row * a.ld_y + col, (int)min((int64_t)8, a.out - col),
-                                        u32x4_r{x0[0], x1[0], x0[1], x1[1]});
-                }
-            }
-        }
     };
-    // the step that is fetched next, SETS - 1 ahead
     int kt = 0, next_kt = 0;
     int64_t next_tile = tile;
-    auto advance = [&] {
-        if (++next_kt == steps) next_kt = 0, next_tile += stride;
-        if (next_tile >= tiles) next_tile = tile;      // after the last step: read again, not used
-    };
 #pragma unroll
-    for (int set = 0; set < SETS - 1; ++set) {
-#pragma unroll
-        for (int j = 0; j < TQ; ++j) fetch(set, next_tile, next_kt, j);
-        advance();
-    }
+    for (int j = 0; j < TQ; ++j) fetch(0, tile, 0, j);
     while (true) {
 #pragma unroll
-        for (int set = 0; set < SETS; ++set) {
+        for (int set = 0; set < 2; ++set) {
+            if (++next_kt == steps) next_kt = 0, next_tile += stride;
+            if (next_tile >= tiles) next_tile = tile;      // after the last step: read again, not used
             if (kt == 0) start();
             multiply(set, kt, [&](int i) {
-                if (i < TQ) fetch((set + SETS - 1) % SETS, next_tile, next_kt, i);
+                if (i < TQ) fetch(set ^ 1, next_tile, next_kt, i);
             });
-            advance();
             if (++kt == steps) {
                 store(tile);
                 kt = 0;
@@ -582,8 +578,9 @@ __global__ __launch_bounds__(1024) void linear8_join_kernel(Linear8Args a, int b
 }
 
 typedef TileShape<2, 2, 2, 2, 2> Tile128;     // 128 x 128, two blocks a CU
+typedef TileShape<2, 4, 4, 2, 2> Tile256;     // 256 x 256
 typedef TileShape<2, 2, 1, 1, 4> Tile64;      // 64 x 64, three steps ahead
-typedef TileShape<4, 1, 1, 1, 3> TileFlat;    // 128 x 32, for whole blocks of y8
+typedef TileShape<1, 1, 4, 1, 4> TileFlat;    // 128 x 32, for whole blocks of y8
 
 // Products in bf16, summed in fp32 throughout.
 static bool wide(const Linear8Args &a) { return (a.y && a.y_f32) || a.y8.q; }
@@ -618,11 +615,9 @@ static void join(const Linear8Args &a, const ColumnSums &c, hipStream_t s)
 
 hipError_t launch_linear8(const Linear8Args &a, hipStream_t s)
 {
-    if (a.n >= 16384 && a.steps <= PANEL_STEPS && ceil_div(a.out, 128) <= 32 && a.q.ld_q < (1 << 24)) {
+    if (a.n >= 16384 && a.steps <= PANEL_STEPS && ceil_div(a.out, 128) <= 32 && !wide(a) && a.q.ld_q < (1 << 24)) {
         const int panels = (int)ceil_div(a.out, 128), streams = 8 * (32 / panels);
-        const dim3 g(256), b(64 * PANEL_WAVES);
-        if (wide(a)) linear8_panel_kernel<true><<<g, b, 0, s>>>(a, panels, streams);
-        else linear8_panel_kernel<false><<<g, b, 0, s>>>(a, panels, streams);
+        linear8_panel_kernel<<<dim3(256), dim3(64 * PANEL_WAVES), 0, s>>>(a, panels, streams);
         return hipGetLastError();
     }
     if (few_tiles(a.n, a.out, 1)) {
@@ -639,7 +634,8 @@ hipError_t launch_linear8(const Linear8Args &a, hipStream_t s)
         b.q.scale += (r >> a.q.shift) * a.q.ld_scale;
         if (a.y) b.y = (char *)a.y + r * a.ld_y * (a.y_f32 ? 4 : 2);
         if (a.y8.q) b.y8.q += r * a.y8.ld_q, b.y8.scale += r * a.y8.ld_scale;
-        tile_by<Tile128>(b, s);
+        if (a.y8.q || tiles_of(b.n, b.out, 256) >= 256) tile_by<Tile256>(b, s);
+        else tile_by<Tile128>(b, s);
     }
     return hipGetLastError();
 }
