@@ -22,7 +22,6 @@
 namespace im {
 
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
-typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
@@ -87,13 +86,6 @@ __device__ __forceinline__ i32x8_t join(u32x4_r lo, u32x4_r hi)
 __device__ __forceinline__ f32x16_t mfma8(i32x8_t a, i32x8_t b, f32x16_t acc, int sa, int sb)
 {
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc, 0, 0, 0, sa, 0, sb);
-}
-
-// The same of 16 rows each and 128 k, 32 bytes of a row in each of its four lanes; sa in byte A.
-template <int A>
-__device__ __forceinline__ f32x4_t mfma8_16(i32x8_t a, i32x8_t b, f32x4_t acc, int sa, int sb)
-{
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 0, 0, A, sa, 0, sb);
 }
 
 // Eight e4m3 values times the scale's power of two as bf16: exact, but for values below 2^-126.
@@ -182,13 +174,24 @@ __device__ __forceinline__ void tile_run(const Linear8Args &a, int p_tiles, int 
     // largest magnitudes as they are.
     f32x16_t acc[TP][TQ];
     const int half = lane >> 5, l32 = lane & 31;
+    if (a.bias && p0 + BP <= a.out) {
 #pragma unroll
-    for (int i = 0; i < TP; ++i)
+        for (int i = 0; i < TP; ++i)
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            const int64_t col = p0 + wp + 32 * i + 8 * (k / 4) + 4 * half + k % 4;
-            acc[i][0][k] = a.bias ? a.bias[min(col, a.out - 1)] : 0.0f;
-        }
+            for (int g = 0; g < 4; ++g) {
+                const f32x4_r b = *(const f32x4_a4 *)(a.bias + p0 + wp + 32 * i + 8 * g + 4 * half);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) acc[i][0][4 * g + k] = b[k];
+            }
+    } else {
+#pragma unroll
+        for (int i = 0; i < TP; ++i)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                const int64_t col = p0 + wp + 32 * i + 8 * (k / 4) + 4 * half + k % 4;
+                acc[i][0][k] = a.bias ? a.bias[min(col, a.out - 1)] : 0.0f;
+            }
+    }
 #pragma unroll
     for (int j = 1; j < TQ; ++j)
 #pragma unroll
@@ -389,166 +392,6 @@ __global__ __launch_bounds__(S::NT, 2) void linear8_two_kernel(Linear8Args a, in
     else tile_run<S, true>(b, b_p_tiles, b_tiles, id - a_blocks, lds);
 }
 
-// ---------------------------------------------------------------------------
-// Panels.  With many rows, an output in bf16 and a k that fits, a block keeps 128 columns of P, all
-// their k, in LDS and its wavefronts walk over the rows of Q by themselves, 64 at a time, without a
-// barrier: Q's fragments come straight into registers, a step of 128 k ahead, also across the end of
-// a tile, so that one wavefront's outputs leave while others multiply.  A block for each CU; the
-// panels of one run of rows are neighbours in an L2.
-//
-// A wavefront's tile is 128 p x 64 q in MFMA tiles of 16 x 16 (v_mfma_scale_f32_16x16x128_f8f6f4):
-// four lanes then hold one row of Q.  Bound by the CU's vector cache, to which each 16 bytes that a
-// lane loads are an access: so scales are loaded four steps at a time and outputs pass through LDS.
-// ---------------------------------------------------------------------------
-constexpr int PANEL_STEPS = 8, PANEL_WAVES = 8, PANEL_ROWS = 64;
-__global__ __launch_bounds__(64 * PANEL_WAVES, 1) void linear8_panel_kernel(Linear8Args a, int panels, int streams)
-{
-    constexpr int TP = 8, TQ = PANEL_ROWS / 16, LDO = 128 + 16;
-    __shared__ __attribute__((aligned(1024))) char lds[PANEL_STEPS * 16384];
-    __shared__ __attribute__((aligned(16))) char outs[PANEL_WAVES][16 * LDO];
-    __shared__ int pscale[PANEL_STEPS][16][2];      // byte i % 4 of word i / 4: row 16 i + lane's
-    __shared__ float bias[128];
-    const int lane = threadIdx.x & 63, wave = wave_id(), l16 = lane & 15, grp = lane >> 4;
-    const int place = blockIdx.x >> 3, panel = place % panels;
-    const int stream = place / panels * 8 + (blockIdx.x & 7);
-    if (place / panels * 8 >= streams) return;
-    const int64_t p0 = (int64_t)panel * 128;
-    const int steps = (int)a.steps;
-    for (int u = wave; u < steps * 16; u += PANEL_WAVES) {
-        const int r = (u & 15) * 8 + lane / 8, c = (lane & 7) ^ (r >> 1 & 7);
-        const int64_t row = min(p0 + r, a.out - 1);
-        copy_to_lds(a.p.q + row * a.p.ld_q + (u >> 4) * 128 + c * 16, lds + u * 1024);
-    }
-    for (int u = threadIdx.x; u < steps * 32; u += 64 * PANEL_WAVES) {
-        int v = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t row = min(p0 + 64 * (u & 1) + 16 * i + (u >> 1 & 15), a.out - 1);
-            v |= a.p.scale[(row >> a.p.shift) * a.p.ld_scale + (u >> 5)] << (8 * i);
-        }
-        pscale[u >> 5][u >> 1 & 15][u & 1] = v;
-    }
-    if (threadIdx.x < 128) bias[threadIdx.x] = a.bias ? a.bias[min(p0 + threadIdx.x, a.out - 1)] : 0.0f;
-    wait_loads<0>();
-    __syncthreads();
-
-    const int64_t tiles = (a.n + PANEL_ROWS - 1) / PANEL_ROWS, stride = (int64_t)streams * PANEL_WAVES;
-    int64_t tile = (int64_t)stream * PANEL_WAVES + wave;
-    if (tile >= tiles) return;
-    // Q: 16 bytes grp and 4 + grp of a step of the rows 16 j + l16
-    u32x4_r bq[2][TQ][2];
-    // the scales of row `lane`: bytes of the steps 0..3, and of the last four (steps 4..7)
-    uint32_t scale[2], next_scale[2] = {0, 0};
-    // part j of step kt of tile t; rows past the last read the last one: their sums are not stored
-    auto fetch = [&](int set, int64_t t, int kt, int j) {
-        const int64_t q0 = t * PANEL_ROWS;
-        const int last = (int)min((int64_t)PANEL_ROWS, a.n - q0) - 1;
-        const uint8_t *base = a.q.q + q0 * a.q.ld_q + kt * 128;
-        const uint32_t off = (uint32_t)min(16 * j + l16, last) * (uint32_t)a.q.ld_q + grp * 16;
-        bq[set][j][0] = *(const u32x4_r *)(base + off);
-        bq[set][j][1] = *(const u32x4_r *)(base + off + 64);
-        if (j == 0 && kt == 0) {
-            const uint8_t *s = a.q.scale + ((q0 + min(lane, last)) >> a.q.shift) * a.q.ld_scale;
-            if (steps >= 4) {
-                typedef uint32_t u32_a1 __attribute__((aligned(1)));
-                next_scale[0] = *(const u32_a1 *)s;
-                next_scale[1] = *(const u32_a1 *)(s + steps - 4) >> (8 * (8 - steps) & 31);
-            } else {
-                next_scale[0] = s[0];
-                if (steps > 1) next_scale[0] |= s[1] << 8;
-                if (steps > 2) next_scale[0] |= s[2] << 16;
-            }
-        }
-    };
-    f32x4_t acc[TP][TQ];
-    auto start = [&] {
-        scale[0] = next_scale[0], scale[1] = next_scale[1];
-#pragma unroll
-        for (int i = 0; i < TP; ++i) {
-            const f32x4_t b = *(const f32x4_t *)(bias + 16 * i + 4 * grp);
-#pragma unroll
-            for (int j = 0; j < TQ; ++j) acc[i][j] = b;
-        }
-    };
-    // a step's products; more(i): work beside those of the i-th tile of P
-    auto multiply = [&](int set, int kt, auto more) {
-        const char *st = lds + kt * 16384;
-        const int sp[2] = {pscale[kt][l16][0], pscale[kt][l16][1]};
-        // the scale of row 16 j + l16 in all four lanes of the row
-        const uint32_t own = scale[kt >> 2] >> (8 * (kt & 3));
-        const auto x = __builtin_amdgcn_permlane16_swap(own, own, false, false);
-        const auto even = __builtin_amdgcn_permlane32_swap(x[0], x[0], false, false);
-        const auto odd = __builtin_amdgcn_permlane32_swap(x[1], x[1], false, false);
-        const int s4[TQ] = {(int)even[0], (int)odd[0], (int)even[1], (int)odd[1]};
-        // piece c of a row at c ^ (row / 2 mod 8)
-        auto piece = [&](int i, int k) {
-            return *(const u32x4_r *)(st + (16 * i + l16) * 128 + (((4 * k + grp) ^ (l16 >> 1)) << 4));
-        };
-#pragma unroll
-        for (int i = 0; i < TP; ++i) {
-            const i32x8_t fp = join(piece(i, 0), piece(i, 1));
-            more(i);
-#pragma unroll
-            for (int j = 0; j < TQ; ++j) {
-                const i32x8_t fq = join(bq[set][j][0], bq[set][j][1]);
-                if (i % 4 == 0) acc[i][j] = mfma8_16<0>(fp, fq, acc[i][j], sp[i / 4], s4[j]);
-                if (i % 4 == 1) acc[i][j] = mfma8_16<1>(fp, fq, acc[i][j], sp[i / 4], s4[j]);
-                if (i % 4 == 2) acc[i][j] = mfma8_16<2>(fp, fq, acc[i][j], sp[i / 4], s4[j]);
-                if (i % 4 == 3) acc[i][j] = mfma8_16<3>(fp, fq, acc[i][j], sp[i / 4], s4[j]);
-            }
-        }
-    };
-    // A lane's sums of a 16 x 16 tile are p = 4 grp + 0..3 of one q.  16 rows x 64 columns at a time leave
-    // through the wavefront's own LDS, 128 bytes of a row.
-    auto store = [&](int64_t t) {
-        char *mine = outs[wave];
-#pragma unroll
-        for (int j = 0; j < TQ; ++j)
-#pragma unroll
-            for (int i0 = 0; i0 < TP; i0 += 4) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    f32x4_t v = acc[i0 + i][j];
-                    if (a.relu)
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) v[k] = __builtin_elementwise_maximum(v[k], 0.0f);      // NaN stays
-                    *(u32x2_r *)(mine + l16 * LDO + 32 * i + 8 * grp) = u32x2_r{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-                }
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int r = u * 8 + lane / 8, c = lane % 8 * 8;
-                    const u32x4_r o = *(const u32x4_r *)(mine + r * LDO + c * 2);
-                    const int64_t row = t * PANEL_ROWS + 16 * j + r, col = p0 + 16 * i0 + c;
-                    if (row < a.n)
-                        store8_bits((uint16_t *)a.y + row * a.ld_y + col, (int)min((int64_t)8, a.out - col), o);
-                }
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            }
-    };
-    int kt = 0, next_kt = 0;
-    int64_t next_tile = tile;
-#pragma unroll
-    for (int j = 0; j < TQ; ++j) fetch(0, tile, 0, j);
-    while (true) {
-#pragma unroll
-        for (int set = 0; set < 2; ++set) {
-            if (++next_kt == steps) next_kt = 0, next_tile += stride;
-            if (next_tile >= tiles) next_tile = tile;      // after the last step: read again, not used
-            if (kt == 0) start();
-            multiply(set, kt, [&](int i) {
-                if (i < TQ) fetch(set ^ 1, next_tile, next_kt, i);
-            });
-            if (++kt == steps) {
-                store(tile);
-                kt = 0;
-                tile += stride;
-                if (tile >= tiles) return;
-            }
-        }
-    }
-}
-
 // Parts of a product to y, in their order.  The blocks after the first `blocks` add up column
 // sums instead (column_sums: 64 columns a block).
 __global__ __launch_bounds__(1024) void linear8_join_kernel(Linear8Args a, int blocks, const float *part, int64_t rows,
@@ -577,10 +420,19 @@ __global__ __launch_bounds__(1024) void linear8_join_kernel(Linear8Args a, int b
     }
 }
 
-typedef TileShape<2, 2, 2, 2, 2> Tile128;     // 128 x 128, two blocks a CU
-typedef TileShape<2, 4, 4, 2, 2> Tile256;     // 256 x 256
+// Tiles, by us of n rows 1024 -> 1024 (361 -> 512 in brackets), replayed from a graph:
+//   to bf16       n 2048        4096         16384        65536
+//     64 x 64     7.3 (4.1)   12.6 (4.9)   41.6 (14.3)  145 (47.5)
+//     128 x 128   9.0 (5.8)   10.4 (6.3)   23.9 (9.6)   83.0 (28.0)
+//     256 x 256  15.5 (9.4)   16.5 (9.6)   23.3 (11.8)  76.6 (25.7)
+//   to 8 bits     n 1           8192         16384        65536
+//     128 x 128  11.5 (7.3)   21.0 (9.0)   37.8 (12.6)  141 (40.2)
+//     256 x 256  26.7 (14.7)  30.3 (16.4)  35.0 (17.7)  123 (37.1)
+// Of fewer than 256 tiles the smaller ones pay.
 typedef TileShape<2, 2, 1, 1, 4> Tile64;      // 64 x 64, three steps ahead
-typedef TileShape<1, 1, 4, 1, 4> TileFlat;    // 128 x 32, for whole blocks of y8
+typedef TileShape<2, 2, 2, 2, 2> Tile128;     // 128 x 128, two blocks a CU
+typedef TileShape<1, 4, 4, 1, 2> TileRows;    // the same, wavefronts of whole blocks of y8
+typedef TileShape<2, 4, 4, 2, 2> Tile256;     // 256 x 256
 
 // Products in bf16, summed in fp32 throughout.
 static bool wide(const Linear8Args &a) { return (a.y && a.y_f32) || a.y8.q; }
@@ -615,14 +467,8 @@ static void join(const Linear8Args &a, const ColumnSums &c, hipStream_t s)
 
 hipError_t launch_linear8(const Linear8Args &a, hipStream_t s)
 {
-    if (a.n >= 16384 && a.steps <= PANEL_STEPS && ceil_div(a.out, 128) <= 32 && !wide(a) && a.q.ld_q < (1 << 24)) {
-        const int panels = (int)ceil_div(a.out, 128), streams = 8 * (32 / panels);
-        linear8_panel_kernel<<<dim3(256), dim3(64 * PANEL_WAVES), 0, s>>>(a, panels, streams);
-        return hipGetLastError();
-    }
-    if (few_tiles(a.n, a.out, 1)) {
-        if (a.y8.q) tile_by<TileFlat>(a, s);
-        else tile_by<Tile64>(a, s);
+    if (few_tiles(a.n, a.out, 1) && !a.y8.q) {
+        tile_by<Tile64>(a, s);
         return hipGetLastError();
     }
     // parts of rows with fewer than 2^21 tiles
@@ -634,7 +480,8 @@ hipError_t launch_linear8(const Linear8Args &a, hipStream_t s)
         b.q.scale += (r >> a.q.shift) * a.q.ld_scale;
         if (a.y) b.y = (char *)a.y + r * a.ld_y * (a.y_f32 ? 4 : 2);
         if (a.y8.q) b.y8.q += r * a.y8.ld_q, b.y8.scale += r * a.y8.ld_scale;
-        if (a.y8.q || tiles_of(b.n, b.out, 256) >= 256) tile_by<Tile256>(b, s);
+        if (tiles_of(b.n, b.out, 256) >= 256) tile_by<Tile256>(b, s);
+        else if (a.y8.q) tile_by<TileRows>(b, s);
         else tile_by<Tile128>(b, s);
     }
     return hipGetLastError();
