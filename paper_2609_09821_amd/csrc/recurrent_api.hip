@@ -82,7 +82,8 @@ im_status check_layer8(int64_t n, int64_t in, int64_t out, int32_t dtype)
     im_status s = check_rows(n, in, dtype);
     if (s != IM_OK) return s;
     if (out < 1) return invalid("out must be >= 1");
-    if (in > MAX_WIDTH || out > MAX_WIDTH) return unsupported("in or out above 2^20");
+    if (in > MAX_WIDTH || out > MAX_WIDTH || in * out > MAX_ROWS)
+        return unsupported("in or out above 2^20, or in * out above 2^30");
     return IM_OK;
 }
 
@@ -260,7 +261,9 @@ im_status im_block_linear(const im_layer8 *p, void *stream)
 
 int64_t im_block_linear_grad_workspace(int64_t n, int64_t in, int64_t out)
 {
-    if (n < 0 || n > MAX_ROWS || in < 1 || in > MAX_WIDTH || out < 1 || out > MAX_WIDTH) return -1;
+    if (n < 0 || n > MAX_ROWS || in < 1 || in > MAX_WIDTH || out < 1 || out > MAX_WIDTH ||
+        in * out > MAX_ROWS)
+        return -1;
     return grad_space(n, in, out).bytes;
 }
 

@@ -251,12 +251,18 @@ def test_linear8(n, i, o, rows, out):
         tol = tol + 7 * 2.0 ** -13 * mass
     if relu:
         y64 = np.maximum(y64, 0)
-    y = None if out == "8" else _rows(torch.zeros(n, o, dtype=DT["f32" if out in ("f32", "both32") else "bf16"]), n % 3)
+    behind = None
+    if out == "8":
+        y = None
+    else:
+        y = _rows(torch.full((n + 1, o), 7.0, dtype=DT["f32" if out in ("f32", "both32") else "bf16"]), n % 3)
+        y, behind = y[:n], y[n:]
     y8, qrest, srest = _filled(n, o) if out in ("8", "both", "both32") else (None, None, None)
     im.linear8(x8, w8, None if bias is None else bias.cuda(), y, y8=y8, relu=relu)
     if y is not None:
         half = O.HALF["f32" if out in ("f32", "both32") else "bf16"]
         assert (np.abs(_np(y) - y64) <= tol + half * 1.01 * (np.abs(y64) + tol)).all()
+        assert (behind == 7).all()
     if y8 is not None:
         back = torch.zeros(n, o, device="cuda")
         im.block8_load(y8, back)
@@ -281,7 +287,37 @@ def test_linear8_of_whole_numbers_is_exact(n, i, o):
     assert torch.equal(again.q.view(torch.uint8), y8.q.view(torch.uint8)) and torch.equal(again.scale, y8.scale)
 
 
-@pytest.mark.parametrize("n", [3, 40, 200, 600])
+def test_linear8_of_many_rows():
+    """The largest tiles, with ends in both directions, every output."""
+    n, i, o = 66000, 200, 300
+    g = _gen(n)
+    x8, w8 = im.Block8.empty(n, i), im.Block8.empty(o, i, 128)
+    x = torch.randn(n, i, generator=g).cuda()
+    im.block8_store(x, x8)
+    im.block8_store(torch.randn(o, i, generator=g).cuda(), w8)
+    bias = torch.randn(o, generator=g).cuda()
+    xv, wv = (torch.zeros(*b.shape, device="cuda") for b in (x8, w8))
+    im.block8_load(x8, xv)
+    im.block8_load(w8, wv)
+    want = (xv.double() @ wv.double().t() + bias.double()).clamp(min=0)
+    mass = xv.double().abs() @ wv.double().abs().t() + bias.double().abs()
+    for out in ("f32", "bf16", "8"):
+        y8 = im.Block8.empty(n, o) if out != "bf16" else None
+        y = torch.full((n + 1, o), 7.0, device="cuda", dtype=DT["bf16" if out == "bf16" else "f32"])
+        im.linear8(x8, w8, bias, None if out == "8" else y[:n], y8=y8, relu=True)
+        tol = (i + 2) * 2 * O.U32 * mass + (7 * 2.0 ** -13 * mass if out == "bf16" else 0)
+        if out != "8":
+            half = O.HALF["f32" if out == "f32" else "bf16"] * 1.01
+            assert bool(((y[:n].double() - want).abs() <= tol + half * (want + tol)).all())
+            assert (y[n] == 7).all()
+        if y8 is not None:
+            im.block8_load(y8, y[:n])
+            step = torch.exp2(y8.scale.double() - 127).repeat_interleave(128, 1)[:, :o]
+            assert bool(((y[:n].double() - want).abs() <= 2.0 ** -4 * 1.001 * (want + tol) + 2.0 ** -10 * step + tol).all())
+            assert not y8.q.view(torch.uint8)[:, o:].any()
+
+
+@pytest.mark.parametrize("n", [3, 40, 200, 600, 66000])
 def test_linear8_of_blocks_that_are_not_finite(n):
     """A row with a NaN or an infinity is NaN in y, and no other; the extreme scales."""
     g = _gen(n, 8)
@@ -294,6 +330,12 @@ def test_linear8_of_blocks_that_are_not_finite(n):
     bad = torch.isnan(y).all(1).cpu()
     assert bad[1] and bad[2] and not torch.isnan(y[~bad.cuda()]).any() and int(bad.sum()) == 2
     assert (y[0] == 0).all()
+    yb, y8 = torch.zeros(n, 200, device="cuda", dtype=torch.bfloat16), im.Block8.empty(n, 200)
+    im.linear8(x8, w8, None, yb, relu=True)
+    im.linear8(x8, w8, None, None, y8=y8, relu=True)
+    im.block8_load(y8, y)
+    for t in (yb, y):
+        assert torch.equal(torch.isnan(t).all(1).cpu(), bad) and torch.equal(torch.isnan(t).any(1).cpu(), bad)
     big, small = torch.full((n, 128), 3.0e38), torch.full((4, 128), 1e-36)
     b8, bv = _pair(big, 1)
     s8, sv = _pair(small, 1)
@@ -468,6 +510,90 @@ def test_gated_scan_step_by_step():
     for t in range(T):
         im.gated_scan(gate[t:t + 1], x[t:t + 1], one[t:t + 1], s2, s2, None, f[0, t:t + 1], f[1, t:t + 1])
     assert torch.equal(one, whole) and torch.equal(s1, s2)
+
+
+@pytest.mark.parametrize("T", [20, 3000])
+def test_gated_scan_of_other_layouts(T):
+    """Flags that are bool, or one of the two; gates that all envs share; strides of both orders."""
+    n, d = 5, 40
+    gate, x, dh, flags, c0, _ = _scan_case(T, n, d, "bf16", True, True, 6)
+    gate[:] = gate[:, :1]
+    g, xs, f = gate.cuda(), x.cuda(), flags.cuda()
+    either = f[0] | f[1]
+    want, h = torch.zeros_like(xs), torch.zeros_like(xs)
+    im.gated_scan(g, xs, want, c0.cuda(), None, None, f[0], f[1])
+    shared = g[:, :1].expand(T, n, d)
+    for term, trunc in ((either, None), (None, either != 0), (f[0] != 0, f[1] != 0)):
+        h.zero_()
+        im.gated_scan(shared, xs, h, c0.cuda(), None, None, term, trunc)
+        assert torch.equal(h, want)
+    wide = torch.zeros(T, n + 3, dtype=torch.uint8, device="cuda")
+    wide[:, :n] = either
+    by_env = xs.transpose(0, 1).contiguous().transpose(0, 1)
+    out = torch.zeros(n, T, d, dtype=x.dtype, device="cuda").transpose(0, 1)
+    im.gated_scan(g, by_env, out, c0.cuda(), None, None, wide[:, :n])
+    assert torch.equal(out, want)
+
+
+# --------------------------------------------------------------- far offsets
+def test_gated_scan_of_envs_far_apart():
+    """Rows of one step 36 MB apart, env by env, give the bits of rows that lie together."""
+    T, n, d = 70000, 3, 256
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    gate, x = (torch.randn(T, n, d, device="cuda", generator=g).bfloat16() for _ in range(2))
+    far = [t.transpose(0, 1).contiguous().transpose(0, 1) for t in (gate, x)]
+    want, h = torch.zeros_like(x), torch.zeros_like(far[1])
+    keep, keep2 = (torch.zeros(-(-T // 16), n, d, device="cuda") for _ in range(2))
+    im.gated_scan(gate, x, want, keep=keep)
+    im.gated_scan(*far, h, keep=keep2)
+    assert torch.equal(h, want) and torch.equal(keep, keep2)
+    outs = [torch.zeros_like(x) for _ in range(2)] + [torch.zeros_like(far[1]) for _ in range(2)]
+    im.gated_scan_grad(x, gate, x, keep, *outs[:2])
+    im.gated_scan_grad(far[1], *far, keep, *outs[2:])
+    assert torch.equal(outs[0], outs[2]) and torch.equal(outs[1], outs[3])
+
+
+def test_offsets_that_pass_32_bits():
+    """Arrays of more than 4 GB: their last rows as alone."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    n, d = 2200064, 1024
+    x = torch.randint(-15, 16, (n, d), device="cuda", generator=g, dtype=torch.int8).bfloat16()
+    y, h = torch.empty_like(x), torch.empty_like(x)
+    rstd = torch.zeros(n, device="cuda")
+    x8, xt = im.Block8.empty(n, d), im.Block8.empty(d, n)
+    im.rms_norm(x, None, y, rstd, residual=x, h=h, y8=x8)
+    tail = slice(n - 128, n)
+    xl, yl, rl, l8, lt = (x[tail].contiguous(), torch.zeros(128, d, dtype=x.dtype, device="cuda"),
+                          torch.zeros(128, device="cuda"), im.Block8.empty(128, d), im.Block8.empty(d, 128))
+    im.rms_norm(xl, None, yl, rl, residual=xl, y8=l8)
+    assert torch.equal(y[tail], yl) and torch.equal(rstd[tail], rl) and torch.equal(h[tail], xl + xl)
+    assert torch.equal(x8.q[tail].view(torch.uint8), l8.q.view(torch.uint8))
+    im.rms_norm_grad(y, h, None, rstd, y)
+    im.rms_norm_grad(yl, h[tail], None, rl, yl)
+    assert torch.equal(y[tail], yl)
+    im.block8_store(x, x8, xt)
+    im.block8_store(xl, l8, lt)
+    assert torch.equal(x8.q[tail].view(torch.uint8), l8.q.view(torch.uint8))
+    assert torch.equal(xt.q[:, -128:].view(torch.uint8), lt.q.view(torch.uint8))
+    assert torch.equal(xt.scale[:, -1], lt.scale[:, 0])
+    im.block8_load(x8, y)
+    assert torch.equal(y, x)
+    # whole numbers: exact in any order
+    w8 = im.Block8.empty(d, d, 128)
+    im.block8_store(torch.eye(d, device="cuda"), w8)
+    im.linear8(x8, w8, None, y)
+    assert torch.equal(y, x)
+    del h, x8, xt
+    # two steps of 2.2 GB
+    s = x.view(2, n // 2, d)
+    out = torch.zeros_like(s)
+    im.gated_scan(s, s, out)
+    last = s[:, -2:].contiguous()
+    want = torch.zeros_like(last)
+    im.gated_scan(last, last, want)
+    assert torch.equal(out[:, -2:], want)
 
 
 # ---------------------------------------------------------- differences, graphs

@@ -136,6 +136,7 @@ def _layer(**over):
     (dict(x=None), BAD, "NULL block8"), (dict(w=None), BAD, "NULL block8"),
     (dict(in_=129), BAD, "ld_q"), (dict(in_=(1 << 20) + 1), UNS, "2^20"), (dict(out=(1 << 20) + 1), UNS, "2^20"),
     (dict(n=(1 << 30) + 1), UNS, "2^30"), (dict(y8=_SQUARE16), BAD, "rows must be 1"),
+    (dict(in_=1 << 16, out=1 << 15), UNS, "in * out"),
 ])
 def test_linear8_refuses(lib, over, code, words):
     _refused(lib, lib.im_block_linear(C.byref(_layer(**over)), None), code, words)
@@ -153,6 +154,7 @@ def _layer_grad(**over):
     (dict(xt=None), BAD, "xt"), (dict(wt=None), BAD, "wt"),
     (dict(dx=None, dw=None, db=None), BAD, "no output"), (dict(workspace=None), BAD, "workspace"),
     (dict(workspace_bytes=16), BAD, "workspace"), (dict(workspace=P + 8), BAD, "aligned"),
+    (dict(in_=1 << 16, out=1 << 15), UNS, "in * out"),
 ])
 def test_linear8_grad_refuses(lib, over, code, words):
     _refused(lib, lib.im_block_linear_grad(C.byref(_layer_grad(**over)), None), code, words)
@@ -209,7 +211,7 @@ def test_scan_workspace_is_asked_for(lib):
 def test_workspace_sizes(lib):
     assert lib.im_rms_norm_grad_workspace(-1, 8) == lib.im_rms_norm_grad_workspace(4, 0) == -1
     assert lib.im_rms_norm_grad_workspace(4, 8193) == -1 and lib.im_rms_norm_grad_workspace(1 << 20, 512) > 0
-    for a in ((-1, 8, 8), (4, 0, 8), (4, 8, 0), ((1 << 30) + 1, 8, 8), (4, 1 << 21, 8)):
+    for a in ((-1, 8, 8), (4, 0, 8), (4, 8, 0), ((1 << 30) + 1, 8, 8), (4, 1 << 21, 8), (4, 1 << 16, 1 << 15)):
         assert lib.im_block_linear_grad_workspace(*a) == -1
     # dy in 8 bits, twice, with its scales
     assert lib.im_block_linear_grad_workspace(65536, 1024, 512) >= 2 * 65536 * 516
