@@ -107,25 +107,24 @@ __device__ __forceinline__ u32x4_r bits4(const f32x16_t &a, int g)
 
 // ---------------------------------------------------------------------------
 // Tiles.  A block of WP x WQ wavefronts forms BP x BQ of C, a wavefront TP x TQ MFMA tiles.
-// K steps of BK bytes go through a ring of NS stages in LDS by direct loads, NS - 1 steps
+// K steps of 128 bytes go through a ring of NS stages in LDS by direct loads, NS - 1 steps
 // ahead, their scales as a word a row after them; a step has one barrier.  Direct loads write
 // 64 consecutive 16-byte pieces, so a stage has no padding: pieces are permuted in their row
 // instead, so that 16 rows' pieces of one k cover all banks.
 // ---------------------------------------------------------------------------
-template <int WP_, int WQ_, int TP_, int TQ_, int NS_, int BK_ = 128>
+template <int WP_, int WQ_, int TP_, int TQ_, int NS_>
 struct TileShape {
-    static constexpr int WP = WP_, WQ = WQ_, TP = TP_, TQ = TQ_, NS = NS_, BK = BK_;
-    static constexpr int SLOTS = BK / 16, ROWS = 64 / SLOTS;             // pieces of a row, rows of a copy
+    static constexpr int WP = WP_, WQ = WQ_, TP = TP_, TQ = TQ_, NS = NS_;
     static constexpr int NT = 64 * WP * WQ, WAVES = WP * WQ, BP = 32 * WP * TP, BQ = 32 * WQ * TQ;
-    static constexpr int UP = BP * SLOTS / NT, UQ = BQ * SLOTS / NT;             // 16-byte pieces of a thread
+    static constexpr int UP = BP * 8 / NT, UQ = BQ * 8 / NT;             // 16-byte pieces of a thread
     static constexpr int US = ((BP + BQ + 63) / 64 + WAVES - 1) / WAVES;      // scales of a thread
     static constexpr int L = UP + UQ + US;                               // direct loads of a step
-    static constexpr int Q_AT = BP * BK, S_AT = Q_AT + BQ * BK, STAGE = S_AT + US * WAVES * 256;
+    static constexpr int Q_AT = BP * 128, S_AT = Q_AT + BQ * 128, STAGE = S_AT + US * WAVES * 256;
     static constexpr int LDO = 128 + 16, OUT = 32 * LDO;                 // bytes of a wavefront's 32 output rows
     static constexpr int LDS = std::max(NS * STAGE, WAVES * OUT);
     // piece c of row r lies at c ^ perm(r)
-    __device__ static int perm(int r) { return BK == 64 ? r >> 2 & 3 : r >> 1 & 7; }
-    static_assert(UP * NT == BP * SLOTS && UQ * NT == BQ * SLOTS, "whole pieces");
+    __device__ static int perm(int r) { return r >> 1 & 7; }
+    static_assert(UP * NT == BP * 8 && UQ * NT == BQ * 8, "whole pieces");
 };
 
 template <typename S, bool WIDE>
@@ -136,9 +135,8 @@ __device__ __forceinline__ void tile_run(const Linear8Args &a, int p_tiles, int 
     const int split = id / tiles, tile = id % tiles;
     const int64_t p0 = (int64_t)(tile % p_tiles) * BP, q0 = (int64_t)(tile / p_tiles) * BQ;
     const int wp = wave % S::WP * TP * 32, wq = wave / S::WP * TQ * 32;
-    constexpr int BK = S::BK, PER = 128 / BK;      // steps of a block of k
     const int64_t k0 = a.steps * split / a.splits;
-    const int nk = (int)(a.steps * (split + 1) / a.splits - k0) * PER;
+    const int nk = (int)(a.steps * (split + 1) / a.splits - k0);
 
     // Addresses of this thread's pieces and scales.  Rows past the last read the last one: their
     // sums are not stored.
@@ -146,8 +144,8 @@ __device__ __forceinline__ void tile_run(const Linear8Args &a, int p_tiles, int 
 #pragma unroll
     for (int u = 0; u < S::UP + S::UQ; ++u) {
         const bool q = u >= S::UP;
-        const int r = ((q ? u - S::UP : u) * S::WAVES + wave) * S::ROWS + lane / S::SLOTS;
-        const int c = lane % S::SLOTS ^ S::perm(r);
+        const int r = ((q ? u - S::UP : u) * S::WAVES + wave) * 8 + lane / 8;
+        const int c = (lane & 7) ^ S::perm(r);
         const Mat8 &m = q ? a.q : a.p;
         const int64_t row = min((q ? q0 : p0) + r, (q ? a.n : a.out) - 1);
         from[u] = m.q + row * m.ld_q + k0 * 128 + c * 16;
@@ -161,14 +159,17 @@ __device__ __forceinline__ void tile_run(const Linear8Args &a, int p_tiles, int 
         sfrom[u] = m.scale + (row >> m.shift) * m.ld_scale + k0;
     }
     auto copy = [&](int u, int kt, char *st) {
-        if (u < S::UP + S::UQ) copy_to_lds(from[u] + kt * BK, st + (u * S::WAVES + wave) * 1024);
-        else copy_byte_to_lds(sfrom[u - S::UP - S::UQ] + kt / PER,
+        if (u < S::UP + S::UQ) copy_to_lds(from[u] + kt * 128, st + (u * S::WAVES + wave) * 1024);
+        else copy_byte_to_lds(sfrom[u - S::UP - S::UQ] + kt,
                               st + S::S_AT + ((u - S::UP - S::UQ) * S::WAVES + wave) * 256);
     };
+    for (int kt = 0; kt < NS - 1 && kt < nk; ++kt)
+#pragma unroll
+        for (int u = 0; u < S::L; ++u) copy(u, kt, lds + kt * S::STAGE);
     // 16 bytes of one of 32 rows: half h of the wavefront takes piece 2 s + h
     auto piece = [&](const char *at, int row, int s) {
         const int r = row + (lane & 31);
-        return *(const u32x4_r *)(at + r * BK + (((2 * s + (lane >> 5)) ^ S::perm(r)) << 4));
+        return *(const u32x4_r *)(at + r * 128 + (((2 * s + (lane >> 5)) ^ S::perm(r)) << 4));
     };
     // The sums start from the bias.  Columns past the last are copies of it, which leave their rows'
     // largest magnitudes as they are.
@@ -221,9 +222,9 @@ __device__ __forceinline__ void tile_run(const Linear8Args &a, int p_tiles, int 
         read(0);
         if constexpr (WIDE) {
 #pragma unroll
-            for (int s = 0; s < BK / 32; ++s) {
-                if (s + 1 < BK / 32) read(s + 1);
-                more_copies(s, BK / 32);
+            for (int s = 0; s < 4; ++s) {
+                if (s + 1 < 4) read(s + 1);
+                more_copies(s, 4);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     bf16x8_t fp[TP], fq[TQ];
@@ -246,7 +247,7 @@ __device__ __forceinline__ void tile_run(const Linear8Args &a, int p_tiles, int 
         } else {
             u32x4_r cp[TP], cq[TQ];
 #pragma unroll
-            for (int s = 0; s < BK / 64; ++s) {
+            for (int s = 0; s < 2; ++s) {
                 read(2 * s + 1);
 #pragma unroll
                 for (int i = 0; i < TP; ++i) cp[i] = bp[0][i];
@@ -257,8 +258,8 @@ __device__ __forceinline__ void tile_run(const Linear8Args &a, int p_tiles, int 
                 for (int i = 0; i < TP; ++i) fp[i] = join(cp[i], bp[1][i]);
 #pragma unroll
                 for (int j = 0; j < TQ; ++j) fq[j] = join(cq[j], bq[1][j]);
-                if (s + 1 < BK / 64) read(2 * s + 2);
-                more_copies(s, BK / 64);
+                if (s + 1 < 2) read(2 * s + 2);
+                more_copies(s, 2);
 #pragma unroll
                 for (int i = 0; i < TP; ++i)
 #pragma unroll
@@ -267,9 +268,6 @@ __device__ __forceinline__ void tile_run(const Linear8Args &a, int p_tiles, int 
             }
         }
     };
-    for (int kt = 0; kt < NS - 1 && kt < nk; ++kt)
-#pragma unroll
-        for (int u = 0; u < S::L; ++u) copy(u, kt, lds + kt * S::STAGE);
     int kt = 0;
     for (; kt + NS - 1 < nk; ++kt) {
         wait_loads<(NS - 2) * S::L>();
@@ -286,8 +284,8 @@ __device__ __forceinline__ void tile_run(const Linear8Args &a, int p_tiles, int 
     // through a part of LDS of the wavefront's own, in pieces of 16 bytes, up to 128 of a row.
     meet();
     char *mine = lds + wave * S::OUT, *to = mine + l32 * S::LDO + 4 * half;
-    // `wide` bytes of each row from `mine` to the columns col.. (in bytes) of rows of ld bytes; of
-    // `end` bytes
+    // Of each row in `mine` row_bytes to y's rows of ld bytes, from byte `col` on, up to byte `end`;
+    // values of `unit` bytes.
     auto leave = [&](auto row_bytes, char *y, int64_t ld, int j, int64_t col, int64_t end, int unit) {
         constexpr int LANES = decltype(row_bytes)::value / 16, ROWS = 64 / LANES;
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
