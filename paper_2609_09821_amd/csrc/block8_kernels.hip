@@ -16,6 +16,9 @@ static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // is 16 neighbouring lanes; a column's meets in LDS, as does the whole tile's where it has one scale.
 // The transposed bytes are put together from a thread's four rows and pass through LDS, so that
 // both outputs leave in whole 128-byte blocks.
+// 65536 x 512 bf16 with a mask, both outputs and column sums: 46 us, 202 MB at 4.4 TB/s; 4095 x 1024 both
+// ways 10.2 us, one tile a CU from load to store.  With 256 threads of eight rows, which hold twice the
+// registers, 57 and 12 us.  Loads without branches in whole tiles gained nothing (49 and 10.2 us).
 // C, TR: which outputs; SQUARE: one scale a tile; MASK: x counts as 0 where not y > 0.
 // ---------------------------------------------------------------------------
 constexpr int ST_NT = 512, ST_ROWS = 4, ST_GROUPS = ST_NT / 16;
@@ -174,7 +177,8 @@ hipError_t launch_block8_store(const StoreArgs &a, bool f32, hipStream_t s)
 }
 
 // ---------------------------------------------------------------------------
-// Restores: 16 lanes a block of 128 values.
+// Restores: 16 lanes a block of 128 values.  65536 x 1024 to bf16: 31 us, 202 MB at 6.5 TB/s, of which the
+// caches still hold what was stored just before.
 // ---------------------------------------------------------------------------
 template <typename E>
 __global__ __launch_bounds__(256) void block8_load_kernel(Mat8 c, int64_t n, int64_t d, E *x, int64_t ld_x)

