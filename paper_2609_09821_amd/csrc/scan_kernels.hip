@@ -27,11 +27,11 @@ constexpr int SCAN_V = 2;
 // V values of a row as words, at any address of their element's alignment.  The last piece of a
 // row whose width is no multiple of V takes the last V values of the row: `lo` of them belong
 // to the piece before, which alone stores them.  Rows of fewer than V values: value by value.
-// What a launch does: a chunk's map alone; a chunk's steps; all steps, arrays that no cache holds
-// (their loads and stores are marked as such: 32 x 16384 x 256 bf16 forward 181 -> 165 us, the
-// gradient 330 -> 290; the chunks' second launch reads what the first one left in the caches, and
+// What a launch does: chunks' maps alone; chunks' steps; all steps; all steps of arrays that no cache holds
+// (their loads and stores are marked as such: 32 x 16384 x 256 bf16 forward 181 us, 165 marked, the
+// gradient 330 and 290; the chunks' second launch reads what the first one left in the caches, and
 // takes 108 us for 95 if marked).
-enum { MAP, STEPS, STREAM };
+enum { MAP, CHUNKS, STEPS, STREAM };
 
 template <typename E, int V, int MODE>
 struct StepPiece {
@@ -125,51 +125,49 @@ __device__ __forceinline__ void gates(float g, float &a, float &b)
     b = g < 0.0f ? r : s;
 }
 
-// Whether an env's episode ends with each of KEEP steps, a bit a step.
-struct Ends {
-    const uint8_t *f1, *f2;      // null: none do
-    int64_t ld, env;
-    bool one;                    // all lanes have the same env
-    __device__ __forceinline__ void init(const ScanArgs &a, int64_t e)
-    {
-        f1 = a.term ? a.term : a.trunc, f2 = a.trunc ? a.trunc : a.term;
-        ld = a.ld_flags, env = e;
-        const int lo = __builtin_amdgcn_readfirstlane((int)e);
-        one = __ballot((int)e != lo) == 0 && __ballot(true) == ~0ull;
+// Whether all of the wavefront's lanes are there and have the same env.
+__device__ __forceinline__ bool one_env(int64_t env)
+{
+    return __ballot((int)env != __builtin_amdgcn_readfirstlane((int)env)) == 0 && __ballot(true) == ~0ull;
+}
+
+// Whether the env's episode ends with each of the U steps from t on, a bit a step (of the last ones
+// some may not exist).  Where a wavefront has one env, its lanes take a byte each, the steps' first
+// flags and their second ones.
+template <int U>
+__device__ __forceinline__ uint32_t load_ends(const ScanArgs &a, int64_t env, bool one, int64_t t, int64_t t1)
+{
+    const uint8_t *f1 = a.term ? a.term : a.trunc, *f2 = a.trunc ? a.trunc : a.term;
+    if (!f1) return 0;
+    if (one) {
+        const int lane = threadIdx.x & 63;
+        const int64_t q = min(t + (lane & (U - 1)), t1 - 1);
+        const uint64_t m = __ballot(lane < 2 * U && (lane < U ? f1 : f2)[q * a.ld_flags + env] != 0);
+        return (uint32_t)(m | m >> U) & ((1u << U) - 1);
     }
-    // Steps t .. t + KEEP - 1 (of the last ones some may not exist).  Where a wavefront has one env,
-    // its lanes take a byte each, the steps' first flags and their second ones.
-    __device__ __forceinline__ uint32_t load(int64_t t, int64_t t1) const
-    {
-        if (!f1) return 0;
-        if (one) {
-            const int lane = threadIdx.x & 63;
-            const int64_t q = min(t + (lane & (KEEP - 1)), t1 - 1);
-            const uint64_t m = __ballot(lane < 2 * KEEP && (lane < KEEP ? f1 : f2)[q * ld + env] != 0);
-            return (uint32_t)(m | m >> KEEP) & ((1u << KEEP) - 1);
-        }
-        uint32_t m[KEEP], e = 0;
+    uint32_t m[U], e = 0;
 #pragma unroll
-        for (int u = 0; u < KEEP; ++u) {
-            const int64_t q = min(t + u, t1 - 1) * ld + env;
-            m[u] = f1[q] | f2[q];
-        }
-#pragma unroll
-        for (int u = 0; u < KEEP; ++u) e |= m[u] ? 1u << u : 0;
-        return e;
+    for (int u = 0; u < U; ++u) {
+        const int64_t q = min(t + u, t1 - 1) * a.ld_flags + env;
+        m[u] = f1[q] | f2[q];
     }
-};
+#pragma unroll
+    for (int u = 0; u < U; ++u) e |= m[u] ? 1u << u : 0;
+    return e;
+}
 
 // ---------------------------------------------------------------------------
 // A chunk's steps forward.  MAP: its map alone, from gate and x.  Bound by HBM: 32 x 16384 x 256
-// bf16 165 us, 823 MB at 5.0 TB/s; few envs by the latency of the loads, eight steps at a time (32
-// steps of one env 10.8 us).
+// bf16 155 us, 823 MB at 5.3 TB/s; few envs by the latency of the loads, 16 steps at a time (32 steps
+// of one env 10.0 us).
 // ---------------------------------------------------------------------------
 template <typename E, int V, typename O, int MODE>
 __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, int64_t pieces)
 {
     typedef StepPiece<E, V, MODE> P;
-    constexpr int U = KEEP / 2;      // steps whose loads are in flight together
+    // steps whose loads are in flight together: with 16 all steps of 32 x 16384 x 256 bf16 take 155 us,
+    // 165 with 8; chunks of 16383 x 2 x 361 floats, of which more wavefronts run beside each other, 70 and 60
+    constexpr int U = MODE == MAP || MODE == CHUNKS ? KEEP / 2 : KEEP;
     const int64_t id = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
     if (id >= a.n * pieces) return;
     const int64_t env = id / pieces, chunk = blockIdx.y;
@@ -182,8 +180,7 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, int64_t pieces)
     x.init(a.x, a.st_x, a.ld_x, env, first, pc.at);
     h.init(a.h, a.st_h, a.ld_h, env, first, pc.at);
     const int64_t row = env * a.d;                 // of the states
-    Ends ends;
-    ends.init(a, env);
+    const bool one = one_env(env);
 
     float c[V], p[V];
 #pragma unroll
@@ -197,7 +194,7 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, int64_t pieces)
     }
     typename P::word_t wg[2][U], wx[2][U];
     // steps past the last: the last once more
-    auto fetch = [&](int s, int64_t t) {
+    auto fetch = [&](int s, int64_t t) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t q = min(t + u, t1 - 1);
@@ -205,7 +202,7 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, int64_t pieces)
             wx[s][u] = pc.load(x[q]);
         }
     };
-    auto walk = [&](int s, int64_t t, uint32_t end) {
+    auto walk = [&](int s, int64_t t, uint32_t end) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (t + u >= t1) break;
@@ -230,22 +227,26 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, int64_t pieces)
     uint32_t next = 0;
     if (t0 < t1) {
         fetch(0, t0);
-        next = ends.load(t0, t1);
+        next = load_ends<U>(a, env, one, t0, t1);
     }
-    for (int64_t t = t0; t < t1; t += KEEP) {
+    int64_t t = t0;
+    auto turn = [&](auto set) __attribute__((always_inline)) {
+        constexpr int s = decltype(set)::value;
         const uint32_t end = next;
-        if (t + U < t1) fetch(1, t + U);
-        if (MODE != MAP && a.keep)
+        if (t + U < t1) {
+            fetch(s ^ 1, t + U);
+            next = load_ends<U>(a, env, one, t + U, t1);
+        }
+        if (MODE != MAP && a.keep && t % KEEP == 0)
 #pragma unroll
             for (int k = 0; k < V; ++k)
                 if (k >= pc.lo && k < pc.hi) a.keep[t / KEEP * a.n * a.d + row + pc.at + k] = c[k];
-        walk(0, t, end);
-        if (t + U >= t1) break;
-        if (t + KEEP < t1) {
-            fetch(0, t + KEEP);
-            next = ends.load(t + KEEP, t1);
-        }
-        walk(1, t + U, end >> U);
+        walk(s, t, end);
+        t += U;
+    };
+    while (t < t1) {
+        turn(std::integral_constant<int, 0>());
+        if (t < t1) turn(std::integral_constant<int, 1>());
     }
     if constexpr (MODE == MAP) {
         float *m = a.maps + chunk * 2 * a.n * a.d + row;
@@ -286,8 +287,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 3 : 2) void scan_grad_kernel(
     dgate.init(a.dgate, a.st_dgate, a.ld_dgate, env, first, pc.at);
     dx.init(a.dx, a.st_dx, a.ld_dx, env, first, pc.at);
     const int64_t row = env * a.d;
-    Ends ends;
-    ends.init(a, env);
+    const bool one = one_env(env);
 
     float D[V], p[V];
 #pragma unroll
@@ -310,7 +310,7 @@ __global__ __launch_bounds__(256, sizeof(E) == 2 ? 3 : 2) void scan_grad_kernel(
         }
 #pragma unroll
         for (int u = 0; u < KEEP; ++u) wd[u] = pc.load(dh[t + min(u, steps - 1)]);
-        const uint32_t end = ends.load(t, t1);
+        const uint32_t end = load_ends<KEEP>(a, env, one, t, t1);
         float ga[KEEP][V], gb[KEEP][V], diff[KEEP][V];
         float c[V];
 #pragma unroll
@@ -420,9 +420,9 @@ __global__ __launch_bounds__(64 * COMPOSE_WAVES) void compose_kernel(ScanArgs a)
 
 // Steps of a chunk, by us of T x n x 512 bf16 forward (and backward), from a graph:
 //             T 96 n 1     T 128 n 64    T 128 n 128   T 512 n 128    T 512 n 256    T 1024 n 1
-//   one       27.3 (38.5)  36.1 (53.0)   39.8 (54.7)   140 (196)      161 (202)      264 (380)
-//   chunks    22.1 (27.5)  36.9 (45.0)   53.6 (62.8)   94.8 (135)     189 (258)      22.4 (28.0)
-// and 64 steps of one env 19.1 (26.8) in one launch, 22.0 (27.3) in three.  Chunks leave some
+//   one       26.5 (40.3)  34.8 (55.0)   37.4 (56.2)   134 (202)      140 (211)      261 (398)
+//   chunks    21.8 (27.8)  36.9 (45.0)   53.6 (62.8)   100 (133)      189 (258)      22.3 (28.3)
+// and 64 steps of one env 18.1 (28.0) in one launch, 22.0 (27.3) in three.  Chunks leave some
 // 262144 threads; of 16383 x 2 x 361 floats with chunks of 16, 32, 64 and 128 steps 72, 64, 70, 91
 // (97, 95, 95, 117).
 int64_t scan_chunk(int64_t T, int64_t n, int64_t d)
@@ -455,7 +455,8 @@ static void scan_by(const ScanArgs &a, bool grad, hipStream_t s)
         else compose_kernel<false><<<gc, bc, 0, s>>>(a);
     }
     const int64_t bytes = a.T * a.n * a.d * (int64_t)sizeof(E) * (grad ? 5 : 3);
-    if (a.chunks == 1 && bytes > INFINITY_CACHE) scan_launch<E, O, STREAM>(a, grad, g, b, pieces, s);
+    if (a.chunks > 1) scan_launch<E, O, CHUNKS>(a, grad, g, b, pieces, s);
+    else if (bytes > INFINITY_CACHE) scan_launch<E, O, STREAM>(a, grad, g, b, pieces, s);
     else scan_launch<E, O, STEPS>(a, grad, g, b, pieces, s);
 }
 
