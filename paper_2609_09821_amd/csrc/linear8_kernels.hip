@@ -21,6 +21,7 @@
 
 namespace im {
 
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
@@ -88,6 +89,13 @@ __device__ __forceinline__ f32x16_t mfma8(i32x8_t a, i32x8_t b, f32x16_t acc, in
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc, 0, 0, 0, sa, 0, sb);
 }
 
+// The same of 16 rows each and 128 k, 32 bytes of a row in each of its four lanes; sa in byte A.
+template <int A>
+__device__ __forceinline__ f32x4_t mfma8_16(i32x8_t a, i32x8_t b, f32x4_t acc, int sa, int sb)
+{
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 0, 0, A, sa, 0, sb);
+}
+
 // Eight e4m3 values times the scale's power of two as bf16: exact, but for values below 2^-126.
 __device__ __forceinline__ bf16x8_t widen8(uint32_t lo, uint32_t hi, float scale)
 {
@@ -113,10 +121,9 @@ __device__ __forceinline__ u32x4_r bits4(const f32x16_t &a, int g)
 // instead, so that 16 rows' pieces of one k cover all banks.
 //
 // 65536 rows 1024 -> 1024 to bf16: 80 us, 1.72 PFLOP/s (hipBLASLt with one scale for each operand and no
-// bias 87); 59 without the outputs, of which HBM takes 27 alone: a 256 x 256 tile has a CU for itself,
-// so that nothing multiplies while it stores.  Two blocks of 256 x 128 a CU store beside each other's
-// products but load more (88 us); weights held in LDS, with rows that come straight into registers, are
-// bound by the 16-byte pieces of the vector cache (84 us), and weights in registers by LDS (113 us).
+// bias 87), 97 with all arrays out of HBM; 59 without the outputs, of which HBM takes 27 alone: a 256 x 256
+// tile has a CU for itself, so that nothing multiplies while it stores.  Two blocks of 256 x 128 a CU store
+// beside each other's products but load more (88 us).
 // To fp32: 144 us.  dw of 65536 rows 1024 -> 512: 76 us in 16 parts and 8 to join them; tiles of 256 x 256,
 // 256 x 128 and eight wavefronts a tile are no faster (82, 85, 79), and rows of x^T that lie a multiple
 // of 64 KB apart cost 10 us.
@@ -399,6 +406,167 @@ __global__ __launch_bounds__(S::NT, 2) void linear8_two_kernel(Linear8Args a, in
     else tile_run<S, true>(b, b_p_tiles, b_tiles, id - a_blocks, lds);
 }
 
+// ---------------------------------------------------------------------------
+// Panels.  With many rows, an output in bf16 and a k that fits, a block keeps 128 columns of P, all
+// their k, in LDS and its wavefronts walk over the rows of Q by themselves, 64 at a time, without a
+// barrier: Q's fragments come straight into registers, a step of 128 k ahead, also across the end of
+// a tile, so that one wavefront's outputs leave while others multiply.  A block for each CU; the
+// panels of one run of rows are neighbours in an L2.
+//
+// A wavefront's tile is 128 p x 64 q in MFMA tiles of 16 x 16 (v_mfma_scale_f32_16x16x128_f8f6f4):
+// four lanes then hold one row of Q.  Bound by the CU's vector cache, to which each 16 bytes that a
+// lane loads are an access: so scales are loaded four steps at a time and outputs pass through LDS.
+// 65536 rows 1024 -> 1024: 84 us, 90 with all arrays out of HBM.  Weights in registers, rows in LDS: 113.
+// ---------------------------------------------------------------------------
+constexpr int PANEL_STEPS = 8, PANEL_WAVES = 8, PANEL_ROWS = 64;
+__global__ __launch_bounds__(64 * PANEL_WAVES, 1) void linear8_panel_kernel(Linear8Args a, int panels, int streams)
+{
+    constexpr int TP = 8, TQ = PANEL_ROWS / 16, LDO = 128 + 16;
+    __shared__ __attribute__((aligned(1024))) char lds[PANEL_STEPS * 16384];
+    __shared__ __attribute__((aligned(16))) char outs[PANEL_WAVES][16 * LDO];
+    __shared__ int pscale[PANEL_STEPS][16][2];      // byte i % 4 of word i / 4: row 16 i + lane's
+    __shared__ float bias[128];
+    const int lane = threadIdx.x & 63, wave = wave_id(), l16 = lane & 15, grp = lane >> 4;
+    const int place = blockIdx.x >> 3, panel = place % panels;
+    const int stream = place / panels * 8 + (blockIdx.x & 7);
+    if (place / panels * 8 >= streams) return;
+    const int64_t p0 = (int64_t)panel * 128;
+    const int steps = (int)a.steps;
+    for (int u = wave; u < steps * 16; u += PANEL_WAVES) {
+        const int r = (u & 15) * 8 + lane / 8, c = (lane & 7) ^ (r >> 1 & 7);
+        const int64_t row = min(p0 + r, a.out - 1);
+        copy_to_lds(a.p.q + row * a.p.ld_q + (u >> 4) * 128 + c * 16, lds + u * 1024);
+    }
+    for (int u = threadIdx.x; u < steps * 32; u += 64 * PANEL_WAVES) {
+        int v = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t row = min(p0 + 64 * (u & 1) + 16 * i + (u >> 1 & 15), a.out - 1);
+            v |= a.p.scale[(row >> a.p.shift) * a.p.ld_scale + (u >> 5)] << (8 * i);
+        }
+        pscale[u >> 5][u >> 1 & 15][u & 1] = v;
+    }
+    if (threadIdx.x < 128) bias[threadIdx.x] = a.bias ? a.bias[min(p0 + threadIdx.x, a.out - 1)] : 0.0f;
+    wait_loads<0>();
+    __syncthreads();
+
+    const int64_t tiles = (a.n + PANEL_ROWS - 1) / PANEL_ROWS, stride = (int64_t)streams * PANEL_WAVES;
+    int64_t tile = (int64_t)stream * PANEL_WAVES + wave;
+    if (tile >= tiles) return;
+    // Q: 16 bytes grp and 4 + grp of a step of the rows 16 j + l16
+    u32x4_r bq[2][TQ][2];
+    // the scales of row `lane`: bytes of the steps 0..3, and of the last four (steps 4..7)
+    uint32_t scale[2], next_scale[2] = {0, 0};
+    // part j of step kt of tile t; rows past the last read the last one: their sums are not stored
+    auto fetch = [&](int set, int64_t t, int kt, int j) {
+        const int64_t q0 = t * PANEL_ROWS;
+        const int last = (int)min((int64_t)PANEL_ROWS, a.n - q0) - 1;
+        const uint8_t *base = a.q.q + q0 * a.q.ld_q + kt * 128;
+        const uint32_t off = (uint32_t)min(16 * j + l16, last) * (uint32_t)a.q.ld_q + grp * 16;
+        bq[set][j][0] = *(const u32x4_r *)(base + off);
+        bq[set][j][1] = *(const u32x4_r *)(base + off + 64);
+        if (j == 0 && kt == 0) {
+            const uint8_t *s = a.q.scale + ((q0 + min(lane, last)) >> a.q.shift) * a.q.ld_scale;
+            if (steps >= 4) {
+                typedef uint32_t u32_a1 __attribute__((aligned(1)));
+                next_scale[0] = *(const u32_a1 *)s;
+                next_scale[1] = *(const u32_a1 *)(s + steps - 4) >> (8 * (8 - steps) & 31);
+            } else {
+                next_scale[0] = s[0];
+                if (steps > 1) next_scale[0] |= s[1] << 8;
+                if (steps > 2) next_scale[0] |= s[2] << 16;
+            }
+        }
+    };
+    f32x4_t acc[TP][TQ];
+    auto start = [&] {
+        scale[0] = next_scale[0], scale[1] = next_scale[1];
+#pragma unroll
+        for (int i = 0; i < TP; ++i) {
+            const f32x4_t b = *(const f32x4_t *)(bias + 16 * i + 4 * grp);
+#pragma unroll
+            for (int j = 0; j < TQ; ++j) acc[i][j] = b;
+        }
+    };
+    // a step's products; more(i): work beside those of the i-th tile of P
+    auto multiply = [&](int set, int kt, auto more) {
+        const char *st = lds + kt * 16384;
+        const int sp[2] = {pscale[kt][l16][0], pscale[kt][l16][1]};
+        // the scale of row 16 j + l16 in all four lanes of the row
+        const uint32_t own = scale[kt >> 2] >> (8 * (kt & 3));
+        const auto x = __builtin_amdgcn_permlane16_swap(own, own, false, false);
+        const auto even = __builtin_amdgcn_permlane32_swap(x[0], x[0], false, false);
+        const auto odd = __builtin_amdgcn_permlane32_swap(x[1], x[1], false, false);
+        const int s4[TQ] = {(int)even[0], (int)odd[0], (int)even[1], (int)odd[1]};
+        // piece c of a row at c ^ (row / 2 mod 8)
+        auto piece = [&](int i, int k) {
+            return *(const u32x4_r *)(st + (16 * i + l16) * 128 + (((4 * k + grp) ^ (l16 >> 1)) << 4));
+        };
+#pragma unroll
+        for (int i = 0; i < TP; ++i) {
+            const i32x8_t fp = join(piece(i, 0), piece(i, 1));
+            more(i);
+#pragma unroll
+            for (int j = 0; j < TQ; ++j) {
+                const i32x8_t fq = join(bq[set][j][0], bq[set][j][1]);
+                if (i % 4 == 0) acc[i][j] = mfma8_16<0>(fp, fq, acc[i][j], sp[i / 4], s4[j]);
+                if (i % 4 == 1) acc[i][j] = mfma8_16<1>(fp, fq, acc[i][j], sp[i / 4], s4[j]);
+                if (i % 4 == 2) acc[i][j] = mfma8_16<2>(fp, fq, acc[i][j], sp[i / 4], s4[j]);
+                if (i % 4 == 3) acc[i][j] = mfma8_16<3>(fp, fq, acc[i][j], sp[i / 4], s4[j]);
+            }
+        }
+    };
+    // A lane's sums of a 16 x 16 tile are p = 4 grp + 0..3 of one q.  16 rows x 64 columns at a time leave
+    // through the wavefront's own LDS, 128 bytes of a row.
+    auto store = [&](int64_t t) {
+        char *mine = outs[wave];
+#pragma unroll
+        for (int j = 0; j < TQ; ++j)
+#pragma unroll
+            for (int i0 = 0; i0 < TP; i0 += 4) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    f32x4_t v = acc[i0 + i][j];
+                    if (a.relu)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) v[k] = __builtin_elementwise_maximum(v[k], 0.0f);      // NaN stays
+                    *(u32x2_r *)(mine + l16 * LDO + 32 * i + 8 * grp) = u32x2_r{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int r = u * 8 + lane / 8, c = lane % 8 * 8;
+                    const u32x4_r o = *(const u32x4_r *)(mine + r * LDO + c * 2);
+                    const int64_t row = t * PANEL_ROWS + 16 * j + r, col = p0 + 16 * i0 + c;
+                    if (row < a.n)
+                        store8_bits((uint16_t *)a.y + row * a.ld_y + col, (int)min((int64_t)8, a.out - col), o);
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            }
+    };
+    int kt = 0, next_kt = 0;
+    int64_t next_tile = tile;
+#pragma unroll
+    for (int j = 0; j < TQ; ++j) fetch(0, tile, 0, j);
+    while (true) {
+#pragma unroll
+        for (int set = 0; set < 2; ++set) {
+            if (++next_kt == steps) next_kt = 0, next_tile += stride;
+            if (next_tile >= tiles) next_tile = tile;      // after the last step: read again, not used
+            if (kt == 0) start();
+            multiply(set, kt, [&](int i) {
+                if (i < TQ) fetch(set ^ 1, next_tile, next_kt, i);
+            });
+            if (++kt == steps) {
+                store(tile);
+                kt = 0;
+                tile += stride;
+                if (tile >= tiles) return;
+            }
+        }
+    }
+}
+
 // Parts of a product to y, in their order.  The blocks after the first `blocks` add up column
 // sums instead (column_sums: 64 columns a block).
 __global__ __launch_bounds__(1024) void linear8_join_kernel(Linear8Args a, int blocks, const float *part, int64_t rows,
@@ -427,7 +595,7 @@ __global__ __launch_bounds__(1024) void linear8_join_kernel(Linear8Args a, int b
     }
 }
 
-// Tiles, by us of n rows 1024 -> 1024 (361 -> 512 in brackets), replayed from a graph:
+// Sides of tiles, by us of n rows 1024 -> 1024 (361 -> 512 in brackets), replayed from a graph:
 //   to bf16       n 2048        4096         16384        65536
 //     64 x 64     7.3 (4.1)   12.6 (4.9)   41.6 (14.3)  145 (47.5)
 //     128 x 128   9.0 (5.8)   10.4 (6.3)   23.9 (9.6)   83.0 (28.0)
@@ -448,6 +616,19 @@ static int64_t tiles_of(int64_t n, int64_t out, int side) { return ceil_div(n, s
 
 // Few tiles of 128 x 128 leave CUs without one.
 static bool few_tiles(int64_t n, int64_t out, int64_t splits) { return tiles_of(n, out, 128) * splits < 256; }
+
+// Panels or tiles, by us of n rows to bf16, inputs and outputs out of HBM (panels / tiles):
+//   n                 16384        65536        131072       262144
+//   1024 -> 1024   29.8 / 27.1  89.8 / 96.6  163 / 183    315 / 356
+//    361 -> 512    16.3 / 11.1  30.7 / 30.0  55.8 / 56.3  102 / 109
+//    512 -> 69     15.6 /  6.6  18.8 / 19.6  26.3 / 35.7  45.3 / 65.6
+// Panels pay from more than two tiles for each wavefront on, a single panel already from half a one.
+static bool in_panels(const Linear8Args &a)
+{
+    const int64_t panels = ceil_div(a.out, 128), tiles = ceil_div(a.n, PANEL_ROWS) * panels;
+    const bool enough = tiles > 2 * 256 * PANEL_WAVES || (panels == 1 && a.n >= 65536);
+    return enough && !wide(a) && a.steps <= PANEL_STEPS && panels <= 32 && a.q.ld_q < (1 << 24);
+}
 
 int linear8_splits(int64_t n, int64_t out, int64_t steps)
 {
@@ -474,6 +655,11 @@ static void join(const Linear8Args &a, const ColumnSums &c, hipStream_t s)
 
 hipError_t launch_linear8(const Linear8Args &a, hipStream_t s)
 {
+    if (in_panels(a)) {
+        const int panels = (int)ceil_div(a.out, 128), streams = 8 * (32 / panels);
+        linear8_panel_kernel<<<dim3(256), dim3(64 * PANEL_WAVES), 0, s>>>(a, panels, streams);
+        return hipGetLastError();
+    }
     if (few_tiles(a.n, a.out, 1) && !a.y8.q) {
         tile_by<Tile64>(a, s);
         return hipGetLastError();

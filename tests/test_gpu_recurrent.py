@@ -317,6 +317,36 @@ def test_linear8_of_many_rows():
             assert not y8.q.view(torch.uint8)[:, o:].any()
 
 
+@pytest.mark.parametrize("i,o,rows,pad", [(40, 69, (1, 128), 1), (129, 100, (128, 1), 0), (300, 801, (1, 1), 3), (512, 1024, (1, 128), 0),
+                                          (640, 897, (128, 128), 8), (1000, 1100, (1, 128), 2)])
+def test_linear8_of_panels(i, o, rows, pad):
+    """Many rows to bf16: one to eight blocks of k, ends in both directions, a row that is NaN and one of zeros."""
+    n = 65601
+    g = _gen(i, o)
+    x = torch.randn(n, i, generator=g)
+    x[7 if rows[0] == 1 else slice(0, 128)] = 0.0
+    x[n - 1, i - 1] = float("nan")
+    x8, w8 = im.Block8.empty(n, i, rows[0]), im.Block8.empty(o, i, rows[1])
+    im.block8_store(x.cuda(), x8)
+    im.block8_store(torch.randn(o, i, generator=g).cuda(), w8)
+    bias = torch.randn(o, generator=g).cuda()
+    xv, wv = (torch.zeros(*b.shape, device="cuda") for b in (x8, w8))
+    im.block8_load(x8, xv)
+    im.block8_load(w8, wv)
+    bad = torch.isnan(xv).any(1)
+    assert 1 <= int(bad.sum()) <= rows[0]
+    xv[bad] = 0.0
+    want = (xv.double() @ wv.double().t() + bias.double()).clamp(min=0)
+    mass = xv.double().abs() @ wv.double().abs().t() + bias.double().abs()
+    y = _rows(torch.full((n + 1, o), 7.0, dtype=torch.bfloat16), pad)
+    im.linear8(x8, w8, bias, y[:n], relu=True)
+    assert torch.isnan(y[:n][bad]).all() and (y[n] == 7).all()
+    # as for the tiles: eight products are added to a unit of 2^-13 of the largest's power of two
+    tol = (i + 2) * 2 * O.U32 * mass + 7 * 2.0 ** -13 * mass
+    err = (y[:n].double() - want).abs()
+    assert bool((err <= tol + O.HALF["bf16"] * 1.01 * (want + tol))[~bad].all())
+
+
 @pytest.mark.parametrize("n", [3, 40, 200, 600, 66000])
 def test_linear8_of_blocks_that_are_not_finite(n):
     """A row with a NaN or an infinity is NaN in y, and no other; the extreme scales."""
