@@ -863,7 +863,8 @@ im_status im_block_linear_grad(const im_layer8_grad *a, void *stream);
  * lie together.  state_out (float [n][d], NULL: not wanted; may be state) = c_(T-1); with
  * T = 1 the call is one step of a rollout.  keep (float [ceil(T / IM_SCAN_KEEP)][n][d],
  * NULL: not wanted): c before the steps 0, IM_SCAN_KEEP, .., for the gradient.  The sums
- * and the state are fp32.  0 <= T, n <= 2^30, 1 <= d, n d <= 2^31 (IM_ERR_UNSUPPORTED
+ * and the state are fp32; an infinite state may become a NaN where the product of many steps'
+ * gates underflows.  0 <= T, n <= 2^30, 1 <= d, n d <= 2^31 (IM_ERR_UNSUPPORTED
  * above).
  * workspace: im_gated_scan_workspace(T, n, d) bytes, 16-byte aligned (0 where the steps of
  * all envs are walked one after the other).

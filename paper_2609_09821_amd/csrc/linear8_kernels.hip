@@ -137,7 +137,8 @@ struct TileShape {
     static constexpr int L = UP + UQ + US;                               // direct loads of a step
     static constexpr int Q_AT = BP * 128, S_AT = Q_AT + BQ * 128, STAGE = S_AT + US * WAVES * 256;
     static constexpr int LDO = 128 + 16, OUT = 32 * LDO;                 // bytes of a wavefront's 32 output rows
-    static constexpr int LDS = std::max(NS * STAGE, WAVES * OUT);
+    static constexpr bool WHOLE = TP == 4 || (TP == 1 && WP == 4);       // a y8 block's columns meet
+    static constexpr int LDS = std::max(NS * STAGE, WAVES * OUT + (TP == 1 && WP == 4 ? TQ * WAVES * 128 : 0));
     // piece c of row r lies at c ^ perm(r)
     __device__ static int perm(int r) { return r >> 1 & 7; }
     static_assert(UP * NT == BP * 8 && UQ * NT == BQ * 8, "whole pieces");
@@ -334,7 +335,8 @@ __device__ __forceinline__ void tile_run(const Linear8Args &a, int p_tiles, int 
             for (int i = 0; i < TP; ++i)
 #pragma unroll
                 for (int k = 0; k < 16; ++k) acc[i][j][k] = __builtin_elementwise_maximum(acc[i][j][k], 0.0f);   // NaN stays
-        if constexpr (WIDE && TP == 4) {
+        // A block of y8 is a wavefront's columns or, with one tile a wavefront, those of four.
+        if constexpr (WIDE && S::WHOLE) {
             if (a.y8.q) {
                 uint32_t top = 0;
 #pragma unroll
@@ -342,9 +344,17 @@ __device__ __forceinline__ void tile_run(const Linear8Args &a, int p_tiles, int 
 #pragma unroll
                     for (int k = 0; k < 16; ++k) top = max(top, magnitude(acc[i][j][k]));
                 top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+                if constexpr (TP == 1) {
+                    uint32_t *tops = (uint32_t *)(lds + S::WAVES * S::OUT) + j * S::WAVES * 32;
+                    tops[wave * 32 + l32] = top;
+                    meet();
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) top = max(top, tops[(wave / 4 * 4 + w) * 32 + l32]);
+                }
                 const int s = block8_scale(top);
                 const int64_t row = q0 + wq + 32 * j + l32, col = p0 + wp;
-                if (half == 0 && row < a.n && col < a.out) a.y8.scale[row * a.y8.ld_scale + col / 128] = (uint8_t)s;
+                if (half == 0 && col % 128 == 0 && row < a.n && col < a.out)
+                    a.y8.scale[row * a.y8.ld_scale + col / 128] = (uint8_t)s;
 #pragma unroll
                 for (int i = 0; i < TP; ++i)
 #pragma unroll
@@ -353,7 +363,7 @@ __device__ __forceinline__ void tile_run(const Linear8Args &a, int p_tiles, int 
                         const int64_t nv = a.out - col - (32 * i + 8 * g + 4 * half);
                         *(uint32_t *)(to + 32 * i + 8 * g) = block8_pack4(v, s, (int)max(min(nv, (int64_t)4), (int64_t)0));
                     }
-                leave(Int<128>(), (char *)a.y8.q, a.y8.ld_q, j, col, (a.out + 127) / 128 * 128, 4);
+                leave(Int<32 * TP>(), (char *)a.y8.q, a.y8.ld_q, j, col, (a.out + 127) / 128 * 128, 4);
             }
         }
         if (!a.y) continue;
@@ -600,13 +610,15 @@ __global__ __launch_bounds__(1024) void linear8_join_kernel(Linear8Args a, int b
 //     64 x 64     7.3 (4.1)   12.6 (4.9)   41.6 (14.3)  145 (47.5)
 //     128 x 128   9.0 (5.8)   10.4 (6.3)   23.9 (9.6)   83.0 (28.0)
 //     256 x 256  15.5 (9.4)   16.5 (9.6)   23.3 (11.8)  76.6 (25.7)
-//   to 8 bits     n 1           8192         16384        65536
-//     128 x 128  11.5 (7.3)   21.0 (9.0)   37.8 (12.6)  141 (40.2)
-//     256 x 256  26.7 (14.7)  30.3 (16.4)  35.0 (17.7)  123 (37.1)
-// Of fewer than 256 tiles the smaller ones pay.
+//   to 8 bits     n 1           2048         8192         16384        65536
+//     128 x 32    7.1 (4.8)   14.0 (5.4)   49.0 (17.1)
+//     128 x 128  11.4 (7.0)   12.4 (7.6)   21.1 (8.5)   36.1 (12.0)  141 (40.2)
+//     256 x 256  26.7 (14.7)               30.3 (16.4)  35.0 (17.7)  123 (37.1)
+// Of fewer than 256 tiles the smaller ones pay; 128 x 32 while each has a CU.
 typedef TileShape<2, 2, 1, 1, 4> Tile64;      // 64 x 64, three steps ahead
 typedef TileShape<2, 2, 2, 2, 2> Tile128;     // 128 x 128, two blocks a CU
 typedef TileShape<1, 4, 4, 1, 2> TileRows;    // the same, wavefronts of whole blocks of y8
+typedef TileShape<4, 1, 1, 1, 4> TileFlat;    // 128 x 32, four wavefronts a block of y8
 typedef TileShape<2, 4, 4, 2, 2> Tile256;     // 256 x 256
 
 // Products in bf16, summed in fp32 throughout.
@@ -674,6 +686,7 @@ hipError_t launch_linear8(const Linear8Args &a, hipStream_t s)
         if (a.y) b.y = (char *)a.y + r * a.ld_y * (a.y_f32 ? 4 : 2);
         if (a.y8.q) b.y8.q += r * a.y8.ld_q, b.y8.scale += r * a.y8.ld_scale;
         if (tiles_of(b.n, b.out, 256) >= 256) tile_by<Tile256>(b, s);
+        else if (a.y8.q && ceil_div(b.n, 32) * ceil_div(b.out, 128) <= 256) tile_by<TileFlat>(b, s);
         else if (a.y8.q) tile_by<TileRows>(b, s);
         else tile_by<Tile128>(b, s);
     }

@@ -340,7 +340,7 @@ def test_linear8_of_panels(i, o, rows, pad):
     mass = xv.double().abs() @ wv.double().abs().t() + bias.double().abs()
     y = _rows(torch.full((n + 1, o), 7.0, dtype=torch.bfloat16), pad)
     im.linear8(x8, w8, bias, y[:n], relu=True)
-    assert torch.isnan(y[:n][bad]).all() and (y[n] == 7).all()
+    assert torch.isnan(y[:n][bad]).all() and (y[n] == 7).all() and torch.isnan(y._base[:, o:]).all()
     # as for the tiles: eight products are added to a unit of 2^-13 of the largest's power of two
     tol = (i + 2) * 2 * O.U32 * mass + 7 * 2.0 ** -13 * mass
     err = (y[:n].double() - want).abs()
