@@ -616,6 +616,7 @@ __global__ __launch_bounds__(1024) void linear8_join_kernel(Linear8Args a, int b
 //     256 x 256  26.7 (14.7)               30.3 (16.4)  35.0 (17.7)  123 (37.1)
 // Of fewer than 256 tiles the smaller ones pay; 128 x 32 while each has a CU.
 typedef TileShape<2, 2, 1, 1, 4> Tile64;      // 64 x 64, three steps ahead
+typedef TileShape<2, 2, 1, 1, 2> Tile64Many;  // four blocks a CU beside each other
 typedef TileShape<2, 2, 2, 2, 2> Tile128;     // 128 x 128, two blocks a CU
 typedef TileShape<1, 4, 4, 1, 2> TileRows;    // the same, wavefronts of whole blocks of y8
 typedef TileShape<4, 1, 1, 1, 4> TileFlat;    // 128 x 32, four wavefronts a block of y8
@@ -627,7 +628,7 @@ static bool wide(const Linear8Args &a) { return (a.y && a.y_f32) || a.y8.q; }
 static int64_t tiles_of(int64_t n, int64_t out, int side) { return ceil_div(n, side) * ceil_div(out, side); }
 
 // Few tiles of 128 x 128 leave CUs without one.
-static bool few_tiles(int64_t n, int64_t out, int64_t splits) { return tiles_of(n, out, 128) * splits < 256; }
+static bool few_tiles(int64_t n, int64_t out) { return tiles_of(n, out, 128) < 256; }
 
 // Panels or tiles, by us of n rows to bf16, inputs and outputs out of HBM (panels / tiles):
 //   n                 16384        65536        131072       262144
@@ -642,11 +643,21 @@ static bool in_panels(const Linear8Args &a)
     return enough && !wide(a) && a.steps <= PANEL_STEPS && panels <= 32 && a.q.ld_q < (1 << 24);
 }
 
+// Parts of dw: of tiles of 128 x 128 where they come to 400 (two a CU at most), else of 64 x 64.  A part
+// has four steps at least, eight where the tiles alone fill the CUs.  Both gradients by us of rows, in and
+// out, bf16, from a graph, with 64 x 64 below 256 parts, 400 and 512:
+//   2000 x 1024 x 1024   33.6  27.3  27.5       4096 x 1024 x 512    35.4   31.7   31.9
+//   16384 x 361 x 512    43.8  39.4  39.4       16384 x 361 x 1024   59.0   58.9   57.2
+//   8192 x 538 x 1024    47.4  47.5  45.7       65536 x 361 x 1024    165    165    196
+// 1024 x 1024 x 1024 in parts of four steps 20.4, of eight (no second part, no joining) 17.6.
+static bool large_parts(int64_t n, int64_t out, int64_t splits) { return tiles_of(n, out, 128) * splits >= 400; }
+
 int linear8_splits(int64_t n, int64_t out, int64_t steps)
 {
-    const int64_t big = std::max<int64_t>(1, std::min<int64_t>(512 / tiles_of(n, out, 128), steps / 4));
-    if (!few_tiles(n, out, big)) return (int)big;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles_of(n, out, 64), steps / 4));
+    const int64_t large = std::max<int64_t>(1, std::min<int64_t>(512 / tiles_of(n, out, 128), steps / 4));
+    if (large_parts(n, out, large)) return (int)large;
+    const int64_t tiles = tiles_of(n, out, 64);
+    return (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, steps / (tiles >= 256 ? 8 : 4)));
 }
 
 template <typename S>
@@ -656,6 +667,16 @@ static void tile_by(const Linear8Args &a, hipStream_t s)
     const dim3 g((unsigned)(tiles * a.splits)), b(S::NT);
     if (wide(a)) linear8_tile_kernel<S, true><<<g, b, 0, s>>>(a, (int)p_tiles, (int)tiles);
     else linear8_tile_kernel<S, false><<<g, b, 0, s>>>(a, (int)p_tiles, (int)tiles);
+}
+
+template <typename S>
+static void two_by(const Linear8Args &dx, const Linear8Args &dw, hipStream_t s)
+{
+    const int64_t ap = ceil_div(dx.out, S::BP), at = ap * ceil_div(dx.n, S::BQ);
+    const int64_t bp = ceil_div(dw.out, S::BP), bt = bp * ceil_div(dw.n, S::BQ);
+    const dim3 g((unsigned)(at + bt * dw.splits)), b(S::NT);
+    if (wide(dx)) linear8_two_kernel<S, true><<<g, b, 0, s>>>(dx, (int)ap, (int)at, dw, (int)bp, (int)bt);
+    else linear8_two_kernel<S, false><<<g, b, 0, s>>>(dx, (int)ap, (int)at, dw, (int)bp, (int)bt);
 }
 
 static void join(const Linear8Args &a, const ColumnSums &c, hipStream_t s)
@@ -672,7 +693,7 @@ hipError_t launch_linear8(const Linear8Args &a, hipStream_t s)
         linear8_panel_kernel<<<dim3(256), dim3(64 * PANEL_WAVES), 0, s>>>(a, panels, streams);
         return hipGetLastError();
     }
-    if (few_tiles(a.n, a.out, 1) && !a.y8.q) {
+    if (few_tiles(a.n, a.out) && !a.y8.q) {
         tile_by<Tile64>(a, s);
         return hipGetLastError();
     }
@@ -697,14 +718,13 @@ hipError_t launch_linear8(const Linear8Args &a, hipStream_t s)
 hipError_t launch_linear8_grad(const Linear8Args &dx, const Linear8Args &dw, const ColumnSums &c, hipStream_t s)
 {
     hipError_t e = hipSuccess;
-    const bool with_dx = dx.y != nullptr, small = dw.y && few_tiles(dw.n, dw.out, dw.splits);
-    if (with_dx && small && few_tiles(dx.n, dx.out, 1)) {
-        typedef Tile64 S;
-        const int64_t ap = ceil_div(dx.out, S::BP), at = ap * ceil_div(dx.n, S::BQ);
-        const int64_t bp = ceil_div(dw.out, S::BP), bt = bp * ceil_div(dw.n, S::BQ);
-        const dim3 g((unsigned)(at + bt * dw.splits)), b(S::NT);
-        if (wide(dx)) linear8_two_kernel<S, true><<<g, b, 0, s>>>(dx, (int)ap, (int)at, dw, (int)bp, (int)bt);
-        else linear8_two_kernel<S, false><<<g, b, 0, s>>>(dx, (int)ap, (int)at, dw, (int)bp, (int)bt);
+    const bool with_dx = dx.y != nullptr, small = dw.y && !large_parts(dw.n, dw.out, dw.splits);
+    if (with_dx && small && few_tiles(dx.n, dx.out)) {
+        const int64_t blocks = tiles_of(dx.n, dx.out, 64) + tiles_of(dw.n, dw.out, 64) * dw.splits;
+        // of more than two blocks a CU: 4095 x 361 x 1024 29.8 and 27.9 us, 8192 x 361 x 512 34.0 and 31.2,
+        // 256 x 361 x 1024, which has fewer, 12.5 and 13.8
+        if (blocks > 512) two_by<Tile64Many>(dx, dw, s);
+        else two_by<Tile64>(dx, dw, s);
         e = hipGetLastError();
     } else {
         if (with_dx) e = launch_linear8(dx, s);

@@ -377,7 +377,8 @@ def test_linear8_of_blocks_that_are_not_finite(n):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n,i,o,relu,pad", [
     (1, 1, 1, False, 0), (1, 361, 64, True, 0), (5, 40, 200, True, 3), (128, 128, 128, False, 0),
-    (130, 361, 129, True, 1), (1000, 257, 96, False, 0), (4097, 69, 300, True, 0), (9000, 130, 20, False, 5)])
+    (130, 361, 129, True, 1), (1000, 257, 96, False, 0), (4097, 69, 300, True, 0), (9000, 130, 20, False, 5),
+    (4095, 361, 300, True, 1), (1024, 1000, 1020, False, 0), (6500, 640, 1000, True, 2)])
 def test_linear8_grad(n, i, o, relu, pad, dtype):
     g = _gen(n, i, o, 3)
     x, w = torch.randn(n, i, generator=g), torch.randn(o, i, generator=g)
