@@ -5,14 +5,14 @@
 // All three read both operands along k, in whole blocks of 128 (rows are padded with
 // zeros).  MFMA accumulators give a lane one q and four consecutive p per register group.
 //
-// Outputs in bf16: v_mfma_scale_f32_32x32x64_f8f6f4, which multiplies each operand's
-// row by its own power of two, so that scales cost no instruction besides their load.  It adds
-// the products of eight neighbouring k to 14 bits from the largest one's exponent down, and only
-// these sums in fp32 (found by adding one small product to a large one; v_mfma_f32_32x32x16_fp8_fp8
-// gives the same bits): sums of normal values are off by 1.4e-5 of their norm, a hundredth of
-// what an output in bf16 loses.  Outputs in fp32 would lose by it, and in 8 bits values next to the
-// middle of two steps would go to the other one (8.9e-4 of the norm): there the bytes become bf16
-// with their block's scale (exact) and are multiplied by v_mfma_f32_32x32x16_bf16, at half the rate.
+// The bytes become bf16 with their block's scale, exactly, and are multiplied by
+// v_mfma_f32_32x32x16_bf16: every sum is one of fp32, for outputs of all types.  The matrix cores' 8-bit
+// instructions (v_mfma_scale_f32_32x32x64_f8f6f4, v_mfma_f32_32x32x16_fp8_fp8) run at twice the rate,
+// but add the products of eight neighbouring k to 14 bits from the largest one's exponent down before
+// they add the sum in fp32 (found by adding one small product to a large one): sums of normal values
+// are then off by 1.4e-5 of their norm, a hundred times what fp32 loses, and a small product beside
+// a large one is lost whole.  To bf16 they took 81 us of 65536 rows 1024 -> 1024 where fp32's sums take
+// 126 to 132 (hipBLASLt's product of bf16 matrices of that size 133), of one row 4.9 and 6.3.
 #include <algorithm>
 #include <type_traits>
 
@@ -21,9 +21,7 @@
 
 namespace im {
 
-typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
-typedef int i32x8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 #define IM_LDS3 __attribute__((address_space(3)))
@@ -76,26 +74,6 @@ __device__ __forceinline__ void meet()
     asm volatile("" ::: "memory");
 }
 
-__device__ __forceinline__ i32x8_t join(u32x4_r lo, u32x4_r hi)
-{
-    return i32x8_t{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-}
-
-// acc += (a 2^(sa - 127)) (b 2^(sb - 127)) over 64 k.  A lane holds 32 bytes of one row of each
-// operand, its k by the half of the wavefront; both operands are read alike, so that which k is
-// of no matter, and a row has one scale over all 128 k of a block.
-__device__ __forceinline__ f32x16_t mfma8(i32x8_t a, i32x8_t b, f32x16_t acc, int sa, int sb)
-{
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc, 0, 0, 0, sa, 0, sb);
-}
-
-// The same of 16 rows each and 128 k, 32 bytes of a row in each of its four lanes; sa in byte A.
-template <int A>
-__device__ __forceinline__ f32x4_t mfma8_16(i32x8_t a, i32x8_t b, f32x4_t acc, int sa, int sb)
-{
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 0, 0, A, sa, 0, sb);
-}
-
 // Eight e4m3 values times the scale's power of two as bf16: exact, but for values below 2^-126.
 __device__ __forceinline__ bf16x8_t widen8(uint32_t lo, uint32_t hi, float scale)
 {
@@ -120,11 +98,9 @@ __device__ __forceinline__ u32x4_r bits4(const f32x16_t &a, int g)
 // 64 consecutive 16-byte pieces, so a stage has no padding: pieces are permuted in their row
 // instead, so that 16 rows' pieces of one k cover all banks.
 //
-// 65536 rows 1024 -> 1024 to bf16: 80 us, 1.72 PFLOP/s (hipBLASLt with one scale for each operand and no
-// bias 87), 97 with all arrays out of HBM; 59 without the outputs, of which HBM takes 27 alone: a 256 x 256
-// tile has a CU for itself, so that nothing multiplies while it stores.  Two blocks of 256 x 128 a CU store
-// beside each other's products but load more (88 us).
-// To fp32: 144 us.  dw of 65536 rows 1024 -> 512: 76 us in 16 parts and 8 to join them; tiles of 256 x 256,
+// 65536 rows 1024 -> 1024 to bf16: 126 us, 1.09 PFLOP/s, 136 with all arrays out of HBM; to fp32 152 and 156.
+// A 256 x 256 tile has a CU for itself, so that nothing multiplies while it stores.
+// dw of 65536 rows 1024 -> 512: 76 us in 16 parts and 8 to join them; tiles of 256 x 256,
 // 256 x 128 and eight wavefronts a tile are no faster (82, 85, 79), and rows of x^T that lie a multiple
 // of 64 KB apart cost 10 us.
 // ---------------------------------------------------------------------------
@@ -144,7 +120,7 @@ struct TileShape {
     static_assert(UP * NT == BP * 8 && UQ * NT == BQ * 8, "whole pieces");
 };
 
-template <typename S, bool WIDE>
+template <typename S>
 __device__ __forceinline__ void tile_run(const Linear8Args &a, int p_tiles, int tiles, int id, char *lds)
 {
     constexpr int TP = S::TP, TQ = S::TQ, BP = S::BP, BQ = S::BQ, NS = S::NS;
@@ -231,58 +207,31 @@ __device__ __forceinline__ void tile_run(const Linear8Args &a, int p_tiles, int 
 #pragma unroll
             for (int j = 0; j < TQ; ++j) bq[s & 1][j] = piece(st + S::Q_AT, wq + 32 * j, s);
         };
-        auto more_copies = [&](int s, int of) {
+        read(0);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            if (s + 1 < 4) read(s + 1);
             if (more)
 #pragma unroll
-                for (int u = S::L * s / of; u < S::L * (s + 1) / of; ++u) copy(u, kt + NS - 1, ahead);
-        };
-        read(0);
-        if constexpr (WIDE) {
+                for (int u = S::L * s / 4; u < S::L * (s + 1) / 4; ++u) copy(u, kt + NS - 1, ahead);
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                if (s + 1 < 4) read(s + 1);
-                more_copies(s, 4);
+            for (int h = 0; h < 2; ++h) {
+                bf16x8_t fp[TP], fq[TQ];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    bf16x8_t fp[TP], fq[TQ];
+                for (int i = 0; i < TP; ++i)
+                    fp[i] = widen8(bp[s & 1][i][2 * h], bp[s & 1][i][2 * h + 1],
+                                   __uint_as_float((uint32_t)sp[i] << 23));
 #pragma unroll
-                    for (int i = 0; i < TP; ++i)
-                        fp[i] = widen8(bp[s & 1][i][2 * h], bp[s & 1][i][2 * h + 1],
-                                       __uint_as_float((uint32_t)sp[i] << 23));
-#pragma unroll
-                    for (int j = 0; j < TQ; ++j)
-                        fq[j] = widen8(bq[s & 1][j][2 * h], bq[s & 1][j][2 * h + 1],
-                                       __uint_as_float((uint32_t)sq[j] << 23));
-#pragma unroll
-                    for (int i = 0; i < TP; ++i)
-#pragma unroll
-                        for (int j = 0; j < TQ; ++j)
-                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp[i], fq[j], acc[i][j], 0, 0, 0);
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        } else {
-            u32x4_r cp[TP], cq[TQ];
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                read(2 * s + 1);
-#pragma unroll
-                for (int i = 0; i < TP; ++i) cp[i] = bp[0][i];
-#pragma unroll
-                for (int j = 0; j < TQ; ++j) cq[j] = bq[0][j];
-                i32x8_t fp[TP], fq[TQ];
-#pragma unroll
-                for (int i = 0; i < TP; ++i) fp[i] = join(cp[i], bp[1][i]);
-#pragma unroll
-                for (int j = 0; j < TQ; ++j) fq[j] = join(cq[j], bq[1][j]);
-                if (s + 1 < 2) read(2 * s + 2);
-                more_copies(s, 2);
+                for (int j = 0; j < TQ; ++j)
+                    fq[j] = widen8(bq[s & 1][j][2 * h], bq[s & 1][j][2 * h + 1],
+                                   __uint_as_float((uint32_t)sq[j] << 23));
 #pragma unroll
                 for (int i = 0; i < TP; ++i)
 #pragma unroll
-                    for (int j = 0; j < TQ; ++j) acc[i][j] = mfma8(fp[i], fq[j], acc[i][j], sp[i], sq[j]);
-                __builtin_amdgcn_sched_barrier(0);
+                    for (int j = 0; j < TQ; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fp[i], fq[j], acc[i][j], 0, 0, 0);
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
     int kt = 0;
@@ -336,7 +285,7 @@ __device__ __forceinline__ void tile_run(const Linear8Args &a, int p_tiles, int 
 #pragma unroll
                 for (int k = 0; k < 16; ++k) acc[i][j][k] = __builtin_elementwise_maximum(acc[i][j][k], 0.0f);   // NaN stays
         // A block of y8 is a wavefront's columns or, with one tile a wavefront, those of four.
-        if constexpr (WIDE && S::WHOLE) {
+        if constexpr (S::WHOLE) {
             if (a.y8.q) {
                 uint32_t top = 0;
 #pragma unroll
@@ -367,7 +316,7 @@ __device__ __forceinline__ void tile_run(const Linear8Args &a, int p_tiles, int 
             }
         }
         if (!a.y) continue;
-        if (WIDE && a.y_f32) {
+        if (a.y_f32) {
             char *y = (char *)a.y;
             int64_t ld = a.ld_y * 4;
             if (a.part) {
@@ -398,183 +347,22 @@ __device__ __forceinline__ void tile_run(const Linear8Args &a, int p_tiles, int 
     }
 }
 
-template <typename S, bool WIDE>
+template <typename S>
 __global__ __launch_bounds__(S::NT, 2) void linear8_tile_kernel(Linear8Args a, int p_tiles, int tiles)
 {
     __shared__ __attribute__((aligned(1024))) char lds[S::LDS];
-    tile_run<S, WIDE>(a, p_tiles, tiles, xcd_order(blockIdx.x, gridDim.x), lds);
+    tile_run<S>(a, p_tiles, tiles, xcd_order(blockIdx.x, gridDim.x), lds);
 }
 
-// Two products side by side in one launch, a layer's gradients: the second one is wide.
-template <typename S, bool WIDE>
+// Two products side by side in one launch, a layer's gradients.
+template <typename S>
 __global__ __launch_bounds__(S::NT, 2) void linear8_two_kernel(Linear8Args a, int a_tiles, int a_blocks, Linear8Args b,
                                                               int b_p_tiles, int b_tiles)
 {
     __shared__ __attribute__((aligned(1024))) char lds[S::LDS];
     const int id = xcd_order(blockIdx.x, gridDim.x);
-    if (id < a_blocks) tile_run<S, WIDE>(a, a_tiles, a_blocks, id, lds);
-    else tile_run<S, true>(b, b_p_tiles, b_tiles, id - a_blocks, lds);
-}
-
-// ---------------------------------------------------------------------------
-// Panels.  With many rows, an output in bf16 and a k that fits, a block keeps 128 columns of P, all
-// their k, in LDS and its wavefronts walk over the rows of Q by themselves, 64 at a time, without a
-// barrier: Q's fragments come straight into registers, a step of 128 k ahead, also across the end of
-// a tile, so that one wavefront's outputs leave while others multiply.  A block for each CU; the
-// panels of one run of rows are neighbours in an L2.
-//
-// A wavefront's tile is 128 p x 64 q in MFMA tiles of 16 x 16 (v_mfma_scale_f32_16x16x128_f8f6f4):
-// four lanes then hold one row of Q.  Bound by the CU's vector cache, to which each 16 bytes that a
-// lane loads are an access: so scales are loaded four steps at a time and outputs pass through LDS.
-// 65536 rows 1024 -> 1024: 84 us, 90 with all arrays out of HBM.  Weights in registers, rows in LDS: 113.
-// ---------------------------------------------------------------------------
-constexpr int PANEL_STEPS = 8, PANEL_WAVES = 8, PANEL_ROWS = 64;
-__global__ __launch_bounds__(64 * PANEL_WAVES, 1) void linear8_panel_kernel(Linear8Args a, int panels, int streams)
-{
-    constexpr int TP = 8, TQ = PANEL_ROWS / 16, LDO = 128 + 16;
-    __shared__ __attribute__((aligned(1024))) char lds[PANEL_STEPS * 16384];
-    __shared__ __attribute__((aligned(16))) char outs[PANEL_WAVES][16 * LDO];
-    __shared__ int pscale[PANEL_STEPS][16][2];      // byte i % 4 of word i / 4: row 16 i + lane's
-    __shared__ float bias[128];
-    const int lane = threadIdx.x & 63, wave = wave_id(), l16 = lane & 15, grp = lane >> 4;
-    const int place = blockIdx.x >> 3, panel = place % panels;
-    const int stream = place / panels * 8 + (blockIdx.x & 7);
-    if (place / panels * 8 >= streams) return;
-    const int64_t p0 = (int64_t)panel * 128;
-    const int steps = (int)a.steps;
-    for (int u = wave; u < steps * 16; u += PANEL_WAVES) {
-        const int r = (u & 15) * 8 + lane / 8, c = (lane & 7) ^ (r >> 1 & 7);
-        const int64_t row = min(p0 + r, a.out - 1);
-        copy_to_lds(a.p.q + row * a.p.ld_q + (u >> 4) * 128 + c * 16, lds + u * 1024);
-    }
-    for (int u = threadIdx.x; u < steps * 32; u += 64 * PANEL_WAVES) {
-        int v = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t row = min(p0 + 64 * (u & 1) + 16 * i + (u >> 1 & 15), a.out - 1);
-            v |= a.p.scale[(row >> a.p.shift) * a.p.ld_scale + (u >> 5)] << (8 * i);
-        }
-        pscale[u >> 5][u >> 1 & 15][u & 1] = v;
-    }
-    if (threadIdx.x < 128) bias[threadIdx.x] = a.bias ? a.bias[min(p0 + threadIdx.x, a.out - 1)] : 0.0f;
-    wait_loads<0>();
-    __syncthreads();
-
-    const int64_t tiles = (a.n + PANEL_ROWS - 1) / PANEL_ROWS, stride = (int64_t)streams * PANEL_WAVES;
-    int64_t tile = (int64_t)stream * PANEL_WAVES + wave;
-    if (tile >= tiles) return;
-    // Q: 16 bytes grp and 4 + grp of a step of the rows 16 j + l16
-    u32x4_r bq[2][TQ][2];
-    // the scales of row `lane`: bytes of the steps 0..3, and of the last four (steps 4..7)
-    uint32_t scale[2], next_scale[2] = {0, 0};
-    // part j of step kt of tile t; rows past the last read the last one: their sums are not stored
-    auto fetch = [&](int set, int64_t t, int kt, int j) {
-        const int64_t q0 = t * PANEL_ROWS;
-        const int last = (int)min((int64_t)PANEL_ROWS, a.n - q0) - 1;
-        const uint8_t *base = a.q.q + q0 * a.q.ld_q + kt * 128;
-        const uint32_t off = (uint32_t)min(16 * j + l16, last) * (uint32_t)a.q.ld_q + grp * 16;
-        bq[set][j][0] = *(const u32x4_r *)(base + off);
-        bq[set][j][1] = *(const u32x4_r *)(base + off + 64);
-        if (j == 0 && kt == 0) {
-            const uint8_t *s = a.q.scale + ((q0 + min(lane, last)) >> a.q.shift) * a.q.ld_scale;
-            if (steps >= 4) {
-                typedef uint32_t u32_a1 __attribute__((aligned(1)));
-                next_scale[0] = *(const u32_a1 *)s;
-                next_scale[1] = *(const u32_a1 *)(s + steps - 4) >> (8 * (8 - steps) & 31);
-            } else {
-                next_scale[0] = s[0];
-                if (steps > 1) next_scale[0] |= s[1] << 8;
-                if (steps > 2) next_scale[0] |= s[2] << 16;
-            }
-        }
-    };
-    f32x4_t acc[TP][TQ];
-    auto start = [&] {
-        scale[0] = next_scale[0], scale[1] = next_scale[1];
-#pragma unroll
-        for (int i = 0; i < TP; ++i) {
-            const f32x4_t b = *(const f32x4_t *)(bias + 16 * i + 4 * grp);
-#pragma unroll
-            for (int j = 0; j < TQ; ++j) acc[i][j] = b;
-        }
-    };
-    // a step's products; more(i): work beside those of the i-th tile of P
-    auto multiply = [&](int set, int kt, auto more) {
-        const char *st = lds + kt * 16384;
-        const int sp[2] = {pscale[kt][l16][0], pscale[kt][l16][1]};
-        // the scale of row 16 j + l16 in all four lanes of the row
-        const uint32_t own = scale[kt >> 2] >> (8 * (kt & 3));
-        const auto x = __builtin_amdgcn_permlane16_swap(own, own, false, false);
-        const auto even = __builtin_amdgcn_permlane32_swap(x[0], x[0], false, false);
-        const auto odd = __builtin_amdgcn_permlane32_swap(x[1], x[1], false, false);
-        const int s4[TQ] = {(int)even[0], (int)odd[0], (int)even[1], (int)odd[1]};
-        // piece c of a row at c ^ (row / 2 mod 8)
-        auto piece = [&](int i, int k) {
-            return *(const u32x4_r *)(st + (16 * i + l16) * 128 + (((4 * k + grp) ^ (l16 >> 1)) << 4));
-        };
-#pragma unroll
-        for (int i = 0; i < TP; ++i) {
-            const i32x8_t fp = join(piece(i, 0), piece(i, 1));
-            more(i);
-#pragma unroll
-            for (int j = 0; j < TQ; ++j) {
-                const i32x8_t fq = join(bq[set][j][0], bq[set][j][1]);
-                if (i % 4 == 0) acc[i][j] = mfma8_16<0>(fp, fq, acc[i][j], sp[i / 4], s4[j]);
-                if (i % 4 == 1) acc[i][j] = mfma8_16<1>(fp, fq, acc[i][j], sp[i / 4], s4[j]);
-                if (i % 4 == 2) acc[i][j] = mfma8_16<2>(fp, fq, acc[i][j], sp[i / 4], s4[j]);
-                if (i % 4 == 3) acc[i][j] = mfma8_16<3>(fp, fq, acc[i][j], sp[i / 4], s4[j]);
-            }
-        }
-    };
-    // A lane's sums of a 16 x 16 tile are p = 4 grp + 0..3 of one q.  16 rows x 64 columns at a time leave
-    // through the wavefront's own LDS, 128 bytes of a row.
-    auto store = [&](int64_t t) {
-        char *mine = outs[wave];
-#pragma unroll
-        for (int j = 0; j < TQ; ++j)
-#pragma unroll
-            for (int i0 = 0; i0 < TP; i0 += 4) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    f32x4_t v = acc[i0 + i][j];
-                    if (a.relu)
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) v[k] = __builtin_elementwise_maximum(v[k], 0.0f);      // NaN stays
-                    *(u32x2_r *)(mine + l16 * LDO + 32 * i + 8 * grp) = u32x2_r{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-                }
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int r = u * 8 + lane / 8, c = lane % 8 * 8;
-                    const u32x4_r o = *(const u32x4_r *)(mine + r * LDO + c * 2);
-                    const int64_t row = t * PANEL_ROWS + 16 * j + r, col = p0 + 16 * i0 + c;
-                    if (row < a.n)
-                        store8_bits((uint16_t *)a.y + row * a.ld_y + col, (int)min((int64_t)8, a.out - col), o);
-                }
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            }
-    };
-    int kt = 0, next_kt = 0;
-    int64_t next_tile = tile;
-#pragma unroll
-    for (int j = 0; j < TQ; ++j) fetch(0, tile, 0, j);
-    while (true) {
-#pragma unroll
-        for (int set = 0; set < 2; ++set) {
-            if (++next_kt == steps) next_kt = 0, next_tile += stride;
-            if (next_tile >= tiles) next_tile = tile;      // after the last step: read again, not used
-            if (kt == 0) start();
-            multiply(set, kt, [&](int i) {
-                if (i < TQ) fetch(set ^ 1, next_tile, next_kt, i);
-            });
-            if (++kt == steps) {
-                store(tile);
-                kt = 0;
-                tile += stride;
-                if (tile >= tiles) return;
-            }
-        }
-    }
+    if (id < a_blocks) tile_run<S>(a, a_tiles, a_blocks, id, lds);
+    else tile_run<S>(b, b_p_tiles, b_tiles, id - a_blocks, lds);
 }
 
 // Parts of a product to y, in their order.  The blocks after the first `blocks` add up column
@@ -606,10 +394,10 @@ __global__ __launch_bounds__(1024) void linear8_join_kernel(Linear8Args a, int b
 }
 
 // Sides of tiles, by us of n rows 1024 -> 1024 (361 -> 512 in brackets), replayed from a graph:
-//   to bf16       n 2048        4096         16384        65536
-//     64 x 64     7.3 (4.1)   12.6 (4.9)   41.6 (14.3)  145 (47.5)
-//     128 x 128   9.0 (5.8)   10.4 (6.3)   23.9 (9.6)   83.0 (28.0)
-//     256 x 256  15.5 (9.4)   16.5 (9.6)   23.3 (11.8)  76.6 (25.7)
+//   to bf16       n 1          2048         4096         8192         16384        65536
+//     64 x 64      6.3 (4.2)    9.4 (4.7)   17.0 (5.8)   30.9 (10.0)  56.1 (17.7)  206 (61.8)
+//     128 x 128   10.2 (6.0)   11.8 (6.9)   13.2 (7.3)   21.0 (8.3)   36.8 (12.0)  136 (34.9)
+//     256 x 256   24.2 (11.6)  26.2 (13.2)  27.0 (13.5)  29.9 (14.3)  34.3 (16.0)  126 (34.4)
 //   to 8 bits     n 1           2048         8192         16384        65536
 //     128 x 32    7.1 (4.8)   14.0 (5.4)   49.0 (17.1)
 //     128 x 128  11.4 (7.0)   12.4 (7.6)   21.1 (8.5)   36.1 (12.0)  141 (40.2)
@@ -622,34 +410,18 @@ typedef TileShape<1, 4, 4, 1, 2> TileRows;    // the same, wavefronts of whole b
 typedef TileShape<4, 1, 1, 1, 4> TileFlat;    // 128 x 32, four wavefronts a block of y8
 typedef TileShape<2, 4, 4, 2, 2> Tile256;     // 256 x 256
 
-// Products in bf16, summed in fp32 throughout.
-static bool wide(const Linear8Args &a) { return (a.y && a.y_f32) || a.y8.q; }
-
 static int64_t tiles_of(int64_t n, int64_t out, int side) { return ceil_div(n, side) * ceil_div(out, side); }
 
 // Few tiles of 128 x 128 leave CUs without one.
 static bool few_tiles(int64_t n, int64_t out) { return tiles_of(n, out, 128) < 256; }
 
-// Panels or tiles, by us of n rows to bf16, inputs and outputs out of HBM (panels / tiles):
-//   n                 16384        65536        131072       262144
-//   1024 -> 1024   29.8 / 27.1  89.8 / 96.6  163 / 183    315 / 356
-//    361 -> 512    16.3 / 11.1  30.7 / 30.0  55.8 / 56.3  102 / 109
-//    512 -> 69     15.6 /  6.6  18.8 / 19.6  26.3 / 35.7  45.3 / 65.6
-// Panels pay from more than two tiles for each wavefront on, a single panel already from half a one.
-static bool in_panels(const Linear8Args &a)
-{
-    const int64_t panels = ceil_div(a.out, 128), tiles = ceil_div(a.n, PANEL_ROWS) * panels;
-    const bool enough = tiles > 2 * 256 * PANEL_WAVES || (panels == 1 && a.n >= 65536);
-    return enough && !wide(a) && a.steps <= PANEL_STEPS && panels <= 32 && a.q.ld_q < (1 << 24);
-}
-
 // Parts of dw: of tiles of 128 x 128 where they come to 400 (two a CU at most), else of 64 x 64.  A part
 // has four steps at least, eight where the tiles alone fill the CUs.  Both gradients by us of rows, in and
 // out, bf16, from a graph, with 64 x 64 below 256 parts, 400 and 512:
-//   2000 x 1024 x 1024   33.6  27.3  27.5       4096 x 1024 x 512    35.4   31.7   31.9
-//   16384 x 361 x 512    43.8  39.4  39.4       16384 x 361 x 1024   59.0   58.9   57.2
-//   8192 x 538 x 1024    47.4  47.5  45.7       65536 x 361 x 1024    165    165    196
-// 1024 x 1024 x 1024 in parts of four steps 20.4, of eight (no second part, no joining) 17.6.
+//   2000 x 1024 x 1024   36.8  28.4  28.4       4096 x 1024 x 512    37.6   33.9   33.8
+//   16384 x 361 x 512    48.6  44.3  43.5       16384 x 361 x 1024   67.1   67.4   64.9
+//   8192 x 538 x 1024    54.4  54.8  51.6       65536 x 361 x 1024    185    187    216
+// 1024 x 1024 x 1024 in parts of four steps 22.3, of eight (no second part, no joining) 18.6.
 static bool large_parts(int64_t n, int64_t out, int64_t splits) { return tiles_of(n, out, 128) * splits >= 400; }
 
 int linear8_splits(int64_t n, int64_t out, int64_t steps)
@@ -665,8 +437,7 @@ static void tile_by(const Linear8Args &a, hipStream_t s)
 {
     const int64_t p_tiles = ceil_div(a.out, S::BP), tiles = p_tiles * ceil_div(a.n, S::BQ);
     const dim3 g((unsigned)(tiles * a.splits)), b(S::NT);
-    if (wide(a)) linear8_tile_kernel<S, true><<<g, b, 0, s>>>(a, (int)p_tiles, (int)tiles);
-    else linear8_tile_kernel<S, false><<<g, b, 0, s>>>(a, (int)p_tiles, (int)tiles);
+    linear8_tile_kernel<S><<<g, b, 0, s>>>(a, (int)p_tiles, (int)tiles);
 }
 
 template <typename S>
@@ -675,8 +446,7 @@ static void two_by(const Linear8Args &dx, const Linear8Args &dw, hipStream_t s)
     const int64_t ap = ceil_div(dx.out, S::BP), at = ap * ceil_div(dx.n, S::BQ);
     const int64_t bp = ceil_div(dw.out, S::BP), bt = bp * ceil_div(dw.n, S::BQ);
     const dim3 g((unsigned)(at + bt * dw.splits)), b(S::NT);
-    if (wide(dx)) linear8_two_kernel<S, true><<<g, b, 0, s>>>(dx, (int)ap, (int)at, dw, (int)bp, (int)bt);
-    else linear8_two_kernel<S, false><<<g, b, 0, s>>>(dx, (int)ap, (int)at, dw, (int)bp, (int)bt);
+    linear8_two_kernel<S><<<g, b, 0, s>>>(dx, (int)ap, (int)at, dw, (int)bp, (int)bt);
 }
 
 static void join(const Linear8Args &a, const ColumnSums &c, hipStream_t s)
@@ -688,11 +458,6 @@ static void join(const Linear8Args &a, const ColumnSums &c, hipStream_t s)
 
 hipError_t launch_linear8(const Linear8Args &a, hipStream_t s)
 {
-    if (in_panels(a)) {
-        const int panels = (int)ceil_div(a.out, 128), streams = 8 * (32 / panels);
-        linear8_panel_kernel<<<dim3(256), dim3(64 * PANEL_WAVES), 0, s>>>(a, panels, streams);
-        return hipGetLastError();
-    }
     if (few_tiles(a.n, a.out) && !a.y8.q) {
         tile_by<Tile64>(a, s);
         return hipGetLastError();
@@ -721,8 +486,8 @@ hipError_t launch_linear8_grad(const Linear8Args &dx, const Linear8Args &dw, con
     const bool with_dx = dx.y != nullptr, small = dw.y && !large_parts(dw.n, dw.out, dw.splits);
     if (with_dx && small && few_tiles(dx.n, dx.out)) {
         const int64_t blocks = tiles_of(dx.n, dx.out, 64) + tiles_of(dw.n, dw.out, 64) * dw.splits;
-        // of more than two blocks a CU: 4095 x 361 x 1024 29.8 and 27.9 us, 8192 x 361 x 512 34.0 and 31.2,
-        // 256 x 361 x 1024, which has fewer, 12.5 and 13.8
+        // of more than two blocks a CU: 4095 x 361 x 1024 30.5 and 28.2 us, 8192 x 361 x 512 34.1 and 31.9,
+        // 256 x 361 x 1024, which has fewer, 14.4 and 15.3
         if (blocks > 512) two_by<Tile64Many>(dx, dw, s);
         else two_by<Tile64>(dx, dw, s);
         e = hipGetLastError();
