@@ -1172,7 +1172,7 @@ def linear8_grad(dy, xt, wt, dx=None, dw=None, db=None, y=None, workspace=None, 
     elif dw is not None:
         in_ = dw.shape[1]
     else:
-        in_ = 1
+        in_ = 1         # db does not go by it, nor the scratch memory without dw
     f32 = _torch.float32
     ws, nbytes = None, 0
     if n:

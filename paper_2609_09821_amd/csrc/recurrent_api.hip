@@ -284,7 +284,8 @@ im_status im_block_linear_grad(const im_layer8_grad *p, void *stream)
     if (p->dw && p->n > 0 && !p->xt) return invalid("NULL block8: xt");
     if (p->dw && p->n > 0 && (s = check_block8(p->xt, p->in, p->n)) != IM_OK) return s;
     const GradSpace g = grad_space(p->n, p->in, p->out);
-    s = check_workspace(p->workspace, p->workspace_bytes, g.bytes, 16);
+    // the parts, which come last, are dw's: without it `in` does not count
+    s = check_workspace(p->workspace, p->workspace_bytes, p->dw ? g.bytes : g.part, 16);
     if (s != IM_OK) return s;
     if (p->n == 0 && !sums) return IM_OK;
     const hipStream_t st = (hipStream_t)stream;

@@ -1,0 +1,41 @@
+"""Calls of a recurrent policy's blocks that their documentation allows beside the usual ones: outputs
+alone in a given workspace, outputs in the place of inputs, other layouts of flags."""
+import zlib
+
+import numpy as np
+import pytest
+
+from tests import recurrent_oracle as O
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from paper_2609_09821_amd import binding as im  # noqa: E402
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def _gen(*key):
+    g = torch.Generator()
+    g.manual_seed(zlib.crc32(repr(key).encode()))
+    return g
+
+
+def _np(t):
+    return t.detach().float().cpu().double().numpy()
+
+
+@pytest.mark.parametrize("n,i,o", [(1000, 1024, 1024), (1024, 1024, 1024), (40, 361, 69)])
+def test_linear8_grad_outputs_alone_in_the_layers_workspace(n, i, o):
+    g = _gen(n, i, o)
+    dy, x, w = (torch.randn(*z, generator=g).cuda() for z in ((n, o), (n, i), (o, i)))
+    xt, wt = im.Block8.empty(i, n), im.Block8.empty(i, o, 128)
+    im.block8_store(x, None, xt)
+    im.block8_store(w, None, wt)
+    ws = im.linear8_grad_workspace(n, i, o)
+    outs = [torch.zeros(*z, device="cuda") for z in ((n, i), (o, i), (o,))]
+    im.linear8_grad(dy, xt, wt, *outs, workspace=ws)
+    for k in range(3):
+        one = [torch.full_like(t, 7.0) if j == k else None for j, t in enumerate(outs)]
+        im.linear8_grad(dy, xt, wt, *one, workspace=ws)
+        assert torch.equal(one[k], outs[k])

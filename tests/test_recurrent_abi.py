@@ -234,3 +234,16 @@ def test_calls_on_nothing(lib):
     assert lib.im_gated_scan(C.byref(_scan(n=0, gate=None, x=None, h=None)), None) == im.IM_OK
     assert lib.im_gated_scan(C.byref(_scan(T=0, gate=None, x=None, h=None, state_out=None)), None) == im.IM_OK
     assert lib.im_gated_scan_grad(C.byref(_scan_grad(n=0, dh=None)), None) == im.IM_OK
+
+
+@pytest.mark.parametrize("n,i,o", [(1000, 1024, 1024), (1024, 1024, 1024), (1920, 1024, 1024), (40, 361, 69),
+                                   (65536, 1024, 512)])
+def test_the_layers_workspace_serves_each_output_alone(lib, n, i, o):
+    """db alone is asked for without the layer's input width (in = 1, as the binding does): the
+    layer's workspace is large enough.  It is misaligned here, which is looked at last."""
+    need = lib.im_block_linear_grad_workspace(n, i, o)
+    none = dict(dx=None, dw=None, db=None, ld_dy=o, y=None, workspace=P + 8, workspace_bytes=need)
+    for over in (dict(db=P, in_=1), dict(db=P, in_=i), dict(dx=P, in_=i, ld_dx=i, wt=_held(o, i, 128)),
+                 dict(dw=P, in_=i, ld_dw=i, xt=_held(n, i))):
+        a = _layer_grad(**dict(none, n=n, out=o, **over))
+        _refused(lib, lib.im_block_linear_grad(C.byref(a), None), BAD, "aligned")
