@@ -778,8 +778,8 @@ im_status im_rms_norm(const im_rms *a, void *stream);
  * dh the gradient that reaches h past the norm (NULL: none); dx is the gradient of x
  * and of the residual alike.  dy, h, dh, dx of `dtype`; dx may be dy, h or dh (or
  * NULL: not wanted); dgamma [d] float (NULL: not wanted), overwritten (zero for n = 0).
- * workspace: im_rms_norm_grad_workspace(n, d) bytes, 4-byte aligned (not needed
- * without dgamma).
+ * workspace: im_rms_norm_grad_workspace(n, d) bytes, 4-byte aligned: enough for at most n
+ * rows (not needed without dgamma).
  */
 typedef struct {
     int64_t n, d;
@@ -829,7 +829,8 @@ im_status im_block_linear(const im_layer8 *a, void *stream);
  * wt: w^T [in][out] and xt: x^T [in][n] in 8 bits, as im_block_store's t (needed for dx
  * and dw).  dx and dw are summed in fp32.
  * dx, dw and db may each be NULL: not wanted; dw and db are zero for n = 0.
- * workspace: im_block_linear_grad_workspace(...) bytes, 16-byte aligned.
+ * workspace: im_block_linear_grad_workspace(n, in, out) bytes, 16-byte aligned: enough for
+ * every call on at most n rows of the layer.
  */
 typedef struct {
     int64_t n, in, out;
@@ -863,8 +864,8 @@ im_status im_block_linear_grad(const im_layer8_grad *a, void *stream);
  * and the state are fp32; an infinite state may become a NaN where the product of many steps'
  * gates underflows.  0 <= T, n <= 2^30, 1 <= d, n d <= 2^31 (IM_ERR_UNSUPPORTED
  * above).
- * workspace: im_gated_scan_workspace(T, n, d) bytes, 16-byte aligned (0 where the steps of
- * all envs are walked one after the other).
+ * workspace: im_gated_scan_workspace(T, n, d) bytes, 16-byte aligned: enough for every call of
+ * at most T steps, n envs and d values (5 MB at most; 0 for T <= 64, which needs none).
  */
 #define IM_SCAN_KEEP 16
 typedef struct {

@@ -1121,7 +1121,7 @@ def rms_norm(x, gamma, y=None, rstd=None, eps=1e-6, residual=None, h=None, y8=No
 
 
 def rms_norm_grad_workspace(n, d):
-    """A workspace tensor for rms_norm_grad."""
+    """A workspace tensor for rms_norm_grad on at most n rows."""
     return _space(lib().im_rms_norm_grad_workspace(n, d))
 
 
@@ -1156,7 +1156,7 @@ def linear8(x, w, bias, y=None, y8=None, relu=False, stream=None):
 
 
 def linear8_grad_workspace(n, in_, out):
-    """A workspace tensor for linear8_grad."""
+    """A workspace tensor for linear8_grad on at most n rows."""
     return _space(lib().im_block_linear_grad_workspace(n, in_, out))
 
 
@@ -1232,7 +1232,7 @@ def _state(t, n, d, name, dev):
 
 
 def gated_scan_workspace(T, n, d):
-    """A workspace tensor for gated_scan and gated_scan_grad."""
+    """A workspace tensor for gated_scan and gated_scan_grad of at most T steps, n envs and d values."""
     return _space(lib().im_gated_scan_workspace(T, n, d))
 
 

@@ -125,6 +125,8 @@ struct ScanArgs {
 };
 // Steps of a chunk, a multiple of IM_SCAN_KEEP; T or more: one chunk.
 int64_t scan_chunk(int64_t T, int64_t n, int64_t d);
+// Bytes of the maps that any call of at most T steps, n envs and d values takes.
+int64_t scan_workspace_bound(int64_t T, int64_t n, int64_t d);
 hipError_t launch_scan(const ScanArgs &a, bool grad, bool f32, hipStream_t s);
 
 }  // namespace im

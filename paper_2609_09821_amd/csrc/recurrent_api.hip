@@ -108,12 +108,13 @@ im_status check_scan(int64_t T, int64_t n, int64_t d, int32_t dtype, const void 
     return IM_OK;
 }
 
-// Chunks of a scan, and its workspace.
-void plan_scan(ScanArgs &a, void *workspace)
+// Chunks of a scan, and the bytes of their maps.
+int64_t plan_scan(ScanArgs &a, void *workspace)
 {
     a.chunk = std::max<int64_t>(scan_chunk(a.T, a.n, a.d), 1);
     a.chunks = std::max<int64_t>(ceil_div(a.T, a.chunk), 1);
     a.maps = (float *)workspace;
+    return a.chunks > 1 ? a.chunks * 2 * a.n * a.d * (int64_t)sizeof(float) : 0;
 }
 
 }  // namespace
@@ -336,12 +337,7 @@ im_status im_block_linear_grad(const im_layer8_grad *p, void *stream)
 int64_t im_gated_scan_workspace(int64_t T, int64_t n, int64_t d)
 {
     if (T < 0 || T > MAX_ROWS || n < 0 || n > MAX_ROWS || d < 1 || d > MAX_ROWS || n * d > ((int64_t)1 << 31)) return -1;
-    ScanArgs a{};
-    a.T = T;
-    a.n = n;
-    a.d = d;
-    plan_scan(a, nullptr);
-    return a.chunks > 1 ? a.chunks * 2 * n * d * (int64_t)sizeof(float) : 0;
+    return scan_workspace_bound(T, n, d);
 }
 
 im_status im_gated_scan(const im_scan *p, void *stream)
@@ -350,18 +346,18 @@ im_status im_gated_scan(const im_scan *p, void *stream)
     im_status s = check_scan(p->T, p->n, p->d, p->dtype, p->terminated, p->truncated, p->ld_flags);
     if (s != IM_OK) return s;
     if (p->n == 0) return IM_OK;
+    ScanArgs a{};
+    a.T = p->T;
+    a.n = p->n;
+    a.d = p->d;
+    s = check_workspace(p->workspace, p->workspace_bytes, plan_scan(a, p->workspace), 16);
+    if (s != IM_OK) return s;
     if (p->T > 0) {
         if (!apart(p->T, p->n, p->d, p->st_h, p->ld_h)) return invalid("h: steps or rows overlap");
         if (p->st_gate < 0 || p->ld_gate < 0 || p->st_x < 0 || p->ld_x < 0) return invalid("negative stride");
         if (!p->gate || !p->x || !p->h) return invalid("NULL gate, x or h");
     }
-    s = check_workspace(p->workspace, p->workspace_bytes, im_gated_scan_workspace(p->T, p->n, p->d), 16);
-    if (s != IM_OK) return s;
     if (p->T == 0 && !p->state_out) return IM_OK;
-    ScanArgs a{};
-    a.T = p->T;
-    a.n = p->n;
-    a.d = p->d;
     a.gate = p->gate;
     a.st_gate = p->st_gate;
     a.ld_gate = p->ld_gate;
@@ -377,7 +373,6 @@ im_status im_gated_scan(const im_scan *p, void *stream)
     a.ld_h = p->ld_h;
     a.state_out = p->state_out;
     a.keep = p->keep;
-    plan_scan(a, p->workspace);
     return launched(launch_scan(a, false, p->dtype == IM_DTYPE_F32, (hipStream_t)stream), "gated_scan launch");
 }
 
@@ -387,6 +382,12 @@ im_status im_gated_scan_grad(const im_scan_grad *p, void *stream)
     im_status s = check_scan(p->T, p->n, p->d, p->dtype, p->terminated, p->truncated, p->ld_flags);
     if (s != IM_OK) return s;
     if (p->n == 0) return IM_OK;
+    ScanArgs a{};
+    a.T = p->T;
+    a.n = p->n;
+    a.d = p->d;
+    s = check_workspace(p->workspace, p->workspace_bytes, plan_scan(a, p->workspace), 16);
+    if (s != IM_OK) return s;
     if (p->T > 0) {
         if (!apart(p->T, p->n, p->d, p->st_dgate, p->ld_dgate) || !apart(p->T, p->n, p->d, p->st_dx, p->ld_dx))
             return invalid("dgate or dx: steps or rows overlap");
@@ -395,13 +396,7 @@ im_status im_gated_scan_grad(const im_scan_grad *p, void *stream)
         if (!p->dh || !p->gate || !p->x || !p->keep || !p->dgate || !p->dx)
             return invalid("NULL dh, gate, x, keep, dgate or dx");
     }
-    s = check_workspace(p->workspace, p->workspace_bytes, im_gated_scan_workspace(p->T, p->n, p->d), 16);
-    if (s != IM_OK) return s;
     if (p->T == 0 && !p->dstate_out) return IM_OK;
-    ScanArgs a{};
-    a.T = p->T;
-    a.n = p->n;
-    a.d = p->d;
     a.gate = p->gate;
     a.st_gate = p->st_gate;
     a.ld_gate = p->ld_gate;
@@ -423,7 +418,6 @@ im_status im_gated_scan_grad(const im_scan_grad *p, void *stream)
     a.dx = p->dx;
     a.st_dx = p->st_dx;
     a.ld_dx = p->ld_dx;
-    plan_scan(a, p->workspace);
     return launched(launch_scan(a, true, p->dtype == IM_DTYPE_F32, (hipStream_t)stream), "gated_scan_grad launch");
 }
 

@@ -435,6 +435,18 @@ int64_t scan_chunk(int64_t T, int64_t n, int64_t d)
     return std::max<int64_t>(chunk, ceil_div(ceil_div(T, 65535), KEEP) * KEEP);
 }
 
+// A call takes most maps neither at the largest T nor at the largest n: 1000 x 64 x 1024 is cut and
+// 1000 x 65 x 1024 is not, and chunks grow with the lanes.  Chunks have 32 steps at least, and 32 of each 33
+// that T lanes / 262144 comes to (it is rounded down before it is rounded up to 16): there are ceil(T / 32) or
+// 262144 33 / 32 / lanes + 1 at most, of n d values each, which are 2 lanes at most and 65536 where
+// lanes may be cut.
+int64_t scan_workspace_bound(int64_t T, int64_t n, int64_t d)
+{
+    if (T <= 64) return 0;
+    const int64_t values = std::min<int64_t>(n * d, 65536);
+    return std::min(ceil_div(T, 32) * values, 540672 + values) * 2 * (int64_t)sizeof(float);
+}
+
 template <typename E, typename O, int MODE>
 static void scan_launch(const ScanArgs &a, bool grad, dim3 g, dim3 b, int64_t pieces, hipStream_t s)
 {

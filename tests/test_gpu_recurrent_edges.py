@@ -39,3 +39,27 @@ def test_linear8_grad_outputs_alone_in_the_layers_workspace(n, i, o):
         one = [torch.full_like(t, 7.0) if j == k else None for j, t in enumerate(outs)]
         im.linear8_grad(dy, xt, wt, *one, workspace=ws)
         assert torch.equal(one[k], outs[k])
+
+
+@pytest.mark.parametrize("most,calls", [
+    ((1000, 65, 1024), [(1000, 65, 1024), (1000, 64, 1024), (999, 3, 1000), (70, 1, 1), (64, 65, 1024)]),
+    ((2112, 32, 512), [(2112, 32, 512), (2048, 32, 512), (2111, 31, 511), (1, 32, 512)])])
+def test_a_scans_workspace_serves_smaller_calls(most, calls):
+    """One workspace for the largest sizes, none of it written behind its end."""
+    ws = im.gated_scan_workspace(*most)
+    room = torch.full((ws.numel() + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+    ws, behind = room[:ws.numel()], room[ws.numel():]
+    for T, n, d in calls:
+        g = torch.Generator(device="cuda")
+        g.manual_seed(T + n + d)
+        gate, x, dh = (torch.randn(T, n, d, device="cuda", generator=g) for _ in range(3))
+        got = []
+        for w in (ws, None):
+            h, dgate, dx = (torch.zeros_like(x) for _ in range(3))
+            keep = torch.zeros(-(-T // 16), n, d, device="cuda")
+            out, dst = torch.zeros(n, d, device="cuda"), torch.zeros(n, d, device="cuda")
+            im.gated_scan(gate, x, h, None, out, keep, workspace=w)
+            im.gated_scan_grad(dh, gate, x, keep, dgate, dx, None, dst, workspace=w)
+            got.append((h, out, keep, dgate, dx, dst))
+        assert all(torch.equal(a, b) for a, b in zip(*got))
+    assert (behind == 0xA5).all()

@@ -2,6 +2,7 @@
 touch the device, and the workspace sizes."""
 import ctypes as C
 import os
+import random
 
 import pytest
 
@@ -247,3 +248,56 @@ def test_the_layers_workspace_serves_each_output_alone(lib, n, i, o):
                  dict(dw=P, in_=i, ld_dw=i, xt=_held(n, i))):
         a = _layer_grad(**dict(none, n=n, out=o, **over))
         _refused(lib, lib.im_block_linear_grad(C.byref(a), None), BAD, "aligned")
+
+
+def _asked(lib, f, a):
+    """Whether a call without its arrays is refused for its workspace (or for the arrays)."""
+    assert f(C.byref(a), None) == BAD
+    said = lib.im_last_error().decode()
+    assert ("workspace" in said) != ("NULL gate" in said or "NULL dh" in said), said
+    return "workspace" in said
+
+
+def test_a_scans_workspace_serves_smaller_calls(lib):
+    """Sized once for the largest T, n and d, as a program does whose batches vary."""
+    rng = random.Random(7)
+
+    def log(hi):
+        return max(1, int(round(hi ** rng.random())))
+
+    def pair(most, small):
+        ws = lib.im_gated_scan_workspace(*most)
+        assert 0 <= lib.im_gated_scan_workspace(*small) <= ws <= 5 << 20, (most, small)
+        T, n, d = small
+        for f, make in ((lib.im_gated_scan, _scan), (lib.im_gated_scan_grad, _scan_grad)):
+            s = make()
+            over = dict(T=T, n=n, d=d, ld_flags=n, gate=None, workspace_bytes=ws, dh=None)
+            over.update({k: n * d for k in ("st_gate", "st_x", "st_h", "st_dh", "st_dgate", "st_dx")})
+            over.update({k: d for k in ("ld_gate", "ld_x", "ld_h", "ld_dh", "ld_dgate", "ld_dx")})
+            _set(s, {k: v for k, v in over.items() if hasattr(s, k)})
+            assert not _asked(lib, f, s), (most, small)
+
+    pair((1000, 65, 1024), (1000, 64, 1024))
+    pair((2112, 32, 512), (2048, 32, 512))
+    for _ in range(20000):
+        most = log(1 << 20), log(4096), log(2048)
+        pair(most, tuple(rng.choice((v, rng.randint(1, v), max(1, v - 1))) for v in most))
+    # chunks whose length was rounded down the most
+    for lanes in (1, 2, 3, 5, 64, 1000, 8192, 32768):
+        for q in (32, 48, 64, 1024):
+            T = ((q + 1) * 262144 - 1) // lanes
+            for n, d in ((lanes, 1), (lanes, 2), (1, 2 * lanes), (1, 2 * lanes - 1)):
+                pair((T, n, d), (T, n, d))
+
+
+def test_workspaces_grow_with_the_rows(lib):
+    """A workspace for n rows serves every call on fewer."""
+    for i, o in ((1, 1), (361, 1024), (1024, 512), (1024, 1024), (1536, 1408), (2048, 2304), (69, 4096), (3000, 3000)):
+        last = 0
+        for n in list(range(0, 9000, 37)) + [16384, 30000, 65536, 1 << 20]:
+            now = lib.im_block_linear_grad_workspace(n, i, o)
+            assert now >= last, (n, i, o)
+            last = now
+    for d in (1, 30, 361, 512, 1024, 8192):
+        sizes = [lib.im_rms_norm_grad_workspace(n, d) for n in list(range(0, 9000, 7)) + [65536, 1 << 20]]
+        assert sizes == sorted(sizes)
