@@ -415,19 +415,34 @@ static int64_t tiles_of(int64_t n, int64_t out, int side) { return ceil_div(n, s
 // Few tiles of 128 x 128 leave CUs without one.
 static bool few_tiles(int64_t n, int64_t out) { return tiles_of(n, out, 128) < 256; }
 
-// Parts of dw: of tiles of 128 x 128 where they come to 400 (two a CU at most), else of 64 x 64.  A part
-// has four steps at least, eight where the tiles alone fill the CUs.  Both gradients by us of rows, in and
-// out, bf16, from a graph, with 64 x 64 below 256 parts, 400 and 512:
+// Parts of dw, of tiles of 128 x 128 or 64 x 64, two a CU of the larger ones at most.  A part has four steps
+// at least, of 64 x 64 eight where the tiles alone fill the CUs.
+static int64_t large_splits(int64_t n, int64_t out, int64_t steps)
+{
+    return std::max<int64_t>(1, std::min<int64_t>(512 / tiles_of(n, out, 128), steps / 4));
+}
+
+// The larger ones where their parts come to 400.  Both gradients by us of rows, in and out, bf16, from a
+// graph, with 64 x 64 below 256 parts, 400 and 512:
 //   2000 x 1024 x 1024   36.8  28.4  28.4       4096 x 1024 x 512    37.6   33.9   33.8
 //   16384 x 361 x 512    48.6  44.3  43.5       16384 x 361 x 1024   67.1   67.4   64.9
 //   8192 x 538 x 1024    54.4  54.8  51.6       65536 x 361 x 1024    185    187    216
 // 1024 x 1024 x 1024 in parts of four steps 22.3, of eight (no second part, no joining) 18.6.
-static bool large_parts(int64_t n, int64_t out, int64_t splits) { return tiles_of(n, out, 128) * splits >= 400; }
+// From 129 tiles on whole numbers of parts may come to less than 400 at any length: they are larger from 4096
+// rows on, and where the tiles alone fill the CUs from three steps on.  By 64 x 64 and 128 x 128 of n rows:
+//   n                  128           300           1024          2048          4096          16384        65536
+//   1408 -> 1536                                 27.1 / 38.8   41.1 / 50.9   75.0 / 68.7   244 / 196    942 / 661
+//   1536 -> 2048                                 37.6 / 43.8   45.6 / 58.4   84.9 / 81.7   286 / 255   1112 / 882
+//   2048 -> 2304   24.5 / 27.7   38.5 / 32.4   48.7 / 45.3   73.6 / 67.0    116 / 110    408 / 364   1660 / 1358
+static bool large_parts(int64_t n, int64_t out, int64_t steps)
+{
+    const int64_t tiles = tiles_of(n, out, 128);
+    return tiles * large_splits(n, out, steps) >= 400 || (tiles >= 256 && steps > 2) || (tiles >= 128 && steps >= 32);
+}
 
 int linear8_splits(int64_t n, int64_t out, int64_t steps)
 {
-    const int64_t large = std::max<int64_t>(1, std::min<int64_t>(512 / tiles_of(n, out, 128), steps / 4));
-    if (large_parts(n, out, large)) return (int)large;
+    if (large_parts(n, out, steps)) return (int)large_splits(n, out, steps);
     const int64_t tiles = tiles_of(n, out, 64);
     return (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, steps / (tiles >= 256 ? 8 : 4)));
 }
@@ -483,7 +498,7 @@ hipError_t launch_linear8(const Linear8Args &a, hipStream_t s)
 hipError_t launch_linear8_grad(const Linear8Args &dx, const Linear8Args &dw, const ColumnSums &c, hipStream_t s)
 {
     hipError_t e = hipSuccess;
-    const bool with_dx = dx.y != nullptr, small = dw.y && !large_parts(dw.n, dw.out, dw.splits);
+    const bool with_dx = dx.y != nullptr, small = dw.y && !large_parts(dw.n, dw.out, dw.steps);
     if (with_dx && small && few_tiles(dx.n, dx.out)) {
         const int64_t blocks = tiles_of(dx.n, dx.out, 64) + tiles_of(dw.n, dw.out, 64) * dw.splits;
         // of more than two blocks a CU: 4095 x 361 x 1024 30.5 and 28.2 us, 8192 x 361 x 512 34.1 and 31.9,

@@ -63,3 +63,19 @@ def test_a_scans_workspace_serves_smaller_calls(most, calls):
             got.append((h, out, keep, dgate, dx, dst))
         assert all(torch.equal(a, b) for a, b in zip(*got))
     assert (behind == 0xA5).all()
+
+
+@pytest.mark.parametrize("n,i,o", [(200, 2048, 2304), (400, 2048, 2304), (4100, 1408, 1536), (16500, 1536, 2048)])
+def test_linear8_grad_of_wide_layers(n, i, o):
+    """Whole numbers, exact in fp32, at widths where parts of the larger tiles come to less than 400."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(n)
+    dy, x, w = (torch.randint(-7, 8, z, device="cuda", generator=g).float() for z in ((n, o), (n, i), (o, i)))
+    xt, wt = im.Block8.empty(i, n), im.Block8.empty(i, o, 128)
+    im.block8_store(x, None, xt)
+    im.block8_store(w, None, wt)
+    dx, dw, db = (torch.zeros(*z, device="cuda") for z in ((n, i), (o, i), (o,)))
+    im.linear8_grad(dy, xt, wt, dx, dw, db)
+    assert torch.equal(dx, (dy.double() @ w.double()).float())
+    assert torch.equal(dw, (dy.double().t() @ x.double()).float())
+    assert torch.equal(db, dy.double().sum(0).float())

@@ -301,3 +301,12 @@ def test_workspaces_grow_with_the_rows(lib):
     for d in (1, 30, 361, 512, 1024, 8192):
         sizes = [lib.im_rms_norm_grad_workspace(n, d) for n in list(range(0, 9000, 7)) + [65536, 1 << 20]]
         assert sizes == sorted(sizes)
+
+
+@pytest.mark.parametrize("i,o,parts", [(1408, 1536, 3), (1536, 2048, 2), (1024, 512, 16), (1024, 1024, 8), (2048, 2304, 1)])
+def test_many_rows_parts_of_dw(lib, i, o, parts):
+    """The weight gradient of many rows is formed in as many parts as its 128 x 128 tiles leave room
+    for, whatever their number: the workspace holds the parts beside dy in 8 bits and its sums."""
+    n = 65536
+    store = 2 * n * o + n * -(-o // 128) + o * n // 128 + n // 128 * o * 4
+    assert lib.im_block_linear_grad_workspace(n, i, o) == store + (parts * o * i * 4 if parts > 1 else 0)
