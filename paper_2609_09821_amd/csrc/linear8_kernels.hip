@@ -101,8 +101,7 @@ __device__ __forceinline__ u32x4_r bits4(const f32x16_t &a, int g)
 // 65536 rows 1024 -> 1024 to bf16: 126 us, 1.09 PFLOP/s, 136 with all arrays out of HBM; to fp32 152 and 156.
 // A 256 x 256 tile has a CU for itself, so that nothing multiplies while it stores.
 // dw of 65536 rows 1024 -> 512: 76 us in 16 parts and 8 to join them; tiles of 256 x 256,
-// 256 x 128 and eight wavefronts a tile are no faster (82, 85, 79), and rows of x^T that lie a multiple
-// of 64 KB apart cost 10 us.
+// 256 x 128 and eight wavefronts a tile are no faster (82, 85, 79).
 // ---------------------------------------------------------------------------
 template <int WP_, int WQ_, int TP_, int TQ_, int NS_>
 struct TileShape {

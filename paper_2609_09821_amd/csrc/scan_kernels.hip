@@ -264,11 +264,11 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, int64_t pieces)
 // Backwards: D, the gradient of the state that passes on from a step, starts from dstate;
 // at each step G = dh + live D, D = a G.  The states within 16 steps are formed again from the
 // kept one, and with them what G is multiplied by, which takes the place of gate and x in
-// registers.  MAP: the chunk's map of D alone, from gate and dh.  32 x 16384 x 256 bf16 293 us, 1.41 GB
-// at 4.8 TB/s (with three wavefronts a SIMD, which spill five registers; 376 with the two that more registers
+// registers.  MAP: the chunk's map of D alone, from gate and dh.  32 x 16384 x 256 bf16 291 us, 1.41 GB
+// at 4.8 TB/s, with three wavefronts a SIMD, which spill five registers (376 with the two that more registers
 // leave, 639 with four, which spill many; of fp32 260 with two, 309 with three; of bf16 rows so far apart
-// that their offsets take 64 bits 107 us of 32 x 24 x 65536 with two, 241 with three, which spill 77); 16383 x 2 x 361 floats 91 us: maps 25.5, their
-// composition 7.8, steps 57.5, which read gate and dh again.
+// that their offsets take 64 bits 107 us of 32 x 24 x 65536 with two, 241 with three, which spill 77).
+// 16383 x 2 x 361 floats 92 us: maps 25.7, their composition 7.7, steps 59, which read gate and dh again.
 // ---------------------------------------------------------------------------
 template <typename E, int V, typename O, int MODE>
 __global__ __launch_bounds__(256, sizeof(E) == 2 && sizeof(O) == 4 ? 3 : 2) void scan_grad_kernel(ScanArgs a, int64_t pieces)
